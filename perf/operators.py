@@ -1,0 +1,368 @@
+"""What a training or serving step does around the library's channel-last 3x3
+layers: group norm with its activation, the norm's backward pass, the 8-bit
+checkpoint that replaces the saved activation, and the layer's weight gradient.
+
+In a residual block the norm's input x is what the backward pass needs: the norm's
+gradients are formed from it, and the layer's input is act(norm(x)) again.  A
+training program keeps x as it is, or as an 8-bit checkpoint: one code a value,
+x = centre + step * code, centre and step per image and channel.
+
+    norm    y = act(norm(x)), as in serving
+    train   the same with the statistics and the checkpoint stored, and the
+            checkpoint's values read back, as the backward pass begins
+    back    dx, dgamma, dbeta from dy and x
+    back8   the same from dy and the checkpoint of x
+    wgrad   dg of the layer y = conv(x, g) from x and dy
+    wgrad8  dg of y = conv(act(norm(x)), g) from the checkpoint of x and dy
+
+Sizes are those of the library's own layers (VGG-16, ResNet-like stages,
+Inception-v3's grids), batch 1 to 64.
+"""
+import math
+
+import torch
+
+own = False
+
+EPS = 1e-5
+DTYPE = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+CODES = 127.0                    # codes are -127 .. 127
+FLAT = 2.0 ** -100               # half ranges below this are kept as their centre
+
+
+def _case(name, op, dtype, N, C, H, W, G=1, act="none", K=0, pad=1):
+    return {"name": name, "op": op, "dtype": dtype, "N": N, "C": C, "H": H, "W": W, "G": G, "act": act, "K": K,
+            "pad": pad}
+
+
+def listed():
+    return [
+        # the smallest serving call: the norm after an early layer, one image of odd
+        # size, three channels a group
+        _case("norm_n1_c48_57_bf16", "norm", "bf16", 1, 48, 57, 57, G=16, act="relu"),
+        # batch inference, large early images: groups of two channels, 50176 pixels each
+        _case("norm_n32_c64_224", "norm", "f32", 32, 64, 224, 224, G=32, act="silu"),
+        # batch inference at the headline layer's size, half precision tensors
+        _case("norm_n64_c256_56_f16", "norm", "f16", 64, 256, 56, 56, G=32, act="silu"),
+        # a ResNet-like stage's training forward at a small batch
+        _case("train_n8_c128_28_bf16", "train", "bf16", 8, 128, 28, 28, G=32, act="silu"),
+        # the headline layer's training forward
+        _case("train_n64_c256_56", "train", "f32", 64, 256, 56, 56, G=32, act="silu"),
+        # the stage's backward at the small batch, x kept as it is
+        _case("back_n8_c128_28", "back", "f32", 8, 128, 28, 28, G=32, act="silu"),
+        # the headline layer's backward in bfloat16
+        _case("back_n64_c256_56_bf16", "back", "bf16", 64, 256, 56, 56, G=32, act="silu"),
+        # a deep layer's backward from the checkpoint: many channels, a small image
+        _case("back8_n32_c512_14", "back8", "f32", 32, 512, 14, 14, G=32, act="silu"),
+        # large early images from the checkpoint
+        _case("back8_n32_c64_224", "back8", "f32", 32, 64, 224, 224, G=32, act="silu"),
+        # fine-tuning at batch 1: one image's weight gradient, half of the tensors' bits
+        _case("wgrad_n1_c32_56_bf16", "wgrad", "bf16", 1, 32, 56, 56, K=32),
+        # the stage's weight gradient at the small batch
+        _case("wgrad_n8_c128_28", "wgrad", "f32", 8, 128, 28, 28, K=128),
+        # the headline layer's weight gradient, its input formed again from the checkpoint
+        _case("wgrad8_n64_c256_56", "wgrad8", "f32", 64, 256, 56, 56, G=32, act="silu", K=256),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def draw(rng):
+    """One more call of these ranges: odd sizes, odd channel counts, groups of one
+    channel up to one group for all."""
+    every = listed()
+    while True:
+        op = rng.choice(["norm", "train", "back", "back8", "wgrad", "wgrad8"])
+        N, H = _log_int(rng, 1, 64), _log_int(rng, 7, 224)
+        W = H if rng.random() < 0.7 else _log_int(rng, 7, 224)
+        C, K = _log_int(rng, 8, 512), _log_int(rng, 16, 512)
+        if rng.random() < 0.7:                  # channel counts are mostly multiples of 16
+            C, K = (C + 15) // 16 * 16, (K + 15) // 16 * 16
+        groups = [g for g in range(1, C + 1) if C % g == 0]
+        G = rng.choice([g for g in groups if 4 <= g <= 32] or groups) if rng.random() < 0.8 else rng.choice(groups)
+        act = rng.choice(["none", "relu", "silu", "silu", "silu"])
+        dtype = rng.choice(["f32", "f32", "f16", "bf16"])
+        grad = op.startswith("wgrad")
+        c = _case("", op, dtype, N, C, H, W, G=1 if op == "wgrad" else G, act="none" if op == "wgrad" else act,
+                  K=K if grad else 0, pad=rng.choice([0, 1, 1, 1]) if grad else 1)
+        del c["name"]
+        w, same = work(c), [work(e) for e in every if e["op"].startswith("wgrad") == grad]
+        if w["bytes"] <= max(e["bytes"] for e in same) and w["flops"] <= max(e["flops"] for e in same):
+            return c
+
+
+def _size(dtype):
+    return 4 if dtype == "f32" else 2
+
+
+def work(case):
+    """Every input read once and every output written once; 2 flops a product of the
+    weight gradient, which has N Ho Wo C K of them for each of the nine taps, and about
+    20 a value for the norm and its gradient."""
+    N, C, H, W, G, K, s = (case["N"], case["C"], case["H"], case["W"], case["G"], case["K"], _size(case["dtype"]))
+    X, stats, rows, op = N * H * W * C, 8 * N * G, 8 * C, case["op"]
+    code = X + 8 * N * C
+    if op == "norm":
+        return {"bytes": 2 * s * X + rows, "flops": 20 * X}
+    if op == "train":
+        # x in, y and the checkpoint out; the checkpoint in, its values out
+        return {"bytes": 3 * s * X + 2 * code + stats + rows, "flops": 25 * X}
+    if op == "back":
+        return {"bytes": 3 * s * X + stats + 2 * rows, "flops": 30 * X}
+    if op == "back8":
+        return {"bytes": 2 * s * X + code + stats + 2 * rows, "flops": 30 * X}
+    Ho, Wo = H + 2 * case["pad"] - 2, W + 2 * case["pad"] - 2
+    moved = s * N * Ho * Wo * K + 4 * 9 * C * K + (s * X if op == "wgrad" else code + stats + rows)
+    return {"bytes": moved, "flops": 18 * N * Ho * Wo * C * K}
+
+
+# ---------------------------------------------------------------- inputs
+
+def _codes(x):
+    """The checkpoint of x [N][H][W][C]: (codes int8, rows [N][C][2] of centre, step)."""
+    lo, hi = x.float().amin((1, 2)), x.float().amax((1, 2))
+    half, centre = 0.5 * hi - 0.5 * lo, 0.5 * lo + 0.5 * hi
+    flat = half < FLAT
+    inverse = torch.where(flat, torch.zeros_like(half), CODES / half)
+    q = torch.round((x.float() - centre[:, None, None]) * inverse[:, None, None])
+    q = q.clamp(-CODES, CODES).to(torch.int8)
+    return q, torch.stack((centre, torch.where(flat, torch.zeros_like(half), half / CODES)), -1).contiguous()
+
+
+def _inputs(case, seed):
+    """Convolution outputs of unit scale whose channels differ in mean and spread;
+    norm parameters of a trained network; gradients of unit scale; a weight gradient's
+    plain input is an activation, a third of it zero."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    N, C, H, W, G, K, t = (case["N"], case["C"], case["H"], case["W"], case["G"], case["K"], DTYPE[case["dtype"]])
+
+    def randn(*shape):
+        return torch.randn(shape, generator=gen, device="cuda")
+    x = randn(N, H, W, C).mul_(torch.exp(0.3 * randn(C))).add_(0.5 * randn(C))
+    if case["op"] == "wgrad":
+        x = x.clamp_min_(0.0)
+    d = {"x": x.to(t)}
+    if case["op"] == "wgrad":
+        d["dy"] = randn(N, H + 2 * case["pad"] - 2, W + 2 * case["pad"] - 2, K).to(t)
+        return d
+    d["gamma"], d["beta"] = 1.0 + 0.2 * randn(C), 0.3 * randn(C)
+    if case["op"] in ("norm", "train"):
+        return d
+    if case["op"] == "wgrad8":
+        d["dy"] = randn(N, H + 2 * case["pad"] - 2, W + 2 * case["pad"] - 2, K).to(t)
+    else:
+        d["dy"] = randn(N, H, W, C).to(t)
+    # what the forward pass left: the statistics, and with the checkpoint no x
+    groups = d["x"].float().view(N, H * W, G, C // G)
+    var, mean = torch.var_mean(groups, (1, 3), unbiased=False)
+    d["stats"] = torch.stack((mean, torch.rsqrt(var + EPS)), -1).contiguous()
+    if case["op"] in ("back8", "wgrad8"):
+        codes, rows = _codes(d.pop("x"))
+        # the checkpoint's layout: the codes, padded to 16 bytes, then the rows
+        pad = codes.new_zeros(-codes.numel() % 16)
+        d["ckpt"] = torch.cat((codes.view(-1), pad, rows.view(-1).view(torch.int8)))
+    return d
+
+
+def prepare(case, seed):
+    state = {"case": dict(case), **_inputs(case, seed)}
+    if own:
+        state.update(_plan(case, state))
+    return state
+
+
+# ---------------------------------------------------------------- the framework's calls
+
+def _plan(case, d):
+    """Output buffers and workspace, kept from call to call, and the flags."""
+    from paper_1903_01521_amd import binding as B
+    N, C, H, W, G, K, op = (case["N"], case["C"], case["H"], case["W"], case["G"], case["K"], case["op"])
+    flags = {"f32": 0, "f16": B.WINO_IO_F16, "bf16": B.WINO_IO_BF16}[case["dtype"]]
+    flags |= {"none": 0, "relu": B.WINO_FLAG_RELU, "silu": B.WINO_FLAG_SILU}[case["act"]]
+    out = {}
+    if op in ("back8", "wgrad8"):
+        flags |= B.WINO_FLAG_ACT8
+    if op in ("norm", "train"):
+        out["y"] = torch.empty_like(d["x"])
+        if op == "train":
+            out["stats"] = torch.empty((N, G, 2), device="cuda")
+            out["ckpt"] = torch.empty(B.wino_act8_bytes(N, C, H, W), dtype=torch.int8, device="cuda")
+            out["values"] = torch.empty_like(d["x"])
+        ws = B.wino_group_norm_workspace_bytes(N, C, H, W, G, flags)
+    elif op in ("back", "back8"):
+        out["dx"] = torch.empty_like(d["dy"])
+        out["dgamma"], out["dbeta"] = torch.empty(C, device="cuda"), torch.empty(C, device="cuda")
+        ws = B.wino_group_norm_backward_workspace_bytes(N, C, H, W, G, flags)
+    else:
+        out["dg"] = torch.empty((K, C, 3, 3), device="cuda")
+        ws = B.wino_conv2d_wgrad_workspace_bytes(N, C, H, W, K, case["pad"], flags)
+    assert 0 <= ws < 1 << 40
+    space = torch.empty(ws, dtype=torch.int8, device="cuda") if ws else None
+    return {"out": out, "flags": flags, "space": space, "bytes": ws}
+
+
+def _call(s):
+    from paper_1903_01521_amd import binding as B
+    c, out, flags, ws, wsb = s["case"], s["out"], s["flags"], s["space"], s["bytes"]
+    N, C, H, W, G, K, op = c["N"], c["C"], c["H"], c["W"], c["G"], c["K"], c["op"]
+    if op == "norm":
+        B.check(B.wino_group_norm_nhwc(s["x"], s["gamma"], s["beta"], out["y"], None, None, N, C, H, W, G, EPS, flags,
+                                       ws, wsb), "norm")
+        return {"y": out["y"]}
+    if op == "train":
+        B.check(B.wino_group_norm_nhwc(s["x"], s["gamma"], s["beta"], out["y"], out["stats"], out["ckpt"], N, C, H, W,
+                                       G, EPS, flags, ws, wsb), "norm")
+        B.check(B.wino_act8_unpack_nhwc(out["ckpt"], out["values"], N, C, H, W, flags & B.WINO_IO_MASK), "unpack")
+        return {"y": out["y"], "stats": out["stats"], "values": out["values"]}
+    if op in ("back", "back8"):
+        x = s["ckpt"] if op == "back8" else s["x"]
+        B.check(B.wino_group_norm_backward_nhwc(s["dy"], x, s["stats"], s["gamma"], s["beta"], out["dx"],
+                                                out["dgamma"], out["dbeta"], N, C, H, W, G, flags, ws, wsb), "back")
+        return {"dx": out["dx"], "dgamma": out["dgamma"], "dbeta": out["dbeta"]}
+    if op == "wgrad":
+        B.check(B.wino_conv2d_wgrad_nhwc(s["x"], s["dy"], out["dg"], None, None, None, 0, N, C, H, W, K, c["pad"],
+                                         flags, ws, wsb), "wgrad")
+    else:
+        B.check(B.wino_conv2d_wgrad_nhwc(s["ckpt"], s["dy"], out["dg"], s["stats"], s["gamma"], s["beta"], G, N, C, H,
+                                         W, K, c["pad"], flags, ws, wsb), "wgrad")
+    return {"dg": out["dg"]}
+
+
+# ---------------------------------------------------------------- the plain forms
+
+def _read(ckpt, case):
+    """The checkpoint's values, in 32 bits."""
+    N, C, H, W = case["N"], case["C"], case["H"], case["W"]
+    X = N * H * W * C
+    rows = ckpt[X + -X % 16:].view(torch.float32).view(N, 1, 1, C, 2)
+    return ckpt[:X].view(N, H, W, C).float() * rows[..., 1] + rows[..., 0]
+
+
+def _normed(x, stats, case):
+    """(x - mean) * rstd per image and group."""
+    N, H, W, C = x.shape
+    groups = x.view(N, H * W, case["G"], C // case["G"])
+    return ((groups - stats[:, None, :, None, 0]) * stats[:, None, :, None, 1]).view(N, H, W, C)
+
+
+def _act(z, act):
+    return z if act == "none" else z.clamp_min(0.0) if act == "relu" else z / (1.0 + torch.exp(-z))
+
+
+def _plain(s):
+    c = s["case"]
+    N, C, H, W, G, K, op, t = c["N"], c["C"], c["H"], c["W"], c["G"], c["K"], c["op"], DTYPE[c["dtype"]]
+    if op == "wgrad":
+        return {"dg": _taps(s["x"].float(), s["dy"].float(), c)}
+    x = _read(s["ckpt"], c) if op in ("back8", "wgrad8") else s["x"].float()
+    if op in ("norm", "train"):
+        groups = x.view(N, H * W, G, C // G)
+        mean = groups.mean((1, 3))
+        var = (groups - mean[:, None, :, None]).square().mean((1, 3))
+        stats = torch.stack((mean, torch.rsqrt(var + EPS)), -1)
+        y = _act(_normed(x, stats, c) * s["gamma"] + s["beta"], c["act"]).to(t)
+        if op == "norm":
+            return {"y": y}
+        codes, rows = _codes(s["x"])
+        values = (codes.float() * rows[:, None, None, :, 1] + rows[:, None, None, :, 0]).to(t)
+        return {"y": y, "stats": stats, "values": values}
+    n = _normed(x, s["stats"], c)
+    z = n * s["gamma"] + s["beta"]
+    if op == "wgrad8":
+        return {"dg": _taps(_act(z, c["act"]), s["dy"].float(), c)}
+    dz = s["dy"].float()
+    if c["act"] == "relu":
+        dz = dz * (z > 0)
+    elif c["act"] == "silu":
+        sig = 1.0 / (1.0 + torch.exp(-z))
+        dz = dz * (sig * (1.0 + z * (1.0 - sig)))
+    dn = dz * s["gamma"]
+
+    def mean(v):
+        return v.view(N, H * W, G, C // G).mean((1, 3))[:, None, :, None]
+    dx = dn.view(N, H * W, G, C // G) - mean(dn) - n.view(N, H * W, G, C // G) * mean(dn * n)
+    dx = (dx * s["stats"][:, None, :, None, 1]).view(N, H, W, C)
+    return {"dx": dx.to(t), "dgamma": (dz * n).sum((0, 1, 2)), "dbeta": dz.sum((0, 1, 2))}
+
+
+def _taps(a, dy, case):
+    """dg[k][c][r][s] = sum over pixels of a[n][i + r - pad][j + s - pad][c] dy[n][i][j][k]."""
+    p = case["pad"]
+    N, Ho, Wo, K = dy.shape
+    C = a.shape[3]
+    a = torch.nn.functional.pad(a, (0, 0, p, p, p, p))
+    flat = dy.reshape(-1, K)
+    taps = [a[:, r:r + Ho, s:s + Wo].reshape(-1, C).t() @ flat for r in range(3) for s in range(3)]
+    return torch.stack(taps).permute(2, 1, 0).reshape(K, C, 3, 3)
+
+
+def run(state):
+    return _call(state) if own else _plain(state)
+
+
+# ---------------------------------------------------------------- in 64 bits
+
+def _moments64(x, G):
+    """Mean and variance [N][G] of x [N][C][H W] in 64 bits."""
+    N, C, P = x.shape
+    rows = x.reshape(N, G, C // G * P)
+    mean = rows.sum(2) / rows.shape[2]
+    return mean, ((rows - mean[:, :, None]) ** 2).sum(2) / rows.shape[2]
+
+
+def _spread(v, C):
+    """[N][G] to [N][C][1]."""
+    return v.repeat_interleave(C // v.shape[1], 1)[:, :, None]
+
+
+def exact(case, seed):
+    d = _inputs(case, seed)
+    N, C, H, W, G, K, op, act = (case["N"], case["C"], case["H"], case["W"], case["G"], case["K"], case["op"],
+                                 case["act"])
+    if "ckpt" in d:
+        X = N * H * W * C
+        codes = d["ckpt"][:X].view(N, H * W, C).transpose(1, 2).double()
+        rows = d["ckpt"][(X + 15) // 16 * 16:].view(torch.float32).view(N, C, 2).double()
+        x = rows[:, :, :1] + rows[:, :, 1:] * codes
+    else:
+        x = d["x"].view(N, H * W, C).transpose(1, 2).double()
+    a = x
+    if op != "wgrad":
+        if op in ("norm", "train"):
+            mean, var = _moments64(x, G)
+            scale = 1.0 / torch.sqrt(var + EPS)
+        else:
+            mean, scale = d["stats"][..., 0].double(), d["stats"][..., 1].double()
+        n = (x - _spread(mean, C)) * _spread(scale, C)
+        gamma, beta = d["gamma"].double()[None, :, None], d["beta"].double()[None, :, None]
+        z = gamma * n + beta
+        a = z if act == "none" else torch.relu(z) if act == "relu" else z * torch.sigmoid(z)
+    if op in ("norm", "train"):
+        y = a.transpose(1, 2).reshape(N, H, W, C)
+        # the codes come from 32-bit arithmetic: they have no 64-bit value
+        return {"y": y} if op == "norm" else {"y": y, "stats": torch.stack((mean, scale), -1), "values": None}
+    if op in ("wgrad", "wgrad8"):
+        Ho, Wo = H + 2 * case["pad"] - 2, W + 2 * case["pad"] - 2
+        image = torch.nn.functional.pad(a.view(N, C, H, W), (case["pad"],) * 4)
+        dg = torch.zeros((3, 3, K, C), dtype=torch.float64, device=a.device)
+        for i in range(N):
+            dy = d["dy"][i].double().view(Ho * Wo, K).t().contiguous()
+            for r in range(3):
+                for s in range(3):
+                    dg[r, s] += dy @ image[i, :, r:r + Ho, s:s + Wo].reshape(C, -1).t()
+        return {"dg": dg.permute(2, 3, 0, 1).contiguous()}
+    dz = d["dy"].view(N, H * W, C).transpose(1, 2).double()
+    if act == "relu":
+        dz = torch.where(z > 0, dz, torch.zeros_like(dz))
+    elif act == "silu":
+        # d/dz z sigmoid(z) = (z sigmoid(z)) (1 - sigmoid(z)) + sigmoid(z)
+        dz = dz * (a * torch.sigmoid(-z) + torch.sigmoid(z))
+    dbeta, dgamma = dz.sum(2), (dz * n).sum(2)
+    count = C // G * H * W
+    m1 = (gamma[..., 0] * dbeta).view(N, G, -1).sum(2) / count
+    m2 = (gamma[..., 0] * dgamma).view(N, G, -1).sum(2) / count
+    dx = _spread(scale, C) * (gamma * dz - _spread(m1, C) - n * _spread(m2, C))
+    return {"dx": dx.transpose(1, 2).reshape(N, H, W, C), "dgamma": dgamma.sum(0), "dbeta": dbeta.sum(0)}
