@@ -125,10 +125,12 @@ def _codes(x):
     lo, hi = x.float().amin((1, 2)), x.float().amax((1, 2))
     half, centre = 0.5 * hi - 0.5 * lo, 0.5 * lo + 0.5 * hi
     flat = half < FLAT
-    inverse = torch.where(flat, torch.zeros_like(half), CODES / half)
+    # divisions of tensors: by a number torch multiplies with its reciprocal, one rounding more
+    codes = torch.full_like(half, CODES)
+    inverse = torch.where(flat, torch.zeros_like(half), codes / half)
     q = torch.round((x.float() - centre[:, None, None]) * inverse[:, None, None])
     q = q.clamp(-CODES, CODES).to(torch.int8)
-    return q, torch.stack((centre, torch.where(flat, torch.zeros_like(half), half / CODES)), -1).contiguous()
+    return q, torch.stack((centre, torch.where(flat, torch.zeros_like(half), half / codes)), -1).contiguous()
 
 
 def _inputs(case, seed):
