@@ -329,6 +329,85 @@ int wino_conv2d_nhwc(const float* x, const float* U, float* y,
                      int N, int C, int H, int W, int K, int pad, int m,
                      unsigned flags, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- training on channel-last tensors ---------------------------------------
+ * What a training step needs around wino_conv2d_nhwc: group norm with its
+ * activation, its backward pass, an 8-bit checkpoint in place of the saved
+ * activation, and the layer's weight gradient.  (The gradient of the layer's
+ * input is wino_conv2d_nhwc with the filters flipped and their K and C swapped,
+ * g'[c][k][r][s] = g[k][c][2-r][2-s], and pad 2 - pad.)
+ *   Tensors x, y, dx, dy are [N][H][W][C] (dy of a layer [N][Ho][Wo][K]) of fp32,
+ *   or fp16 / bf16 with WINO_IO_F16 / WINO_IO_BF16; parameters, statistics and
+ *   their gradients fp32.  All sums are fp32 in a fixed order.  Outputs must not
+ *   overlap each other or any input.  Tensors may have any address that suits
+ *   their element type (16-byte ones run faster); checkpoints must be on 16-byte
+ *   addresses and workspaces on 4-byte ones, else WINO_ERR_INVALID_ARG.  At most
+ *   2^40 elements a tensor. */
+#define WINO_FLAG_SILU     0x002u   /* y = z * sigmoid(z) (group norm and the calls that undo it) */
+#define WINO_FLAG_ACT8     0x004u   /* x is an 8-bit checkpoint */
+#define WINO_IO_F16        0x040u   /* tensors are fp16 */
+#define WINO_IO_BF16       0x080u   /* tensors are bf16 */
+#define WINO_IO_MASK       0x0C0u
+
+/* 8-bit activation checkpoint of x [N][H][W][C], any element type: int8 codes
+ * [N][H][W][C], zero to 15 bytes up to a multiple of 16, then fp32 rows [N][C][2]
+ * of (centre, step); x is read back as centre + step * code.  Per image and
+ * channel, with lo and hi the least and largest value and half = hi/2 - lo/2:
+ *   centre = lo/2 + hi/2, step = half / 127, code = rint((x - centre) * (127 / half)),
+ * each operation in fp32, so the error is at most half a step (1/508 of the
+ * channel's range) and fp32 rounding.  half < 2^-100: step and codes are 0.  A
+ * channel with an infinite or NaN value is read back as NaN throughout (other
+ * channels are not touched).  wino_act8_bytes: the buffer's size (0 on invalid
+ * arguments).  _pack's workspace may be NULL where its size is 0; (size_t)-1 on
+ * invalid arguments.  flags: WINO_IO_*. */
+size_t wino_act8_bytes(int N, int C, int H, int W);
+size_t wino_act8_workspace_bytes(int N, int C, int H, int W, unsigned flags);
+int wino_act8_pack_nhwc(const void* x, void* q, int N, int C, int H, int W, unsigned flags,
+                        void* workspace, size_t workspace_bytes, void* stream);
+int wino_act8_unpack_nhwc(const void* q, void* x, int N, int C, int H, int W, unsigned flags, void* stream);
+
+/* Group norm with an activation: for each image and each of G groups of D = C/G
+ * neighbouring channels (C % G == 0),
+ *   n = (x - mean) * rstd, rstd = 1 / sqrt(var + eps), z = n * gamma[c] + beta[c], y = act(z)
+ * with mean and (biased) variance over H*W*D values; the variance is that about
+ * the mean, not a difference of squares.
+ *   gamma, beta : [C] fp32 or NULL (1 and 0).   eps >= 0.
+ *   stats : [N][G][2] fp32 of (mean, rstd) or NULL.
+ *   q     : checkpoint of x (wino_act8_bytes) or NULL.
+ *   flags : WINO_FLAG_RELU or WINO_FLAG_SILU or neither; WINO_IO_*.
+ * The workspace's size is 0 where the image of a group fits a workgroup's
+ * registers (one launch, x read once). */
+size_t wino_group_norm_workspace_bytes(int N, int C, int H, int W, int G, unsigned flags);
+int wino_group_norm_nhwc(const void* x, const float* gamma, const float* beta, void* y, float* stats, void* q,
+                         int N, int C, int H, int W, int G, float eps, unsigned flags,
+                         void* workspace, size_t workspace_bytes, void* stream);
+/* y again from x, or with WINO_FLAG_ACT8 from its checkpoint, and the statistics. */
+int wino_group_norm_apply_nhwc(const void* x, const float* stats, const float* gamma, const float* beta, void* y,
+                               int N, int C, int H, int W, int G, unsigned flags, void* stream);
+
+/* Backward pass of wino_group_norm_nhwc, from dy, the statistics and x (or with
+ * WINO_FLAG_ACT8 the checkpoint of x): with dz = dy * act'(z) (ReLU: 0 at z <= 0)
+ *   dbeta = sum dz, dgamma = sum dz * n       (over images and pixels)
+ *   dx = rstd * (gamma * dz - m1 - n * m2), m1, m2 the group's means of gamma * dz
+ *   and gamma * dz * n.
+ *   dgamma, dbeta : [C] fp32, either may be NULL. */
+size_t wino_group_norm_backward_workspace_bytes(int N, int C, int H, int W, int G, unsigned flags);
+int wino_group_norm_backward_nhwc(const void* dy, const void* x, const float* stats, const float* gamma,
+                                  const float* beta, void* dx, float* dgamma, float* dbeta,
+                                  int N, int C, int H, int W, int G, unsigned flags,
+                                  void* workspace, size_t workspace_bytes, void* stream);
+
+/* Weight gradient of the 3x3 layer of wino_conv2d_nhwc:
+ *   dg[k][c][r][s] = sum_{n,i,j} a[n,i+r-pad,j+s-pad,c] * dy[n,i,j,k], fp32 [K][C][3][3],
+ * a read as zero outside the image.  stats NULL: a is x (or with WINO_FLAG_ACT8 the
+ * checkpoint's values), and G, gamma and beta are not read.  Else a is the y of
+ * wino_group_norm_nhwc, formed again from x or its checkpoint on load (flags:
+ * that call's activation), not rounded to 16 bits.
+ *   N*Ho*Wo must be below 2^31. */
+size_t wino_conv2d_wgrad_workspace_bytes(int N, int C, int H, int W, int K, int pad, unsigned flags);
+int wino_conv2d_wgrad_nhwc(const void* x, const void* dy, float* dg, const float* stats, const float* gamma,
+                           const float* beta, int G, int N, int C, int H, int W, int K, int pad, unsigned flags,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- allocation-free variant ------------------------------------------------
  * For callers that cannot allocate device memory (code under HIP graph
  * capture, tight serving loops, harnesses that forbid hipMalloc): the layer of

@@ -12,4 +12,6 @@ package and shares no code, header, table or constant generator with it.
   references of each stage (filter, input and output transform, the per-position
   GEMMs) in the paper's order.
 * :mod:`oracle.nn` -- fp64 ReLU and 2x2 max-pool for layer stacks.
+* :mod:`oracle.train` -- fp64 group norm, its gradients, the 8-bit checkpoint and
+  the weight gradient on channel-last tensors.
 """

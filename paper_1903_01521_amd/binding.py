@@ -2,8 +2,8 @@
 
 Every function here takes the same arguments as its C counterpart in
 ``include/wino.h`` and returns its status / size unchanged.  Device buffers may
-be given as torch CUDA tensors (fp32, contiguous; their data pointers are
-passed) or as raw integer addresses; ``None`` passes NULL.  ``stream=None``
+be given as torch CUDA tensors (fp32, or the element type that WINO_IO_* names,
+or bytes for checkpoints; contiguous; their data pointers are passed) or as raw integer addresses; ``None`` passes NULL.  ``stream=None``
 passes torch's current stream when a GPU is present, else NULL.  All compute
 happens in the HIP kernels of libwino.so; nothing here computes.  If the library
 has not been built, loading raises -- there is no fallback path.
@@ -87,6 +87,17 @@ _SIGS = {
     "wino_filter_bytes_p": ([_c_int] * 3 + [_c_uint], _c_size),
     "wino_filter_transform_p": ([_vp, _vp] + [_c_int] * 3 + [_c_uint, _vp], _c_int),
     "wino_conv2d_nhwc": ([_vp, _vp, _vp] + [_c_int] * 7 + [_c_uint, _vp, _c_size, _vp], _c_int),
+    "wino_act8_bytes": ([_c_int] * 4, _c_size),
+    "wino_act8_workspace_bytes": ([_c_int] * 4 + [_c_uint], _c_size),
+    "wino_act8_pack_nhwc": ([_vp] * 2 + [_c_int] * 4 + [_c_uint, _vp, _c_size, _vp], _c_int),
+    "wino_act8_unpack_nhwc": ([_vp] * 2 + [_c_int] * 4 + [_c_uint, _vp], _c_int),
+    "wino_group_norm_workspace_bytes": ([_c_int] * 5 + [_c_uint], _c_size),
+    "wino_group_norm_nhwc": ([_vp] * 6 + [_c_int] * 5 + [ctypes.c_float, _c_uint, _vp, _c_size, _vp], _c_int),
+    "wino_group_norm_apply_nhwc": ([_vp] * 5 + [_c_int] * 5 + [_c_uint, _vp], _c_int),
+    "wino_group_norm_backward_workspace_bytes": ([_c_int] * 5 + [_c_uint], _c_size),
+    "wino_group_norm_backward_nhwc": ([_vp] * 8 + [_c_int] * 5 + [_c_uint, _vp, _c_size, _vp], _c_int),
+    "wino_conv2d_wgrad_workspace_bytes": ([_c_int] * 6 + [_c_uint], _c_size),
+    "wino_conv2d_wgrad_nhwc": ([_vp] * 6 + [_c_int] * 7 + [_c_uint, _vp, _c_size, _vp], _c_int),
     "wino_conv2d_noalloc": ([_vp, _vp, _vp] + [_c_int] * 7 + [_c_uint, _vp], _c_int),
 }
 
@@ -322,6 +333,92 @@ def wino_conv2d_nhwc(x, U, y, N, C, H, W, K, pad, m, flags=0, workspace=None, wo
                      stream=None) -> int:
     return lib().wino_conv2d_nhwc(_fptr(x), _fptr(U), _fptr(y), N, C, H, W, K, pad, m, flags,
                                   _ptr(workspace), workspace_bytes, _stream(stream))
+
+
+WINO_FLAG_SILU = 0x002
+WINO_FLAG_ACT8 = 0x004
+WINO_IO_F16 = 0x040
+WINO_IO_BF16 = 0x080
+WINO_IO_MASK = 0x0C0
+
+
+def _tptr(t, flags):
+    """A tensor of the element type that WINO_IO_* names."""
+    if t is None or isinstance(t, int):
+        return t
+    torch = _torch or _import_torch()
+    kind = flags & WINO_IO_MASK
+    if t.dtype is not (torch.float16 if kind == WINO_IO_F16 else torch.bfloat16 if kind == WINO_IO_BF16 else torch.float32):
+        raise ValueError("tensors must have the element type that the flags name")
+    return _ptr(t)
+
+
+def _xptr(t, flags):
+    """x: a tensor of the flags' element type, or with WINO_FLAG_ACT8 a checkpoint of bytes."""
+    return _qptr(t) if flags & WINO_FLAG_ACT8 else _tptr(t, flags)
+
+
+def _qptr(t):
+    if t is None or isinstance(t, int):
+        return t
+    if t.element_size() != 1:
+        raise ValueError("checkpoints must be tensors of bytes")
+    return _ptr(t)
+
+
+def wino_act8_bytes(N, C, H, W) -> int:
+    return lib().wino_act8_bytes(N, C, H, W)
+
+
+def wino_act8_workspace_bytes(N, C, H, W, flags=0) -> int:
+    return lib().wino_act8_workspace_bytes(N, C, H, W, flags)
+
+
+def wino_act8_pack_nhwc(x, q, N, C, H, W, flags=0, workspace=None, workspace_bytes=0, stream=None) -> int:
+    return lib().wino_act8_pack_nhwc(_tptr(x, flags), _qptr(q), N, C, H, W, flags, _ptr(workspace), workspace_bytes,
+                                     _stream(stream))
+
+
+def wino_act8_unpack_nhwc(q, x, N, C, H, W, flags=0, stream=None) -> int:
+    return lib().wino_act8_unpack_nhwc(_qptr(q), _tptr(x, flags), N, C, H, W, flags, _stream(stream))
+
+
+def wino_group_norm_workspace_bytes(N, C, H, W, G, flags=0) -> int:
+    return lib().wino_group_norm_workspace_bytes(N, C, H, W, G, flags)
+
+
+def wino_group_norm_nhwc(x, gamma, beta, y, stats, q, N, C, H, W, G, eps, flags=0, workspace=None,
+                         workspace_bytes=0, stream=None) -> int:
+    return lib().wino_group_norm_nhwc(_tptr(x, flags), _fptr(gamma), _fptr(beta), _tptr(y, flags), _fptr(stats),
+                                      _qptr(q), N, C, H, W, G, eps, flags, _ptr(workspace), workspace_bytes,
+                                      _stream(stream))
+
+
+def wino_group_norm_apply_nhwc(x, stats, gamma, beta, y, N, C, H, W, G, flags=0, stream=None) -> int:
+    return lib().wino_group_norm_apply_nhwc(_xptr(x, flags), _fptr(stats), _fptr(gamma), _fptr(beta), _tptr(y, flags),
+                                            N, C, H, W, G, flags, _stream(stream))
+
+
+def wino_group_norm_backward_workspace_bytes(N, C, H, W, G, flags=0) -> int:
+    return lib().wino_group_norm_backward_workspace_bytes(N, C, H, W, G, flags)
+
+
+def wino_group_norm_backward_nhwc(dy, x, stats, gamma, beta, dx, dgamma, dbeta, N, C, H, W, G, flags=0,
+                                  workspace=None, workspace_bytes=0, stream=None) -> int:
+    return lib().wino_group_norm_backward_nhwc(_tptr(dy, flags), _xptr(x, flags), _fptr(stats), _fptr(gamma),
+                                               _fptr(beta), _tptr(dx, flags), _fptr(dgamma), _fptr(dbeta), N, C, H, W,
+                                               G, flags, _ptr(workspace), workspace_bytes, _stream(stream))
+
+
+def wino_conv2d_wgrad_workspace_bytes(N, C, H, W, K, pad, flags=0) -> int:
+    return lib().wino_conv2d_wgrad_workspace_bytes(N, C, H, W, K, pad, flags)
+
+
+def wino_conv2d_wgrad_nhwc(x, dy, dg, stats, gamma, beta, G, N, C, H, W, K, pad, flags=0, workspace=None,
+                           workspace_bytes=0, stream=None) -> int:
+    return lib().wino_conv2d_wgrad_nhwc(_xptr(x, flags), _tptr(dy, flags), _fptr(dg), _fptr(stats), _fptr(gamma),
+                                        _fptr(beta), G, N, C, H, W, K, pad, flags, _ptr(workspace), workspace_bytes,
+                                        _stream(stream))
 
 
 def check(status: int, where: str = "wino") -> None:

@@ -13,9 +13,11 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libwino.so")
-KERNELS = [os.path.join(CSRC, f) for f in ("wino_kernels.hip", "wino_bf3.hip", "wino_bf3_1d.hip", "wino_gemm3.hip")]
-SOURCES = KERNELS + [os.path.join(CSRC, "wino_api.cpp")]
-HEADERS = [os.path.join(CSRC, f) for f in ("wino_device.h", "wino_transforms.h", "wino_internal.h")] + [
+KERNELS = [os.path.join(CSRC, f) for f in ("wino_kernels.hip", "wino_bf3.hip", "wino_bf3_1d.hip", "wino_gemm3.hip",
+                                          "wino_norm.hip", "wino_wgrad.hip")]
+SOURCES = KERNELS + [os.path.join(CSRC, f) for f in ("wino_api.cpp", "wino_train_api.cpp")]
+HEADERS = [os.path.join(CSRC, f) for f in ("wino_device.h", "wino_transforms.h", "wino_internal.h", "wino_checks.h",
+                                           "wino_norm.h", "wino_norm_device.h", "wino_wgrad.h")] + [
     os.path.join(ROOT, "include", "wino.h")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -1,6 +1,7 @@
 // C-ABI of libwino: argument validation, layer planning and dispatch.
 // Every check runs before the first HIP call, so invalid calls enqueue nothing.
 #include "../../include/wino.h"
+#include "wino_checks.h"
 #include "wino_internal.h"
 
 #include <stdint.h>
@@ -9,7 +10,6 @@ using namespace wino;
 
 namespace {
 
-constexpr int64_t kMaxElems = (int64_t)1 << 40;      // per tensor, well inside size_t
 constexpr int64_t kMaxTiles = ((int64_t)1 << 31) - 64;
 
 constexpr unsigned kBlockMask = WINO_BLOCK_1x16 | WINO_BLOCK_4x4, kCsplitShift = 16, kSliceShift = 20;
@@ -25,14 +25,6 @@ int prec_of(unsigned flags) {
 // 16-bit operands: 32-channel chunks, 1 KB per (block, chunk, position).
 size_t c32_elems(const Geom& g) { return (size_t)(g.C + 31) / 32; }
 size_t vh_bytes(const Geom& g) { return (size_t)g.PB * c32_elems(g) * g.T * 1024; }
-
-// Checked product of non-negative int64 values; false on overflow past kMaxElems.
-bool mul_ok(int64_t a, int64_t b, int64_t* out) {
-    if (a < 0 || b < 0) return false;
-    if (a != 0 && b > kMaxElems / a) return false;
-    *out = a * b;
-    return *out <= kMaxElems;
-}
 
 // Supported (m, r): F(2x2,3x3), F(4x4,3x3), F(2x2,5x5).
 bool supported(int m, int r) { return (r == 3 && (m == 2 || m == 4)) || (r == 5 && m == 2); }
@@ -88,13 +80,6 @@ int make_geom_1d(int N, int C, int H, int W, int K, int pad, int m, int r, int a
     g->CQ = (int)CQ; g->KB = (int)KB; g->PB = (int)PB;
     return WINO_OK;
 }
-
-bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-    return x < y + nb && y < x + na;
-}
-
-size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 // Plan: which algorithm, and which fused-kernel variant.
 struct Plan {
@@ -199,8 +184,8 @@ size_t stage3_bytes(const Geom& g) {
 }
 
 // These kernels store and load the workspace 16 bytes at a time; one that is not so
-// aligned counts as none for them (the fused kernel they replace needs none at all).
-bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+// aligned (aligned16) counts as none for them (the fused kernel they replace needs
+// none at all).
 
 // The three stages with the GEMMs on the bf16 matrix cores (NCHW or NHWC).
 hipError_t run_g3(const float* x, const float* U, float* y, void* ws, const Geom& g, bool relu, hipStream_t s) {
@@ -467,8 +452,6 @@ int make_plan_unchecked(const Geom& g, unsigned flags, Plan* p) {
     }
     return WINO_OK;
 }
-
-int hip_status(hipError_t e) { return e == hipSuccess ? WINO_OK : WINO_ERR_HIP; }
 
 }  // namespace
 
