@@ -339,8 +339,8 @@ int wino_conv2d_nhwc(const float* x, const float* U, float* y,
  *   or fp16 / bf16 with WINO_IO_F16 / WINO_IO_BF16; parameters, statistics and
  *   their gradients fp32.  All sums are fp32 in a fixed order.  Outputs must not
  *   overlap each other or any input.  Tensors may have any address that suits
- *   their element type (16-byte ones run faster); checkpoints must be on 16-byte
- *   addresses and workspaces on 4-byte ones, else WINO_ERR_INVALID_ARG.  At most
+ *   their element type (16-byte ones run faster); checkpoints and
+ *   workspaces must be on 16-byte addresses, else WINO_ERR_INVALID_ARG.  At most
  *   2^40 elements a tensor. */
 #define WINO_FLAG_SILU     0x002u   /* y = z * sigmoid(z) (group norm and the calls that undo it) */
 #define WINO_FLAG_ACT8     0x004u   /* x is an 8-bit checkpoint */

@@ -16,7 +16,7 @@ LIB = os.path.join(HERE, "libwino.so")
 KERNELS = [os.path.join(CSRC, f) for f in ("wino_kernels.hip", "wino_bf3.hip", "wino_bf3_1d.hip", "wino_gemm3.hip",
                                           "wino_norm.hip", "wino_wgrad.hip")]
 SOURCES = KERNELS + [os.path.join(CSRC, f) for f in ("wino_api.cpp", "wino_train_api.cpp")]
-HEADERS = [os.path.join(CSRC, f) for f in ("wino_device.h", "wino_transforms.h", "wino_internal.h", "wino_checks.h",
+HEADERS = [os.path.join(CSRC, f) for f in ("wino_device.h", "wino_transforms.h", "wino_internal.h", "wino_checks.h", "wino_fastdiv.h",
                                            "wino_norm.h", "wino_norm_device.h", "wino_wgrad.h")] + [
     os.path.join(ROOT, "include", "wino.h")]
 

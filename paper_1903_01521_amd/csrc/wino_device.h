@@ -107,8 +107,6 @@ __device__ __forceinline__ uint4 us_y(uint4 X, uint2 L) {
 
 // ------------------------------------------------------------------ helpers
 
-__device__ __forceinline__ uint32_t fdiv(uint32_t n, FastDiv d) { return (__umulhi(n, d.m) + n) >> d.l; }
-
 struct TileCoord {
     int n, ti, tj;
     bool valid;

@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "wino.h"
+#include "wino_fastdiv.h"
 
 namespace wino {
 
@@ -35,14 +36,6 @@ struct FusedCfg {
     int csplit;     // waves of one workgroup splitting the channel quads of a unit
     int bw;         // tile-block width: 16 (1 x 16 tiles) or 4 (4 x 4 tiles)
     int nsl;        // channel slices over workgroups (1: none), summed by k_slice_sum
-};
-
-// Division of n < 2^31 by a fixed d >= 1 as ((mulhi(n, m) + n) >> l), with
-// l = ceil(log2 d) and m = floor(2^32 (2^l - d) / d) + 1 (Granlund and
-// Montgomery's round-up method; mulhi(n, m) + n < 2^32 for such n).
-struct FastDiv {
-    uint32_t m;
-    int l;
 };
 
 // Runtime part of the fused kernel's work decomposition (host-computed).

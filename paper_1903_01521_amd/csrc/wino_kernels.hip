@@ -2698,14 +2698,6 @@ hipError_t launch_output_transform(const float* M, float* y, const Geom& g, bool
 
 constexpr int kMaxLdsBytes = 160 * 1024;
 
-static FastDiv make_fastdiv(uint32_t d) {
-    FastDiv f;
-    f.l = 0;
-    while ((1ull << f.l) < d) ++f.l;
-    f.m = (uint32_t)(((1ull << 32) * ((1ull << f.l) - d)) / d + 1);
-    return f;
-}
-
 // The fused kernel's epilogue addresses its four LDS objects as one packed
 // range: check once per instance that the compiled allocation is exactly their
 // total (no padding between them) before its first launch outside a stream

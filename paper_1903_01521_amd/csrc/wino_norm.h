@@ -26,13 +26,14 @@ inline size_t act8_rows_at(const NormShape& s) { return ((size_t)s.N * s.P * s.C
 inline size_t act8_size(const NormShape& s) { return act8_rows_at(s) + (size_t)s.N * s.C * 8; }
 
 // How a pass over the tensor is cut.  A workgroup holds `px` pixels of `cb`
-// channels in registers, `nv` vectors of `vec` channels a thread; its threads
-// are `rows` pixels of cb/vec columns.  one: px is the whole image and cb whole
-// groups, so that the statistics never leave the workgroup; else the image is
-// cut into `chunks` and the statistics are joined by a launch in between.
+// channels in registers, up to `nv` vectors of `vec` channels a thread; its
+// threads are `rows` pixels of cv = cb/vec columns (wrows, parts: see Cut).  one:
+// px is the whole image and cb whole groups, so that the statistics never leave
+// the workgroup; else the image is cut into `chunks` and the statistics are
+// joined by a launch in between.
 struct NormPlan {
-    bool one;
-    int vec, nv, threads, cb, cv, rows, chunks;
+    bool one, fits;                          // fits: below 2^30 workgroups' items
+    int vec, nv, threads, cb, cv, rows, wrows, parts, chunks;
     int64_t px;
     size_t lds, need;                        // dynamic LDS, workspace bytes
 };

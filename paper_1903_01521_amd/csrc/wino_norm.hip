@@ -7,13 +7,13 @@
 // and gamma dz n:
 //   dbeta = sum dz,  dgamma = sum dz n,  dx = rstd (gamma dz - m1 - n m2).
 //
-// All of it is bound by memory: about 20 operations a value.  So a workgroup
-// loads its part of the tensor once and keeps it in registers.  Where a whole
-// image of one group (or a few neighbouring ones) fits, the statistics are taken
-// and the result is formed from there: one read, one write, one launch, and the
-// variance about the mean itself.  Else three launches: every workgroup reduces
-// its pixels, one joins these parts, and a second pass over the tensor forms the
-// result.  All sums are in 32 bits and in a fixed order.
+// All of it is bound by memory, about 20 operations a value, if it reads the
+// tensor once.  So where a whole image of one group (or a few neighbouring ones)
+// fits a workgroup's registers, it is loaded once and the statistics are taken and
+// the result formed from there: one read, one write, one launch, and the variance
+// about the mean itself.  Else three launches: every workgroup reduces its pixels,
+// one joins these parts, and a second pass over the tensor forms the result.  All
+// sums are in 32 bits and in a fixed order.
 #include <math.h>
 
 #include <type_traits>
@@ -24,13 +24,21 @@ namespace wino {
 
 namespace {
 
-constexpr int kMaxBlocks = 1 << 20;           // workgroups of a launch; they loop over the rest
-constexpr int kXcds = 8;
+constexpr unsigned kMaxBlocks = 1 << 20;      // workgroups of a launch; they loop over the rest
+constexpr unsigned kXcds = 8;
+constexpr int kMaxThreads = 512;              // of the one-pass kernels
 
-// The part of the tensor that a workgroup works on, and its threads' share.
+// The part of the tensor that a workgroup works on, and its threads' share.  A
+// thread has one column of `vec` channels and the pixels of its row, `rows`
+// apart.  wrows > 0: a wave holds wrows whole rows of cv lanes (the lanes left
+// over idle) and joins them by lane shuffles; else the columns run on from wave
+// to wave.  `parts` values of each channel are left to join through LDS.
 struct Cut {
-    int C, G, D, cb, cv, rows, ncb, chunks;
-    int64_t P, px, items;                     // px pixels a chunk; items = N * chunks * ncb
+    int C, G, D, cb, cv, rows, wrows, parts;
+    uint32_t ncb, chunks, items, per;         // items = N * chunks * ncb, per XCD
+    int64_t P, px;                            // px pixels a chunk
+    FastDiv dcv, dD, dncb, dchunks;
+    float inv;                                // 1 / (P D)
 };
 
 struct Item {
@@ -41,71 +49,101 @@ struct Item {
 // Item of a virtual block.  Blocks go to the 8 XCDs in turn; each XCD gets
 // neighbouring items, channels fastest, so that workgroups that share the cache
 // lines of a pixel share an L2.
-__device__ __forceinline__ bool item_of(int64_t vb, const Cut& k, Item* it) {
-    const int64_t per = (k.items + kXcds - 1) / kXcds, i = (vb % kXcds) * per + vb / kXcds;
-    if (vb / kXcds >= per || i >= k.items) return false;
-    const int64_t r = i / k.ncb;
+__device__ __forceinline__ bool item_of(uint32_t vb, const Cut& k, Item* it) {
+    const uint32_t i = vb % kXcds * k.per + vb / kXcds;
+    if (i >= k.items) return false;
+    const uint32_t r = fdiv(i, k.dncb), n = fdiv(r, k.dchunks);
     it->c0 = (int)(i - r * k.ncb) * k.cb;
-    it->n = r / k.chunks;
-    it->chunk = (int)(r - it->n * k.chunks);
+    it->n = n;
+    it->chunk = (int)(r - n * k.chunks);
     it->p0 = it->chunk * k.px;
     it->px = k.P - it->p0 < k.px ? k.P - it->p0 : k.px;
     return true;
 }
 
-// A thread's column of channels and first pixel; count: its pixels of the chunk,
-// `rows` apart.
+// A thread's column of channels, first pixel and number of pixels.
 struct Share {
     int col, row, c, count;
 };
 
 __device__ __forceinline__ Share share_of(const Cut& k, const Item& it, int vec) {
     Share s;
-    s.col = (int)threadIdx.x % k.cv;
-    s.row = (int)threadIdx.x / k.cv;
+    const int t = threadIdx.x, i = k.wrows ? t & 63 : t, row = (int)fdiv(i, k.dcv);
+    const bool idle = k.wrows && row >= k.wrows;
+    s.col = idle ? 0 : i - row * k.cv;
+    s.row = idle ? k.rows : k.wrows ? (t >> 6) * k.wrows + row : row;
     s.c = it.c0 + s.col * vec;
     const bool active = s.row < k.rows && s.c < k.C && s.row < it.px;
-    s.count = active ? (int)((it.px - s.row + k.rows - 1) / k.rows) : 0;
+    s.count = active ? (int)((uint32_t)(it.px - s.row + k.rows - 1) / (uint32_t)k.rows) : 0;
     return s;
 }
 
 struct Add {
-    static constexpr float identity = 0.0f;
     __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
 };
-// NaN stays: a channel that holds one has no range.
+// These keep NaN: a channel that holds one has no range.
 struct Low {
     static constexpr float identity = INFINITY;
-    __device__ __forceinline__ float operator()(float a, float b) const { return a != a || a < b ? a : b; }
+    __device__ __forceinline__ float operator()(float a, float b) const { return __builtin_elementwise_minimum(a, b); }
 };
 struct High {
     static constexpr float identity = -INFINITY;
-    __device__ __forceinline__ float operator()(float a, float b) const { return a != a || a > b ? a : b; }
+    __device__ __forceinline__ float operator()(float a, float b) const { return __builtin_elementwise_maximum(a, b); }
 };
 
-// out[cb] = the threads' values of each channel joined: `sub` partial rows, then
-// those; about 2 sqrt(rows) LDS reads a thread.
+// red[parts][cb] = the threads' values of each channel, joined over a wave's rows.
 template <int VEC, typename Op>
-__device__ void col_reduce(const float (&v)[VEC], const Cut& k, int sub, float* red, float* tmp, float* out, Op op) {
-    const int t = threadIdx.x, nt = blockDim.x;
-    if (t < k.rows * k.cv) {
+__device__ __forceinline__ void join_rows(float (&v)[VEC], const Cut& k, float* red, Op op) {
+    const int t = threadIdx.x, lane = t & 63;
+    if (k.wrows) {
+        const int row = (int)fdiv(lane, k.dcv);
+        for (int n = k.wrows; n > 1;) {
+            const int h = (n + 1) / 2;
+            const bool take = row + h < n;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const float o = __shfl(v[j], (lane + h * k.cv) & 63);
+                if (take) v[j] = op(v[j], o);
+            }
+            n = h;
+        }
+        if (lane < k.cv) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) red[(t >> 6) * k.cb + lane * VEC + j] = v[j];
+        }
+    } else if (t < k.rows * k.cv) {
 #pragma unroll
         for (int j = 0; j < VEC; ++j) red[t * VEC + j] = v[j];
     }
-    __syncthreads();
-    for (int i = t; i < sub * k.cb; i += nt) {
-        const int c = i % k.cb;
-        float a = Op::identity;
-        for (int r = i / k.cb; r < k.rows; r += sub) a = op(a, red[r * k.cb + c]);
-        tmp[i] = a;
+}
+
+// red joined over the parts, for channel c.
+template <typename Op>
+__device__ __forceinline__ float join_parts(const Cut& k, const float* red, int c, Op op) {
+    float a = red[c];
+#pragma unroll 4
+    for (int r = 1; r < k.parts; ++r) a = op(a, red[r * k.cb + c]);
+    return a;
+}
+
+// out[g] = sum of weight(c) red[part][c] over the parts and the group's channels,
+// `lanes` neighbouring lanes a group.
+template <typename F>
+__device__ __forceinline__ void join_groups(const Cut& k, const float* red, float* out, F weight) {
+    const int n = k.parts * k.D, groups = (int)fdiv(k.cb, k.dD);
+    const int bits = n >= 64 ? 6 : 32 - __builtin_clz(n | 1) - ((n & (n - 1)) == 0), lanes = 1 << bits;
+    const int per = blockDim.x >> bits, sub = threadIdx.x & (lanes - 1);
+    for (int g0 = 0; g0 < groups; g0 += per) {
+        const int g = g0 + (threadIdx.x >> bits);
+        float a = 0.0f;
+        if (g < groups)
+            for (int i = sub; i < n; i += lanes) {
+                const int part = (int)fdiv(i, k.dD), c = g * k.D + i - part * k.D;
+                a += weight(c) * red[part * k.cb + c];
+            }
+        for (int m = lanes >> 1; m; m >>= 1) a += __shfl_xor(a, m);
+        if (g < groups && sub == 0) out[g] = a;
     }
-    __syncthreads();
-    for (int c = t; c < k.cb; c += nt) {
-        float a = tmp[c];
-        for (int r = 1; r < sub; ++r) a = op(a, tmp[r * k.cb + c]);
-        out[c] = a;
-    }
-    __syncthreads();
 }
 
 __device__ __forceinline__ float wave_sum(float v) {
@@ -114,24 +152,18 @@ __device__ __forceinline__ float wave_sum(float v) {
     return v;
 }
 
-// gsum[g] = sum of csum over the group's channels, a wave a group.
-template <typename F>
-__device__ __forceinline__ void group_reduce(int groups, int D, float* gsum, F value) {
-    const int lane = threadIdx.x & 63;
-    for (int g = threadIdx.x >> 6; g < groups; g += blockDim.x >> 6) {
-        float a = 0.0f;
-        for (int d = lane; d < D; d += 64) a += value(g * D + d);
-        a = wave_sum(a);
-        if (lane == 0) gsum[g] = a;
-    }
-    __syncthreads();
+template <typename T, int VEC, int NV>
+__device__ __forceinline__ void pin(Held<T, VEC> (&h)[NV]) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) h[i].pin();
 }
 
-template <typename F>
-__device__ __forceinline__ void with_act(Act act, F&& f) {
-    if (act == Act::Silu) f(std::integral_constant<Act, Act::Silu>());
-    else if (act == Act::Relu) f(std::integral_constant<Act, Act::Relu>());
-    else f(std::integral_constant<Act, Act::None>());
+// p moved on, so that the compiler does not keep the addresses of an earlier pass
+// over the same pixels in registers.
+template <typename T>
+__device__ __forceinline__ void advance(T*& p, size_t step) {
+    p += step;
+    asm volatile("" : "+v"(p));
 }
 
 // ------------------------------------------------------------------ forward
@@ -145,152 +177,234 @@ struct FwdArgs {
     float* rows;
     float* part;                              // [N][chunks][C][4] of mean, squares about it, low, high
     float eps;
-    Act act;
-    int sub;
+    bool relu;
 };
 
-// One image of whole groups (ONE), or the parts of the statistics.
-template <typename T, int VEC, int NV, bool ONE>
-__global__ __launch_bounds__(1024) void k_norm(FwdArgs a, Cut k) {
+// One image of whole groups.
+template <typename T, int VEC, int NV, bool SILU>
+__global__ __launch_bounds__(kMaxThreads) void k_norm(FwdArgs a, Cut k) {
     extern __shared__ float lds[];
-    float* red = lds;
-    float* tmp = red + k.rows * k.cb;
-    float* ca = tmp + a.sub * k.cb;
-    float *cl = ca + k.cb, *ch = cl + k.cb, *gm = ch + k.cb, *gr = gm + k.cb;
+    const int words = k.parts * k.cb;
+    float *red = lds, *rl = red + words, *rh = rl + words, *cl = rh + words;
+    float *ch = cl + k.cb, *gm = ch + k.cb, *gr = gm + k.cb;
     Item it;
-    for (int64_t vb = blockIdx.x; vb / kXcds < (k.items + kXcds - 1) / kXcds; vb += gridDim.x) {
+    for (uint32_t vb = blockIdx.x; vb < k.per * kXcds; vb += gridDim.x) {
         if (!item_of(vb, k, &it)) continue;
         const Share s = share_of(k, it, VEC);
-        const size_t at = ((size_t)it.n * k.P + it.p0 + s.row) * k.C + s.c, step = (size_t)k.rows * k.C;
-        Raw<T, VEC> raw[NV];
+        const size_t at = ((size_t)it.n * k.P + s.row) * k.C + s.c, step = (size_t)k.rows * k.C;
+        Held<T, VEC> raw[NV];
+        const T* x = (const T*)a.x + at;
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (i < s.count) raw[i] = *(const Raw<T, VEC>*)((const T*)a.x + at + i * step);
-        const bool norm = !ONE || a.y || a.stats;
-        float mean[VEC], v[VEC];
+        for (int i = 0; i < NV; ++i, advance(x, step))
+            if (i < s.count) raw[i].load(x);
+        const bool norm = a.y || a.stats;
+        float mean[VEC], v[VEC];              // mean: first the group's first value, which the sums are about
         if (norm) {
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) v[j] = 0.0f;
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (i < s.count)
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) v[j] += (float)raw[i].v[j];
-            col_reduce(v, k, a.sub, red, tmp, ca, Add());
-            if constexpr (ONE) {
-                const float inv = 1.0f / ((float)k.P * (float)k.D);
-                group_reduce(k.cb / k.D, k.D, gm, [&](int c) { return ca[c] * inv; });
-            }
+            const T* group = (const T*)a.x + (size_t)it.n * k.P * k.C + it.c0;
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                const int c = s.col * VEC + j;
-                mean[j] = ONE ? gm[c / k.D] : ca[c] / (float)it.px;
+                mean[j] = (float)group[fdiv(s.col * VEC + j, k.dD) * k.D];
                 v[j] = 0.0f;
             }
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 if (i < s.count)
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) {
-                        const float d = (float)raw[i].v[j] - mean[j];
-                        v[j] += d * d;
-                    }
-            col_reduce(v, k, a.sub, red, tmp, ca, Add());
-            if constexpr (ONE) {
-                const float inv = 1.0f / ((float)k.P * (float)k.D), eps = a.eps;
-                group_reduce(k.cb / k.D, k.D, gr, [&](int c) { return ca[c] * inv; });
-                for (int g = threadIdx.x; g < k.cb / k.D; g += blockDim.x) {
-                    gr[g] = 1.0f / sqrtf(gr[g] + eps);
-                    if (a.stats) {
-                        float* st = a.stats + ((size_t)it.n * k.G + it.c0 / k.D + g) * 2;
-                        st[0] = gm[g];
-                        st[1] = gr[g];
-                    }
-                }
-                __syncthreads();
-            }
+                    for (int j = 0; j < VEC; ++j) v[j] += raw[i].value(j) - mean[j];
+            join_rows(v, k, red, Add());
         }
         if (a.codes) {
+            pin(raw);
+            float hi[VEC];
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) v[j] = Low::identity;
+            for (int j = 0; j < VEC; ++j) {
+                v[j] = Low::identity;
+                hi[j] = High::identity;
+            }
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 if (i < s.count)
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) v[j] = Low()((float)raw[i].v[j], v[j]);
-            col_reduce(v, k, a.sub, red, tmp, cl, Low());
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) v[j] = High::identity;
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (i < s.count)
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) v[j] = High()((float)raw[i].v[j], v[j]);
-            col_reduce(v, k, a.sub, red, tmp, ch, High());
-        }
-        if constexpr (!ONE) {
-            // the mean of the channel's pixels of this chunk is in the threads of row 0
-            if (s.row == 0 && s.c < k.C) {
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    const int c = s.col * VEC + j;
-                    float* p = a.part + (((size_t)it.n * k.chunks + it.chunk) * k.C + it.c0 + c) * 4;
-                    p[0] = mean[j];
-                    p[1] = ca[c];
-                    p[2] = a.codes ? cl[c] : 0.0f;
-                    p[3] = a.codes ? ch[c] : 0.0f;
-                }
-            }
-        } else {
-            if (a.codes) {
-                Row r[VEC];
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    const int c = s.col * VEC + j;
-                    r[j] = row_of(cl[c], ch[c]);
-                    if (s.row == 0) {
-                        float* p = a.rows + ((size_t)it.n * k.C + s.c + j) * 2;
-                        p[0] = r[j].centre;
-                        p[1] = r[j].step;
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-                    if (i < s.count) {
-                        Raw<int8_t, VEC> q;
-#pragma unroll
-                        for (int j = 0; j < VEC; ++j) q.v[j] = code_of((float)raw[i].v[j], r[j]);
-                        *(Raw<int8_t, VEC>*)(a.codes + at + i * step) = q;
-                    }
-            }
-            if (a.y) {
-                Affine f[VEC];
-                if (s.count)
 #pragma unroll
                     for (int j = 0; j < VEC; ++j) {
-                        const int c = s.col * VEC + j;
-                        f[j] = Affine{mean[j], gr[c / k.D], a.gamma ? a.gamma[s.c + j] : 1.0f,
-                                      a.beta ? a.beta[s.c + j] : 0.0f};
+                        v[j] = Low()(raw[i].value(j), v[j]);
+                        hi[j] = High()(raw[i].value(j), hi[j]);
                     }
-                with_act(a.act, [&](auto act) {
-#pragma unroll
-                    for (int i = 0; i < NV; ++i)
-                        if (i < s.count) {
-                            Raw<T, VEC> o;
-#pragma unroll
-                            for (int j = 0; j < VEC; ++j)
-                                o.v[j] = (T)act_of<act.value>(f[j].z(f[j].norm((float)raw[i].v[j])));
-                            *(Raw<T, VEC>*)((T*)a.y + at + i * step) = o;
-                        }
-                });
+            join_rows(v, k, rl, Low());
+            join_rows(hi, k, rh, High());
+        }
+        __syncthreads();
+        if (a.codes)
+            for (int c = threadIdx.x; c < k.cb; c += blockDim.x) {
+                const Row r = row_of(join_parts(k, rl, c, Low()), join_parts(k, rh, c, High()));
+                cl[c] = r.centre;
+                ch[c] = r.inverse;
+                float* p = a.rows + ((size_t)it.n * k.C + it.c0 + c) * 2;
+                p[0] = r.centre;
+                p[1] = r.step;
             }
+        if (norm) join_groups(k, red, gm, [&](int) { return k.inv; });
+        __syncthreads();
+        if (norm) {
+            pin(raw);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                mean[j] += gm[fdiv(s.col * VEC + j, k.dD)];
+                v[j] = 0.0f;
+            }
+            if (a.stats && s.row == 0)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const int g = (int)fdiv(s.col * VEC + j, k.dD);
+                    if (s.col * VEC + j == g * k.D) a.stats[((size_t)it.n * k.G + fdiv(it.c0, k.dD) + g) * 2] = mean[j];
+                }
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (i < s.count)
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) {
+                        const float d = raw[i].value(j) - mean[j];
+                        v[j] = fmaf(d, d, v[j]);
+                    }
+            join_rows(v, k, red, Add());
+            __syncthreads();
+            join_groups(k, red, gr, [&](int) { return k.inv; });
+            __syncthreads();
+            if (a.stats)
+                for (int g = threadIdx.x; g < (int)fdiv(k.cb, k.dD); g += blockDim.x)
+                    a.stats[((size_t)it.n * k.G + fdiv(it.c0, k.dD) + g) * 2 + 1] = rstd_of(gr[g], a.eps);
+        }
+        if (a.codes) {
+            pin(raw);
+            float centre[VEC], inverse[VEC];
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                centre[j] = cl[s.col * VEC + j];
+                inverse[j] = ch[s.col * VEC + j];
+            }
+            int8_t* codes = a.codes + at;
+#pragma unroll
+            for (int i = 0; i < NV; ++i, advance(codes, step))
+                if (i < s.count) {
+                    uint32_t q[VEC];
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) q[j] = code_bits(raw[i].value(j), centre[j], inverse[j]);
+                    store_codes(codes, q);
+                }
+        }
+        if (a.y) {
+            pin(raw);
+            Norm<SILU, false> f[VEC];
+            if (s.count)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const float st[2] = {mean[j], rstd_of(gr[fdiv(s.col * VEC + j, k.dD)], a.eps)};
+                    f[j].set(st, a.gamma ? a.gamma[s.c + j] : 1.0f, a.beta ? a.beta[s.c + j] : 0.0f, nullptr);
+                }
+            T* y = (T*)a.y + at;
+#pragma unroll
+            for (int i = 0; i < NV; ++i, advance(y, step))
+                if (i < s.count) {
+                    Raw<T, VEC> o;
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) o.v[j] = (T)act_of<SILU>(f[j].z(f[j].n(raw[i].value(j))), a.relu);
+                    put(y, o);
+                }
         }
         __syncthreads();                      // the next item writes the LDS arrays
     }
 }
 
+// The parts of the statistics of a chunk of an image: a thread's sums are about its
+// own first value, so that a mean far from zero costs nothing, and are joined as
+// means, about the chunk's first value, and squares about the chunk's mean.
+template <typename T, int VEC, bool CODES>
+__global__ __launch_bounds__(256) void k_norm_part(FwdArgs a, Cut k) {
+    constexpr int U = VEC == 1 ? 16 : 8;      // loads in flight
+    extern __shared__ float lds[];
+    const int words = k.parts * k.cb;
+    float *red = lds, *rl = red + words, *rh = rl + words, *cm = rh + words, *cr = cm + k.cb;
+    Item it;
+    for (uint32_t vb = blockIdx.x; vb < k.per * kXcds; vb += gridDim.x) {
+        if (!item_of(vb, k, &it)) continue;
+        const Share s = share_of(k, it, VEC);
+        const size_t step = (size_t)k.rows * k.C;
+        const T* x = (const T*)a.x + ((size_t)it.n * k.P + it.p0 + s.row) * k.C + s.c;
+        float first[VEC], s1[VEC], s2[VEC], lo[VEC], hi[VEC];
+        Held<T, VEC> raw[U], ref;
+        if (s.count) {
+            raw[0].load(x);
+            ref.load(x - (size_t)s.row * k.C);
+        }
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            first[j] = s.count ? raw[0].value(j) : 0.0f;
+            s1[j] = s2[j] = 0.0f;
+            lo[j] = Low::identity;
+            hi[j] = High::identity;
+        }
+        auto take = [&](const Held<T, VEC>& r) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const float v = r.value(j), d = v - first[j];
+                s1[j] += d;
+                s2[j] = fmaf(d, d, s2[j]);
+                if constexpr (CODES) {
+                    lo[j] = Low()(v, lo[j]);
+                    hi[j] = High()(v, hi[j]);
+                }
+            }
+        };
+        int i = 0;
+        for (; i + U <= s.count; i += U) {
+#pragma unroll
+            for (int u = 0; u < U; ++u, x += step) raw[u].load(x);
+#pragma unroll
+            for (int u = 0; u < U; ++u) take(raw[u]);
+        }
+        for (; i < s.count; ++i, x += step) {
+            raw[0].load(x);
+            take(raw[0]);
+        }
+        const float n = (float)s.count;
+        float mean[VEC];
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const float d = s.count ? s1[j] / n : 0.0f;
+            mean[j] = first[j] + d;
+            s2[j] = s2[j] - s1[j] * d;
+            const float r = s.count ? ref.value(j) : 0.0f;
+            s1[j] = n * (mean[j] - r);
+            if (s.row == 0) cr[s.col * VEC + j] = r;
+        }
+        join_rows(s1, k, red, Add());
+        if (CODES) {
+            join_rows(lo, k, rl, Low());
+            join_rows(hi, k, rh, High());
+        }
+        __syncthreads();
+        for (int c = threadIdx.x; c < k.cb; c += blockDim.x) cm[c] = cr[c] + join_parts(k, red, c, Add()) / (float)it.px;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const float d = mean[j] - cm[s.col * VEC + j];
+            s2[j] = s.count ? fmaf(n * d, d, s2[j]) : 0.0f;
+        }
+        join_rows(s2, k, red, Add());
+        __syncthreads();
+        for (int c = threadIdx.x; c < k.cb && it.c0 + c < k.C; c += blockDim.x) {
+            Raw<float, 4> o;
+            o.v[0] = cm[c];
+            o.v[1] = join_parts(k, red, c, Add());
+            o.v[2] = CODES ? join_parts(k, rl, c, Low()) : 0.0f;
+            o.v[3] = CODES ? join_parts(k, rh, c, High()) : 0.0f;
+            *(Raw<float, 4>*)(a.part + (((size_t)it.n * k.chunks + it.chunk) * k.C + it.c0 + c) * 4) = o;
+        }
+        __syncthreads();
+    }
+}
+
 // Joins the parts of one image and group: mean and variance about it, and each
-// channel's range.  A workgroup an (image, group).
+// channel's row.  A workgroup an (image, group).
 __global__ __launch_bounds__(256) void k_norm_join(const float* __restrict__ part, float* __restrict__ stats,
                                                    float* __restrict__ rows, float* __restrict__ inverse, Cut k,
                                                    int64_t groups, float eps) {
@@ -301,7 +415,6 @@ __global__ __launch_bounds__(256) void k_norm_join(const float* __restrict__ par
         const int g = (int)(ng - n * k.G);
         const float* p = part + ((size_t)n * k.chunks * k.C + (size_t)g * k.D) * 4;
         const int64_t all = (int64_t)k.chunks * k.D;
-        const float inv = 1.0f / ((float)k.P * (float)k.D);
         auto total = [&](auto value) {
             float a = 0.0f;
             for (int64_t i = threadIdx.x; i < all; i += 256) {
@@ -316,29 +429,36 @@ __global__ __launch_bounds__(256) void k_norm_join(const float* __restrict__ par
             return acc[0] + acc[1] + acc[2] + acc[3];
         };
         if (stats) {
-            const float mean = total([&](const float* q, float px) { return q[0] * px; }) * inv;
+            const float ref = p[0], mean = ref + total([&](const float* q, float px) { return (q[0] - ref) * px; }) * k.inv;
             const float var = total([&](const float* q, float px) {
                 const float d = q[0] - mean;
                 return q[1] + px * d * d;
-            }) * inv;
+            }) * k.inv;
             if (threadIdx.x == 0) {
                 stats[((size_t)n * k.G + g) * 2] = mean;
-                stats[((size_t)n * k.G + g) * 2 + 1] = 1.0f / sqrtf(var + eps);
+                stats[((size_t)n * k.G + g) * 2 + 1] = rstd_of(var, eps);
             }
         }
         if (rows)
-            for (int d = threadIdx.x; d < k.D; d += 256) {
+            for (int d = wave; d < k.D; d += 4) {
                 float lo = Low::identity, hi = High::identity;
-                for (int ch = 0; ch < k.chunks; ++ch) {
+                for (int ch = lane; ch < (int)k.chunks; ch += 64) {
                     const float* q = p + ((size_t)ch * k.C + d) * 4;
                     lo = Low()(q[2], lo);
                     hi = High()(q[3], hi);
                 }
-                const Row r = row_of(lo, hi);
-                float* o = rows + ((size_t)n * k.C + (size_t)g * k.D + d) * 2;
-                o[0] = r.centre;
-                o[1] = r.step;
-                inverse[(size_t)n * k.C + (size_t)g * k.D + d] = r.inverse;
+#pragma unroll
+                for (int m = 32; m; m >>= 1) {
+                    lo = Low()(lo, __shfl_xor(lo, m));
+                    hi = High()(hi, __shfl_xor(hi, m));
+                }
+                if (lane == 0) {
+                    const Row r = row_of(lo, hi);
+                    const size_t c = (size_t)n * k.C + (size_t)g * k.D + d;
+                    rows[c * 2] = r.centre;
+                    rows[c * 2 + 1] = r.step;
+                    inverse[c] = r.inverse;
+                }
             }
     }
 }
@@ -350,70 +470,66 @@ struct ApplyArgs {
     void* y;
     int8_t* out;                              // codes to write, from x, with rows and
     const float* inverse;                     // 1 / step [N][C]
-    Act act;
+    bool relu;
 };
 
 // The second pass: y (and the codes) from x or codes and the statistics.
-template <typename T, int VEC, bool X8>
+template <typename T, int VEC, bool X8, bool SILU>
 __global__ __launch_bounds__(256) void k_norm_apply(ApplyArgs a, Cut k) {
     constexpr int U = VEC == 1 ? 8 : 4;       // loads in flight
     typedef typename std::conditional<X8, int8_t, T>::type S;
     Item it;
-    for (int64_t vb = blockIdx.x; vb / kXcds < (k.items + kXcds - 1) / kXcds; vb += gridDim.x) {
+    for (uint32_t vb = blockIdx.x; vb < k.per * kXcds; vb += gridDim.x) {
         if (!item_of(vb, k, &it)) continue;
         const Share s = share_of(k, it, VEC);
         if (!s.count) continue;
-        const size_t at = ((size_t)it.n * k.P + it.p0 + s.row) * k.C + s.c, step = (size_t)k.rows * k.C;
-        const S* src = (X8 ? (const S*)a.codes : (const S*)a.x) + at;
-        Affine f[VEC];
-        Row r[VEC];
+        size_t at = ((size_t)it.n * k.P + it.p0 + s.row) * k.C + s.c;
+        const size_t step = (size_t)k.rows * k.C;
+        const S* src = X8 ? (const S*)a.codes : (const S*)a.x;
+        Norm<SILU, X8> f[VEC];
+        float centre[VEC], inverse[VEC], stp[VEC];
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
             const int c = s.c + j;
-            if (a.stats) {
-                const float* st = a.stats + ((size_t)it.n * k.G + c / k.D) * 2;
-                f[j] = Affine{st[0], st[1], a.gamma ? a.gamma[c] : 1.0f, a.beta ? a.beta[c] : 0.0f};
-            }
-            if (X8 || a.out) {
-                const float* p = a.rows + ((size_t)it.n * k.C + c) * 2;
-                r[j].centre = p[0];
-                r[j].step = p[1];
-                r[j].inverse = a.out ? a.inverse[(size_t)it.n * k.C + c] : 0.0f;
-            }
+            const float* row = a.rows + ((size_t)it.n * k.C + c) * 2;
+            if (a.stats)
+                f[j].set(a.stats + ((size_t)it.n * k.G + fdiv(c, k.dD)) * 2, a.gamma ? a.gamma[c] : 1.0f,
+                         a.beta ? a.beta[c] : 0.0f, row);
+            centre[j] = X8 || a.out ? row[0] : 0.0f;
+            stp[j] = X8 ? row[1] : 1.0f;
+            inverse[j] = a.out ? a.inverse[(size_t)it.n * k.C + c] : 0.0f;
         }
-        with_act(a.act, [&](auto act) {
-            for (int i0 = 0; i0 < s.count; i0 += U) {
-                Raw<S, VEC> raw[U];
+        auto give = [&](const Held<S, VEC>& r, size_t at) {
+            if (a.y) {
+                Raw<T, VEC> o;
 #pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (i0 + u < s.count) raw[u] = *(const Raw<S, VEC>*)(src + (i0 + u) * step);
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (i0 + u < s.count) {
-                        Raw<T, VEC> o;
-#pragma unroll
-                        for (int j = 0; j < VEC; ++j) {
-                            float v;
-                            if constexpr (X8) v = value_of(raw[u].v[j], r[j].centre, r[j].step);
-                            else v = (float)raw[u].v[j];
-                            o.v[j] = (T)(a.stats ? act_of<act.value>(f[j].z(f[j].norm(v))) : v);
-                        }
-                        if (a.y) *(Raw<T, VEC>*)((T*)a.y + at + (i0 + u) * step) = o;
-                    }
-                if constexpr (!X8) {
-                    if (a.out) {
-#pragma unroll
-                        for (int u = 0; u < U; ++u)
-                            if (i0 + u < s.count) {
-                                Raw<int8_t, VEC> q;
-#pragma unroll
-                                for (int j = 0; j < VEC; ++j) q.v[j] = code_of((float)raw[u].v[j], r[j]);
-                                *(Raw<int8_t, VEC>*)(a.out + at + (i0 + u) * step) = q;
-                            }
-                    }
+                for (int j = 0; j < VEC; ++j) {
+                    const float v = r.value(j);
+                    o.v[j] = (T)(a.stats ? act_of<SILU>(f[j].z(f[j].n(v)), a.relu)
+                                 : X8    ? value_of(v, centre[j], stp[j])
+                                         : v);
                 }
+                put((T*)a.y + at, o);
             }
-        });
+            if (!X8 && a.out) {
+                uint32_t q[VEC];
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) q[j] = code_bits(r.value(j), centre[j], inverse[j]);
+                store_codes(a.out + at, q);
+            }
+        };
+        Held<S, VEC> raw[U];
+        int i = 0;
+        for (; i + U <= s.count; i += U, at += U * step) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) raw[u].get(src + at + u * step);
+#pragma unroll
+            for (int u = 0; u < U; ++u) give(raw[u], at + u * step);
+        }
+        for (; i < s.count; ++i, at += step) {
+            raw[0].get(src + at);
+            give(raw[0], at);
+        }
     }
 }
 
@@ -425,129 +541,209 @@ struct BwdArgs {
     const float *rows, *stats, *gamma, *beta;
     void* dx;
     float* part;                              // [N][chunks][C][2] of sum dz, sum dz n
-    float* means;                             // [N][G][2] of m1, m2 (not ONE)
-    Act act;
-    int sub;
+    float* means;                             // [N][G][2] of m1, m2 (not of k_norm_back)
+    bool relu;
 };
 
-// One thread's channel constants.
-template <int VEC, bool X8>
-__device__ __forceinline__ void bwd_rows(const BwdArgs& a, const Cut& k, int64_t n, int c0, Affine (&f)[VEC],
-                                         float (&centre)[VEC], float (&step)[VEC]) {
+template <int VEC, bool SILU, bool X8>
+__device__ __forceinline__ void set_norm(Norm<SILU, X8> (&f)[VEC], const BwdArgs& a, const Cut& k, int64_t n, int c0) {
 #pragma unroll
     for (int j = 0; j < VEC; ++j) {
         const int c = c0 + j;
-        const float* st = a.stats + ((size_t)n * k.G + c / k.D) * 2;
-        f[j] = Affine{st[0], st[1], a.gamma ? a.gamma[c] : 1.0f, a.beta ? a.beta[c] : 0.0f};
-        if constexpr (X8) {
-            centre[j] = a.rows[((size_t)n * k.C + c) * 2];
-            step[j] = a.rows[((size_t)n * k.C + c) * 2 + 1];
-        }
+        f[j].set(a.stats + ((size_t)n * k.G + fdiv(c, k.dD)) * 2, a.gamma ? a.gamma[c] : 1.0f,
+                 a.beta ? a.beta[c] : 0.0f, X8 ? a.rows + ((size_t)n * k.C + c) * 2 : nullptr);
     }
 }
 
-template <bool X8, typename S, int VEC>
-__device__ __forceinline__ float x_of(const Raw<S, VEC>& raw, int j, const float (&centre)[VEC],
-                                      const float (&step)[VEC]) {
-    if constexpr (X8) return value_of(raw.v[j], centre[j], step[j]);
-    else return (float)raw.v[j];
-}
+// dx = dz scale + n slope + shift
+struct Grad {
+    float scale, slope, shift;
+    __device__ __forceinline__ void set(float rstd, float gamma, float m1, float m2) {
+        scale = rstd * gamma;
+        slope = -rstd * m2;
+        shift = -rstd * m1;
+    }
+    __device__ __forceinline__ float operator()(float dz, float n) const { return fmaf(dz, scale, fmaf(n, slope, shift)); }
+};
 
-template <typename T, int VEC, int NV, bool X8, bool ONE>
-__global__ __launch_bounds__(1024) void k_norm_back(BwdArgs a, Cut k) {
+// One image of whole groups: dy and x are loaded once, and dz takes dy's registers.
+template <typename T, int VEC, int NV, bool X8, bool SILU>
+__global__ __launch_bounds__(kMaxThreads) void k_norm_back(BwdArgs a, Cut k) {
     extern __shared__ float lds[];
     typedef typename std::conditional<X8, int8_t, T>::type S;
-    float* red = lds;
-    float* tmp = red + k.rows * k.cb;
-    float* cz = tmp + a.sub * k.cb;
-    float *cn = cz + k.cb, *g1 = cn + k.cb, *g2 = g1 + k.cb;
+    const int words = k.parts * k.cb;
+    float *rz = lds, *rn = rz + words, *g1 = rn + words, *g2 = g1 + k.cb;
     Item it;
-    for (int64_t vb = blockIdx.x; vb / kXcds < (k.items + kXcds - 1) / kXcds; vb += gridDim.x) {
+    for (uint32_t vb = blockIdx.x; vb < k.per * kXcds; vb += gridDim.x) {
         if (!item_of(vb, k, &it)) continue;
         const Share s = share_of(k, it, VEC);
-        const size_t at = ((size_t)it.n * k.P + it.p0 + s.row) * k.C + s.c, step = (size_t)k.rows * k.C;
+        const size_t at = ((size_t)it.n * k.P + s.row) * k.C + s.c, step = (size_t)k.rows * k.C;
         const S* src = (X8 ? (const S*)a.codes : (const S*)a.x) + at;
-        Raw<T, VEC> dy[NV];
-        Raw<S, VEC> x[NV];
+        const T* grad = (const T*)a.dy + at;
+        Held<float, VEC> dz[NV];              // dy as loaded, in the first words, then dz
+        Held<S, VEC> x[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i, advance(src, step), advance(grad, step))
+            if (i < s.count) {
+                x[i].load(src);
+                Held<T, VEC> dy;
+                dy.load(grad);
+#pragma unroll
+                for (int w = 0; w < Held<T, VEC>::kWords; ++w) dz[i].w[w] = dy.w[w];
+            }
+        Norm<SILU, X8> f[VEC];
+        float sz[VEC], sn[VEC];
+        if (s.count) set_norm<VEC, SILU, X8>(f, a, k, it.n, s.c);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) sz[j] = sn[j] = 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if (i < s.count) {
-                dy[i] = *(const Raw<T, VEC>*)((const T*)a.dy + at + i * step);
-                x[i] = *(const Raw<S, VEC>*)(src + i * step);
+                Held<T, VEC> dy;
+#pragma unroll
+                for (int w = 0; w < Held<T, VEC>::kWords; ++w) dy.w[w] = dz[i].w[w];
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const float n = f[j].n(x[i].value(j)), d = act_grad<SILU>(f[j].z(n), dy.value(j), a.relu);
+                    dz[i].w[j] = __float_as_uint(d);
+                    sz[j] += d;
+                    sn[j] = fmaf(d, n, sn[j]);
+                }
+                dz[i].pin();
+                x[i].pin();
             }
-        Affine f[VEC];
-        float centre[VEC], stp[VEC], sz[VEC], sn[VEC];
-        if (s.count) bwd_rows<VEC, X8>(a, k, it.n, s.c, f, centre, stp);
+        join_rows(sz, k, rz, Add());
+        join_rows(sn, k, rn, Add());
+        __syncthreads();
+        for (int c = threadIdx.x; c < k.cb; c += blockDim.x) {
+            Raw<float, 2> o;
+            o.v[0] = join_parts(k, rz, c, Add());
+            o.v[1] = join_parts(k, rn, c, Add());
+            *(Raw<float, 2>*)(a.part + ((size_t)it.n * k.C + it.c0 + c) * 2) = o;
+        }
+        auto weight = [&](int c) { return a.gamma ? a.gamma[it.c0 + c] * k.inv : k.inv; };
+        join_groups(k, rz, g1, weight);
+        join_groups(k, rn, g2, weight);
+        __syncthreads();
+        pin(x);
+        Grad h[VEC];
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const int g = (int)fdiv(s.col * VEC + j, k.dD);
+            h[j].set(f[j].rstd, f[j].gamma, g1[g], g2[g]);
+        }
+        T* dx = (T*)a.dx + at;
+#pragma unroll
+        for (int i = 0; i < NV; ++i, advance(dx, step))
+            if (i < s.count) {
+                Raw<T, VEC> o;
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) o.v[j] = (T)h[j](dz[i].value(j), f[j].n(x[i].value(j)));
+                put(dx, o);
+            }
+        __syncthreads();
+    }
+}
+
+// The parts of the sums of a chunk of an image.
+template <typename T, int VEC, bool X8, bool SILU>
+__global__ __launch_bounds__(256) void k_norm_back_part(BwdArgs a, Cut k) {
+    constexpr int U = VEC == 1 ? 8 : 4;
+    extern __shared__ float lds[];
+    typedef typename std::conditional<X8, int8_t, T>::type S;
+    float *rz = lds, *rn = rz + k.parts * k.cb;
+    Item it;
+    for (uint32_t vb = blockIdx.x; vb < k.per * kXcds; vb += gridDim.x) {
+        if (!item_of(vb, k, &it)) continue;
+        const Share s = share_of(k, it, VEC);
+        size_t at = ((size_t)it.n * k.P + it.p0 + s.row) * k.C + s.c;
+        const size_t step = (size_t)k.rows * k.C;
+        const S* src = X8 ? (const S*)a.codes : (const S*)a.x;
+        Norm<SILU, X8> f[VEC];
+        float sz[VEC], sn[VEC];
+        if (s.count) set_norm<VEC, SILU, X8>(f, a, k, it.n, s.c);
 #pragma unroll
         for (int j = 0; j < VEC; ++j) sz[j] = sn[j] = 0.0f;
-        with_act(a.act, [&](auto act) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (i < s.count)
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) {
-                        const float n = f[j].norm(x_of<X8, S, VEC>(x[i], j, centre, stp));
-                        const float dz = dact<act.value>(f[j].z(n), (float)dy[i].v[j]);
-                        sz[j] += dz;
-                        sn[j] += dz * n;
-                    }
-        });
-        col_reduce(sz, k, a.sub, red, tmp, cz, Add());
-        col_reduce(sn, k, a.sub, red, tmp, cn, Add());
-        for (int c = threadIdx.x; c < k.cb && it.c0 + c < k.C; c += blockDim.x) {
-            float* p = a.part + (((size_t)it.n * k.chunks + it.chunk) * k.C + it.c0 + c) * 2;
-            p[0] = cz[c];
-            p[1] = cn[c];
-        }
-        if constexpr (ONE) {
-            const float inv = 1.0f / ((float)k.P * (float)k.D);
-            auto weight = [&](int c) { return a.gamma ? a.gamma[it.c0 + c] * inv : inv; };
-            group_reduce(k.cb / k.D, k.D, g1, [&](int c) { return cz[c] * weight(c); });
-            group_reduce(k.cb / k.D, k.D, g2, [&](int c) { return cn[c] * weight(c); });
-            float m1[VEC], m2[VEC];
+        auto take = [&](const Held<S, VEC>& x, const Held<T, VEC>& dy) {
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                const int g = (s.col * VEC + j) / k.D;
-                m1[j] = g1[g];
-                m2[j] = g2[g];
+                const float n = f[j].n(x.value(j));
+                const float dz = act_grad<SILU>(f[j].z(n), dy.value(j), a.relu);
+                sz[j] += dz;
+                sn[j] = fmaf(dz, n, sn[j]);
             }
-            with_act(a.act, [&](auto act) {
+        };
+        Held<S, VEC> x[U];
+        Held<T, VEC> dy[U];
+        int i = 0;
+        for (; i + U <= s.count; i += U, at += U * step) {
 #pragma unroll
-                for (int i = 0; i < NV; ++i)
-                    if (i < s.count) {
-                        Raw<T, VEC> o;
+            for (int u = 0; u < U; ++u) {
+                x[u].load(src + at + u * step);
+                dy[u].load((const T*)a.dy + at + u * step);
+            }
 #pragma unroll
-                        for (int j = 0; j < VEC; ++j) {
-                            const float n = f[j].norm(x_of<X8, S, VEC>(x[i], j, centre, stp));
-                            const float dz = dact<act.value>(f[j].z(n), (float)dy[i].v[j]);
-                            o.v[j] = (T)(f[j].rstd * (dz * f[j].gamma - m1[j] - n * m2[j]));
-                        }
-                        *(Raw<T, VEC>*)((T*)a.dx + at + i * step) = o;
-                    }
-            });
+            for (int u = 0; u < U; ++u) take(x[u], dy[u]);
+        }
+        for (; i < s.count; ++i, at += step) {
+            x[0].load(src + at);
+            dy[0].load((const T*)a.dy + at);
+            take(x[0], dy[0]);
+        }
+        join_rows(sz, k, rz, Add());
+        join_rows(sn, k, rn, Add());
+        __syncthreads();
+        for (int c = threadIdx.x; c < k.cb && it.c0 + c < k.C; c += blockDim.x) {
+            Raw<float, 2> o;
+            o.v[0] = join_parts(k, rz, c, Add());
+            o.v[1] = join_parts(k, rn, c, Add());
+            *(Raw<float, 2>*)(a.part + (((size_t)it.n * k.chunks + it.chunk) * k.C + it.c0 + c) * 2) = o;
         }
         __syncthreads();
     }
 }
 
-// means[n][g] = the group's m1, m2 from its channels' parts.  A workgroup an
-// (image, group).
+// Joins the chunks' parts of one image and group: sums[n][c] of dz and dz n, and
+// means[n][g] = m1, m2.  A workgroup an (image, group).
 __global__ __launch_bounds__(256) void k_norm_back_join(const float* __restrict__ part, const float* __restrict__ gamma,
-                                                        float* __restrict__ means, Cut k, int64_t groups) {
-    __shared__ float acc[8];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+                                                        float* __restrict__ sums, float* __restrict__ means, Cut k,
+                                                        int64_t groups) {
+    __shared__ float acc[8], red[2][256];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    // columns of channels, and threads along the chunks
+    int wide = 1;
+    while (wide < 256 && wide < k.D) wide *= 2;
+    const int col = t & (wide - 1), row = t / wide, rows = 256 / wide;
     for (int64_t ng = blockIdx.x; ng < groups; ng += gridDim.x) {
         const int64_t n = ng / k.G;
         const int g = (int)(ng - n * k.G);
         const float* p = part + ((size_t)n * k.chunks * k.C + (size_t)g * k.D) * 2;
-        const float inv = 1.0f / ((float)k.P * (float)k.D);
         float m1 = 0.0f, m2 = 0.0f;
-        for (int64_t i = threadIdx.x; i < (int64_t)k.chunks * k.D; i += 256) {
-            const int64_t ch = i / k.D, d = i - ch * k.D;
-            const float w = gamma ? gamma[(size_t)g * k.D + d] * inv : inv;
-            const float* q = p + ((size_t)ch * k.C + d) * 2;
-            m1 += q[0] * w;
-            m2 += q[1] * w;
+        for (int d0 = 0; d0 < k.D; d0 += wide) {
+            const int d = d0 + col;
+            float z = 0.0f, v = 0.0f;
+            if (d < k.D)
+                for (int ch = row; ch < (int)k.chunks; ch += rows) {
+                    const float* q = p + ((size_t)ch * k.C + d) * 2;
+                    z += q[0];
+                    v += q[1];
+                }
+            __syncthreads();
+            red[0][t] = z;
+            red[1][t] = v;
+            __syncthreads();
+            if (t < wide && d < k.D) {
+                for (int r = 1; r < rows; ++r) {
+                    z += red[0][r * wide + t];
+                    v += red[1][r * wide + t];
+                }
+                float* o = sums + ((size_t)n * k.C + (size_t)g * k.D + d) * 2;
+                o[0] = z;
+                o[1] = v;
+                const float w = gamma ? gamma[(size_t)g * k.D + d] * k.inv : k.inv;
+                m1 += z * w;
+                m2 += v * w;
+            }
         }
         m1 = wave_sum(m1);
         m2 = wave_sum(m2);
@@ -556,71 +752,72 @@ __global__ __launch_bounds__(256) void k_norm_back_join(const float* __restrict_
             acc[wave * 2 + 1] = m2;
         }
         __syncthreads();
-        if (threadIdx.x < 2)
-            means[((size_t)n * k.G + g) * 2 + threadIdx.x] =
-                acc[threadIdx.x] + acc[threadIdx.x + 2] + acc[threadIdx.x + 4] + acc[threadIdx.x + 6];
+        if (t < 2) means[((size_t)n * k.G + g) * 2 + t] = acc[t] + acc[t + 2] + acc[t + 4] + acc[t + 6];
         __syncthreads();
     }
 }
 
-template <typename T, int VEC, bool X8>
+template <typename T, int VEC, bool X8, bool SILU>
 __global__ __launch_bounds__(256) void k_norm_back_apply(BwdArgs a, Cut k) {
     constexpr int U = VEC == 1 ? 8 : 4;
     typedef typename std::conditional<X8, int8_t, T>::type S;
     Item it;
-    for (int64_t vb = blockIdx.x; vb / kXcds < (k.items + kXcds - 1) / kXcds; vb += gridDim.x) {
+    for (uint32_t vb = blockIdx.x; vb < k.per * kXcds; vb += gridDim.x) {
         if (!item_of(vb, k, &it)) continue;
         const Share s = share_of(k, it, VEC);
         if (!s.count) continue;
-        const size_t at = ((size_t)it.n * k.P + it.p0 + s.row) * k.C + s.c, step = (size_t)k.rows * k.C;
-        const S* src = (X8 ? (const S*)a.codes : (const S*)a.x) + at;
-        Affine f[VEC];
-        float centre[VEC], stp[VEC], m1[VEC], m2[VEC];
-        bwd_rows<VEC, X8>(a, k, it.n, s.c, f, centre, stp);
+        size_t at = ((size_t)it.n * k.P + it.p0 + s.row) * k.C + s.c;
+        const size_t step = (size_t)k.rows * k.C;
+        const S* src = X8 ? (const S*)a.codes : (const S*)a.x;
+        Norm<SILU, X8> f[VEC];
+        Grad h[VEC];
+        set_norm<VEC, SILU, X8>(f, a, k, it.n, s.c);
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-            const float* m = a.means + ((size_t)it.n * k.G + (s.c + j) / k.D) * 2;
-            m1[j] = m[0];
-            m2[j] = m[1];
+            const float* m = a.means + ((size_t)it.n * k.G + fdiv(s.c + j, k.dD)) * 2;
+            h[j].set(f[j].rstd, f[j].gamma, m[0], m[1]);
         }
-        with_act(a.act, [&](auto act) {
-            for (int i0 = 0; i0 < s.count; i0 += U) {
-                Raw<T, VEC> dy[U];
-                Raw<S, VEC> x[U];
+        auto give = [&](const Held<S, VEC>& x, const Held<T, VEC>& dy, size_t at) {
+            Raw<T, VEC> o;
 #pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (i0 + u < s.count) {
-                        dy[u] = *(const Raw<T, VEC>*)((const T*)a.dy + at + (i0 + u) * step);
-                        x[u] = *(const Raw<S, VEC>*)(src + (i0 + u) * step);
-                    }
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (i0 + u < s.count) {
-                        Raw<T, VEC> o;
-#pragma unroll
-                        for (int j = 0; j < VEC; ++j) {
-                            const float n = f[j].norm(x_of<X8, S, VEC>(x[u], j, centre, stp));
-                            const float dz = dact<act.value>(f[j].z(n), (float)dy[u].v[j]);
-                            o.v[j] = (T)(f[j].rstd * (dz * f[j].gamma - m1[j] - n * m2[j]));
-                        }
-                        *(Raw<T, VEC>*)((T*)a.dx + at + (i0 + u) * step) = o;
-                    }
+            for (int j = 0; j < VEC; ++j) {
+                const float n = f[j].n(x.value(j));
+                o.v[j] = (T)h[j](act_grad<SILU>(f[j].z(n), dy.value(j), a.relu), n);
             }
-        });
+            put((T*)a.dx + at, o);
+        };
+        Held<S, VEC> x[U];
+        Held<T, VEC> dy[U];
+        int i = 0;
+        for (; i + U <= s.count; i += U, at += U * step) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                x[u].get(src + at + u * step);
+                dy[u].get((const T*)a.dy + at + u * step);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) give(x[u], dy[u], at + u * step);
+        }
+        for (; i < s.count; ++i, at += step) {
+            x[0].get(src + at);
+            dy[0].get((const T*)a.dy + at);
+            give(x[0], dy[0], at);
+        }
     }
 }
 
-// dgamma, dbeta: the parts of every image and chunk, 32 channels a workgroup.
-__global__ __launch_bounds__(256) void k_norm_params(const float* __restrict__ part, float* __restrict__ dgamma,
-                                                     float* __restrict__ dbeta, int64_t lists, int C) {
+// dgamma, dbeta: every image's sums, 32 channels a workgroup.
+__global__ __launch_bounds__(256) void k_norm_params(const float* __restrict__ sums, float* __restrict__ dgamma,
+                                                     float* __restrict__ dbeta, int N, int C) {
     __shared__ float acc[2][8][32];
     const int c = blockIdx.x * 32 + (threadIdx.x & 31), row = threadIdx.x >> 5;
     float z = 0.0f, n = 0.0f;
     if (c < C)
-        for (int64_t i = row; i < lists; i += 8) {
-            const float* p = part + ((size_t)i * C + c) * 2;
-            z += p[0];
-            n += p[1];
+#pragma unroll 4
+        for (int i = row; i < N; i += 8) {
+            const Raw<float, 2> p = *(const Raw<float, 2>*)(sums + ((size_t)i * C + c) * 2);
+            z += p.v[0];
+            n += p.v[1];
         }
     acc[0][row][threadIdx.x & 31] = z;
     acc[1][row][threadIdx.x & 31] = n;
@@ -637,22 +834,28 @@ __global__ __launch_bounds__(256) void k_norm_params(const float* __restrict__ p
 
 // ------------------------------------------------------------------ host
 
+int vector_of(const NormShape& s, bool aligned) { return aligned && s.C % 4 == 0 ? 4 : 1; }
 int64_t gcd(int64_t a, int64_t b) { return b ? gcd(b, a % b) : a; }
-int sub_rows(int threads, int rows, int cb) {
-    int s = 1;
-    while (s * s < rows && (s + 1) * cb <= threads) ++s;
-    return s;
+
+int64_t items_of(const NormShape& s, const NormPlan& p) {
+    return (int64_t)s.N * p.chunks * ((s.C + p.cb - 1) / p.cb);
 }
 
 Cut cut_of(const NormShape& s, const NormPlan& p) {
     Cut k;
     k.C = s.C; k.G = s.G; k.D = s.D;
-    k.cb = p.cb; k.cv = p.cv; k.rows = p.rows;
-    k.ncb = (s.C + p.cb - 1) / p.cb;
-    k.chunks = p.chunks;
+    k.cb = p.cb; k.cv = p.cv; k.rows = p.rows; k.wrows = p.wrows; k.parts = p.parts;
+    k.ncb = (uint32_t)((s.C + p.cb - 1) / p.cb);
+    k.chunks = (uint32_t)p.chunks;
+    k.items = (uint32_t)items_of(s, p);
+    k.per = (k.items + kXcds - 1) / kXcds;
     k.P = s.P;
     k.px = p.px;
-    k.items = (int64_t)s.N * p.chunks * k.ncb;
+    k.dcv = make_fastdiv(p.cv);
+    k.dD = make_fastdiv(s.D);
+    k.dncb = make_fastdiv(k.ncb);
+    k.dchunks = make_fastdiv(k.chunks);
+    k.inv = 1.0f / ((float)s.P * (float)s.D);
     return k;
 }
 
@@ -661,169 +864,187 @@ unsigned blocks_of(int64_t items) {
     return (unsigned)(b < kMaxBlocks ? b : kMaxBlocks);
 }
 
-// The cut of the element-wise pass: 256 threads, 16 pixels a thread.
+// The rows of a workgroup's threads: whole rows by wave where they leave few
+// lanes idle.
+void set_rows(NormPlan* p, int threads, int cv) {
+    p->threads = threads;
+    p->cv = cv;
+    p->cb = cv * p->vec;
+    p->wrows = cv <= 32 && 64 / cv * cv >= 56 ? 64 / cv : 0;
+    p->rows = p->wrows ? threads / 64 * p->wrows : threads / cv;
+    p->parts = p->wrows ? threads / 64 : p->rows;
+}
+
+// Chunks of least to most rows of the workgroup's threads, for about 1024
+// workgroups in all (norm N = 1, 64 channels at 112x112: 13 us with 4 rows, 17 with
+// 16; N = 16, 256 at 56x56: 34 with 12 to 16, 40 with 4).
+void set_chunks(NormPlan* p, const NormShape& s, int64_t least, int64_t most) {
+    const int64_t steps = (s.P + p->rows - 1) / p->rows, ncb = (s.C + p->cb - 1) / p->cb;
+    int64_t per = steps * s.N * ncb / 1024;
+    per = per < least ? least : per > most ? most : per;
+    p->px = per * p->rows;
+    p->chunks = (int)((s.P + p->px - 1) / p->px);
+}
+
+// The cut of the element-wise pass.
 NormPlan apply_plan(const NormShape& s, bool aligned) {
     NormPlan p = {};
-    const int full = 16 / io_size(s.io);
-    p.vec = aligned && s.C % full == 0 ? full : 1;
-    p.threads = 256;
+    p.vec = vector_of(s, aligned);
     const int cols = (s.C + p.vec - 1) / p.vec;
-    p.cv = cols < 256 ? cols : 256;
-    p.cb = p.cv * p.vec;
-    p.rows = 256 / p.cv;
-    p.px = (int64_t)p.rows * 16;
-    p.chunks = (int)((s.P + p.px - 1) / p.px);
+    set_rows(&p, 256, cols < 256 ? cols : 256);
+    set_chunks(&p, s, 4, 16);
     return p;
 }
 
-// f(T, VEC) for the element type and vector width.
+// f(T, VEC, SILU) for the element type, vector width and activation.
 template <typename F>
-void with_type(Io io, int vec, F&& f) {
-    if (io == Io::F32) {
-        if (vec == 1) f(float(), std::integral_constant<int, 1>());
-        else f(float(), std::integral_constant<int, 4>());
-    } else if (io == Io::F16) {
-        if (vec == 1) f(_Float16(), std::integral_constant<int, 1>());
-        else f(_Float16(), std::integral_constant<int, 8>());
-    } else {
-        if (vec == 1) f(__bf16(), std::integral_constant<int, 1>());
-        else f(__bf16(), std::integral_constant<int, 8>());
-    }
+void with_type(const NormShape& s, int vec, F&& f) {
+    auto act = [&](auto t, auto v) {
+        if (s.act == Act::Silu) f(t, v, std::true_type());
+        else f(t, v, std::false_type());
+    };
+    auto go = [&](auto t) {
+        if (vec == 1) act(t, std::integral_constant<int, 1>());
+        else act(t, std::integral_constant<int, 4>());
+    };
+    if (s.io == Io::F32) go(float());
+    else if (s.io == Io::F16) go(_Float16());
+    else go(__bf16());
 }
+
+// Vectors that a thread may hold, of x or of dy and x: up to 32 and up to 72
+// registers, so that a CU has two workgroups at least.
+template <int VEC>
+constexpr int held(bool backward, bool many) {
+    return VEC == 1 ? (many ? 64 : 16) / (backward ? 2 : 1) : backward ? (many ? 9 : 4) : (many ? 16 : 8);
+}
+int held_of(int vec, bool backward, bool many) { return vec == 1 ? held<1>(backward, many) : held<4>(backward, many); }
 
 }  // namespace
 
 NormPlan norm_plan(const NormShape& s, bool backward, bool aligned) {
     NormPlan p = {};
-    const int full = 16 / io_size(s.io);
-    p.vec = aligned && s.C % full == 0 ? full : 1;
-    const int most = (p.vec == 1 ? 64 : 16) / (backward ? 2 : 1);
-    // one pass: whole groups whose image fits the registers
+    p.vec = vector_of(s, aligned);
+    // One pass, where whole groups' image fits a workgroup's registers, 64 bytes of a
+    // pixel at least: with 32 the caches move half lines (N = 64, 256 channels at
+    // 56x56: 237 us, in three launches 106), which pays only as long as the workgroups
+    // are few (N = 1: 12 and 16, N = 4: 18 and 20).  N = 32, 512 channels at 14x14: 9 us
+    // in one pass, 19 in three launches.
     const int64_t unit = (int64_t)s.D / gcd(s.D, p.vec) * p.vec;
-    for (int64_t k = 1; !p.one && unit * k <= 1024 && unit * k <= s.C; ++k) {
-        if (s.C % (unit * k)) continue;
-        const int64_t cb = unit * k;
-        if (cb * io_size(s.io) < 32 && cb < s.C && cb < 1024 && s.P * cb / p.vec < 256 * most) continue;
-        for (int threads = 256; threads <= 1024 && !p.one; threads *= 2) {
-            const int cv = (int)(cb / p.vec);
-            if (cv > threads) continue;
-            const int rows = threads / cv;
-            for (int nv = most / 4; nv <= most && !p.one; nv *= 4) {
-                if (s.P > (int64_t)rows * nv) continue;
-                p.one = true;
-                p.nv = nv;
-                p.threads = threads;
-                p.cb = (int)cb;
-                p.cv = cv;
-                p.rows = rows;
-                p.chunks = 1;
-                p.px = s.P;
+    for (int64_t cb = unit; !p.one && cb <= 512 && cb <= s.C; cb += unit) {
+        const bool wide = cb * io_size(s.io) >= 64 || cb == s.C;
+        if (s.C % cb || cb / p.vec > kMaxThreads || (!wide && s.N * (s.C / cb) > 128)) continue;
+        for (int threads = 256; threads <= kMaxThreads && !p.one; threads *= 2)
+            for (int many = 0; many < 2 && !p.one && cb / p.vec <= threads; ++many) {
+                set_rows(&p, threads, (int)(cb / p.vec));
+                p.nv = held_of(p.vec, backward, many);
+                p.one = s.P <= (int64_t)p.rows * p.nv;
             }
-        }
     }
-    if (!p.one) {
-        p.threads = 256;
-        p.nv = most;
+    if (p.one) {
+        p.chunks = 1;
+        p.px = s.P;
+    } else {
         const int cols = (s.C + p.vec - 1) / p.vec;
-        p.cv = cols < 128 ? cols : 128;
-        p.cb = p.cv * p.vec;
-        p.rows = p.threads / p.cv;
-        p.px = (int64_t)p.rows * p.nv;
-        p.chunks = (int)((s.P + p.px - 1) / p.px);
+        set_rows(&p, 256, cols < 128 ? cols : 128);
+        set_chunks(&p, s, 4, 1 << 20);
     }
-    const int sub = sub_rows(p.threads, p.rows, p.cb);
-    p.lds = ((size_t)p.rows * p.cb + (size_t)sub * p.cb + 5 * (size_t)p.cb) * sizeof(float);
-    const size_t lists = (size_t)s.N * p.chunks * s.C, groups = (size_t)s.N * s.G * 2 * sizeof(float);
-    if (backward) p.need = lists * 2 * sizeof(float) + (p.one ? 0 : groups);
-    else p.need = p.one ? 0 : (lists * 4 + (size_t)s.N * s.C) * sizeof(float) + groups;
+    p.lds = ((backward ? 2 : 3) * (size_t)p.parts + 4) * p.cb * sizeof(float);
+    const size_t lists = (size_t)s.N * p.chunks * s.C, all = (size_t)s.N * s.C, groups = (size_t)s.N * s.G * 2;
+    p.need = (backward ? all * 2 + (p.one ? 0 : lists * 2 + groups) : p.one ? 0 : lists * 4 + all + groups) * sizeof(float);
+    p.fits = items_of(s, p) < (int64_t)1 << 30 && items_of(s, apply_plan(s, aligned)) < (int64_t)1 << 30;
     return p;
 }
 
 hipError_t launch_norm_apply(const NormApply& a, const NormShape& s, bool aligned, hipStream_t st) {
     const NormPlan p = apply_plan(s, aligned);
     const Cut k = cut_of(s, p);
-    const ApplyArgs g{a.x, a.codes, a.rows, a.stats, a.gamma, a.beta, a.y, nullptr, nullptr, s.act};
-    with_type(s.io, p.vec, [&](auto t, auto vec) {
+    const ApplyArgs g{a.x, a.codes, a.rows, a.stats, a.gamma, a.beta, a.y, nullptr, nullptr, s.act == Act::Relu};
+    with_type(s, p.vec, [&](auto t, auto vec, auto silu) {
         typedef decltype(t) T;
-        if (a.codes) k_norm_apply<T, vec.value, true><<<blocks_of(k.items), 256, 0, st>>>(g, k);
-        else k_norm_apply<T, vec.value, false><<<blocks_of(k.items), 256, 0, st>>>(g, k);
+        if (a.codes) k_norm_apply<T, vec.value, true, silu.value><<<blocks_of(k.items), 256, 0, st>>>(g, k);
+        else k_norm_apply<T, vec.value, false, silu.value><<<blocks_of(k.items), 256, 0, st>>>(g, k);
     });
     return hipGetLastError();
 }
 
 hipError_t launch_norm(const NormFwd& a, const NormShape& s, const NormPlan& p, void* ws, hipStream_t st) {
     const Cut k = cut_of(s, p);
+    const bool relu = s.act == Act::Relu;
+    if (p.one) {
+        const FwdArgs g{a.x, a.gamma, a.beta, a.y, a.stats, a.codes, a.rows, nullptr, a.eps, relu};
+        with_type(s, p.vec, [&](auto t, auto vec, auto silu) {
+            typedef decltype(t) T;
+            constexpr int V = vec.value;
+            constexpr bool SILU = silu.value;
+            const unsigned b = blocks_of(k.items);
+            if (p.nv == held<V>(false, true)) k_norm<T, V, held<V>(false, true), SILU><<<b, p.threads, p.lds, st>>>(g, k);
+            else k_norm<T, V, held<V>(false, false), SILU><<<b, p.threads, p.lds, st>>>(g, k);
+        });
+        return hipGetLastError();
+    }
+    const Cut kq = cut_of(s, apply_plan(s, p.vec > 1));
+    const int64_t groups = (int64_t)s.N * s.G;
     float* part = (float*)ws;
     float* inverse = part + (size_t)s.N * p.chunks * s.C * 4;
     float* own = inverse + (size_t)s.N * s.C;                  // the statistics, where the caller wants none
-    const FwdArgs g{a.x, a.gamma, a.beta, a.y, a.stats, a.codes, a.rows, part, a.eps, s.act,
-                    sub_rows(p.threads, p.rows, p.cb)};
-    with_type(s.io, p.vec, [&](auto t, auto vec) {
+    float* stats = a.stats ? a.stats : a.y ? own : nullptr;
+    const FwdArgs g{a.x, a.gamma, a.beta, a.y, stats, a.codes, a.rows, part, a.eps, relu};
+    const ApplyArgs h{a.x, nullptr, a.rows, a.y ? stats : nullptr, a.gamma, a.beta, a.y, a.codes, inverse, relu};
+    hipError_t e = hipSuccess;
+    with_type(s, p.vec, [&](auto t, auto vec, auto silu) {
         typedef decltype(t) T;
-        constexpr int V = vec.value, most = V == 1 ? 64 : 16;
-        const unsigned b = blocks_of(k.items);
-        if (!p.one) k_norm<T, V, most, false><<<b, p.threads, p.lds, st>>>(g, k);
-        else if (p.nv == most) k_norm<T, V, most, true><<<b, p.threads, p.lds, st>>>(g, k);
-        else k_norm<T, V, most / 4, true><<<b, p.threads, p.lds, st>>>(g, k);
+        if (a.codes) k_norm_part<T, vec.value, true><<<blocks_of(k.items), p.threads, p.lds, st>>>(g, k);
+        else k_norm_part<T, vec.value, false><<<blocks_of(k.items), p.threads, p.lds, st>>>(g, k);
+        e = hipGetLastError();
+        if (e != hipSuccess) return;
+        k_norm_join<<<blocks_of(groups), 256, 0, st>>>(part, stats, a.codes ? a.rows : nullptr, inverse, k, groups, a.eps);
+        e = hipGetLastError();
+        if (e != hipSuccess || (!a.y && !a.codes)) return;
+        k_norm_apply<T, vec.value, false, silu.value><<<blocks_of(kq.items), 256, 0, st>>>(h, kq);
+        e = hipGetLastError();
     });
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || p.one) return e;
-    const bool norm = a.y || a.stats;
-    float* stats = a.stats ? a.stats : own;
-    k_norm_join<<<blocks_of((int64_t)s.N * s.G), 256, 0, st>>>(part, norm ? stats : nullptr,
-                                                              a.codes ? a.rows : nullptr, inverse, k, (int64_t)s.N * s.G,
-                                                              a.eps);
-    e = hipGetLastError();
-    if (e != hipSuccess || (!a.y && !a.codes)) return e;
-    const NormPlan q = apply_plan(s, p.vec > 1);
-    const Cut kq = cut_of(s, q);
-    const ApplyArgs h{a.x, nullptr, a.rows, a.y ? stats : nullptr, a.gamma, a.beta, a.y, a.codes, inverse,
-                      s.act};
-    with_type(s.io, q.vec, [&](auto t, auto vec) {
-        typedef decltype(t) T;
-        k_norm_apply<T, vec.value, false><<<blocks_of(kq.items), 256, 0, st>>>(h, kq);
-    });
-    return hipGetLastError();
+    return e;
 }
 
 hipError_t launch_norm_backward(const NormBwd& a, const NormShape& s, const NormPlan& p, void* ws, hipStream_t st) {
+    const bool x8 = a.codes != nullptr, relu = s.act == Act::Relu;
     const Cut k = cut_of(s, p);
-    float* part = (float*)ws;
-    float* means = part + (size_t)s.N * p.chunks * s.C * 2;
-    const BwdArgs g{a.dy, a.x, a.codes, a.rows, a.stats, a.gamma, a.beta, a.dx, part, means, s.act,
-                    sub_rows(p.threads, p.rows, p.cb)};
-    const bool x8 = a.codes != nullptr;
-    with_type(s.io, p.vec, [&](auto t, auto vec) {
+    float* sums = (float*)ws;                                  // [N][C][2]
+    float* part = p.one ? sums : sums + (size_t)s.N * s.C * 2;
+    float* means = p.one ? nullptr : part + (size_t)s.N * p.chunks * s.C * 2;
+    const BwdArgs g{a.dy, a.x, a.codes, a.rows, a.stats, a.gamma, a.beta, a.dx, part, means, relu};
+    hipError_t e = hipSuccess;
+    with_type(s, p.vec, [&](auto t, auto vec, auto silu) {
         typedef decltype(t) T;
-        constexpr int V = vec.value, most = V == 1 ? 64 : 16;
+        constexpr int V = vec.value;
+        constexpr bool SILU = silu.value;
         const unsigned b = blocks_of(k.items);
-        auto go = [&](auto c8) {
-            constexpr bool X8 = c8.value;
-            if (!p.one) k_norm_back<T, V, most / 2, X8, false><<<b, p.threads, p.lds, st>>>(g, k);
-            else if (p.nv == most / 2) k_norm_back<T, V, most / 2, X8, true><<<b, p.threads, p.lds, st>>>(g, k);
-            else k_norm_back<T, V, most / 8, X8, true><<<b, p.threads, p.lds, st>>>(g, k);
+        auto go = [&](auto codes) {
+            constexpr bool X8 = codes.value;
+            if (p.one) {
+                constexpr int few = held<V>(true, false), most = held<V>(true, true);
+                if (p.nv == most) k_norm_back<T, V, most, X8, SILU><<<b, p.threads, p.lds, st>>>(g, k);
+                else k_norm_back<T, V, few, X8, SILU><<<b, p.threads, p.lds, st>>>(g, k);
+                e = hipGetLastError();
+                return;
+            }
+            const Cut kq = cut_of(s, apply_plan(s, V > 1));
+            const int64_t groups = (int64_t)s.N * s.G;
+            k_norm_back_part<T, V, X8, SILU><<<b, p.threads, p.lds, st>>>(g, k);
+            e = hipGetLastError();
+            if (e != hipSuccess) return;
+            k_norm_back_join<<<blocks_of(groups), 256, 0, st>>>(part, a.gamma, sums, means, k, groups);
+            e = hipGetLastError();
+            if (e != hipSuccess) return;
+            k_norm_back_apply<T, V, X8, SILU><<<blocks_of(kq.items), 256, 0, st>>>(g, kq);
+            e = hipGetLastError();
         };
         if (x8) go(std::true_type());
         else go(std::false_type());
     });
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    if (!p.one) {
-        k_norm_back_join<<<blocks_of((int64_t)s.N * s.G), 256, 0, st>>>(part, a.gamma, means, k, (int64_t)s.N * s.G);
-        e = hipGetLastError();
-        if (e != hipSuccess) return e;
-        const NormPlan q = apply_plan(s, p.vec > 1);
-        const Cut kq = cut_of(s, q);
-        with_type(s.io, q.vec, [&](auto t, auto vec) {
-            typedef decltype(t) T;
-            if (x8) k_norm_back_apply<T, vec.value, true><<<blocks_of(kq.items), 256, 0, st>>>(g, kq);
-            else k_norm_back_apply<T, vec.value, false><<<blocks_of(kq.items), 256, 0, st>>>(g, kq);
-        });
-        e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    if (a.dgamma || a.dbeta)
-        k_norm_params<<<(s.C + 31) / 32, 256, 0, st>>>(part, a.dgamma, a.dbeta, (int64_t)s.N * p.chunks, s.C);
+    if (e != hipSuccess || (!a.dgamma && !a.dbeta)) return e;
+    k_norm_params<<<(s.C + 31) / 32, 256, 0, st>>>(sums, a.dgamma, a.dbeta, s.N, s.C);
     return hipGetLastError();
 }
 

@@ -46,12 +46,12 @@ bool disjoint(const Buf (&b)[n]) {
 
 // The larger of what aligned and unaligned tensors need.
 size_t norm_need(const NormShape& s, bool backward) {
-    const size_t a = norm_plan(s, backward, true).need, b = norm_plan(s, backward, false).need;
-    return a > b ? a : b;
+    const NormPlan a = norm_plan(s, backward, true), b = norm_plan(s, backward, false);
+    return !a.fits || !b.fits ? (size_t)-1 : a.need > b.need ? a.need : b.need;
 }
 
 int space(const void* ws, size_t bytes, size_t need) {
-    return need && (!ws || bytes < need) ? WINO_ERR_WORKSPACE : ((uintptr_t)ws & 3) ? WINO_ERR_INVALID_ARG : WINO_OK;
+    return need && (!ws || bytes < need) ? WINO_ERR_WORKSPACE : !aligned16(ws) ? WINO_ERR_INVALID_ARG : WINO_OK;
 }
 
 float* rows_of(const void* q, const NormShape& s) { return (float*)((char*)q + act8_rows_at(s)); }
@@ -94,6 +94,7 @@ int wino_act8_pack_nhwc(const void* x, void* q, int N, int C, int H, int W, unsi
     if (st != WINO_OK) return st;
     if (flags & ~WINO_IO_MASK) return WINO_ERR_UNSUPPORTED;
     const NormPlan p = norm_plan(s, false, aligned16(x));
+    if (!p.fits) return WINO_ERR_UNSUPPORTED;
     const int sp = space(workspace, workspace_bytes, p.need);
     if (sp != WINO_OK) return sp;
     const Buf bufs[] = {{x, tensor_bytes(s), false}, {q, act8_size(s), true}, {workspace, p.need, true}};
@@ -110,6 +111,7 @@ int wino_act8_unpack_nhwc(const void* q, void* x, int N, int C, int H, int W, un
     if (flags & ~WINO_IO_MASK) return WINO_ERR_UNSUPPORTED;
     const Buf bufs[] = {{x, tensor_bytes(s), true}, {q, act8_size(s), false}};
     if (!disjoint(bufs)) return WINO_ERR_INVALID_ARG;
+    if (!norm_plan(s, false, aligned16(x)).fits) return WINO_ERR_UNSUPPORTED;
     const NormApply a{nullptr, (const int8_t*)q, rows_of(q, s), nullptr, nullptr, nullptr, x};
     return hip_status(launch_norm_apply(a, s, aligned16(x), (hipStream_t)stream));
 }
@@ -127,6 +129,7 @@ int wino_group_norm_nhwc(const void* x, const float* gamma, const float* beta, v
     const int st = make_shape(N, C, H, W, G, flags, 0, &s);
     if (st != WINO_OK) return st;
     const NormPlan p = norm_plan(s, false, aligned16(x) && aligned16(y));
+    if (!p.fits) return WINO_ERR_UNSUPPORTED;
     const int sp = space(workspace, workspace_bytes, p.need);
     if (sp != WINO_OK) return sp;
     const size_t row = (size_t)C * sizeof(float);
@@ -149,6 +152,7 @@ int wino_group_norm_apply_nhwc(const void* x, const float* stats, const float* g
     const Buf bufs[] = {{x, x8 ? act8_size(s) : tensor_bytes(s), false}, {gamma, row, false}, {beta, row, false},
                         {stats, (size_t)N * G * 2 * sizeof(float), false}, {y, tensor_bytes(s), true}};
     if (!disjoint(bufs)) return WINO_ERR_INVALID_ARG;
+    if (!norm_plan(s, false, aligned16(x) && aligned16(y)).fits) return WINO_ERR_UNSUPPORTED;
     const NormApply a{x8 ? nullptr : x, x8 ? (const int8_t*)x : nullptr, x8 ? rows_of(x, s) : nullptr, stats, gamma,
                       beta, y};
     return hip_status(launch_norm_apply(a, s, aligned16(x) && aligned16(y), (hipStream_t)stream));
@@ -168,6 +172,7 @@ int wino_group_norm_backward_nhwc(const void* dy, const void* x, const float* st
     const int st = make_shape(N, C, H, W, G, flags, WINO_FLAG_ACT8, &s);
     if (st != WINO_OK) return st;
     const NormPlan p = norm_plan(s, true, aligned16(x) && aligned16(dy) && aligned16(dx));
+    if (!p.fits) return WINO_ERR_UNSUPPORTED;
     const int sp = space(workspace, workspace_bytes, p.need);
     if (sp != WINO_OK) return sp;
     const size_t row = (size_t)C * sizeof(float), all = tensor_bytes(s);

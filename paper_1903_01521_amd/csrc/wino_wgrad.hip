@@ -20,15 +20,16 @@ __device__ __forceinline__ float a_value(const WgradArgs& a, const WgradShape& s
     float v;
     if constexpr (X8) {
         const float* r = a.rows + ((size_t)n * s.C + c) * 2;
-        v = value_of(a.codes[at], r[0], r[1]);
+        v = value_of((float)a.codes[at], r[0], r[1]);
     } else {
         v = (float)((const T*)a.x)[at];
     }
     if constexpr (NORM) {
         const float* st = a.stats + ((size_t)n * s.G + c / s.D) * 2;
-        const Affine f{st[0], st[1], a.gamma ? a.gamma[c] : 1.0f, a.beta ? a.beta[c] : 0.0f};
-        const float z = f.z(f.norm(v));
-        v = s.act == Act::Silu ? act_of<Act::Silu>(z) : s.act == Act::Relu ? act_of<Act::Relu>(z) : z;
+        Norm<false, false> f;
+        f.set(st, a.gamma ? a.gamma[c] : 1.0f, a.beta ? a.beta[c] : 0.0f, nullptr);
+        const float z = f.z(f.n(v));
+        v = s.act == Act::Silu ? act_of<true>(z, false) : act_of<false>(z, s.act == Act::Relu);
     }
     return v;
 }
