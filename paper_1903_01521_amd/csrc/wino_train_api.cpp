@@ -68,7 +68,8 @@ int make_wgrad(int N, int C, int H, int W, int K, int pad, unsigned flags, Wgrad
     s->norm = false;
     s->x8 = (flags & WINO_FLAG_ACT8) != 0;
     s->G = s->D = 1;
-    return flags_of(flags, WINO_FLAG_ACT8, &s->io, &s->act);
+    const int st = flags_of(flags, WINO_FLAG_ACT8, &s->io, &s->act);
+    return st != WINO_OK ? st : wgrad_fits(*s) ? WINO_OK : WINO_ERR_UNSUPPORTED;
 }
 
 }  // namespace

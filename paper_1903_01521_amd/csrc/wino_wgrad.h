@@ -21,6 +21,7 @@ struct WgradArgs {
     float* dg;                               // [K][C][3][3]
 };
 
+bool wgrad_fits(const WgradShape& s);        // offsets and counts that the kernel handles
 size_t wgrad_workspace(const WgradShape& s);
 hipError_t launch_wgrad(const WgradArgs& a, const WgradShape& s, void* ws, hipStream_t st);
 

@@ -2,10 +2,25 @@
 //   dg[k][c][r][s] = sum over n, i, j of a[n][i + r - pad][j + s - pad][c] dy[n][i][j][k]
 // with a the layer's input, read as zero outside the image: x, a checkpoint's
 // values, or act(norm(either)) formed on load.
+//
+// Nine products over the pixels, on the 16-bit matrix cores.  Their operands have
+// the summed index innermost, eight values of it a lane, while channel-last tensors
+// have it outermost, and the nine taps need it shifted.  Both are met by summing over
+// pixels of eight different images at once (of eight bands of rows, where the batch is
+// no multiple of eight): a lane's eight values are one pixel of eight images, so every
+// tap reads whole 16-byte words, only from another row or column, and the transpose
+// happens in the registers that the eight loads fill.
+//
+// fp32 operands are held in two bf16 terms (16 significand bits), and three of the
+// four products are summed in fp32: a product is off by 2^-16 at most, the result by
+// about 4e-6 of its norm, which is what the F(4x4,3x3) layers are off by; three terms
+// would take six products.  fp16 values are exact in two terms, bf16 ones in one, and
+// fp16 by fp16 runs on the fp16 matrix cores; an input formed on load has two.
 #include <math.h>
 
 #include <type_traits>
 
+#include "wino_device.h"
 #include "wino_norm_device.h"
 #include "wino_wgrad.h"
 
@@ -13,103 +28,422 @@ namespace wino {
 
 namespace {
 
-// a at (n, pixel, c)
-template <typename T, bool X8, bool NORM>
-__device__ __forceinline__ float a_value(const WgradArgs& a, const WgradShape& s, int n, int64_t pixel, int c) {
-    const size_t at = ((size_t)n * s.H * s.W + pixel) * s.C + c;
-    float v;
-    if constexpr (X8) {
-        const float* r = a.rows + ((size_t)n * s.C + c) * 2;
-        v = value_of((float)a.codes[at], r[0], r[1]);
-    } else {
-        v = (float)((const T*)a.x)[at];
+constexpr int kSeg = 8;                       // images or bands that a lane sums over
+
+// How the pixels are walked: segments of `hb` output rows (2^lb to an image), eight
+// segments an octet, strips of columns, and in a strip row by row.
+struct Walk {
+    int lb, hb, segs, strips;
+    int64_t rows;                             // octets * strips * hb
+    int slices, ctiles, ktiles;
+    FastDiv dstrips, dhb;
+};
+
+struct Args {
+    WgradArgs a;
+    WgradShape s;
+    Walk w;
+    float* part;                              // [slices][9][C][K]
+};
+
+// 16-byte words of eight values' terms: hi, and with two terms what is left.
+template <bool F16, int TERMS>
+__device__ __forceinline__ void split8(const float (&v)[kSeg], uint4 (&o)[TERMS]) {
+    typedef typename std::conditional<F16, _Float16, __bf16>::type H;
+    typedef H h8 __attribute__((ext_vector_type(8)));
+    h8 hi;
+#pragma unroll
+    for (int e = 0; e < kSeg; ++e) hi[e] = (H)v[e];
+    o[0] = __builtin_bit_cast(uint4, hi);
+    if constexpr (TERMS == 2) {
+        h8 lo;
+#pragma unroll
+        for (int e = 0; e < kSeg; ++e) lo[e] = (H)(v[e] - (float)hi[e]);
+        o[1] = __builtin_bit_cast(uint4, lo);
     }
-    if constexpr (NORM) {
-        const float* st = a.stats + ((size_t)n * s.G + c / s.D) * 2;
-        Norm<false, false> f;
-        f.set(st, a.gamma ? a.gamma[c] : 1.0f, a.beta ? a.beta[c] : 0.0f, nullptr);
-        const float z = f.z(f.n(v));
-        v = s.act == Act::Silu ? act_of<true>(z, false) : act_of<false>(z, s.act == Act::Relu);
-    }
-    return v;
 }
 
-// 16 channels x 16 filters a workgroup, a thread a pair; rows of the batch
-// [r0, r1) by slice; part [slices][9][C][K].
-template <typename T, bool X8, bool NORM>
-__global__ __launch_bounds__(256) void k_wgrad(WgradArgs a, WgradShape s, float* part, int slices) {
-    __shared__ float la[3][18][16], ld[16][16];
-    const int kt = (s.K + 15) / 16, ct = (s.C + 15) / 16;
-    const int slice = blockIdx.x / (kt * ct), tile = blockIdx.x % (kt * ct);
-    const int c0 = tile / kt * 16, k0 = tile % kt * 16;
-    const int lo = threadIdx.x & 15, hi = threadIdx.x >> 4;
-    const int64_t all = (int64_t)s.N * s.Ho, r0 = all * slice / slices, r1 = all * (slice + 1) / slices;
-    float acc[9] = {};
-    for (int64_t row = r0; row < r1; ++row) {
-        const int n = (int)(row / s.Ho), i = (int)(row % s.Ho);
-        for (int j0 = 0; j0 < s.Wo; j0 += 16) {
-            __syncthreads();
-            for (int e = threadIdx.x; e < 3 * 18 * 16; e += 256) {
-                const int c = c0 + e % 16, col = j0 + e / 16 % 18 - s.pad, y = i + e / (16 * 18) - s.pad;
-                const bool in = c < s.C && col >= 0 && col < s.W && y >= 0 && y < s.H;
-                la[e / (16 * 18)][e / 16 % 18][e % 16] =
-                    in ? a_value<T, X8, NORM>(a, s, n, (int64_t)y * s.W + col, c) : 0.0f;
+// One step of the walk: local row t of a strip of an octet; below the first row of
+// the range only the input's row is fetched.
+struct Step {
+    int oct, strip, t, end;                   // rows up to `end`
+    bool active;
+};
+
+// WC waves of 16 channels, by KW waves of 64 filters or KS waves of 4 columns each.
+// T: the tensors' type; TA, TB: terms of the input and of dy.
+template <typename T, bool X8, bool NORM, int WC, int KW, int KS>
+struct Wgrad {
+    static constexpr bool kF16 = std::is_same<T, _Float16>::value && !X8 && !NORM;
+    static constexpr int TA = kF16 || (std::is_same<T, __bf16>::value && !X8 && !NORM) ? 1 : 2;
+    static constexpr int TB = kF16 || std::is_same<T, __bf16>::value ? 1 : 2;
+    static constexpr int kWaves = WC * KW * KS, kThreads = kWaves * 64;
+    static constexpr int CT = 16 * WC, KT = 64 * KW, kCols = 4 * KS, kACols = kCols + 2;
+    static constexpr int kAItems = kACols * CT / 64, kItems = kAItems + kCols * KT / 64;
+    static constexpr int kPer = (kItems + kWaves - 1) / kWaves;       // items a wave loads
+    typedef typename std::conditional<X8, int8_t, T>::type S;
+
+    struct Lds {
+        uint4 a[4][TA][kACols][CT];           // ring of input rows
+        uint4 d[2][TB][kCols][KT];
+        float2 f[2][kSeg][CT];                // the channels' norm, by image, of this octet and the next
+    };
+
+    const Args& g;
+    Lds& l;
+    const int wave, lane, c0, k0;
+    int64_t row, row1;                        // rows still to be entered
+    Step next;                                // the step fetched last or next
+    int first;                                // its strip's first active row
+    uint32_t raw[kPer][kSeg];
+    uint32_t ok[kPer];                        // which of the eight are inside the image
+    f32x4 acc[9][4];
+
+    __device__ __forceinline__ Wgrad(const Args& args, Lds& lds, int c, int k, int64_t r0, int64_t r1)
+        : g(args), l(lds), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), lane(threadIdx.x & 63), c0(c), k0(k),
+          row(r0), row1(r1) {}
+
+    // The steps of rows [row, row1): of each strip's share two rows more.
+    __device__ __forceinline__ bool enter() {
+        if (row >= row1) return false;
+        const int unit = (int)fdiv((uint32_t)row, g.w.dhb), t = (int)(row - (int64_t)unit * g.w.hb);
+        next.oct = (int)fdiv(unit, g.w.dstrips);
+        next.strip = unit - next.oct * g.w.strips;
+        next.end = row1 - row < g.w.hb - t ? t + (int)(row1 - row) : g.w.hb;
+        next.t = t - 2;
+        next.active = false;
+        row += next.end - t;
+        first = t;
+        return true;
+    }
+    __device__ __forceinline__ bool advance() {
+        if (next.t + 1 < next.end) {
+            ++next.t;
+            next.active = next.t >= first;
+            return true;
+        }
+        return enter();
+    }
+
+    // The norm's constants of an octet: z = v scale + shift.
+    __device__ __forceinline__ void fill_norm(int oct) {
+        if constexpr (NORM) {
+            for (int i = threadIdx.x; i < kSeg * CT; i += kThreads) {
+                const int e = i / CT, c = c0 + i % CT, seg = oct * kSeg + e;
+                float2 f = make_float2(0.0f, 0.0f);
+                if (c < g.s.C && seg < g.w.segs) {
+                    const int n = seg >> g.w.lb;
+                    const float* st = g.a.stats + ((size_t)n * g.s.G + c / g.s.D) * 2;
+                    const float* r = X8 ? g.a.rows + ((size_t)n * g.s.C + c) * 2 : nullptr;
+                    const float gamma = g.a.gamma ? g.a.gamma[c] : 1.0f, beta = g.a.beta ? g.a.beta[c] : 0.0f;
+                    f.x = st[1] * gamma * (X8 ? r[1] : 1.0f);
+                    f.y = fmaf((X8 ? r[0] : 0.0f) - st[0], st[1] * gamma, beta);
+                }
+                l.f[oct & 1][e][i % CT] = f;
             }
-            const int j = j0 + hi, k = k0 + lo;
-            ld[hi][lo] = j < s.Wo && k < s.K
-                             ? (float)((const T*)a.dy)[(((size_t)n * s.Ho + i) * s.Wo + j) * s.K + k]
-                             : 0.0f;
-            __syncthreads();
-            for (int p = 0; p < 16; ++p) {
-                const float d = ld[p][lo];
-#pragma unroll
-                for (int t = 0; t < 9; ++t) acc[t] += la[t / 3][p + t % 3][hi] * d;
+        } else if constexpr (X8) {
+            for (int i = threadIdx.x; i < kSeg * CT; i += kThreads) {
+                const int e = i / CT, c = c0 + i % CT, seg = oct * kSeg + e;
+                const float* r = g.a.rows + ((size_t)(seg >> g.w.lb) * g.s.C + c) * 2;
+                l.f[oct & 1][e][i % CT] = c < g.s.C && seg < g.w.segs ? make_float2(r[1], r[0]) : make_float2(0.0f, 0.0f);
             }
         }
     }
-    const int c = c0 + hi, k = k0 + lo;
-    if (c < s.C && k < s.K)
-        for (int t = 0; t < 9; ++t) part[(((size_t)slice * 9 + t) * s.C + c) * s.K + k] = acc[t];
+
+    // Loads of step `next` into raw: the input's row t + 2 of the strip's columns and
+    // one more on each side, dy's row t.  A lane takes one column and channel, of the
+    // eight segments.
+    __device__ __forceinline__ void fetch() {
+#pragma unroll
+        for (int p = 0; p < kPer; ++p) {
+            const int item = wave + p * kWaves;
+            const bool input = item < kAItems;
+            if (item >= kItems || (!input && !next.active)) continue;
+            // column of the image and channel, and the rows of the eight segments
+            const int at = input ? item * 64 + lane : (item - kAItems) * 64 + lane;
+            const int col = next.strip * kCols + (input ? at / CT - g.s.pad : at / KT);
+            const int ch = input ? c0 + at % CT : k0 + at % KT;
+            const int wide = input ? g.s.W : g.s.Wo, high = input ? g.s.H : g.s.Ho, chs = input ? g.s.C : g.s.K;
+            const bool inside = col >= 0 && col < wide && ch < chs;
+            const uint32_t off = inside ? (uint32_t)col * chs + ch : 0;
+            ok[p] = 0;
+#pragma unroll
+            for (int e = 0; e < kSeg; ++e) {
+                const int seg = next.oct * kSeg + e, n = seg >> g.w.lb, top = (seg & ((1 << g.w.lb) - 1)) * g.w.hb + next.t;
+                const int y = input ? top + 2 - g.s.pad : top;
+                raw[p][e] = 0;
+                if (seg < g.w.segs && y >= 0 && y < high) {
+                    const size_t base = ((size_t)n * high + y) * wide * chs;
+                    if (inside) {
+                        if (input) {
+                            const S* q = (X8 ? (const S*)g.a.codes : (const S*)g.a.x) + base;
+                            raw[p][e] = sizeof(S) == 4 ? ((const uint32_t*)q)[off] : sizeof(S) == 2 ? ((const uint16_t*)q)[off]
+                                                                                                      : ((const uint8_t*)q)[off];
+                        } else {
+                            const T* q = (const T*)g.a.dy + base;
+                            raw[p][e] = sizeof(T) == 4 ? ((const uint32_t*)q)[off] : ((const uint16_t*)q)[off];
+                        }
+                        ok[p] |= 1u << e;
+                    }
+                }
+            }
+        }
+    }
+
+    template <typename V>
+    static __device__ __forceinline__ float value(uint32_t w) {
+        Held<V, 1> h;
+        h.w[0] = w;
+        return h.value(0);
+    }
+
+    // The fetched values to LDS, in terms: `slot` of the ring, buffer slot & 1 of dy.
+    __device__ __forceinline__ void store(int slot, const Step& s) {
+#pragma unroll
+        for (int p = 0; p < kPer; ++p) {
+            const int item = wave + p * kWaves;
+            const bool input = item < kAItems;
+            if (item >= kItems || (!input && !s.active)) continue;
+            float v[kSeg];
+            if (input) {
+                const int at = item * 64 + lane, c = at % CT;
+#pragma unroll
+                for (int e = 0; e < kSeg; ++e) {
+                    v[e] = value<S>(raw[p][e]);
+                    if constexpr (X8 || NORM) {
+                        const float2 f = l.f[s.oct & 1][e][c];
+                        v[e] = fmaf(v[e], f.x, f.y);
+                        if constexpr (NORM) v[e] = g.s.act == Act::Silu ? act_of<true>(v[e], false) : act_of<false>(v[e], g.s.act == Act::Relu);
+                        v[e] = ok[p] >> e & 1 ? v[e] : 0.0f;
+                    }
+                }
+                uint4 o[TA];
+                split8<kF16, TA>(v, o);
+#pragma unroll
+                for (int t = 0; t < TA; ++t) l.a[slot & 3][t][at / CT][c] = o[t];
+            } else {
+                const int at = (item - kAItems) * 64 + lane;
+#pragma unroll
+                for (int e = 0; e < kSeg; ++e) v[e] = value<T>(raw[p][e]);
+                uint4 o[TB];
+                split8<kF16, TB>(v, o);
+#pragma unroll
+                for (int t = 0; t < TB; ++t) l.d[slot & 1][t][at / KT][at % KT] = o[t];
+            }
+        }
+    }
+
+    // The nine taps of step `slot`: input rows of the last three steps.
+    __device__ __forceinline__ void multiply(int slot) {
+        const int wc = wave % WC, wk = wave / WC, ks = KS > 1 ? wk : 0, kw = KS > 1 ? 0 : wk;
+        const int col = ks * 4 + (lane >> 4), c = wc * 16 + (lane & 15);
+        uint4 b[4][TB];
+#pragma unroll
+        for (int f = 0; f < 4; ++f)
+#pragma unroll
+            for (int t = 0; t < TB; ++t) b[f][t] = l.d[slot & 1][t][col][kw * 64 + f * 16 + (lane & 15)];
+        uint4 a[TA];
+#pragma unroll
+        for (int t = 0; t < TA; ++t) a[t] = l.a[(slot + 2) & 3][t][col][c];
+#pragma unroll
+        for (int tap = 0; tap < 9; ++tap) {
+            uint4 ahead[TA];
+            if (tap < 8) {
+#pragma unroll
+                for (int t = 0; t < TA; ++t) ahead[t] = l.a[(slot + 2 + (tap + 1) / 3) & 3][t][col + (tap + 1) % 3][c];
+            }
+#pragma unroll
+            for (int p = 0; p < TA + TB - 1; ++p) {
+                // hi hi, then hi lo and lo hi
+                const int ta = TB == 2 ? p == 2 : p, tb = TB == 2 && p == 1;
+#pragma unroll
+                for (int f = 0; f < 4; ++f) acc[tap][f] = mfma16x16x32<kF16 ? 1 : 2>(a[ta], b[f][tb], acc[tap][f]);
+            }
+#pragma unroll
+            for (int t = 0; t < TA; ++t) a[t] = ahead[t];
+        }
+    }
+
+    __device__ __forceinline__ void sync() {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        wg_barrier();
+    }
+
+    __device__ __forceinline__ void run() {
+#pragma unroll
+        for (int tap = 0; tap < 9; ++tap)
+#pragma unroll
+            for (int f = 0; f < 4; ++f) acc[tap][f] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (!enter()) return;
+        // now: the step multiplied; ready: the step in raw
+        fill_norm(next.oct);
+        fetch();
+        Step ready = next;
+        sync();
+        store(0, ready);
+        Step now = ready;
+        bool more = advance();
+        if (more) {
+            if (next.oct != now.oct) fill_norm(next.oct);
+            fetch();
+            ready = next;
+        }
+        sync();
+        // half of the waves, one of each SIMD's two, convert before they multiply, so
+        // that one has the matrix cores while the other has the vector units
+        const bool early = wave >= kWaves / 2;
+        for (int slot = 0;; ++slot) {
+            const Step after = ready;
+            bool fetched = false;
+            auto refill = [&]() {
+                if (!more) return;
+                store(slot + 1, after);
+                fetched = advance();
+                if (fetched) fetch();
+            };
+            if (early) refill();
+            if (now.active) multiply(slot);
+            if (!early) refill();
+            if (fetched && next.oct != after.oct) fill_norm(next.oct);
+            if (!more) break;
+            now = after;
+            ready = next;
+            more = fetched;
+            sync();
+        }
+    }
+
+    // acc to part: c = 4 (lane / 16) + i of the wave's 16, k = lane % 16 of each 16.
+    __device__ __forceinline__ void finish(int slice) {
+        const int wc = wave % WC, wk = wave / WC, kw = KS > 1 ? 0 : wk;
+        if constexpr (KS > 1) {
+            // the columns' halves joined through LDS, in order
+            static_assert(KS == 2, "two halves");
+            f32x4(*red)[4][64] = (f32x4(*)[4][64])&l;
+#pragma unroll
+            for (int tap = 0; tap < 9; ++tap) {
+                sync();
+                if (wk == 1)
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) red[wc][f][lane] = acc[tap][f];
+                sync();
+                if (wk == 0)
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) acc[tap][f] += red[wc][f][lane];
+            }
+            if (wk) return;
+        }
+#pragma unroll
+        for (int tap = 0; tap < 9; ++tap)
+#pragma unroll
+            for (int f = 0; f < 4; ++f)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int c = c0 + wc * 16 + (lane >> 4) * 4 + i, k = k0 + kw * 64 + f * 16 + (lane & 15);
+                    if (c < g.s.C && k < g.s.K) g.part[(((size_t)slice * 9 + tap) * g.s.C + c) * g.s.K + k] = acc[tap][f][i];
+                }
+    }
+};
+
+// A workgroup a tile of channels and filters and a slice of the rows; tiles of the
+// same slice run on one XCD, so that they share its rows in L2.
+template <typename T, bool X8, bool NORM, int WC, int KW, int KS>
+__global__ __launch_bounds__(WC* KW* KS * 64, 2) void k_wgrad(Args g) {
+    typedef Wgrad<T, X8, NORM, WC, KW, KS> W;
+    __shared__ typename W::Lds lds;
+    const int tiles = g.w.ctiles * g.w.ktiles, per = (g.w.slices * tiles + 7) / 8;
+    const int item = blockIdx.x % 8 * per + blockIdx.x / 8;
+    if (item >= g.w.slices * tiles) return;
+    const int slice = item / tiles, tile = item % tiles;
+    W w(g, lds, tile % g.w.ctiles * W::CT, tile / g.w.ctiles * W::KT, g.w.rows * slice / g.w.slices,
+        g.w.rows * (slice + 1) / g.w.slices);
+    w.run();
+    w.finish(slice);
 }
 
-// dg = the slices' sum, to [K][C][3][3].
+// dg [K][C][3][3] = the slices' sum, in order: 8 channels x 32 filters a workgroup,
+// through LDS so that reads run along the filters and writes along the taps.
 __global__ __launch_bounds__(256) void k_wgrad_sum(const float* __restrict__ part, float* __restrict__ dg, int C, int K,
                                                    int slices) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, all = (int64_t)9 * C * K;
-    if (i >= all) return;
-    const int64_t kc = i / 9, t = i % 9, k = kc / C, c = kc % C;
-    float v = 0.0f;
-    for (int sl = 0; sl < slices; ++sl) v += part[(((size_t)sl * 9 + t) * C + c) * K + k];
-    dg[i] = v;
+    __shared__ float out[32][73];
+    const int kb = (K + 31) / 32, c0 = blockIdx.x / kb * 8, k0 = blockIdx.x % kb * 32, k = threadIdx.x & 31;
+    const int c = threadIdx.x >> 5;
+    if (c0 + c < C && k0 + k < K) {
+        const size_t plane = (size_t)C * K;
+        const float* p = part + (size_t)(c0 + c) * K + k0 + k;
+        float v[9] = {};
+        for (int sl = 0; sl < slices; ++sl)
+#pragma unroll
+            for (int t = 0; t < 9; ++t) v[t] += p[((size_t)sl * 9 + t) * plane];
+#pragma unroll
+        for (int t = 0; t < 9; ++t) out[k][c * 9 + t] = v[t];
+    }
+    __syncthreads();
+    const int wide = (C - c0 < 8 ? C - c0 : 8) * 9;
+    for (int i = threadIdx.x; i < 32 * 72; i += 256) {
+        const int kk = i / 72, j = i % 72;
+        if (k0 + kk < K && j < wide) dg[((size_t)(k0 + kk) * C + c0) * 9 + j] = out[kk][j];
+    }
 }
 
-int slices_of(const WgradShape& s) {
-    const int64_t tiles = (int64_t)((s.K + 15) / 16) * ((s.C + 15) / 16), rows = (int64_t)s.N * s.Ho;
-    int64_t n = tiles >= 2048 ? 1 : 2048 / tiles;
-    return (int)(n < rows ? n : rows);
+// Two forms: 128 filters and strips of 4 columns, or 64 filters and strips of 8 whose
+// halves go to different waves.
+bool wide_of(const WgradShape& s) { return s.K > 64; }
+
+Walk walk_of(const WgradShape& s) {
+    Walk w;
+    const bool wide = wide_of(s);
+    w.lb = s.N % 8 == 0 ? 0 : s.N % 4 == 0 ? 1 : s.N % 2 == 0 ? 2 : 3;
+    const int bands = 1 << w.lb;
+    w.hb = (s.Ho + bands - 1) / bands;
+    w.segs = s.N << w.lb;
+    w.strips = (s.Wo + (wide ? 3 : 7)) / (wide ? 4 : 8);
+    w.rows = (int64_t)(w.segs / 8) * w.strips * w.hb;
+    w.ctiles = (s.C + 63) / 64;
+    w.ktiles = (s.K + (wide ? 127 : 63)) / (wide ? 128 : 64);
+    w.dstrips = make_fastdiv(w.strips);
+    w.dhb = make_fastdiv(w.hb);
+    // Slices: a step takes about 1.6 us and a slice two more than its rows; its part is
+    // written and read, 72 bytes a filter and channel at 4 TB/s.  The sum of both is
+    // least at this number; one workgroup a CU, and two rows at least.
+    const double best = sqrt((double)w.rows * 1.6e-6 * 4e12 / (72.0 * s.C * s.K));
+    int64_t n = 256 / ((int64_t)w.ctiles * w.ktiles);
+    if (n > best) n = (int64_t)best;
+    if (n > w.rows / 2) n = w.rows / 2;
+    w.slices = n < 1 ? 1 : (int)n;
+    return w;
 }
 
 }  // namespace
 
-size_t wgrad_workspace(const WgradShape& s) { return (size_t)slices_of(s) * 9 * s.C * s.K * sizeof(float); }
+bool wgrad_fits(const WgradShape& s) {
+    const Walk w = walk_of(s);
+    return (int64_t)s.W * s.C < 1 << 29 && (int64_t)s.Wo * s.K < 1 << 29 && w.rows < (int64_t)1 << 30 &&
+           (int64_t)w.slices * w.ctiles * w.ktiles < 1 << 30 && (int64_t)s.N * 8 < (int64_t)1 << 30;
+}
+
+size_t wgrad_workspace(const WgradShape& s) { return (size_t)walk_of(s).slices * 9 * s.C * s.K * sizeof(float); }
 
 hipError_t launch_wgrad(const WgradArgs& a, const WgradShape& s, void* ws, hipStream_t st) {
-    const int slices = slices_of(s);
-    const unsigned grid = (unsigned)slices * ((s.K + 15) / 16) * ((s.C + 15) / 16);
-    auto go = [&](auto t) {
+    const Args g{a, s, walk_of(s), (float*)ws};
+    const unsigned grid = ((unsigned)g.w.slices * g.w.ctiles * g.w.ktiles + 7) / 8 * 8;
+    auto go = [&](auto t, auto x8, auto norm) {
         typedef decltype(t) T;
-        if (s.x8 && s.norm) k_wgrad<T, true, true><<<grid, 256, 0, st>>>(a, s, (float*)ws, slices);
-        else if (s.x8) k_wgrad<T, true, false><<<grid, 256, 0, st>>>(a, s, (float*)ws, slices);
-        else if (s.norm) k_wgrad<T, false, true><<<grid, 256, 0, st>>>(a, s, (float*)ws, slices);
-        else k_wgrad<T, false, false><<<grid, 256, 0, st>>>(a, s, (float*)ws, slices);
+        if (wide_of(s)) k_wgrad<T, x8.value, norm.value, 4, 2, 1><<<grid, 512, 0, st>>>(g);
+        else k_wgrad<T, x8.value, norm.value, 4, 1, 2><<<grid, 512, 0, st>>>(g);
     };
-    if (s.io == Io::F32) go(float());
-    else if (s.io == Io::F16) go(_Float16());
-    else go(__bf16());
+    auto with = [&](auto t) {
+        if (s.x8 && s.norm) go(t, std::true_type(), std::true_type());
+        else if (s.x8) go(t, std::true_type(), std::false_type());
+        else if (s.norm) go(t, std::false_type(), std::true_type());
+        else go(t, std::false_type(), std::false_type());
+    };
+    if (s.io == Io::F32) with(float());
+    else if (s.io == Io::F16) with(_Float16());
+    else with(__bf16());
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const int64_t all = (int64_t)9 * s.C * s.K;
-    k_wgrad_sum<<<(unsigned)((all + 255) / 256), 256, 0, st>>>((const float*)ws, a.dg, s.C, s.K, slices);
+    k_wgrad_sum<<<(unsigned)((s.K + 31) / 32) * ((s.C + 7) / 8), 256, 0, st>>>((const float*)ws, a.dg, s.C, s.K, g.w.slices);
     return hipGetLastError();
 }
 
