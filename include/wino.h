@@ -406,8 +406,8 @@ int wino_group_norm_backward_nhwc(const void* dy, const void* x, const float* st
  *   significand bits: results are within about 4e-6 of the exact ones in norm, as
  *   F(4x4,3x3) layers are; 16-bit tensors are exact.  Operands that are not finite, or
  *   at least 3.39e38, give NaN where fp32 would give infinities.
- *   N*Ho*Wo must be below 2^31 (INVALID_ARG), and W*C and Wo*K below 2^29
- *   (UNSUPPORTED). */
+ *   N*Ho*Wo must be below 2^31 (INVALID_ARG), and (H + 2*pad + 16)*W*C and
+ *   (H + 2*pad + 16)*Wo*K below 2^29 (UNSUPPORTED). */
 size_t wino_conv2d_wgrad_workspace_bytes(int N, int C, int H, int W, int K, int pad, unsigned flags);
 int wino_conv2d_wgrad_nhwc(const void* x, const void* dy, float* dg, const float* stats, const float* gamma,
                            const float* beta, int G, int N, int C, int H, int W, int K, int pad, unsigned flags,

@@ -812,13 +812,24 @@ __global__ __launch_bounds__(256) void k_norm_params(const float* __restrict__ s
     __shared__ float acc[2][8][32];
     const int c = blockIdx.x * 32 + (threadIdx.x & 31), row = threadIdx.x >> 5;
     float z = 0.0f, n = 0.0f;
-    if (c < C)
-#pragma unroll 4
-        for (int i = row; i < N; i += 8) {
+    if (c < C) {
+        int i = row;
+        for (; i + 24 < N; i += 32) {         // four loads in flight
+            Raw<float, 2> p[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) p[u] = *(const Raw<float, 2>*)(sums + ((size_t)(i + u * 8) * C + c) * 2);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                z += p[u].v[0];
+                n += p[u].v[1];
+            }
+        }
+        for (; i < N; i += 8) {
             const Raw<float, 2> p = *(const Raw<float, 2>*)(sums + ((size_t)i * C + c) * 2);
             z += p.v[0];
             n += p.v[1];
         }
+    }
     acc[0][row][threadIdx.x & 31] = z;
     acc[1][row][threadIdx.x & 31] = n;
     __syncthreads();

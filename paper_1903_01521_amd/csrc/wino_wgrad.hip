@@ -29,11 +29,12 @@ namespace wino {
 namespace {
 
 constexpr int kSeg = 8;                       // images or bands that a lane sums over
+constexpr uint32_t kOutside = 1u << 31;        // an offset past every image
 
 // How the pixels are walked: segments of `hb` output rows (2^lb to an image), eight
 // segments an octet, strips of columns, and in a strip row by row.
 struct Walk {
-    int lb, hb, segs, strips;
+    int lb, hb, strips;
     int64_t rows;                             // octets * strips * hb
     int slices, ctiles, ktiles;
     FastDiv dstrips, dhb;
@@ -92,16 +93,20 @@ struct Wgrad {
     const Args& g;
     Lds& l;
     const int wave, lane, c0, k0;
+    const uint32_t in_image, in_row, dy_image, dy_row;        // bytes
     int64_t row, row1;                        // rows still to be entered
     Step next;                                // the step fetched last or next
     int first;                                // its strip's first active row
     uint32_t raw[kPer][kSeg];
-    uint32_t ok[kPer];                        // which of the eight are inside the image
+    uint32_t from[kPer];                      // byte of the first segment's image that a lane loads
     f32x4 acc[9][4];
 
     __device__ __forceinline__ Wgrad(const Args& args, Lds& lds, int c, int k, int64_t r0, int64_t r1)
         : g(args), l(lds), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), lane(threadIdx.x & 63), c0(c), k0(k),
-          row(r0), row1(r1) {}
+          in_image((uint32_t)(args.s.H * args.s.W * args.s.C) * (uint32_t)sizeof(S)),
+          in_row((uint32_t)(args.s.W * args.s.C) * (uint32_t)sizeof(S)),
+          dy_image((uint32_t)(args.s.Ho * args.s.Wo * args.s.K) * (uint32_t)sizeof(T)),
+          dy_row((uint32_t)(args.s.Wo * args.s.K) * (uint32_t)sizeof(T)), row(r0), row1(r1) {}
 
     // The steps of rows [row, row1): of each strip's share two rows more.
     __device__ __forceinline__ bool enter() {
@@ -131,7 +136,7 @@ struct Wgrad {
             for (int i = threadIdx.x; i < kSeg * CT; i += kThreads) {
                 const int e = i / CT, c = c0 + i % CT, seg = oct * kSeg + e;
                 float2 f = make_float2(0.0f, 0.0f);
-                if (c < g.s.C && seg < g.w.segs) {
+                if (c < g.s.C) {
                     const int n = seg >> g.w.lb;
                     const float* st = g.a.stats + ((size_t)n * g.s.G + c / g.s.D) * 2;
                     const float* r = X8 ? g.a.rows + ((size_t)n * g.s.C + c) * 2 : nullptr;
@@ -145,8 +150,32 @@ struct Wgrad {
             for (int i = threadIdx.x; i < kSeg * CT; i += kThreads) {
                 const int e = i / CT, c = c0 + i % CT, seg = oct * kSeg + e;
                 const float* r = g.a.rows + ((size_t)(seg >> g.w.lb) * g.s.C + c) * 2;
-                l.f[oct & 1][e][i % CT] = c < g.s.C && seg < g.w.segs ? make_float2(r[1], r[0]) : make_float2(0.0f, 0.0f);
+                l.f[oct & 1][e][i % CT] = c < g.s.C ? make_float2(r[1], r[0]) : make_float2(0.0f, 0.0f);
             }
+        }
+    }
+
+    // Byte of its own image that a lane loads for segment e, whose band starts lower.
+    __device__ __forceinline__ uint32_t byte_of(uint32_t from, int e, uint32_t row_bytes) const {
+        return from + (uint32_t)((e & ((1 << g.w.lb) - 1)) * g.w.hb) * row_bytes;
+    }
+
+    // Eight loads of one item: an image is a buffer of its own, so that rows above and
+    // below it and lanes beside it (kOutside, and a band's offset) read as zero: images
+    // are below 2^31 bytes, and so are the rows that are asked for outside them.
+    template <typename V>
+    __device__ __forceinline__ void load8(uint32_t (&r)[kSeg], const void* base, uint32_t image, uint32_t row_bytes,
+                                          uint32_t at) {
+        // in scalar registers, as the compiler does not see by itself
+        const int first_image = __builtin_amdgcn_readfirstlane(next.oct) * kSeg >> g.w.lb;
+        const char* p = (const char*)base + (size_t)first_image * image;
+#pragma unroll
+        for (int e = 0; e < kSeg; ++e) {
+            const auto b = __builtin_amdgcn_make_buffer_rsrc((void*)(p + (size_t)(e >> g.w.lb) * image), 0, (int)image, kRsrcWord3);
+            const int o = (int)byte_of(at, e, row_bytes);
+            if constexpr (sizeof(V) == 4) r[e] = __builtin_amdgcn_raw_buffer_load_b32(b, o, 0, 0);
+            else if constexpr (sizeof(V) == 2) r[e] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(b, o, 0, 0);
+            else r[e] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(b, o, 0, 0);
         }
     }
 
@@ -157,35 +186,17 @@ struct Wgrad {
 #pragma unroll
         for (int p = 0; p < kPer; ++p) {
             const int item = wave + p * kWaves;
-            const bool input = item < kAItems;
-            if (item >= kItems || (!input && !next.active)) continue;
-            // column of the image and channel, and the rows of the eight segments
-            const int at = input ? item * 64 + lane : (item - kAItems) * 64 + lane;
-            const int col = next.strip * kCols + (input ? at / CT - g.s.pad : at / KT);
-            const int ch = input ? c0 + at % CT : k0 + at % KT;
-            const int wide = input ? g.s.W : g.s.Wo, high = input ? g.s.H : g.s.Ho, chs = input ? g.s.C : g.s.K;
-            const bool inside = col >= 0 && col < wide && ch < chs;
-            const uint32_t off = inside ? (uint32_t)col * chs + ch : 0;
-            ok[p] = 0;
-#pragma unroll
-            for (int e = 0; e < kSeg; ++e) {
-                const int seg = next.oct * kSeg + e, n = seg >> g.w.lb, top = (seg & ((1 << g.w.lb) - 1)) * g.w.hb + next.t;
-                const int y = input ? top + 2 - g.s.pad : top;
-                raw[p][e] = 0;
-                if (seg < g.w.segs && y >= 0 && y < high) {
-                    const size_t base = ((size_t)n * high + y) * wide * chs;
-                    if (inside) {
-                        if (input) {
-                            const S* q = (X8 ? (const S*)g.a.codes : (const S*)g.a.x) + base;
-                            raw[p][e] = sizeof(S) == 4 ? ((const uint32_t*)q)[off] : sizeof(S) == 2 ? ((const uint16_t*)q)[off]
-                                                                                                      : ((const uint8_t*)q)[off];
-                        } else {
-                            const T* q = (const T*)g.a.dy + base;
-                            raw[p][e] = sizeof(T) == 4 ? ((const uint32_t*)q)[off] : ((const uint16_t*)q)[off];
-                        }
-                        ok[p] |= 1u << e;
-                    }
-                }
+            if (item < kAItems) {
+                const int at = item * 64 + lane, col = next.strip * kCols + at / CT - g.s.pad, ch = c0 + at % CT;
+                const int y = next.t + 2 - g.s.pad;
+                const bool inside = col >= 0 && col < g.s.W && ch < g.s.C;
+                from[p] = inside ? (uint32_t)((y * g.s.W + col) * g.s.C + ch) * (uint32_t)sizeof(S) : kOutside;
+                load8<S>(raw[p], X8 ? (const void*)g.a.codes : g.a.x, in_image, in_row, from[p]);
+            } else if (item < kItems && next.active) {
+                const int at = (item - kAItems) * 64 + lane, col = next.strip * kCols + at / KT, ch = k0 + at % KT;
+                const bool inside = col < g.s.Wo && ch < g.s.K;
+                const uint32_t o = inside ? (uint32_t)((next.t * g.s.Wo + col) * g.s.K + ch) * (uint32_t)sizeof(T) : kOutside;
+                load8<T>(raw[p], g.a.dy, dy_image, dy_row, o);
             }
         }
     }
@@ -214,7 +225,7 @@ struct Wgrad {
                         const float2 f = l.f[s.oct & 1][e][c];
                         v[e] = fmaf(v[e], f.x, f.y);
                         if constexpr (NORM) v[e] = g.s.act == Act::Silu ? act_of<true>(v[e], false) : act_of<false>(v[e], g.s.act == Act::Relu);
-                        v[e] = ok[p] >> e & 1 ? v[e] : 0.0f;
+                        v[e] = byte_of(from[p], e, in_row) < in_image ? v[e] : 0.0f;
                     }
                 }
                 uint4 o[TA];
@@ -252,6 +263,7 @@ struct Wgrad {
 #pragma unroll
                 for (int t = 0; t < TA; ++t) ahead[t] = l.a[(slot + 2 + (tap + 1) / 3) & 3][t][col + (tap + 1) % 3][c];
             }
+            __builtin_amdgcn_sched_barrier(0);        // these reads before this tap's products
 #pragma unroll
             for (int p = 0; p < TA + TB - 1; ++p) {
                 // hi hi, then hi lo and lo hi
@@ -361,28 +373,39 @@ __global__ __launch_bounds__(WC* KW* KS * 64, 2) void k_wgrad(Args g) {
     w.finish(slice);
 }
 
-// dg [K][C][3][3] = the slices' sum, in order: 8 channels x 32 filters a workgroup,
-// through LDS so that reads run along the filters and writes along the taps.
+// dg [K][C][3][3] = the slices' sum, in order: 8 channels x 32 filters x one row of
+// taps a workgroup, through LDS so that reads run along the filters.
 __global__ __launch_bounds__(256) void k_wgrad_sum(const float* __restrict__ part, float* __restrict__ dg, int C, int K,
                                                    int slices) {
-    __shared__ float out[32][73];
-    const int kb = (K + 31) / 32, c0 = blockIdx.x / kb * 8, k0 = blockIdx.x % kb * 32, k = threadIdx.x & 31;
-    const int c = threadIdx.x >> 5;
+    __shared__ float out[32][25];
+    const int r = blockIdx.x % 3, tile = blockIdx.x / 3, kb = (K + 31) / 32;
+    const int c0 = tile / kb * 8, k0 = tile % kb * 32, k = threadIdx.x & 31, c = threadIdx.x >> 5;
     if (c0 + c < C && k0 + k < K) {
         const size_t plane = (size_t)C * K;
-        const float* p = part + (size_t)(c0 + c) * K + k0 + k;
-        float v[9] = {};
-        for (int sl = 0; sl < slices; ++sl)
+        const float* p = part + r * 3 * plane + (size_t)(c0 + c) * K + k0 + k;
+        float v[3] = {};
+        auto add = [&](auto count) {          // slices at a time, so that their loads are in flight together
+            float u[count.value][3];
 #pragma unroll
-            for (int t = 0; t < 9; ++t) v[t] += p[((size_t)sl * 9 + t) * plane];
+            for (int i = 0; i < count.value; ++i)
 #pragma unroll
-        for (int t = 0; t < 9; ++t) out[k][c * 9 + t] = v[t];
+                for (int t = 0; t < 3; ++t) u[i][t] = p[(i * 9 + t) * plane];
+#pragma unroll
+            for (int i = 0; i < count.value; ++i)
+#pragma unroll
+                for (int t = 0; t < 3; ++t) v[t] += u[i][t];
+            p += count.value * 9 * plane;
+        };
+        int sl = 0;
+        for (; sl + 8 <= slices; sl += 8) add(std::integral_constant<int, 8>());
+        for (; sl < slices; ++sl) add(std::integral_constant<int, 1>());
+#pragma unroll
+        for (int t = 0; t < 3; ++t) out[k][c * 3 + t] = v[t];
     }
     __syncthreads();
-    const int wide = (C - c0 < 8 ? C - c0 : 8) * 9;
-    for (int i = threadIdx.x; i < 32 * 72; i += 256) {
-        const int kk = i / 72, j = i % 72;
-        if (k0 + kk < K && j < wide) dg[((size_t)(k0 + kk) * C + c0) * 9 + j] = out[kk][j];
+    for (int i = threadIdx.x; i < 32 * 24; i += 256) {
+        const int kk = i / 24, j = i % 24, cc = c0 + j / 3;
+        if (k0 + kk < K && cc < C) dg[((size_t)(k0 + kk) * C + cc) * 9 + r * 3 + j % 3] = out[kk][j];
     }
 }
 
@@ -396,9 +419,8 @@ Walk walk_of(const WgradShape& s) {
     w.lb = s.N % 8 == 0 ? 0 : s.N % 4 == 0 ? 1 : s.N % 2 == 0 ? 2 : 3;
     const int bands = 1 << w.lb;
     w.hb = (s.Ho + bands - 1) / bands;
-    w.segs = s.N << w.lb;
     w.strips = (s.Wo + (wide ? 3 : 7)) / (wide ? 4 : 8);
-    w.rows = (int64_t)(w.segs / 8) * w.strips * w.hb;
+    w.rows = ((int64_t)s.N << w.lb) / 8 * w.strips * w.hb;
     w.ctiles = (s.C + 63) / 64;
     w.ktiles = (s.K + (wide ? 127 : 63)) / (wide ? 128 : 64);
     w.dstrips = make_fastdiv(w.strips);
@@ -418,7 +440,9 @@ Walk walk_of(const WgradShape& s) {
 
 bool wgrad_fits(const WgradShape& s) {
     const Walk w = walk_of(s);
-    return (int64_t)s.W * s.C < 1 << 29 && (int64_t)s.Wo * s.K < 1 << 29 && w.rows < (int64_t)1 << 30 &&
+    // 32-bit offsets into an image, also of the rows above and below it
+    const int64_t high = (int64_t)s.H + 2 * (int64_t)s.pad + 16, top = (int64_t)1 << 29;
+    return high < top && s.W < top / high && s.C < top / high / s.W && s.Wo < top / high && s.K < top / high / s.Wo && w.rows < (int64_t)1 << 30 &&
            (int64_t)w.slices * w.ctiles * w.ktiles < 1 << 30 && (int64_t)s.N * 8 < (int64_t)1 << 30;
 }
 
@@ -443,7 +467,7 @@ hipError_t launch_wgrad(const WgradArgs& a, const WgradShape& s, void* ws, hipSt
     else with(__bf16());
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    k_wgrad_sum<<<(unsigned)((s.K + 31) / 32) * ((s.C + 7) / 8), 256, 0, st>>>((const float*)ws, a.dg, s.C, s.K, g.w.slices);
+    k_wgrad_sum<<<(unsigned)((s.K + 31) / 32) * ((s.C + 7) / 8) * 3, 256, 0, st>>>((const float*)ws, a.dg, s.C, s.K, g.w.slices);
     return hipGetLastError();
 }
 
