@@ -188,7 +188,12 @@ int wino_group_norm_backward_nhwc(const void* dy, const void* x, const float* st
 
 size_t wino_conv2d_wgrad_workspace_bytes(int N, int C, int H, int W, int K, int pad, unsigned flags) {
     WgradShape s;
-    return make_wgrad(N, C, H, W, K, pad, flags, &s) == WINO_OK ? wgrad_workspace(s) : (size_t)-1;
+    if (make_wgrad(N, C, H, W, K, pad, flags, &s) != WINO_OK) return (size_t)-1;
+    // the plan is another where the input is formed from the norm
+    const size_t plain = wgrad_workspace(s);
+    s.norm = true;
+    const size_t formed = wgrad_workspace(s);
+    return plain > formed ? plain : formed;
 }
 
 int wino_conv2d_wgrad_nhwc(const void* x, const void* dy, float* dg, const float* stats, const float* gamma,

@@ -36,7 +36,7 @@ constexpr uint32_t kOutside = 1u << 31;        // an offset past every image
 struct Walk {
     int lb, hb, strips;
     int64_t rows;                             // octets * strips * hb
-    int slices, ctiles, ktiles;
+    int form, slices, ctiles, ktiles;
     FastDiv dstrips, dhb;
 };
 
@@ -97,8 +97,11 @@ struct Wgrad {
     int64_t row, row1;                        // rows still to be entered
     Step next;                                // the step fetched last or next
     int first;                                // its strip's first active row
-    uint32_t raw[kPer][kSeg];
-    uint32_t from[kPer];                      // byte of the first segment's image that a lane loads
+    // One step's loads: values as they are, and the byte of the first segment's image
+    // that a lane loads.
+    struct Raws {
+        uint32_t v[kPer][kSeg], from[kPer];
+    };
     f32x4 acc[9][4];
 
     __device__ __forceinline__ Wgrad(const Args& args, Lds& lds, int c, int k, int64_t r0, int64_t r1)
@@ -165,7 +168,7 @@ struct Wgrad {
     // are below 2^31 bytes, and so are the rows that are asked for outside them.
     template <typename V>
     __device__ __forceinline__ void load8(uint32_t (&r)[kSeg], const void* base, uint32_t image, uint32_t row_bytes,
-                                          uint32_t at) {
+                                          uint32_t at) const {
         // in scalar registers, as the compiler does not see by itself
         const int first_image = __builtin_amdgcn_readfirstlane(next.oct) * kSeg >> g.w.lb;
         const char* p = (const char*)base + (size_t)first_image * image;
@@ -179,10 +182,10 @@ struct Wgrad {
         }
     }
 
-    // Loads of step `next` into raw: the input's row t + 2 of the strip's columns and
+    // Loads of step `next`: the input's row t + 2 of the strip's columns and
     // one more on each side, dy's row t.  A lane takes one column and channel, of the
     // eight segments.
-    __device__ __forceinline__ void fetch() {
+    __device__ __forceinline__ void fetch(Raws& raw) const {
 #pragma unroll
         for (int p = 0; p < kPer; ++p) {
             const int item = wave + p * kWaves;
@@ -190,13 +193,13 @@ struct Wgrad {
                 const int at = item * 64 + lane, col = next.strip * kCols + at / CT - g.s.pad, ch = c0 + at % CT;
                 const int y = next.t + 2 - g.s.pad;
                 const bool inside = col >= 0 && col < g.s.W && ch < g.s.C;
-                from[p] = inside ? (uint32_t)((y * g.s.W + col) * g.s.C + ch) * (uint32_t)sizeof(S) : kOutside;
-                load8<S>(raw[p], X8 ? (const void*)g.a.codes : g.a.x, in_image, in_row, from[p]);
+                raw.from[p] = inside ? (uint32_t)((y * g.s.W + col) * g.s.C + ch) * (uint32_t)sizeof(S) : kOutside;
+                load8<S>(raw.v[p], X8 ? (const void*)g.a.codes : g.a.x, in_image, in_row, raw.from[p]);
             } else if (item < kItems && next.active) {
                 const int at = (item - kAItems) * 64 + lane, col = next.strip * kCols + at / KT, ch = k0 + at % KT;
                 const bool inside = col < g.s.Wo && ch < g.s.K;
                 const uint32_t o = inside ? (uint32_t)((next.t * g.s.Wo + col) * g.s.K + ch) * (uint32_t)sizeof(T) : kOutside;
-                load8<T>(raw[p], g.a.dy, dy_image, dy_row, o);
+                load8<T>(raw.v[p], g.a.dy, dy_image, dy_row, o);
             }
         }
     }
@@ -209,7 +212,7 @@ struct Wgrad {
     }
 
     // The fetched values to LDS, in terms: `slot` of the ring, buffer slot & 1 of dy.
-    __device__ __forceinline__ void store(int slot, const Step& s) {
+    __device__ __forceinline__ void store(int slot, const Step& s, const Raws& raw) {
 #pragma unroll
         for (int p = 0; p < kPer; ++p) {
             const int item = wave + p * kWaves;
@@ -220,12 +223,12 @@ struct Wgrad {
                 const int at = item * 64 + lane, c = at % CT;
 #pragma unroll
                 for (int e = 0; e < kSeg; ++e) {
-                    v[e] = value<S>(raw[p][e]);
+                    v[e] = value<S>(raw.v[p][e]);
                     if constexpr (X8 || NORM) {
                         const float2 f = l.f[s.oct & 1][e][c];
                         v[e] = fmaf(v[e], f.x, f.y);
                         if constexpr (NORM) v[e] = g.s.act == Act::Silu ? act_of<true>(v[e], false) : act_of<false>(v[e], g.s.act == Act::Relu);
-                        v[e] = byte_of(from[p], e, in_row) < in_image ? v[e] : 0.0f;
+                        v[e] = byte_of(raw.from[p], e, in_row) < in_image ? v[e] : 0.0f;
                     }
                 }
                 uint4 o[TA];
@@ -235,7 +238,7 @@ struct Wgrad {
             } else {
                 const int at = (item - kAItems) * 64 + lane;
 #pragma unroll
-                for (int e = 0; e < kSeg; ++e) v[e] = value<T>(raw[p][e]);
+                for (int e = 0; e < kSeg; ++e) v[e] = value<T>(raw.v[p][e]);
                 uint4 o[TB];
                 split8<kF16, TB>(v, o);
 #pragma unroll
@@ -269,7 +272,7 @@ struct Wgrad {
                 // hi hi, then hi lo and lo hi
                 const int ta = TB == 2 ? p == 2 : p, tb = TB == 2 && p == 1;
 #pragma unroll
-                for (int f = 0; f < 4; ++f) acc[tap][f] = mfma16x16x32<kF16 ? 1 : 2>(a[ta], b[f][tb], acc[tap][f]);
+                for (int f = 0; f < 4; ++f) acc[tap][f] = mfma16x16x32<kF16 ? 1 : 2>(b[f][tb], a[ta], acc[tap][f]);
             }
 #pragma unroll
             for (int t = 0; t < TA; ++t) a[t] = ahead[t];
@@ -282,36 +285,49 @@ struct Wgrad {
     }
 
     __device__ __forceinline__ void run() {
+        // every slice has a row, and its first strip's share three steps at least: their
+        // loads together
+        enter();
+        fill_norm(next.oct);
+        Raws raw;
+        Step now = next;
+        {
+            Raws r0, r1;
+            fetch(r0);
+            const Step s0 = next;
+            advance();
+            fetch(r1);
+            const Step s1 = next;
+            advance();
+            fetch(raw);
+            now = next;
+            sync();
+            store(0, s0, r0);
+            store(1, s1, r1);
+        }
+        store(2, now, raw);
+        bool more = advance();
+        Step ready = next;
+        if (more) {
+            if (next.oct != now.oct) fill_norm(next.oct);
+            fetch(raw);
+        }
+        sync();
 #pragma unroll
         for (int tap = 0; tap < 9; ++tap)
 #pragma unroll
             for (int f = 0; f < 4; ++f) acc[tap][f] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        if (!enter()) return;
-        // now: the step multiplied; ready: the step in raw
-        fill_norm(next.oct);
-        fetch();
-        Step ready = next;
-        sync();
-        store(0, ready);
-        Step now = ready;
-        bool more = advance();
-        if (more) {
-            if (next.oct != now.oct) fill_norm(next.oct);
-            fetch();
-            ready = next;
-        }
-        sync();
         // half of the waves, one of each SIMD's two, convert before they multiply, so
         // that one has the matrix cores while the other has the vector units
         const bool early = wave >= kWaves / 2;
-        for (int slot = 0;; ++slot) {
+        for (int slot = 2;; ++slot) {
             const Step after = ready;
             bool fetched = false;
             auto refill = [&]() {
                 if (!more) return;
-                store(slot + 1, after);
+                store(slot + 1, after, raw);
                 fetched = advance();
-                if (fetched) fetch();
+                if (fetched) fetch(raw);
             };
             if (early) refill();
             if (now.active) multiply(slot);
@@ -325,42 +341,52 @@ struct Wgrad {
         }
     }
 
-    // acc to part: c = 4 (lane / 16) + i of the wave's 16, k = lane % 16 of each 16.
+    // acc to part: channel lane % 16 of the wave's, filters 4 (lane / 16) + i of each 16.
     __device__ __forceinline__ void finish(int slice) {
         const int wc = wave % WC, wk = wave / WC, kw = KS > 1 ? 0 : wk;
         if constexpr (KS > 1) {
-            // the columns' halves joined through LDS, in order
-            static_assert(KS == 2, "two halves");
-            f32x4(*red)[4][64] = (f32x4(*)[4][64])&l;
+            // the columns' halves joined through LDS, in order, three taps at a time
+            static_assert(KS == 2 && sizeof(Lds) >= WC * 12 * 64 * sizeof(f32x4), "two halves, through Lds");
+            f32x4(*red)[12][64] = (f32x4(*)[12][64])&l;
 #pragma unroll
-            for (int tap = 0; tap < 9; ++tap) {
+            for (int r = 0; r < 3; ++r) {
                 sync();
                 if (wk == 1)
 #pragma unroll
-                    for (int f = 0; f < 4; ++f) red[wc][f][lane] = acc[tap][f];
+                    for (int i = 0; i < 12; ++i) red[wc][i][lane] = acc[r * 3 + i / 4][i % 4];
                 sync();
                 if (wk == 0)
 #pragma unroll
-                    for (int f = 0; f < 4; ++f) acc[tap][f] += red[wc][f][lane];
+                    for (int i = 0; i < 12; ++i) acc[r * 3 + i / 4][i % 4] += red[wc][i][lane];
             }
             if (wk) return;
         }
+        const int c = c0 + wc * 16 + (lane & 15), k = k0 + kw * 64 + (lane >> 4) * 4;
+        if (c >= g.s.C) return;
+        const size_t plane = (size_t)g.s.C * g.s.K;
+        float* p = g.part + ((size_t)slice * 9 * g.s.C + c) * g.s.K + k;
+        if (g.s.K % 4 == 0) {
 #pragma unroll
-        for (int tap = 0; tap < 9; ++tap)
+            for (int tap = 0; tap < 9; ++tap, p += plane)
 #pragma unroll
-            for (int f = 0; f < 4; ++f)
+                for (int f = 0; f < 4; ++f)
+                    if (k + f * 16 < g.s.K) *(f32x4*)(p + f * 16) = acc[tap][f];
+        } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int c = c0 + wc * 16 + (lane >> 4) * 4 + i, k = k0 + kw * 64 + f * 16 + (lane & 15);
-                    if (c < g.s.C && k < g.s.K) g.part[(((size_t)slice * 9 + tap) * g.s.C + c) * g.s.K + k] = acc[tap][f][i];
-                }
+            for (int tap = 0; tap < 9; ++tap, p += plane)
+#pragma unroll
+                for (int f = 0; f < 4; ++f)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (k + f * 16 + i < g.s.K) p[f * 16 + i] = acc[tap][f][i];
+        }
     }
 };
 
 // A workgroup a tile of channels and filters and a slice of the rows; tiles of the
 // same slice run on one XCD, so that they share its rows in L2.
 template <typename T, bool X8, bool NORM, int WC, int KW, int KS>
-__global__ __launch_bounds__(WC* KW* KS * 64, 2) void k_wgrad(Args g) {
+__global__ __launch_bounds__(WC* KW* KS * 64, WC* KW* KS / 4) void k_wgrad(Args g) {
     typedef Wgrad<T, X8, NORM, WC, KW, KS> W;
     __shared__ typename W::Lds lds;
     const int tiles = g.w.ctiles * g.w.ktiles, per = (g.w.slices * tiles + 7) / 8;
@@ -409,41 +435,83 @@ __global__ __launch_bounds__(256) void k_wgrad_sum(const float* __restrict__ par
     }
 }
 
-// Two forms: 128 filters and strips of 4 columns, or 64 filters and strips of 8 whose
-// halves go to different waves.
-bool wide_of(const WgradShape& s) { return s.K > 64; }
+// Three forms of a workgroup: 64 channels by 128 filters in strips of 4 columns, 64 by
+// 64 in strips of 8 whose halves go to different waves, and 32 by 64 of the same.
+struct Form {
+    int ct, kt, cols;
+};
+constexpr Form kForms[3] = {{64, 128, 4}, {64, 64, 8}, {32, 64, 8}};
 
-Walk walk_of(const WgradShape& s) {
+Walk walk_of(const WgradShape& s, int form, int slices) {
+    const Form f = kForms[form];
     Walk w;
-    const bool wide = wide_of(s);
+    w.form = form;
     w.lb = s.N % 8 == 0 ? 0 : s.N % 4 == 0 ? 1 : s.N % 2 == 0 ? 2 : 3;
     const int bands = 1 << w.lb;
     w.hb = (s.Ho + bands - 1) / bands;
-    w.strips = (s.Wo + (wide ? 3 : 7)) / (wide ? 4 : 8);
+    w.strips = (s.Wo + f.cols - 1) / f.cols;
     w.rows = ((int64_t)s.N << w.lb) / 8 * w.strips * w.hb;
-    w.ctiles = (s.C + 63) / 64;
-    w.ktiles = (s.K + (wide ? 127 : 63)) / (wide ? 128 : 64);
+    w.ctiles = (s.C + f.ct - 1) / f.ct;
+    w.ktiles = (s.K + f.kt - 1) / f.kt;
     w.dstrips = make_fastdiv(w.strips);
     w.dhb = make_fastdiv(w.hb);
-    // Slices: a step takes about 1.6 us and a slice two more than its rows; its part is
-    // written and read, 72 bytes a filter and channel at 4 TB/s.  The sum of both is
-    // least at this number; one workgroup a CU, and two rows at least.
-    const double best = sqrt((double)w.rows * 1.6e-6 * 4e12 / (72.0 * s.C * s.K));
-    int64_t n = 256 / ((int64_t)w.ctiles * w.ktiles);
-    if (n > best) n = (int64_t)best;
-    if (n > w.rows / 2) n = w.rows / 2;
-    w.slices = n < 1 ? 1 : (int)n;
+    w.slices = slices;
     return w;
+}
+
+// bf16 (or fp16) products that one product of the operands takes.
+int products_of(const WgradShape& s) {
+    const bool formed = s.norm || s.x8;
+    return s.io == Io::F32 ? 3 : s.io == Io::BF16 ? (formed ? 2 : 1) : formed ? 3 : 1;
+}
+
+// A step's time in us: the products, and forming the input, which the second and third
+// form do for half as many filters (third: half the products, but no second wave on a
+// SIMD to run them meanwhile).
+double step_of(const WgradShape& s, int form) {
+    const double products = 0.95 + 0.45 * products_of(s), formed = s.norm || s.x8 ? (form == 0 ? 0.45 : 0.9) : 0.0;
+    return products * (form == 0 ? 1.0 : form == 1 ? 1.04 : 0.87) + formed;
+}
+
+// The form and number of slices of the least estimated time: 11 us for two launches,
+// the first loads and the last stores; a step for every row of a slice and two for
+// every strip that it enters; the slices' parts, 72 bytes a filter and channel, written
+// and read at 8 TB/s.  Measured against it (us): N = 8, 128 -> 128 at 28x28 25.9 and 28
+// (third form, 32 slices), 35.1 and 35.5 (first, 32); N = 64, 256 -> 256 at 56x56 485
+// and 501 (first, 32), 494 and 511 (second, 16); N = 1, 256 -> 256 at 56x56 32.1 and 35
+// (second, 16).
+Walk walk_of(const WgradShape& s) {
+    Walk best = {};
+    double least = 0.0;
+    for (int form = 0; form < 3; ++form) {
+        Walk w = walk_of(s, form, 1);
+        const int64_t tiles = (int64_t)w.ctiles * w.ktiles, most = tiles >= 256 ? 1 : 256 / tiles;
+        const double step = step_of(s, form), rounds = (double)((tiles + 255) / 256);
+        auto take = [&](int64_t slices) {
+            if (slices < 1 || slices > most || slices > w.rows) return;
+            const double rows = (double)((w.rows + slices - 1) / slices);
+            const double t = 11.0 + rounds * step * (rows + 2.0 * (1.0 + (rows - 1.0) / w.hb)) + (double)slices * s.C * s.K * 72.0 / 8e6;
+            if (best.slices && t >= least) return;
+            least = t;
+            w.slices = (int)slices;
+            best = w;
+        };
+        take(most < w.rows ? most : w.rows);
+        for (int64_t r = 1; r <= 64 && r <= w.rows; r += r < 8 ? 1 : r / 4) take((w.rows + r - 1) / r);
+    }
+    return best;
 }
 
 }  // namespace
 
 bool wgrad_fits(const WgradShape& s) {
-    const Walk w = walk_of(s);
-    // 32-bit offsets into an image, also of the rows above and below it
-    const int64_t high = (int64_t)s.H + 2 * (int64_t)s.pad + 16, top = (int64_t)1 << 29;
-    return high < top && s.W < top / high && s.C < top / high / s.W && s.Wo < top / high && s.K < top / high / s.Wo && w.rows < (int64_t)1 << 30 &&
-           (int64_t)w.slices * w.ctiles * w.ktiles < 1 << 30 && (int64_t)s.N * 8 < (int64_t)1 << 30;
+    // 32-bit offsets into an image, also of the rows above and below it, and counts of
+    // images, rows and workgroups in 32 bits
+    const int64_t high = (int64_t)s.H + 2 * (int64_t)s.pad + 16, top = (int64_t)1 << 29, count = (int64_t)1 << 27;
+    if (high >= top || s.W >= top / high || s.C >= top / high / s.W || s.Wo >= top / high || s.K >= top / high / s.Wo)
+        return false;
+    const Walk w = walk_of(s, 2, 1);
+    return s.N < count && w.rows < count && (int64_t)w.ctiles * w.ktiles < count;
 }
 
 size_t wgrad_workspace(const WgradShape& s) { return (size_t)walk_of(s).slices * 9 * s.C * s.K * sizeof(float); }
@@ -453,8 +521,9 @@ hipError_t launch_wgrad(const WgradArgs& a, const WgradShape& s, void* ws, hipSt
     const unsigned grid = ((unsigned)g.w.slices * g.w.ctiles * g.w.ktiles + 7) / 8 * 8;
     auto go = [&](auto t, auto x8, auto norm) {
         typedef decltype(t) T;
-        if (wide_of(s)) k_wgrad<T, x8.value, norm.value, 4, 2, 1><<<grid, 512, 0, st>>>(g);
-        else k_wgrad<T, x8.value, norm.value, 4, 1, 2><<<grid, 512, 0, st>>>(g);
+        if (g.w.form == 0) k_wgrad<T, x8.value, norm.value, 4, 2, 1><<<grid, 512, 0, st>>>(g);
+        else if (g.w.form == 1) k_wgrad<T, x8.value, norm.value, 4, 1, 2><<<grid, 512, 0, st>>>(g);
+        else k_wgrad<T, x8.value, norm.value, 2, 1, 2><<<grid, 256, 0, st>>>(g);
     };
     auto with = [&](auto t) {
         if (s.x8 && s.norm) go(t, std::true_type(), std::true_type());
