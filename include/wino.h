@@ -402,10 +402,12 @@ int wino_group_norm_backward_nhwc(const void* dy, const void* x, const float* st
  * checkpoint's values), and G, gamma and beta are not read.  Else a is the y of
  * wino_group_norm_nhwc, formed again from x or its checkpoint on load (flags:
  * that call's activation), not rounded to 16 bits.
- *   fp32 operands (and inputs formed on load) are held in two bf16 terms, 16
- *   significand bits: results are within about 4e-6 of the exact ones in norm, as
- *   F(4x4,3x3) layers are; 16-bit tensors are exact.  Operands that are not finite, or
- *   at least 3.39e38, give NaN where fp32 would give infinities.
+ *   fp32 operands (and inputs formed on load) are held in two fp16 terms, 22
+ *   significand bits, scaled so that the tensor's largest finite value is 2^14: results
+ *   are as near the exact ones as fp32 sums of fp32 products are, and values below 2^-17
+ *   of the largest are off by less than 2^-39 of it.  Values that are not finite give
+ *   results that are not (NaN where fp32 would give infinities), in their channel or
+ *   filter.  16-bit tensors are exact.
  *   N*Ho*Wo must be below 2^31 (INVALID_ARG), and (H + 2*pad + 16)*W*C and
  *   (H + 2*pad + 16)*Wo*K below 2^29 (UNSUPPORTED). */
 size_t wino_conv2d_wgrad_workspace_bytes(int N, int C, int H, int W, int K, int pad, unsigned flags);

@@ -11,11 +11,13 @@
 // tap reads whole 16-byte words, only from another row or column, and the transpose
 // happens in the registers that the eight loads fill.
 //
-// fp32 operands are held in two bf16 terms (16 significand bits), and three of the
-// four products are summed in fp32: a product is off by 2^-16 at most, the result by
-// about 4e-6 of its norm, which is what the F(4x4,3x3) layers are off by; three terms
-// would take six products.  fp16 values are exact in two terms, bf16 ones in one, and
-// fp16 by fp16 runs on the fp16 matrix cores; an input formed on load has two.
+// fp32 operands are held in two fp16 terms, 22 significand bits, and three of the four
+// products are summed in fp32: a product is off by 2^-21 at most, and results are as
+// near the exact ones as fp32 sums are (two bf16 terms, 16 bits, gave 4.5e-6 of the
+// norm where these give 2e-7).  For fp16's range they are scaled by a power of two that
+// takes the tensor's largest finite value to 2^14, found by a launch before: values
+// below 2^-17 of it lose bits, in all less than 2^-39 of it.  bf16 values have one term
+// then, and tensors that are both bf16 or both fp16 are multiplied as they are.
 #include <math.h>
 
 #include <type_traits>
@@ -28,6 +30,7 @@ namespace wino {
 
 namespace {
 
+constexpr int kMost = 1024;                   // blocks that look for a tensor's largest magnitude
 constexpr int kSeg = 8;                       // images or bands that a lane sums over
 constexpr uint32_t kOutside = 1u << 31;        // an offset past every image
 
@@ -45,23 +48,48 @@ struct Args {
     WgradShape s;
     Walk w;
     float* part;                              // [slices][9][C][K]
+    uint32_t* most;                           // magnitudes, as bits: `nx` of the input, then `nd` of dy
+    int nx, nd;                               // none: not scaled
 };
 
 // 16-byte words of eight values' terms: hi, and with two terms what is left.
-template <bool F16, int TERMS>
+template <typename H, int TERMS>
 __device__ __forceinline__ void split8(const float (&v)[kSeg], uint4 (&o)[TERMS]) {
-    typedef typename std::conditional<F16, _Float16, __bf16>::type H;
-    typedef H h8 __attribute__((ext_vector_type(8)));
-    h8 hi;
+    typedef H h2 __attribute__((ext_vector_type(2)));
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    uint32_t hi[4], lo[4];
 #pragma unroll
-    for (int e = 0; e < kSeg; ++e) hi[e] = (H)v[e];
-    o[0] = __builtin_bit_cast(uint4, hi);
-    if constexpr (TERMS == 2) {
-        h8 lo;
-#pragma unroll
-        for (int e = 0; e < kSeg; ++e) lo[e] = (H)(v[e] - (float)hi[e]);
-        o[1] = __builtin_bit_cast(uint4, lo);
+    for (int i = 0; i < 4; ++i) {
+        const f2 x = {v[2 * i], v[2 * i + 1]};
+        const h2 h = __builtin_convertvector(x, h2);
+        hi[i] = __builtin_bit_cast(uint32_t, h);
+        if constexpr (TERMS == 2) {
+            const f2 back = __builtin_convertvector(h, f2), left = {x[0] - back[0], x[1] - back[1]};
+            lo[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(left, h2));
+        }
     }
+    o[0] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+    if constexpr (TERMS == 2) o[1] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+}
+
+// The power of two for a tensor whose largest magnitude has these bits, which goes to
+// 2^14, and two values' larger one: infinities and NaN do not count.
+__device__ __forceinline__ int exponent_of(uint32_t bits) {
+    const int e = bits ? 14 + 127 - (int)(bits >> 23) : 0;
+    return e < -126 ? -126 : e > 126 ? 126 : e;
+}
+__device__ __forceinline__ float power(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
+__device__ __forceinline__ uint32_t larger(uint32_t m, float v) {
+    const uint32_t b = __float_as_uint(v) & 0x7fffffffu;
+    return b < 0x7f800000u && b > m ? b : m;
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t m) {
+#pragma unroll
+    for (int i = 32; i; i >>= 1) {
+        const uint32_t o = (uint32_t)__shfl_xor((int)m, i);
+        m = o > m ? o : m;
+    }
+    return m;
 }
 
 // One step of the walk: local row t of a strip of an octet; below the first row of
@@ -75,9 +103,10 @@ struct Step {
 // T: the tensors' type; TA, TB: terms of the input and of dy.
 template <typename T, bool X8, bool NORM, int WC, int KW, int KS>
 struct Wgrad {
-    static constexpr bool kF16 = std::is_same<T, _Float16>::value && !X8 && !NORM;
-    static constexpr int TA = kF16 || (std::is_same<T, __bf16>::value && !X8 && !NORM) ? 1 : 2;
-    static constexpr int TB = kF16 || std::is_same<T, __bf16>::value ? 1 : 2;
+    static constexpr bool kAsIs = sizeof(T) == 2 && !X8 && !NORM;     // both tensors in 16 bits, unscaled
+    static constexpr int TA = kAsIs ? 1 : 2, TB = sizeof(T) == 2 ? 1 : 2;
+    typedef typename std::conditional<kAsIs && std::is_same<T, __bf16>::value, __bf16, _Float16>::type H;
+    static constexpr int kPrec = std::is_same<H, _Float16>::value ? 1 : 2;
     static constexpr int kWaves = WC * KW * KS, kThreads = kWaves * 64;
     static constexpr int CT = 16 * WC, KT = 64 * KW, kCols = 4 * KS, kACols = kCols + 2;
     static constexpr int kAItems = kACols * CT / 64, kItems = kAItems + kCols * KT / 64;
@@ -97,6 +126,7 @@ struct Wgrad {
     int64_t row, row1;                        // rows still to be entered
     Step next;                                // the step fetched last or next
     int first;                                // its strip's first active row
+    float in_scale, dy_scale;
     // One step's loads: values as they are, and the byte of the first segment's image
     // that a lane loads.
     struct Raws {
@@ -104,12 +134,12 @@ struct Wgrad {
     };
     f32x4 acc[9][4];
 
-    __device__ __forceinline__ Wgrad(const Args& args, Lds& lds, int c, int k, int64_t r0, int64_t r1)
+    __device__ __forceinline__ Wgrad(const Args& args, Lds& lds, int c, int k, int64_t r0, int64_t r1, float si, float sd)
         : g(args), l(lds), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), lane(threadIdx.x & 63), c0(c), k0(k),
           in_image((uint32_t)(args.s.H * args.s.W * args.s.C) * (uint32_t)sizeof(S)),
           in_row((uint32_t)(args.s.W * args.s.C) * (uint32_t)sizeof(S)),
           dy_image((uint32_t)(args.s.Ho * args.s.Wo * args.s.K) * (uint32_t)sizeof(T)),
-          dy_row((uint32_t)(args.s.Wo * args.s.K) * (uint32_t)sizeof(T)), row(r0), row1(r1) {}
+          dy_row((uint32_t)(args.s.Wo * args.s.K) * (uint32_t)sizeof(T)), row(r0), row1(r1), in_scale(si), dy_scale(sd) {}
 
     // The steps of rows [row, row1): of each strip's share two rows more.
     __device__ __forceinline__ bool enter() {
@@ -153,7 +183,7 @@ struct Wgrad {
             for (int i = threadIdx.x; i < kSeg * CT; i += kThreads) {
                 const int e = i / CT, c = c0 + i % CT, seg = oct * kSeg + e;
                 const float* r = g.a.rows + ((size_t)(seg >> g.w.lb) * g.s.C + c) * 2;
-                l.f[oct & 1][e][i % CT] = c < g.s.C ? make_float2(r[1], r[0]) : make_float2(0.0f, 0.0f);
+                l.f[oct & 1][e][i % CT] = c < g.s.C ? make_float2(r[1] * in_scale, r[0] * in_scale) : make_float2(0.0f, 0.0f);
             }
         }
     }
@@ -219,28 +249,41 @@ struct Wgrad {
             const bool input = item < kAItems;
             if (item >= kItems || (!input && !s.active)) continue;
             float v[kSeg];
-            if (input) {
+            if constexpr (kAsIs) {                    // the operands are the tensors' own 16 bits
+                const int at = (input ? item : item - kAItems) * 64 + lane;
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = raw.v[p][2 * i] | raw.v[p][2 * i + 1] << 16;
+                const uint4 o = make_uint4(w[0], w[1], w[2], w[3]);
+                if (input) l.a[slot & 3][0][at / CT][at % CT] = o;
+                else l.d[slot & 1][0][at / KT][at % KT] = o;
+            } else if (input) {
                 const int at = item * 64 + lane, c = at % CT;
 #pragma unroll
                 for (int e = 0; e < kSeg; ++e) {
                     v[e] = value<S>(raw.v[p][e]);
-                    if constexpr (X8 || NORM) {
+                    if constexpr (!X8 && !NORM) {
+                        v[e] *= in_scale;
+                    } else {
                         const float2 f = l.f[s.oct & 1][e][c];
                         v[e] = fmaf(v[e], f.x, f.y);
-                        if constexpr (NORM) v[e] = g.s.act == Act::Silu ? act_of<true>(v[e], false) : act_of<false>(v[e], g.s.act == Act::Relu);
+                        if constexpr (NORM) {
+                            const bool silu = g.s.act == Act::Silu;
+                            v[e] = in_scale * (silu ? act_of<true>(v[e], false) : act_of<false>(v[e], g.s.act == Act::Relu));
+                        }
                         v[e] = byte_of(raw.from[p], e, in_row) < in_image ? v[e] : 0.0f;
                     }
                 }
                 uint4 o[TA];
-                split8<kF16, TA>(v, o);
+                split8<H, TA>(v, o);
 #pragma unroll
                 for (int t = 0; t < TA; ++t) l.a[slot & 3][t][at / CT][c] = o[t];
             } else {
                 const int at = (item - kAItems) * 64 + lane;
 #pragma unroll
-                for (int e = 0; e < kSeg; ++e) v[e] = value<T>(raw.v[p][e]);
+                for (int e = 0; e < kSeg; ++e) v[e] = value<T>(raw.v[p][e]) * dy_scale;
                 uint4 o[TB];
-                split8<kF16, TB>(v, o);
+                split8<H, TB>(v, o);
 #pragma unroll
                 for (int t = 0; t < TB; ++t) l.d[slot & 1][t][at / KT][at % KT] = o[t];
             }
@@ -272,7 +315,7 @@ struct Wgrad {
                 // hi hi, then hi lo and lo hi
                 const int ta = TB == 2 ? p == 2 : p, tb = TB == 2 && p == 1;
 #pragma unroll
-                for (int f = 0; f < 4; ++f) acc[tap][f] = mfma16x16x32<kF16 ? 1 : 2>(b[f][tb], a[ta], acc[tap][f]);
+                for (int f = 0; f < 4; ++f) acc[tap][f] = mfma16x16x32<kPrec>(b[f][tb], a[ta], acc[tap][f]);
             }
 #pragma unroll
             for (int t = 0; t < TA; ++t) a[t] = ahead[t];
@@ -342,7 +385,7 @@ struct Wgrad {
     }
 
     // acc to part: channel lane % 16 of the wave's, filters 4 (lane / 16) + i of each 16.
-    __device__ __forceinline__ void finish(int slice) {
+    __device__ __forceinline__ void finish(int slice, int exponent) {
         const int wc = wave % WC, wk = wave / WC, kw = KS > 1 ? 0 : wk;
         if constexpr (KS > 1) {
             // the columns' halves joined through LDS, in order, three taps at a time
@@ -361,6 +404,13 @@ struct Wgrad {
             }
             if (wk) return;
         }
+        if constexpr (!kAsIs)
+#pragma unroll
+            for (int tap = 0; tap < 9; ++tap)
+#pragma unroll
+                for (int f = 0; f < 4; ++f)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[tap][f][i] = ldexpf(acc[tap][f][i], -exponent);
         const int c = c0 + wc * 16 + (lane & 15), k = k0 + kw * 64 + (lane >> 4) * 4;
         if (c >= g.s.C) return;
         const size_t plane = (size_t)g.s.C * g.s.K;
@@ -383,20 +433,99 @@ struct Wgrad {
     }
 };
 
+// The largest magnitudes: of blocks below nx of the input's (a raw tensor's, the
+// checkpoint's rows', or the norm's bound |gamma| sqrt(D P) + |beta|, doubled for what a
+// checkpoint adds), of the others of dy's.
+template <typename T>
+__device__ uint32_t most_of(const T* p, int64_t n, int block, int blocks) {
+    constexpr int V = 16 / sizeof(T);
+    uint32_t m = 0;
+    int64_t done = 0;
+    if (((uintptr_t)p & 15) == 0) {
+        const int64_t all = n / V, step = (int64_t)blocks * 256;
+        int64_t i = (int64_t)block * 256 + threadIdx.x;
+        auto take = [&](const Held<T, V>& h) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) m = larger(m, h.value(j));
+        };
+        for (; i + 3 * step < all; i += 4 * step) {
+            Held<T, V> h[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) h[u].load(p + (i + u * step) * V);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) take(h[u]);
+        }
+        for (; i < all; i += step) {
+            Held<T, V> h;
+            h.load(p + i * V);
+            take(h);
+        }
+        done = all * V;
+    }
+    for (int64_t i = done + (int64_t)block * 256 + threadIdx.x; i < n; i += (int64_t)blocks * 256) m = larger(m, (float)p[i]);
+    return m;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_wgrad_most(Args g) {
+    __shared__ uint32_t waves[4];
+    const int b = blockIdx.x;
+    uint32_t m = 0;
+    if (b >= g.nx) {
+        m = most_of((const T*)g.a.dy, (int64_t)g.s.N * g.s.Ho * g.s.Wo * g.s.K, b - g.nx, g.nd);
+    } else if (g.s.norm) {
+        const float bound = 2.0f * sqrtf((float)g.s.D * (float)g.s.H * (float)g.s.W);
+        for (int c = b * 256 + threadIdx.x; c < g.s.C; c += g.nx * 256)
+            m = larger(m, fabsf(g.a.gamma ? g.a.gamma[c] : 1.0f) * bound + fabsf(g.a.beta ? g.a.beta[c] : 0.0f));
+    } else if (g.s.x8) {
+        for (int64_t i = (int64_t)b * 256 + threadIdx.x; i < (int64_t)g.s.N * g.s.C; i += (int64_t)g.nx * 256)
+            m = larger(m, fabsf(g.a.rows[i * 2]) + kCodes * g.a.rows[i * 2 + 1]);
+    } else {
+        m = most_of((const T*)g.a.x, (int64_t)g.s.N * g.s.H * g.s.W * g.s.C, b, g.nx);
+    }
+    m = wave_max(m);
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = m;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < 4; ++w) m = waves[w] > m ? waves[w] : m;
+        g.most[b] = m;
+    }
+}
+
 // A workgroup a tile of channels and filters and a slice of the rows; tiles of the
 // same slice run on one XCD, so that they share its rows in L2.
 template <typename T, bool X8, bool NORM, int WC, int KW, int KS>
 __global__ __launch_bounds__(WC* KW* KS * 64, WC* KW* KS / 4) void k_wgrad(Args g) {
     typedef Wgrad<T, X8, NORM, WC, KW, KS> W;
     __shared__ typename W::Lds lds;
+    __shared__ uint32_t most[2][W::kWaves];
     const int tiles = g.w.ctiles * g.w.ktiles, per = (g.w.slices * tiles + 7) / 8;
     const int item = blockIdx.x % 8 * per + blockIdx.x / 8;
     if (item >= g.w.slices * tiles) return;
     const int slice = item / tiles, tile = item % tiles;
+    int in_exp = 0, dy_exp = 0;
+    if constexpr (!W::kAsIs) {
+        uint32_t mx = 0, md = 0;
+        for (int i = threadIdx.x; i < g.nx; i += W::kThreads) mx = g.most[i] > mx ? g.most[i] : mx;
+        for (int i = threadIdx.x; i < g.nd; i += W::kThreads) md = g.most[g.nx + i] > md ? g.most[g.nx + i] : md;
+        mx = wave_max(mx);
+        md = wave_max(md);
+        if ((threadIdx.x & 63) == 0) {
+            most[0][threadIdx.x >> 6] = mx;
+            most[1][threadIdx.x >> 6] = md;
+        }
+        __syncthreads();
+        for (int w = 0; w < W::kWaves; ++w) {
+            mx = most[0][w] > mx ? most[0][w] : mx;
+            md = most[1][w] > md ? most[1][w] : md;
+        }
+        in_exp = __builtin_amdgcn_readfirstlane(exponent_of(mx));
+        dy_exp = __builtin_amdgcn_readfirstlane(exponent_of(md));
+    }
     W w(g, lds, tile % g.w.ctiles * W::CT, tile / g.w.ctiles * W::KT, g.w.rows * slice / g.w.slices,
-        g.w.rows * (slice + 1) / g.w.slices);
+        g.w.rows * (slice + 1) / g.w.slices, power(in_exp), power(dy_exp));
     w.run();
-    w.finish(slice);
+    w.finish(slice, in_exp + dy_exp);
 }
 
 // dg [K][C][3][3] = the slices' sum, in order: 8 channels x 32 filters x one row of
@@ -459,11 +588,8 @@ Walk walk_of(const WgradShape& s, int form, int slices) {
     return w;
 }
 
-// bf16 (or fp16) products that one product of the operands takes.
-int products_of(const WgradShape& s) {
-    const bool formed = s.norm || s.x8;
-    return s.io == Io::F32 ? 3 : s.io == Io::BF16 ? (formed ? 2 : 1) : formed ? 3 : 1;
-}
+// Products on the matrix cores that one product of the operands takes.
+int products_of(const WgradShape& s) { return s.io == Io::F32 ? 3 : s.norm || s.x8 ? 2 : 1; }
 
 // A step's time in us: the products, and forming the input, which the second and third
 // form do for half as many filters (third: half the products, but no second wave on a
@@ -514,10 +640,25 @@ bool wgrad_fits(const WgradShape& s) {
     return s.N < count && w.rows < count && (int64_t)w.ctiles * w.ktiles < count;
 }
 
-size_t wgrad_workspace(const WgradShape& s) { return (size_t)walk_of(s).slices * 9 * s.C * s.K * sizeof(float); }
+size_t wgrad_workspace(const WgradShape& s) {
+    return (size_t)walk_of(s).slices * 9 * s.C * s.K * sizeof(float) + 2 * kMost * sizeof(uint32_t);
+}
 
 hipError_t launch_wgrad(const WgradArgs& a, const WgradShape& s, void* ws, hipStream_t st) {
-    const Args g{a, s, walk_of(s), (float*)ws};
+    Args g{a, s, walk_of(s), (float*)ws, nullptr, 0, 0};
+    g.most = (uint32_t*)(g.part + (size_t)g.w.slices * 9 * s.C * s.K);
+    auto blocks = [](int64_t n) { return (int)(n > (int64_t)kMost * 8192 ? kMost : (n + 8191) / 8192); };
+    if (s.norm) g.nx = 1;
+    else if (s.x8) g.nx = blocks((int64_t)s.N * s.C);
+    else if (s.io == Io::F32) g.nx = blocks((int64_t)s.N * s.H * s.W * s.C);
+    if (s.io == Io::F32 || (s.io == Io::BF16 && g.nx)) g.nd = blocks((int64_t)s.N * s.Ho * s.Wo * s.K);
+    if (g.nx + g.nd) {
+        if (s.io == Io::F32) k_wgrad_most<float><<<g.nx + g.nd, 256, 0, st>>>(g);
+        else if (s.io == Io::F16) k_wgrad_most<_Float16><<<g.nx + g.nd, 256, 0, st>>>(g);
+        else k_wgrad_most<__bf16><<<g.nx + g.nd, 256, 0, st>>>(g);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
     const unsigned grid = ((unsigned)g.w.slices * g.w.ctiles * g.w.ktiles + 7) / 8 * 8;
     auto go = [&](auto t, auto x8, auto norm) {
         typedef decltype(t) T;
