@@ -468,7 +468,7 @@ const char* wino_status_string(int status) {
     }
 }
 
-int wino_version(void) { return 100; }
+int wino_version(void) { return 101; }
 
 size_t wino_filter_bytes_r(int C, int K, int m, int r) {
     if (C <= 0 || K <= 0 || !supported(m, r)) return 0;

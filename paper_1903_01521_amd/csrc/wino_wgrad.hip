@@ -188,23 +188,31 @@ struct Wgrad {
         }
     }
 
-    // Byte of its own image that a lane loads for segment e, whose band starts lower.
+    // Byte of its own image that a lane loads for segment e: of its e mod 2^lb th band.
     __device__ __forceinline__ uint32_t byte_of(uint32_t from, int e, uint32_t row_bytes) const {
-        return from + (uint32_t)((e & ((1 << g.w.lb) - 1)) * g.w.hb) * row_bytes;
+        const uint32_t band = (uint32_t)g.w.hb * row_bytes;
+        const uint32_t b1 = g.w.lb >= 1 ? band : 0, b2 = g.w.lb >= 2 ? 2 * band : 0, b4 = g.w.lb >= 3 ? 4 * band : 0;
+        return from + (e & 1 ? b1 : 0) + (e & 2 ? b2 : 0) + (e & 4 ? b4 : 0);
     }
 
     // Eight loads of one item: an image is a buffer of its own, so that rows above and
     // below it and lanes beside it (kOutside, and a band's offset) read as zero: images
-    // are below 2^31 bytes, and so are the rows that are asked for outside them.
+    // are below 2^31 bytes, and so are the rows that are asked for outside them.  The
+    // image's address goes on from segment to segment, which takes few scalar registers.
     template <typename V>
     __device__ __forceinline__ void load8(uint32_t (&r)[kSeg], const void* base, uint32_t image, uint32_t row_bytes,
                                           uint32_t at) const {
         // in scalar registers, as the compiler does not see by itself
         const int first_image = __builtin_amdgcn_readfirstlane(next.oct) * kSeg >> g.w.lb;
         const char* p = (const char*)base + (size_t)first_image * image;
+        const uint32_t i1 = g.w.lb == 0 ? image : 0, i2 = g.w.lb <= 1 ? image : 0, i4 = g.w.lb <= 2 ? image : 0;
 #pragma unroll
         for (int e = 0; e < kSeg; ++e) {
-            const auto b = __builtin_amdgcn_make_buffer_rsrc((void*)(p + (size_t)(e >> g.w.lb) * image), 0, (int)image, kRsrcWord3);
+            if (e) {
+                p += e & 1 ? i1 : e & 2 ? i2 : i4;
+                asm volatile("" : "+s"(p));
+            }
+            const auto b = __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, (int)image, kRsrcWord3);
             const int o = (int)byte_of(at, e, row_bytes);
             if constexpr (sizeof(V) == 4) r[e] = __builtin_amdgcn_raw_buffer_load_b32(b, o, 0, 0);
             else if constexpr (sizeof(V) == 2) r[e] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(b, o, 0, 0);
@@ -212,24 +220,31 @@ struct Wgrad {
         }
     }
 
-    // Loads of step `next`: the input's row t + 2 of the strip's columns and
-    // one more on each side, dy's row t.  A lane takes one column and channel, of the
-    // eight segments.
+    // Loads of step `next`: the input's row t + 2 of the strip's columns and one more on
+    // each side, dy's row t.  A lane takes one column and channel, of the eight segments.
+    // One code path for both where their elements are as wide: the compiler joins two
+    // and then waits for the loads at once.
     __device__ __forceinline__ void fetch(Raws& raw) const {
 #pragma unroll
         for (int p = 0; p < kPer; ++p) {
             const int item = wave + p * kWaves;
-            if (item < kAItems) {
-                const int at = item * 64 + lane, col = next.strip * kCols + at / CT - g.s.pad, ch = c0 + at % CT;
-                const int y = next.t + 2 - g.s.pad;
-                const bool inside = col >= 0 && col < g.s.W && ch < g.s.C;
-                raw.from[p] = inside ? (uint32_t)((y * g.s.W + col) * g.s.C + ch) * (uint32_t)sizeof(S) : kOutside;
-                load8<S>(raw.v[p], X8 ? (const void*)g.a.codes : g.a.x, in_image, in_row, raw.from[p]);
-            } else if (item < kItems && next.active) {
-                const int at = (item - kAItems) * 64 + lane, col = next.strip * kCols + at / KT, ch = k0 + at % KT;
-                const bool inside = col < g.s.Wo && ch < g.s.K;
-                const uint32_t o = inside ? (uint32_t)((next.t * g.s.Wo + col) * g.s.K + ch) * (uint32_t)sizeof(T) : kOutside;
-                load8<T>(raw.v[p], g.a.dy, dy_image, dy_row, o);
+            const bool input = item < kAItems;
+            if (item >= kItems || (!input && !next.active)) continue;
+            const int at = (input ? item : item - kAItems) * 64 + lane;
+            const int wide = input ? g.s.W : g.s.Wo, chs = input ? g.s.C : g.s.K;
+            const int col = next.strip * kCols + (input ? at / CT - g.s.pad : at / KT), ch = input ? c0 + at % CT : k0 + at % KT;
+            const int y = input ? next.t + 2 - g.s.pad : next.t;
+            const bool inside = col >= 0 && col < wide && ch < chs;
+            const uint32_t value = (uint32_t)((y * wide + col) * chs + ch);
+            if constexpr (!X8) {
+                const uint32_t from = inside ? value * (uint32_t)sizeof(T) : kOutside;
+                raw.from[p] = from;
+                load8<T>(raw.v[p], input ? g.a.x : g.a.dy, input ? in_image : dy_image, input ? in_row : dy_row, from);
+            } else if (input) {
+                raw.from[p] = inside ? value : kOutside;
+                load8<S>(raw.v[p], g.a.codes, in_image, in_row, raw.from[p]);
+            } else {
+                load8<T>(raw.v[p], g.a.dy, dy_image, dy_row, inside ? value * (uint32_t)sizeof(T) : kOutside);
             }
         }
     }
@@ -259,20 +274,28 @@ struct Wgrad {
                 else l.d[slot & 1][0][at / KT][at % KT] = o;
             } else if (input) {
                 const int at = item * 64 + lane, c = at % CT;
+                if constexpr (!X8 && !NORM) {
 #pragma unroll
-                for (int e = 0; e < kSeg; ++e) {
-                    v[e] = value<S>(raw.v[p][e]);
-                    if constexpr (!X8 && !NORM) {
-                        v[e] *= in_scale;
-                    } else {
-                        const float2 f = l.f[s.oct & 1][e][c];
-                        v[e] = fmaf(v[e], f.x, f.y);
-                        if constexpr (NORM) {
-                            const bool silu = g.s.act == Act::Silu;
-                            v[e] = in_scale * (silu ? act_of<true>(v[e], false) : act_of<false>(v[e], g.s.act == Act::Relu));
+                    for (int e = 0; e < kSeg; ++e) v[e] = value<S>(raw.v[p][e]) * in_scale;
+                } else {
+                    float2 f[kSeg];                   // read together
+#pragma unroll
+                    for (int e = 0; e < kSeg; ++e) f[e] = l.f[s.oct & 1][e][c];
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int e = 0; e < kSeg; ++e) v[e] = fmaf(value<S>(raw.v[p][e]), f[e].x, f[e].y);
+                    if constexpr (NORM) {
+                        if (g.s.act == Act::Silu) {
+#pragma unroll
+                            for (int e = 0; e < kSeg; ++e) v[e] = in_scale * act_of<true>(v[e], false);
+                        } else {
+                            const bool relu = g.s.act == Act::Relu;
+#pragma unroll
+                            for (int e = 0; e < kSeg; ++e) v[e] = in_scale * act_of<false>(v[e], relu);
                         }
-                        v[e] = byte_of(raw.from[p], e, in_row) < in_image ? v[e] : 0.0f;
                     }
+#pragma unroll
+                    for (int e = 0; e < kSeg; ++e) v[e] = byte_of(raw.from[p], e, in_row) < in_image ? v[e] : 0.0f;
                 }
                 uint4 o[TA];
                 split8<H, TA>(v, o);

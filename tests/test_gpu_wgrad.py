@@ -171,3 +171,25 @@ def test_repeats_on_a_stream_and_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(first, dg)
+
+
+def test_tensors_past_4_gib():
+    # 2.7e9 values a tensor; all but the last image zero, so that dg is that image's own.
+    # Both calls sum in 32 bits in another order: SUM of the sums of absolute values.
+    N, H, W, C, K = 41, 1024, 1024, 64, 64
+    gen = torch.Generator(device=h.DEV)
+    gen.manual_seed(0)
+    x = torch.zeros((N, H, W, C), dtype=torch.bfloat16, device=h.DEV)
+    dy = torch.zeros((N, H, W, K), dtype=torch.bfloat16, device=h.DEV)
+    x[-1].copy_(torch.randn((H, W, C), generator=gen, device=h.DEV))
+    dy[-1].copy_(torch.randn((H, W, K), generator=gen, device=h.DEV))
+
+    def call(x, dy):
+        n = x.shape[0]
+        dg = torch.empty((K, C, 3, 3), device=h.DEV)
+        wsb = B.wino_conv2d_wgrad_workspace_bytes(n, C, H, W, K, 1, B.WINO_IO_BF16)
+        B.check(B.wino_conv2d_wgrad_nhwc(x, dy, dg, None, None, None, 0, n, C, H, W, K, 1, B.WINO_IO_BF16, h.space(wsb), wsb))
+        return dg
+    whole, last = call(x, dy), call(x[-1:], dy[-1:])
+    size = call(x[-1:].abs(), dy[-1:].abs())
+    assert bool(((whole - last).abs() <= h.SUM * size).all()) and float(last.abs().max()) > 0
