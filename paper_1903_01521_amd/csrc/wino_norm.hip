@@ -91,21 +91,52 @@ struct High {
     __device__ __forceinline__ float operator()(float a, float b) const { return __builtin_elementwise_maximum(a, b); }
 };
 
+// v joined with the lanes `ROR` further on, in turn, of each row of 16 (DPP row_ror).
+template <int ROR, typename Op>
+__device__ __forceinline__ float join_ror(float v, Op op) {
+    const int i = __float_as_int(v);
+    return op(v, __int_as_float(__builtin_amdgcn_update_dpp(i, i, 0x120 | ROR, 0xf, 0xf, false)));
+}
+
+// v joined over the lanes whose numbers differ by multiples of `apart`, a power of two:
+// rotations within the rows of 16, then the rows' swaps.  No LDS, 8 cycles a step where
+// a shuffle through LDS takes about 120.
+template <typename Op>
+__device__ __forceinline__ float join_lanes(float v, int apart, Op op) {
+    if (apart <= 8) v = join_ror<8>(v, op);
+    if (apart <= 4) v = join_ror<4>(v, op);
+    if (apart <= 2) v = join_ror<2>(v, op);
+    if (apart <= 1) v = join_ror<1>(v, op);
+    if (apart <= 16) {
+        const auto q = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = op(__uint_as_float(q[0]), __uint_as_float(q[1]));
+    }
+    const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return op(__uint_as_float(q[0]), __uint_as_float(q[1]));
+}
+
+__device__ __forceinline__ float wave_sum(float v) { return join_lanes(v, 1, Add()); }
+
 // red[parts][cb] = the threads' values of each channel, joined over a wave's rows.
 template <int VEC, typename Op>
 __device__ __forceinline__ void join_rows(float (&v)[VEC], const Cut& k, float* red, Op op) {
     const int t = threadIdx.x, lane = t & 63;
     if (k.wrows) {
-        const int row = (int)fdiv(lane, k.dcv);
-        for (int n = k.wrows; n > 1;) {
-            const int h = (n + 1) / 2;
-            const bool take = row + h < n;
+        if (k.wrows * k.cv == 64) {           // both powers of two
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                const float o = __shfl(v[j], (lane + h * k.cv) & 63);
-                if (take) v[j] = op(v[j], o);
+            for (int j = 0; j < VEC; ++j) v[j] = join_lanes(v[j], k.cv, op);
+        } else {
+            const int row = (int)fdiv(lane, k.dcv);
+            for (int n = k.wrows; n > 1;) {
+                const int h = (n + 1) / 2;
+                const bool take = row + h < n;
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const float o = __shfl(v[j], (lane + h * k.cv) & 63);
+                    if (take) v[j] = op(v[j], o);
+                }
+                n = h;
             }
-            n = h;
         }
         if (lane < k.cv) {
 #pragma unroll
@@ -141,15 +172,11 @@ __device__ __forceinline__ void join_groups(const Cut& k, const float* red, floa
                 const int part = (int)fdiv(i, k.dD), c = g * k.D + i - part * k.D;
                 a += weight(c) * red[part * k.cb + c];
             }
-        for (int m = lanes >> 1; m; m >>= 1) a += __shfl_xor(a, m);
+        if (lanes == 64) a = wave_sum(a);
+        else
+            for (int m = lanes >> 1; m; m >>= 1) a += __shfl_xor(a, m);
         if (g < groups && sub == 0) out[g] = a;
     }
-}
-
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m);
-    return v;
 }
 
 template <typename T, int VEC, int NV>
