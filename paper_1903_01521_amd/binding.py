@@ -342,13 +342,18 @@ WINO_IO_BF16 = 0x080
 WINO_IO_MASK = 0x0C0
 
 
+_io_dtypes = None      # WINO_IO_* -> torch's type, once a tensor was passed
+
+
 def _tptr(t, flags):
     """A tensor of the element type that WINO_IO_* names."""
+    global _io_dtypes
     if t is None or isinstance(t, int):
         return t
-    torch = _torch or _import_torch()
-    kind = flags & WINO_IO_MASK
-    if t.dtype is not (torch.float16 if kind == WINO_IO_F16 else torch.bfloat16 if kind == WINO_IO_BF16 else torch.float32):
+    if _io_dtypes is None:
+        torch = _import_torch()
+        _io_dtypes = {0: torch.float32, WINO_IO_F16: torch.float16, WINO_IO_BF16: torch.bfloat16}
+    if t.dtype is not _io_dtypes.get(flags & WINO_IO_MASK):
         raise ValueError("tensors must have the element type that the flags name")
     return _ptr(t)
 

@@ -458,7 +458,7 @@ struct Wgrad {
 
 // The largest magnitudes: of blocks below nx of the input's (a raw tensor's, the
 // checkpoint's rows', or the norm's bound |gamma| sqrt(D P) + |beta|, doubled for what a
-// checkpoint adds), of the others of dy's.
+// checkpoint adds), of the others of dy's.  205 MB in 33 us, 6.3 TB/s.
 template <typename T>
 __device__ uint32_t most_of(const T* p, int64_t n, int block, int blocks) {
     constexpr int V = 16 / sizeof(T);
@@ -516,7 +516,12 @@ __global__ __launch_bounds__(256) void k_wgrad_most(Args g) {
 }
 
 // A workgroup a tile of channels and filters and a slice of the rows; tiles of the
-// same slice run on one XCD, so that they share its rows in L2.
+// same slice run on one XCD, so that they share its rows in L2.  144 accumulators a lane
+// hold the nine taps of 16 channels by 64 filters: a step reads 18 words of the input and
+// 8 of dy from LDS for 108 products, so the matrix cores bound it (N = 64, 256 -> 256 at
+// 56x56, fp32: 495 us, 1.43 PFLOP/s of fp16 products; formed from the checkpoint with
+// SiLU 560, the matrix cores 60% busy; bf16, one product of each, 285 us, 0.83 PFLOP/s,
+// bound by the loads of two bytes a lane).  Small layers are a chain of steps of 1.3 us.
 template <typename T, bool X8, bool NORM, int WC, int KW, int KS>
 __global__ __launch_bounds__(WC* KW* KS * 64, WC* KW* KS / 4) void k_wgrad(Args g) {
     typedef Wgrad<T, X8, NORM, WC, KW, KS> W;
@@ -625,10 +630,11 @@ double step_of(const WgradShape& s, int form) {
 // The form and number of slices of the least estimated time: 11 us for two launches,
 // the first loads and the last stores; a step for every row of a slice and two for
 // every strip that it enters; the slices' parts, 72 bytes a filter and channel, written
-// and read at 8 TB/s.  Measured against it (us): N = 8, 128 -> 128 at 28x28 25.9 and 28
-// (third form, 32 slices), 35.1 and 35.5 (first, 32); N = 64, 256 -> 256 at 56x56 485
-// and 501 (first, 32), 494 and 511 (second, 16); N = 1, 256 -> 256 at 56x56 32.1 and 35
-// (second, 16).
+// and read at 8 TB/s.  (The launch for the scale is the same for all.)  Against every
+// form at 4 to 224 slices its choice was within 6% of the best (us): N = 8, 128 -> 128 at
+// 28x28 31.4 (third form, 28 slices; first form 35.7 at best); N = 1, 256 -> 256 at 56x56
+// 37.4 (second, 13; 36.1 at 16); N = 32, 512 -> 512 at 14x14 97.5 (second, 4; 97.3);
+// N = 32, 256 -> 256 at 28x28 in bf16 59.3 (59.5).
 Walk walk_of(const WgradShape& s) {
     Walk best = {};
     double least = 0.0;
