@@ -232,7 +232,8 @@ struct Wgrad {
             if (item >= kItems || (!input && !next.active)) continue;
             const int at = (input ? item : item - kAItems) * 64 + lane;
             const int wide = input ? g.s.W : g.s.Wo, chs = input ? g.s.C : g.s.K;
-            const int col = next.strip * kCols + (input ? at / CT - g.s.pad : at / KT), ch = input ? c0 + at % CT : k0 + at % KT;
+            const int col = next.strip * kCols + (input ? at / CT - g.s.pad : at / KT);
+            const int ch = input ? c0 + at % CT : k0 + at % KT;
             const int y = input ? next.t + 2 - g.s.pad : next.t;
             const bool inside = col >= 0 && col < wide && ch < chs;
             const uint32_t value = (uint32_t)((y * wide + col) * chs + ch);
@@ -645,7 +646,8 @@ Walk walk_of(const WgradShape& s) {
         auto take = [&](int64_t slices) {
             if (slices < 1 || slices > most || slices > w.rows) return;
             const double rows = (double)((w.rows + slices - 1) / slices);
-            const double t = 11.0 + rounds * step * (rows + 2.0 * (1.0 + (rows - 1.0) / w.hb)) + (double)slices * s.C * s.K * 72.0 / 8e6;
+            const double parts = (double)slices * s.C * s.K * 72.0 / 8e6;
+            const double t = 11.0 + rounds * step * (rows + 2.0 * (1.0 + (rows - 1.0) / w.hb)) + parts;
             if (best.slices && t >= least) return;
             least = t;
             w.slices = (int)slices;
@@ -706,7 +708,8 @@ hipError_t launch_wgrad(const WgradArgs& a, const WgradShape& s, void* ws, hipSt
     else with(__bf16());
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    k_wgrad_sum<<<(unsigned)((s.K + 31) / 32) * ((s.C + 7) / 8) * 3, 256, 0, st>>>((const float*)ws, a.dg, s.C, s.K, g.w.slices);
+    const unsigned blocks3 = (unsigned)((s.K + 31) / 32) * ((s.C + 7) / 8) * 3;
+    k_wgrad_sum<<<blocks3, 256, 0, st>>>((const float*)ws, a.dg, s.C, s.K, g.w.slices);
     return hipGetLastError();
 }
 

@@ -32,7 +32,9 @@ def test_workspace_bytes():
         assert f(0, 128, 28, 28, 32, 0) == MAX
         assert f(8, 128, 28, 28, 32, 0x100) == MAX
         assert f(8, 128, 28, 28, 32, B.WINO_IO_F16 | B.WINO_IO_BF16) == MAX
+        assert f(2**31 - 1, 4, 1, 1, 4, 0) == MAX               # an image a workgroup, past 2^30
     assert B.wino_act8_workspace_bytes(1, 8, 4, 4, B.WINO_FLAG_RELU) == MAX
+    assert B.wino_act8_workspace_bytes(2**31 - 1, 4, 1, 1, 0) == MAX
     assert B.wino_conv2d_wgrad_workspace_bytes(1, 32, 2, 56, 32, 0, 0) == MAX     # no output row
     assert B.wino_conv2d_wgrad_workspace_bytes(1, 32, 56, 56, 32, -1, 0) == MAX
     assert B.wino_conv2d_wgrad_workspace_bytes(64, 8, 8192, 8192, 8, 1, 0) == MAX  # 2^32 pixels
@@ -50,6 +52,7 @@ def _norm(x=at(1), gamma=at(2), beta=at(3), y=at(4), stats=at(5), q=at(6), N=1, 
     (dict(q=at(1)), INV), (dict(stats=at(2)), INV), (dict(N=2**31 - 1, C=2**31 - 2), INV),
     (dict(flags=0x100), UNS), (dict(flags=B.WINO_FLAG_ACT8), UNS), (dict(flags=B.WINO_FLAG_RELU | B.WINO_FLAG_SILU), UNS),
     (dict(flags=B.WINO_IO_F16 | B.WINO_IO_BF16), UNS), (dict(flags=B.WINO_PREC_F16), UNS),
+    (dict(N=2**31 - 1, C=4, H=1, W=1, y=at(4) + (1 << 38)), UNS),
     (dict(C=64, H=512, W=512, G=1), WS), (dict(C=64, H=512, W=512, G=1, ws=at(9), wsb=16), WS),
 ])
 def test_group_norm_refuses(kw, status):
