@@ -354,10 +354,12 @@ int wino_conv2d_nhwc(const float* x, const float* U, float* y,
  * of (centre, step); x is read back as centre + step * code.  Per image and
  * channel, with lo and hi the least and largest value and half = hi/2 - lo/2:
  *   centre = lo/2 + hi/2, step = half / 127, code = rint((x - centre) * (127 / half)),
- * each operation in fp32, so the error is at most half a step (1/508 of the
- * channel's range) and fp32 rounding.  half < 2^-100: step and codes are 0.  A
- * channel with an infinite or NaN value is read back as NaN throughout (other
- * channels are not touched).  wino_act8_bytes: the buffer's size (0 on invalid
+ * each operation in fp32 and codes past 127 or -127 taken as these (the centre's
+ * rounding reaches them in ranges of a few units in its last place), so the error is
+ * at most half a step (1/508 of the channel's range) and fp32 rounding, half a unit in
+ * the last place each of the centre and of the sum.  half < 2^-100: step and codes
+ * are 0.  A channel with an infinite or NaN value is read back as NaN throughout
+ * (other channels are not touched).  wino_act8_bytes: the buffer's size (0 on invalid
  * arguments).  _pack's workspace may be NULL where its size is 0; (size_t)-1 on
  * invalid arguments.  flags: WINO_IO_*. */
 size_t wino_act8_bytes(int N, int C, int H, int W);

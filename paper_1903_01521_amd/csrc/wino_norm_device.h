@@ -135,11 +135,12 @@ __device__ __forceinline__ Row row_of(float lo, float hi) {
     r.inverse = half < kFlat ? 0.0f : kCodes / half;
     return r;
 }
-// The code is the low byte: adding 1.5 * 2^23 rounds to an integer, ties to even.
-// |x - centre| is at most half but for its rounding, so the code is within +-127.
+// The code is the low byte: adding 1.5 * 2^23 rounds to an integer, ties to even.  The
+// centre's rounding takes one end of a range of a few units in its last place past 127
+// (three units: to 169), hence the limits, which keep NaN.
 __device__ __forceinline__ uint32_t code_bits(float x, float centre, float inverse) {
 #pragma clang fp contract(off)
-    const float q = (x - centre) * inverse;
+    const float q = __builtin_elementwise_maximum(__builtin_elementwise_minimum((x - centre) * inverse, kCodes), -kCodes);
     return __float_as_uint(q + 12582912.0f);
 }
 template <int V>
