@@ -74,9 +74,11 @@ __device__ __forceinline__ float rstd_of(float var, float eps) { return 1.0f / s
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
 
 // The activation's argument z and its normalised value n from a stored value v, x
-// itself or a code, for one channel.  SiLU: one fused operation each, on folded
-// constants.  Else (ReLU or none) every step of the definition is rounded: the sign
-// of z, which decides ReLU's gradient, is then the same in both passes.
+// itself or a code, for one channel.  The mean is subtracted first, so that a mean far
+// from zero costs no bits: of x itself, and of a checkpoint's centre.  SiLU of a code:
+// one fused operation on folded constants.  ReLU or none: every step of the definition
+// is rounded, so that the sign of z, which decides ReLU's gradient, is the same in both
+// passes.
 template <bool SILU, bool X8>
 struct Norm {
     float scale, shift, gamma, beta, mean, rstd, centre, step;
@@ -87,14 +89,14 @@ struct Norm {
         beta = b;
         centre = X8 ? row[0] : 0.0f;
         step = X8 ? row[1] : 1.0f;
-        if constexpr (SILU) {
-            scale = X8 ? rstd * step : rstd;
-            shift = (X8 ? centre - mean : -mean) * rstd;
+        if constexpr (SILU && X8) {
+            scale = rstd * step;
+            shift = (centre - mean) * rstd;
         }
     }
     __device__ __forceinline__ float n(float v) const {
 #pragma clang fp contract(off)
-        if constexpr (SILU) return fmaf(v, scale, shift);
+        if constexpr (SILU && X8) return fmaf(v, scale, shift);
         const float x = X8 ? v * step + centre : v;
         return (x - mean) * rstd;
     }
