@@ -116,7 +116,7 @@ struct Wgrad {
     struct Lds {
         uint4 a[4][TA][kACols][CT];           // ring of input rows
         uint4 d[2][TB][kCols][KT];
-        float2 f[2][kSeg][CT];                // the channels' norm, by image, of this octet and the next
+        float2 f[2][kSeg][CT];                // constants by image and channel, of this octet and the next
     };
 
     const Args& g;
@@ -127,6 +127,7 @@ struct Wgrad {
     Step next;                                // the step fetched last or next
     int first;                                // its strip's first active row
     float in_scale, dy_scale;
+    float gamma, beta;                        // of the lane's channel, lane % CT of the tile
     // One step's loads: values as they are, and the byte of the first segment's image
     // that a lane loads.
     struct Raws {
@@ -139,7 +140,13 @@ struct Wgrad {
           in_image((uint32_t)(args.s.H * args.s.W * args.s.C) * (uint32_t)sizeof(S)),
           in_row((uint32_t)(args.s.W * args.s.C) * (uint32_t)sizeof(S)),
           dy_image((uint32_t)(args.s.Ho * args.s.Wo * args.s.K) * (uint32_t)sizeof(T)),
-          dy_row((uint32_t)(args.s.Wo * args.s.K) * (uint32_t)sizeof(T)), row(r0), row1(r1), in_scale(si), dy_scale(sd) {}
+          dy_row((uint32_t)(args.s.Wo * args.s.K) * (uint32_t)sizeof(T)), row(r0), row1(r1), in_scale(si), dy_scale(sd) {
+        if constexpr (NORM && !X8) {
+            const int own = c0 + lane % CT;
+            gamma = g.a.gamma && own < g.s.C ? g.a.gamma[own] : 1.0f;
+            beta = g.a.beta && own < g.s.C ? g.a.beta[own] : 0.0f;
+        }
+    }
 
     // The steps of rows [row, row1): of each strip's share two rows more.
     __device__ __forceinline__ bool enter() {
@@ -163,7 +170,8 @@ struct Wgrad {
         return enter();
     }
 
-    // The norm's constants of an octet: z = v scale + shift.
+    // The constants of an octet: mean and rstd of x; of a checkpoint, whose centre the
+    // mean is subtracted from, those of z = code scale + shift.
     __device__ __forceinline__ void fill_norm(int oct) {
         if constexpr (NORM) {
             for (int i = threadIdx.x; i < kSeg * CT; i += kThreads) {
@@ -172,10 +180,14 @@ struct Wgrad {
                 if (c < g.s.C) {
                     const int n = seg >> g.w.lb;
                     const float* st = g.a.stats + ((size_t)n * g.s.G + c / g.s.D) * 2;
-                    const float* r = X8 ? g.a.rows + ((size_t)n * g.s.C + c) * 2 : nullptr;
-                    const float gamma = g.a.gamma ? g.a.gamma[c] : 1.0f, beta = g.a.beta ? g.a.beta[c] : 0.0f;
-                    f.x = st[1] * gamma * (X8 ? r[1] : 1.0f);
-                    f.y = fmaf((X8 ? r[0] : 0.0f) - st[0], st[1] * gamma, beta);
+                    if constexpr (X8) {
+                        const float* r = g.a.rows + ((size_t)n * g.s.C + c) * 2;
+                        const float scale = st[1] * (g.a.gamma ? g.a.gamma[c] : 1.0f);
+                        f.x = scale * r[1];
+                        f.y = fmaf(r[0] - st[0], scale, g.a.beta ? g.a.beta[c] : 0.0f);
+                    } else {
+                        f = make_float2(st[0], st[1]);
+                    }
                 }
                 l.f[oct & 1][e][i % CT] = f;
             }
@@ -257,6 +269,20 @@ struct Wgrad {
         return h.value(0);
     }
 
+    // The activation's argument: of x as the norm's own passes form it (folded constants
+    // lose the bits of a mean far from zero, and take 600 us where this takes 610 at
+    // N = 64, 256 -> 256, 56x56); of a code it is there already.
+    template <bool SILU>
+    __device__ __forceinline__ float argument(float v, float2 f) const {
+        if constexpr (X8) return v;
+        Norm<SILU, false> norm;
+        norm.mean = f.x;
+        norm.rstd = f.y;
+        norm.gamma = gamma;
+        norm.beta = beta;
+        return norm.z(norm.n(v));
+    }
+
     // The fetched values to LDS, in terms: `slot` of the ring, buffer slot & 1 of dy.
     __device__ __forceinline__ void store(int slot, const Step& s, const Raws& raw) {
 #pragma unroll
@@ -284,15 +310,18 @@ struct Wgrad {
                     for (int e = 0; e < kSeg; ++e) f[e] = l.f[s.oct & 1][e][c];
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int e = 0; e < kSeg; ++e) v[e] = fmaf(value<S>(raw.v[p][e]), f[e].x, f[e].y);
+                    for (int e = 0; e < kSeg; ++e) {
+                        const float stored = value<S>(raw.v[p][e]);
+                        v[e] = X8 ? fmaf(stored, f[e].x, f[e].y) : stored;
+                    }
                     if constexpr (NORM) {
                         if (g.s.act == Act::Silu) {
 #pragma unroll
-                            for (int e = 0; e < kSeg; ++e) v[e] = in_scale * act_of<true>(v[e], false);
+                            for (int e = 0; e < kSeg; ++e) v[e] = in_scale * act_of<true>(argument<true>(v[e], f[e]), false);
                         } else {
                             const bool relu = g.s.act == Act::Relu;
 #pragma unroll
-                            for (int e = 0; e < kSeg; ++e) v[e] = in_scale * act_of<false>(v[e], relu);
+                            for (int e = 0; e < kSeg; ++e) v[e] = in_scale * act_of<false>(argument<false>(v[e], f[e]), relu);
                         }
                     }
 #pragma unroll
