@@ -404,13 +404,19 @@ int wino_group_norm_backward_nhwc(const void* dy, const void* x, const float* st
  * a read as zero outside the image.  stats NULL: a is x (or with WINO_FLAG_ACT8 the
  * checkpoint's values), and G, gamma and beta are not read.  Else a is the y of
  * wino_group_norm_nhwc, formed again from x or its checkpoint on load (flags:
- * that call's activation), not rounded to 16 bits.
+ * that call's activation; stats: that call's of this x), not rounded to 16 bits.
  *   fp32 operands (and inputs formed on load) are held in two fp16 terms, 22
- *   significand bits, scaled so that the tensor's largest finite value is 2^14: results
- *   are as near the exact ones as fp32 sums of fp32 products are, and values below 2^-17
- *   of the largest are off by less than 2^-39 of it.  Values that are not finite give
- *   results that are not (NaN where fp32 would give infinities), in their channel or
- *   filter.  16-bit tensors are exact.
+ *   significand bits, each channel and each filter scaled by its own power of two, so
+ *   that the largest finite value that it may hold is 2^14: a product is off by less
+ *   than 2^-20 of itself, sums of many as little as fp32 sums are, and a value below 2^-17
+ *   of that largest one by less than 2^-39 of it.  The largest one is that of the tensor's
+ *   channel or filter; of a checkpoint |centre| + 127 step; through the norm
+ *   2 |gamma| sqrt(D H W) + |beta| or, of a checkpoint,
+ *   |gamma| (|centre - mean| + 127 step) rstd + |beta|.  Two fp16 tensors, or two bf16
+ *   ones, are multiplied exactly, and fp16 dy always; bf16 dy with an input formed on load
+ *   has one scaled fp16 term, exact from 2^-31 of its filter's largest value, off by
+ *   less than 2^-39 of it below.  Sums are fp32.  Values that are not finite give results
+ *   that are not (NaN where fp32 would give infinities), in their channel or filter.
  *   N*Ho*Wo must be below 2^31 (INVALID_ARG), and (H + 2*pad + 16)*W*C and
  *   (H + 2*pad + 16)*Wo*K below 2^29 (UNSUPPORTED). */
 size_t wino_conv2d_wgrad_workspace_bytes(int N, int C, int H, int W, int K, int pad, unsigned flags);

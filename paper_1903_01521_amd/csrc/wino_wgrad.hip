@@ -12,12 +12,15 @@
 // happens in the registers that the eight loads fill.
 //
 // fp32 operands are held in two fp16 terms, 22 significand bits, and three of the four
-// products are summed in fp32: a product is off by 2^-21 at most, and results are as
-// near the exact ones as fp32 sums are (two bf16 terms, 16 bits, gave 4.5e-6 of the
-// norm where these give 2e-7).  For fp16's range they are scaled by a power of two that
-// takes the tensor's largest finite value to 2^14, found by a launch before: values
-// below 2^-17 of it lose bits, in all less than 2^-39 of it.  bf16 values have one term
-// then, and tensors that are both bf16 or both fp16 are multiplied as they are.
+// products are summed in fp32: a product is off by less than 2^-20 (2^-22 from each
+// operand and from the term left out), and results of many products as near the exact
+// ones as fp32 sums are (two bf16 terms, 16 bits, gave 4.5e-6 of the norm where these
+// give 2e-7).  For fp16's range every channel of the input and every filter of dy is
+// scaled by a power of two of its own, which takes the largest finite value that it
+// holds to 2^14, found by a launch before: values below 2^-17 of that lose bits, in all
+// less than 2^-39 of it.  dg has one channel and one filter an element, so what the others
+// hold costs it nothing.  bf16 values have one term then (exact from 2^-31 of their
+// filter's largest), and tensors that are both bf16 or both fp16 are multiplied as they are.
 #include <math.h>
 
 #include <type_traits>
@@ -30,7 +33,8 @@ namespace wino {
 
 namespace {
 
-constexpr int kMost = 1024;                   // blocks that look for a tensor's largest magnitude
+constexpr int kMost = 256;                    // blocks that look for a tensor's largest magnitudes
+constexpr int kMostThreads = 1024;
 constexpr int kSeg = 8;                       // images or bands that a lane sums over
 constexpr uint32_t kOutside = 1u << 31;        // an offset past every image
 
@@ -48,7 +52,7 @@ struct Args {
     WgradShape s;
     Walk w;
     float* part;                              // [slices][9][C][K]
-    uint32_t* most;                           // magnitudes, as bits: `nx` of the input, then `nd` of dy
+    uint8_t* most;                            // exponents: nx rows of the input's channels, nd of dy's filters
     int nx, nd;                               // none: not scaled
 };
 
@@ -72,25 +76,47 @@ __device__ __forceinline__ void split8(const float (&v)[kSeg], uint4 (&o)[TERMS]
     if constexpr (TERMS == 2) o[1] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
 }
 
-// The power of two for a tensor whose largest magnitude has these bits, which goes to
-// 2^14, and two values' larger one: infinities and NaN do not count.
-__device__ __forceinline__ int exponent_of(uint32_t bits) {
-    const int e = bits ? 14 + 127 - (int)(bits >> 23) : 0;
-    return e < -126 ? -126 : e > 126 ? 126 : e;
+// The power of two for a channel or filter whose largest magnitude has this biased
+// exponent, which goes to 2^14, and two values' larger one: infinities and NaN do not count.
+__device__ __forceinline__ int exponent_of(uint32_t biased) {
+    const int e = 14 + 127 - (int)biased;
+    return e > 126 ? 126 : e;
 }
 __device__ __forceinline__ float power(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
 __device__ __forceinline__ uint32_t larger(uint32_t m, float v) {
     const uint32_t b = __float_as_uint(v) & 0x7fffffffu;
     return b < 0x7f800000u && b > m ? b : m;
 }
-__device__ __forceinline__ uint32_t wave_max(uint32_t m) {
+__host__ __device__ __forceinline__ int most_row(int channels) { return (channels + 3) / 4 * 4; }
+
+// Four channels from c on of a row's bytes, the largest of `rows` rows, `per` apart.
+struct Most4 {
+    uint32_t m[4];
+    __device__ __forceinline__ void load(const uint8_t* most, int rows, int channels, int c, int row, int per) {
+        const int stride = most_row(channels);
+        m[0] = m[1] = m[2] = m[3] = 0;
+        if (c >= channels) return;
+        for (int r = row; r < rows; r += 4 * per) {
+            uint32_t w[4];                    // four loads in flight, of the last row again past it
 #pragma unroll
-    for (int i = 32; i; i >>= 1) {
-        const uint32_t o = (uint32_t)__shfl_xor((int)m, i);
-        m = o > m ? o : m;
+            for (int u = 0; u < 4; ++u) {
+                const int at = r + u * per < rows ? r + u * per : rows - 1;
+                w[u] = *(const uint32_t*)(most + (size_t)at * stride + c);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t e = w[u] >> (8 * j) & 0xff;
+                    m[j] = e > m[j] ? e : m[j];
+                }
+        }
     }
-    return m;
-}
+    __device__ __forceinline__ void join(uint32_t* exps) const {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) atomicMax(exps + j, m[j]);
+    }
+};
 
 // One step of the walk: local row t of a strip of an octet; below the first row of
 // the range only the input's row is fetched.
@@ -126,8 +152,9 @@ struct Wgrad {
     int64_t row, row1;                        // rows still to be entered
     Step next;                                // the step fetched last or next
     int first;                                // its strip's first active row
-    float in_scale, dy_scale;
-    float gamma, beta;                        // of the lane's channel, lane % CT of the tile
+    const uint32_t *in_exps, *dy_exps;        // of the tile's channels' and filters' largest values, in LDS
+    float in_scale, dy_scale;                 // of the lane's channel, lane % CT of the tile, and
+    float gamma, beta;                        // filter; its channel's parameters
     // One step's loads: values as they are, and the byte of the first segment's image
     // that a lane loads.
     struct Raws {
@@ -135,12 +162,16 @@ struct Wgrad {
     };
     f32x4 acc[9][4];
 
-    __device__ __forceinline__ Wgrad(const Args& args, Lds& lds, int c, int k, int64_t r0, int64_t r1, float si, float sd)
+    __device__ __forceinline__ Wgrad(const Args& args, Lds& lds, int c, int k, int64_t r0, int64_t r1, const uint32_t* xe, const uint32_t* de)
         : g(args), l(lds), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), lane(threadIdx.x & 63), c0(c), k0(k),
           in_image((uint32_t)(args.s.H * args.s.W * args.s.C) * (uint32_t)sizeof(S)),
           in_row((uint32_t)(args.s.W * args.s.C) * (uint32_t)sizeof(S)),
           dy_image((uint32_t)(args.s.Ho * args.s.Wo * args.s.K) * (uint32_t)sizeof(T)),
-          dy_row((uint32_t)(args.s.Wo * args.s.K) * (uint32_t)sizeof(T)), row(r0), row1(r1), in_scale(si), dy_scale(sd) {
+          dy_row((uint32_t)(args.s.Wo * args.s.K) * (uint32_t)sizeof(T)), row(r0), row1(r1), in_exps(xe), dy_exps(de) {
+        static_assert(64 % CT == 0 && KT % 64 == 0, "a lane's channel and filter are the same in all its items");
+        static_assert(KT == 64 || (KT == 128 && kAItems % 2 == 0 && kWaves % 2 == 0), "and its wave's half of them");
+        in_scale = kAsIs ? 1.0f : power(exponent_of(in_exps[lane % CT]));
+        dy_scale = kAsIs ? 1.0f : power(exponent_of(dy_exps[(wave * 64 + lane) % KT]));
         if constexpr (NORM && !X8) {
             const int own = c0 + lane % CT;
             gamma = g.a.gamma && own < g.s.C ? g.a.gamma[own] : 1.0f;
@@ -438,7 +469,7 @@ struct Wgrad {
     }
 
     // acc to part: channel lane % 16 of the wave's, filters 4 (lane / 16) + i of each 16.
-    __device__ __forceinline__ void finish(int slice, int exponent) {
+    __device__ __forceinline__ void finish(int slice) {
         const int wc = wave % WC, wk = wave / WC, kw = KS > 1 ? 0 : wk;
         if constexpr (KS > 1) {
             // the columns' halves joined through LDS, in order, three taps at a time
@@ -457,13 +488,17 @@ struct Wgrad {
             }
             if (wk) return;
         }
-        if constexpr (!kAsIs)
+        if constexpr (!kAsIs) {
+            const int in = exponent_of(in_exps[wc * 16 + (lane & 15)]);
 #pragma unroll
-            for (int tap = 0; tap < 9; ++tap)
+            for (int f = 0; f < 4; ++f)
 #pragma unroll
-                for (int f = 0; f < 4; ++f)
+                for (int i = 0; i < 4; ++i) {
+                    const int exponent = in + exponent_of(dy_exps[kw * 64 + f * 16 + (lane >> 4) * 4 + i]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[tap][f][i] = ldexpf(acc[tap][f][i], -exponent);
+                    for (int tap = 0; tap < 9; ++tap) acc[tap][f][i] = ldexpf(acc[tap][f][i], -exponent);
+                }
+        }
         const int c = c0 + wc * 16 + (lane & 15), k = k0 + kw * 64 + (lane >> 4) * 4;
         if (c >= g.s.C) return;
         const size_t plane = (size_t)g.s.C * g.s.K;
@@ -486,20 +521,44 @@ struct Wgrad {
     }
 };
 
-// The largest magnitudes: of blocks below nx of the input's (a raw tensor's, the
-// checkpoint's rows', or the norm's bound |gamma| sqrt(D P) + |beta|, doubled for what a
-// checkpoint adds), of the others of dy's.  205 MB in 33 us, 6.3 TB/s.
+// The exponents of a channel-last tensor's largest magnitudes, n values of C channels:
+// row `block` of `blocks`.  16 bytes a load of whichever C: a run of C / gcd(C, V) vectors
+// is whole pixels, so a thread that moves on by whole runs keeps its V channels.  (One
+// value a load, each thread a channel, for tensors off 16-byte addresses and for more runs'
+// vectors than threads.)  205 MB in 33 us, 6.3 TB/s.
 template <typename T>
-__device__ uint32_t most_of(const T* p, int64_t n, int block, int blocks) {
-    constexpr int V = 16 / sizeof(T);
-    uint32_t m = 0;
-    int64_t done = 0;
-    if (((uintptr_t)p & 15) == 0) {
-        const int64_t all = n / V, step = (int64_t)blocks * 256;
-        int64_t i = (int64_t)block * 256 + threadIdx.x;
+__device__ __forceinline__ void most_of(const T* p, int64_t n, int C, int block, int blocks, uint32_t* lds, uint8_t* out) {
+    constexpr int V = 16 / sizeof(T), threads = kMostThreads;
+    const int g = C % V == 0 ? V : C % 4 == 0 ? 4 : C % 2 == 0 ? 2 : 1;      // gcd(C, V): V is 4 or 8
+    const int t = threadIdx.x, run = C / g;
+    if (((uintptr_t)p & 15) || run > threads) {
+        const int64_t pixels = n / C;
+        const int per = C < threads ? threads / C : 1;
+        for (int c0 = 0; c0 < C; c0 += threads) {
+            const int c = c0 + t % (C < threads ? C : threads), row = C < threads ? t / C : 0;
+            uint32_t m = 0;
+            if (c < C && row < per)
+                for (int64_t i = (int64_t)block * per + row; i < pixels; i += (int64_t)blocks * per)
+                    m = larger(m, (float)p[i * C + c]);
+            lds[t] = 0;
+            __syncthreads();
+            if (c < C && row < per) atomicMax(lds + (c - c0), m);
+            __syncthreads();
+            if (c0 + t < C) out[c0 + t] = (uint8_t)(lds[t] >> 23);
+            __syncthreads();
+        }
+        return;
+    }
+    const int per = threads / run, col = t % run, row = t / run;
+    for (int c = t; c < C; c += threads) lds[c] = 0;
+    __syncthreads();
+    uint32_t m[V] = {};
+    const int64_t all = n / V, step = (int64_t)blocks * per * run;
+    if (row < per) {
+        int64_t i = ((int64_t)block * per + row) * run + col;
         auto take = [&](const Held<T, V>& h) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) m = larger(m, h.value(j));
+            for (int j = 0; j < V; ++j) m[j] = larger(m[j], h.value(j));
         };
         for (; i + 3 * step < all; i += 4 * step) {
             Held<T, V> h[4];
@@ -513,35 +572,49 @@ __device__ uint32_t most_of(const T* p, int64_t n, int block, int blocks) {
             h.load(p + i * V);
             take(h);
         }
-        done = all * V;
+#pragma unroll
+        for (int j = 0, c = col * V % C; j < V; ++j, c = c + 1 < C ? c + 1 : 0) atomicMax(lds + c, m[j]);
     }
-    for (int64_t i = done + (int64_t)block * 256 + threadIdx.x; i < n; i += (int64_t)blocks * 256) m = larger(m, (float)p[i]);
-    return m;
+    if (block == 0 && t < n - all * V) atomicMax(lds + (all * V + t) % C, larger(0, (float)p[all * V + t]));
+    __syncthreads();
+    for (int c = t; c < C; c += threads) out[c] = (uint8_t)(lds[c] >> 23);
 }
 
+// The largest magnitude that a channel may have, a row for one block in nx: a raw
+// tensor's own, the norm's |gamma| 2 sqrt(D H W) + |beta| (|n| is at most sqrt(D H W) for
+// its own statistics; twice that for their roundings), a checkpoint's |centre| + 127 step,
+// or through the norm |gamma| (|centre - mean| + 127 step) rstd + |beta|; dy's own of the
+// other blocks.
 template <typename T>
-__global__ __launch_bounds__(256) void k_wgrad_most(Args g) {
-    __shared__ uint32_t waves[4];
-    const int b = blockIdx.x;
-    uint32_t m = 0;
+__global__ __launch_bounds__(kMostThreads) void k_wgrad_most(Args g) {
+    __shared__ uint32_t lds[kMostThreads * 16 / sizeof(T)];
+    const int b = blockIdx.x, C = g.s.C;
+    uint8_t* out = g.most + (size_t)b * most_row(C);
+    const float top = 0x1.fffffep127f;        // a finite bound past this is this
     if (b >= g.nx) {
-        m = most_of((const T*)g.a.dy, (int64_t)g.s.N * g.s.Ho * g.s.Wo * g.s.K, b - g.nx, g.nd);
+        out = g.most + (size_t)g.nx * most_row(C) + (size_t)(b - g.nx) * most_row(g.s.K);
+        most_of((const T*)g.a.dy, (int64_t)g.s.N * g.s.Ho * g.s.Wo * g.s.K, g.s.K, b - g.nx, g.nd, lds, out);
+    } else if (g.s.x8) {
+        for (int c = threadIdx.x; c < C; c += kMostThreads) {
+            uint32_t m = 0;
+            const float gamma = g.s.norm && g.a.gamma ? fabsf(g.a.gamma[c]) : 1.0f;
+            const float beta = g.s.norm && g.a.beta ? fabsf(g.a.beta[c]) : 0.0f;
+            for (int n = b; n < g.s.N; n += g.nx) {
+                const float* r = g.a.rows + ((size_t)n * C + c) * 2;
+                const float* st = g.s.norm ? g.a.stats + ((size_t)n * g.s.G + c / g.s.D) * 2 : nullptr;
+                const float reach = (fabsf(r[0] - (st ? st[0] : 0.0f)) + kCodes * r[1]) * (st ? st[1] : 1.0f);
+                m = larger(m, reach * gamma + beta > top ? top : reach * gamma + beta);
+            }
+            out[c] = (uint8_t)(m >> 23);
+        }
     } else if (g.s.norm) {
         const float bound = 2.0f * sqrtf((float)g.s.D * (float)g.s.H * (float)g.s.W);
-        for (int c = b * 256 + threadIdx.x; c < g.s.C; c += g.nx * 256)
-            m = larger(m, fabsf(g.a.gamma ? g.a.gamma[c] : 1.0f) * bound + fabsf(g.a.beta ? g.a.beta[c] : 0.0f));
-    } else if (g.s.x8) {
-        for (int64_t i = (int64_t)b * 256 + threadIdx.x; i < (int64_t)g.s.N * g.s.C; i += (int64_t)g.nx * 256)
-            m = larger(m, fabsf(g.a.rows[i * 2]) + kCodes * g.a.rows[i * 2 + 1]);
+        for (int c = threadIdx.x; c < C; c += kMostThreads) {
+            const float v = fabsf(g.a.gamma ? g.a.gamma[c] : 1.0f) * bound + fabsf(g.a.beta ? g.a.beta[c] : 0.0f);
+            out[c] = (uint8_t)(larger(0, v > top ? top : v) >> 23);
+        }
     } else {
-        m = most_of((const T*)g.a.x, (int64_t)g.s.N * g.s.H * g.s.W * g.s.C, b, g.nx);
-    }
-    m = wave_max(m);
-    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = m;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < 4; ++w) m = waves[w] > m ? waves[w] : m;
-        g.most[b] = m;
+        most_of((const T*)g.a.x, (int64_t)g.s.N * g.s.H * g.s.W * C, C, b, g.nx, lds, out);
     }
 }
 
@@ -556,34 +629,28 @@ template <typename T, bool X8, bool NORM, int WC, int KW, int KS>
 __global__ __launch_bounds__(WC* KW* KS * 64, WC* KW* KS / 4) void k_wgrad(Args g) {
     typedef Wgrad<T, X8, NORM, WC, KW, KS> W;
     __shared__ typename W::Lds lds;
-    __shared__ uint32_t most[2][W::kWaves];
+    __shared__ uint32_t exps[W::CT + W::KT];
     const int tiles = g.w.ctiles * g.w.ktiles, per = (g.w.slices * tiles + 7) / 8;
     const int item = blockIdx.x % 8 * per + blockIdx.x / 8;
     if (item >= g.w.slices * tiles) return;
     const int slice = item / tiles, tile = item % tiles;
-    int in_exp = 0, dy_exp = 0;
+    const int c0 = tile % g.w.ctiles * W::CT, k0 = tile / g.w.ctiles * W::KT;
     if constexpr (!W::kAsIs) {
-        uint32_t mx = 0, md = 0;
-        for (int i = threadIdx.x; i < g.nx; i += W::kThreads) mx = g.most[i] > mx ? g.most[i] : mx;
-        for (int i = threadIdx.x; i < g.nd; i += W::kThreads) md = g.most[g.nx + i] > md ? g.most[g.nx + i] : md;
-        mx = wave_max(mx);
-        md = wave_max(md);
-        if ((threadIdx.x & 63) == 0) {
-            most[0][threadIdx.x >> 6] = mx;
-            most[1][threadIdx.x >> 6] = md;
-        }
+        // the rows' largest, all loads before the first wait; unscaled: what exponent_of takes to 0
+        constexpr int ccols = W::CT / 4, kcols = W::KT / 4;
+        const int t = threadIdx.x;
+        Most4 in, dy;
+        in.load(g.most, g.nx, g.s.C, c0 + t % ccols * 4, t / ccols, W::kThreads / ccols);
+        dy.load(g.most + (size_t)g.nx * most_row(g.s.C), g.nd, g.s.K, k0 + t % kcols * 4, t / kcols, W::kThreads / kcols);
+        if (t < W::CT + W::KT) exps[t] = (t < W::CT ? g.nx : g.nd) ? 0 : 14 + 127;
         __syncthreads();
-        for (int w = 0; w < W::kWaves; ++w) {
-            mx = most[0][w] > mx ? most[0][w] : mx;
-            md = most[1][w] > md ? most[1][w] : md;
-        }
-        in_exp = __builtin_amdgcn_readfirstlane(exponent_of(mx));
-        dy_exp = __builtin_amdgcn_readfirstlane(exponent_of(md));
+        in.join(exps + t % ccols * 4);
+        dy.join(exps + W::CT + t % kcols * 4);
+        __syncthreads();
     }
-    W w(g, lds, tile % g.w.ctiles * W::CT, tile / g.w.ctiles * W::KT, g.w.rows * slice / g.w.slices,
-        g.w.rows * (slice + 1) / g.w.slices, power(in_exp), power(dy_exp));
+    W w(g, lds, c0, k0, g.w.rows * slice / g.w.slices, g.w.rows * (slice + 1) / g.w.slices, exps, exps + W::CT);
     w.run();
-    w.finish(slice, in_exp + dy_exp);
+    w.finish(slice);
 }
 
 // dg [K][C][3][3] = the slices' sum, in order: 8 channels x 32 filters x one row of
@@ -688,6 +755,21 @@ Walk walk_of(const WgradShape& s) {
     return best;
 }
 
+// Rows of exponents, of the input and of dy: none where both tensors are multiplied as
+// they are, and fp16's own dy is not scaled.
+struct Scales {
+    int nx, nd;
+};
+Scales scales_of(const WgradShape& s) {
+    auto blocks = [](int64_t n) { return (int)(n > (int64_t)kMost * 8192 ? kMost : (n + 8191) / 8192); };
+    Scales m = {0, 0};
+    if (s.x8) m.nx = s.N < kMost ? s.N : kMost;
+    else if (s.norm) m.nx = 1;
+    else if (s.io == Io::F32) m.nx = blocks((int64_t)s.N * s.H * s.W * s.C);
+    if (s.io == Io::F32 || (s.io == Io::BF16 && m.nx)) m.nd = blocks((int64_t)s.N * s.Ho * s.Wo * s.K);
+    return m;
+}
+
 }  // namespace
 
 bool wgrad_fits(const WgradShape& s) {
@@ -701,21 +783,21 @@ bool wgrad_fits(const WgradShape& s) {
 }
 
 size_t wgrad_workspace(const WgradShape& s) {
-    return (size_t)walk_of(s).slices * 9 * s.C * s.K * sizeof(float) + 2 * kMost * sizeof(uint32_t);
+    const Scales m = scales_of(s);
+    return (size_t)walk_of(s).slices * 9 * s.C * s.K * sizeof(float) + (size_t)m.nx * most_row(s.C) +
+           (size_t)m.nd * most_row(s.K);
 }
 
 hipError_t launch_wgrad(const WgradArgs& a, const WgradShape& s, void* ws, hipStream_t st) {
     Args g{a, s, walk_of(s), (float*)ws, nullptr, 0, 0};
-    g.most = (uint32_t*)(g.part + (size_t)g.w.slices * 9 * s.C * s.K);
-    auto blocks = [](int64_t n) { return (int)(n > (int64_t)kMost * 8192 ? kMost : (n + 8191) / 8192); };
-    if (s.norm) g.nx = 1;
-    else if (s.x8) g.nx = blocks((int64_t)s.N * s.C);
-    else if (s.io == Io::F32) g.nx = blocks((int64_t)s.N * s.H * s.W * s.C);
-    if (s.io == Io::F32 || (s.io == Io::BF16 && g.nx)) g.nd = blocks((int64_t)s.N * s.Ho * s.Wo * s.K);
+    g.most = (uint8_t*)(g.part + (size_t)g.w.slices * 9 * s.C * s.K);
+    const Scales m = scales_of(s);
+    g.nx = m.nx;
+    g.nd = m.nd;
     if (g.nx + g.nd) {
-        if (s.io == Io::F32) k_wgrad_most<float><<<g.nx + g.nd, 256, 0, st>>>(g);
-        else if (s.io == Io::F16) k_wgrad_most<_Float16><<<g.nx + g.nd, 256, 0, st>>>(g);
-        else k_wgrad_most<__bf16><<<g.nx + g.nd, 256, 0, st>>>(g);
+        if (s.io == Io::F32) k_wgrad_most<float><<<g.nx + g.nd, kMostThreads, 0, st>>>(g);
+        else if (s.io == Io::F16) k_wgrad_most<_Float16><<<g.nx + g.nd, kMostThreads, 0, st>>>(g);
+        else k_wgrad_most<__bf16><<<g.nx + g.nd, kMostThreads, 0, st>>>(g);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
