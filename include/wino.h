@@ -337,11 +337,12 @@ int wino_conv2d_nhwc(const float* x, const float* U, float* y,
  * g'[c][k][r][s] = g[k][c][2-r][2-s], and pad 2 - pad.)
  *   Tensors x, y, dx, dy are [N][H][W][C] (dy of a layer [N][Ho][Wo][K]) of fp32,
  *   or fp16 / bf16 with WINO_IO_F16 / WINO_IO_BF16; parameters, statistics and
- *   their gradients fp32.  All sums are fp32 in a fixed order.  Outputs must not
- *   overlap each other or any input.  Tensors may have any address that suits
- *   their element type (16-byte ones run faster); checkpoints and
- *   workspaces must be on 16-byte addresses, else WINO_ERR_INVALID_ARG.  At most
- *   2^40 elements a tensor (INVALID_ARG) and 2^30 workgroups' shares of one
+ *   their gradients fp32.  Sums are in a fixed order and held in fp32, the norm's in
+ *   short parts, so that none is off by more than 2^-16 of the sum of absolute values
+ *   whatever its length.  Outputs must not overlap each other or any input.  Tensors
+ *   may have any address that suits their element type (16-byte ones run faster);
+ *   checkpoints and workspaces must be on 16-byte addresses, else
+ *   WINO_ERR_INVALID_ARG.  At most 2^40 elements a tensor (INVALID_ARG) and 2^30 workgroups' shares of one
  *   (UNSUPPORTED; reached only by more than 2^30 images of a few values). */
 #define WINO_FLAG_SILU     0x002u   /* y = z * sigmoid(z) (group norm and the calls that undo it) */
 #define WINO_FLAG_ACT8     0x004u   /* x is an 8-bit checkpoint */

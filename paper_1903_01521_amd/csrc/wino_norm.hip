@@ -12,8 +12,11 @@
 // fits a workgroup's registers, it is loaded once and the statistics are taken and
 // the result formed from there: one read, one write, one launch, and the variance
 // about the mean itself.  Else three launches: every workgroup reduces its pixels,
-// one joins these parts, and a second pass over the tensor forms the result.  All
-// sums are in 32 bits and in a fixed order.
+// one joins these parts, and a second pass over the tensor forms the result.  Sums are in
+// a fixed order: a thread's in 32 bits, of kFlush terms and then of kFlush of these, so
+// that with the joins (64 bits where they are long) no sum is more than 256 roundings off,
+// whatever the tensor's size (4096 terms in turn: 6e-5 of the sum; the second level costs
+// 1% of the large tensors' time at most, 3% one channel a lane).
 #include <math.h>
 
 #include <type_traits>
@@ -27,6 +30,7 @@ namespace {
 constexpr unsigned kMaxBlocks = 1 << 20;      // workgroups of a launch; they loop over the rest
 constexpr unsigned kXcds = 8;
 constexpr int kMaxThreads = 512;              // of the one-pass kernels
+constexpr int kFlush = 64;                    // terms of a thread's sum before they join its total
 
 // The part of the tensor that a workgroup works on, and its threads' share.  A
 // thread has one column of `vec` channels and the pixels of its row, `rows`
@@ -183,6 +187,16 @@ template <typename T, int VEC, int NV>
 __device__ __forceinline__ void pin(Held<T, VEC> (&h)[NV]) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) h[i].pin();
+}
+
+// A thread's sums since the last time to its totals.
+template <int VEC>
+__device__ __forceinline__ void flush(float (&sum)[VEC], float (&total)[VEC]) {
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+        total[j] += sum[j];
+        sum[j] = 0.0f;
+    }
 }
 
 // p moved on, so that the compiler does not keep the addresses of an earlier pass
@@ -343,10 +357,12 @@ __global__ __launch_bounds__(kMaxThreads) void k_norm(FwdArgs a, Cut k) {
     }
 }
 
-// The parts of the statistics of a chunk of an image: a thread's sums are about its
-// own first value, so that a mean far from zero costs nothing, and are joined as
-// means, about the chunk's first value, and squares about the chunk's mean.  Bound by
-// memory: 411 MB (N = 32, 64 channels at 224x224, fp32) in 70 us, 5.9 TB/s.
+// The parts of the statistics of a chunk of an image.  A thread's sums are about its
+// mean so far, at first its first value, and join its mean and squares kFlush values at a
+// time: a mean far from zero costs nothing, and a first value far from the others no more
+// than in one such part (all of 4096 values about it: 12% of the variance).  Threads are
+// joined as means, about the chunk's first value, and squares about the chunk's mean.
+// Bound by memory: 411 MB (N = 32, 64 channels at 224x224, fp32) in 70 us, 5.9 TB/s.
 template <typename T, int VEC, bool CODES>
 __global__ __launch_bounds__(256) void k_norm_part(FwdArgs a, Cut k) {
     constexpr int U = VEC == 1 ? 16 : 8;      // loads in flight
@@ -359,7 +375,7 @@ __global__ __launch_bounds__(256) void k_norm_part(FwdArgs a, Cut k) {
         const Share s = share_of(k, it, VEC);
         const size_t step = (size_t)k.rows * k.C;
         const T* x = (const T*)a.x + ((size_t)it.n * k.P + it.p0 + s.row) * k.C + s.c;
-        float first[VEC], s1[VEC], s2[VEC], lo[VEC], hi[VEC];
+        float first[VEC], off[VEC], m2[VEC], s1[VEC], s2[VEC], lo[VEC], hi[VEC];
         Held<T, VEC> raw[U], ref;
         if (s.count) {
             raw[0].load(x);
@@ -368,14 +384,14 @@ __global__ __launch_bounds__(256) void k_norm_part(FwdArgs a, Cut k) {
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
             first[j] = s.count ? raw[0].value(j) : 0.0f;
-            s1[j] = s2[j] = 0.0f;
+            off[j] = m2[j] = s1[j] = s2[j] = 0.0f;
             lo[j] = Low::identity;
             hi[j] = High::identity;
         }
         auto take = [&](const Held<T, VEC>& r) {
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                const float v = r.value(j), d = v - first[j];
+                const float v = r.value(j), d = v - first[j] - off[j];
                 s1[j] += d;
                 s2[j] = fmaf(d, d, s2[j]);
                 if constexpr (CODES) {
@@ -384,24 +400,35 @@ __global__ __launch_bounds__(256) void k_norm_part(FwdArgs a, Cut k) {
                 }
             }
         };
-        int i = 0;
-        for (; i + U <= s.count; i += U) {
+        static_assert(kFlush % U == 0, "whole batches of loads");
+        for (int i = 0; i < s.count;) {
+            const int before = i, end = i + kFlush < s.count ? i + kFlush : s.count;
+            for (; i + U <= end; i += U) {
 #pragma unroll
-            for (int u = 0; u < U; ++u, x += step) raw[u].load(x);
+                for (int u = 0; u < U; ++u, x += step) raw[u].load(x);
 #pragma unroll
-            for (int u = 0; u < U; ++u) take(raw[u]);
-        }
-        for (; i < s.count; ++i, x += step) {
-            raw[0].load(x);
-            take(raw[0]);
+                for (int u = 0; u < U; ++u) take(raw[u]);
+            }
+            for (; i < end; ++i, x += step) {
+                raw[0].load(x);
+                take(raw[0]);
+            }
+            // the mean moves by the part's share of its distance d
+            const float now = (float)(end - before), share = now / (float)end;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const float d = s1[j] / now;
+                off[j] = fmaf(d, share, off[j]);
+                m2[j] += s2[j] - s1[j] * d + d * d * ((float)before * share);
+                s1[j] = s2[j] = 0.0f;
+            }
         }
         const float n = (float)s.count;
         float mean[VEC];
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-            const float d = s.count ? s1[j] / n : 0.0f;
-            mean[j] = first[j] + d;
-            s2[j] = s2[j] - s1[j] * d;
+            mean[j] = first[j] + off[j];
+            s2[j] = m2[j];
             const float r = s.count ? ref.value(j) : 0.0f;
             s1[j] = n * (mean[j] - r);
             if (s.row == 0) cr[s.col * VEC + j] = r;
@@ -446,13 +473,13 @@ __global__ __launch_bounds__(256) void k_norm_join(const float* __restrict__ par
         const float* p = part + ((size_t)n * k.chunks * k.C + (size_t)g * k.D) * 4;
         const int64_t all = (int64_t)k.chunks * k.D;
         auto total = [&](auto value) {
-            float a = 0.0f;
+            double sum = 0.0;
             for (int64_t i = threadIdx.x; i < all; i += 256) {
                 const int64_t ch = i / k.D, d = i - ch * k.D;
                 const int64_t px = k.P - ch * k.px < k.px ? k.P - ch * k.px : k.px;
-                a += value(p + ((size_t)ch * k.C + d) * 4, (float)px);
+                sum += value(p + ((size_t)ch * k.C + d) * 4, (float)px);
             }
-            a = wave_sum(a);
+            const float a = wave_sum((float)sum);
             __syncthreads();
             if (lane == 0) acc[wave] = a;
             __syncthreads();
@@ -710,23 +737,31 @@ __global__ __launch_bounds__(256) void k_norm_back_part(BwdArgs a, Cut k) {
         };
         Held<S, VEC> x[U];
         Held<T, VEC> dy[U];
-        int i = 0;
-        for (; i + U <= s.count; i += U, at += U * step) {
+        float tz[VEC], tn[VEC];               // totals
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                x[u].load(src + at + u * step);
-                dy[u].load((const T*)a.dy + at + u * step);
+        for (int j = 0; j < VEC; ++j) tz[j] = tn[j] = 0.0f;
+        static_assert(kFlush % U == 0, "whole batches of loads");
+        for (int i = 0; i < s.count;) {
+            const int end = i + kFlush < s.count ? i + kFlush : s.count;
+            for (; i + U <= end; i += U, at += U * step) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    x[u].load(src + at + u * step);
+                    dy[u].load((const T*)a.dy + at + u * step);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) take(x[u], dy[u]);
             }
-#pragma unroll
-            for (int u = 0; u < U; ++u) take(x[u], dy[u]);
+            for (; i < end; ++i, at += step) {
+                x[0].load(src + at);
+                dy[0].load((const T*)a.dy + at);
+                take(x[0], dy[0]);
+            }
+            flush(sz, tz);
+            flush(sn, tn);
         }
-        for (; i < s.count; ++i, at += step) {
-            x[0].load(src + at);
-            dy[0].load((const T*)a.dy + at);
-            take(x[0], dy[0]);
-        }
-        join_rows(sz, k, rz, Add());
-        join_rows(sn, k, rn, Add());
+        join_rows(tz, k, rz, Add());
+        join_rows(tn, k, rn, Add());
         __syncthreads();
         for (int c = threadIdx.x; c < k.cb && it.c0 + c < k.C; c += blockDim.x) {
             Raw<float, 2> o;
@@ -753,10 +788,10 @@ __global__ __launch_bounds__(256) void k_norm_back_join(const float* __restrict_
         const int64_t n = ng / k.G;
         const int g = (int)(ng - n * k.G);
         const float* p = part + ((size_t)n * k.chunks * k.C + (size_t)g * k.D) * 2;
-        float m1 = 0.0f, m2 = 0.0f;
+        double s1 = 0.0, s2 = 0.0;
         for (int d0 = 0; d0 < k.D; d0 += wide) {
             const int d = d0 + col;
-            float z = 0.0f, v = 0.0f;
+            double z = 0.0, v = 0.0;
             if (d < k.D)
                 for (int ch = row; ch < (int)k.chunks; ch += rows) {
                     const float* q = p + ((size_t)ch * k.C + d) * 2;
@@ -764,8 +799,8 @@ __global__ __launch_bounds__(256) void k_norm_back_join(const float* __restrict_
                     v += q[1];
                 }
             __syncthreads();
-            red[0][t] = z;
-            red[1][t] = v;
+            red[0][t] = (float)z;
+            red[1][t] = (float)v;
             __syncthreads();
             if (t < wide && d < k.D) {
                 for (int r = 1; r < rows; ++r) {
@@ -773,15 +808,14 @@ __global__ __launch_bounds__(256) void k_norm_back_join(const float* __restrict_
                     v += red[1][r * wide + t];
                 }
                 float* o = sums + ((size_t)n * k.C + (size_t)g * k.D + d) * 2;
-                o[0] = z;
-                o[1] = v;
+                o[0] = (float)z;
+                o[1] = (float)v;
                 const float w = gamma ? gamma[(size_t)g * k.D + d] * k.inv : k.inv;
-                m1 += z * w;
-                m2 += v * w;
+                s1 += z * w;
+                s2 += v * w;
             }
         }
-        m1 = wave_sum(m1);
-        m2 = wave_sum(m2);
+        const float m1 = wave_sum((float)s1), m2 = wave_sum((float)s2);
         if (lane == 0) {
             acc[wave * 2] = m1;
             acc[wave * 2 + 1] = m2;
@@ -845,9 +879,9 @@ __global__ __launch_bounds__(256) void k_norm_back_apply(BwdArgs a, Cut k) {
 // dgamma, dbeta: every image's sums, 32 channels a workgroup.
 __global__ __launch_bounds__(256) void k_norm_params(const float* __restrict__ sums, float* __restrict__ dgamma,
                                                      float* __restrict__ dbeta, int N, int C) {
-    __shared__ float acc[2][8][32];
+    __shared__ double acc[2][8][32];
     const int c = blockIdx.x * 32 + (threadIdx.x & 31), row = threadIdx.x >> 5;
-    float z = 0.0f, n = 0.0f;
+    double z = 0.0, n = 0.0;
     if (c < C) {
         int i = row;
         for (; i + 24 < N; i += 32) {         // four loads in flight
@@ -874,8 +908,8 @@ __global__ __launch_bounds__(256) void k_norm_params(const float* __restrict__ s
             z += acc[0][r][threadIdx.x];
             n += acc[1][r][threadIdx.x];
         }
-        if (dbeta) dbeta[c] = z;
-        if (dgamma) dgamma[c] = n;
+        if (dbeta) dbeta[c] = (float)z;
+        if (dgamma) dgamma[c] = (float)n;
     }
 }
 
@@ -994,7 +1028,7 @@ NormPlan norm_plan(const NormShape& s, bool backward, bool aligned) {
     } else {
         const int cols = (s.C + p.vec - 1) / p.vec;
         set_rows(&p, 256, cols < 128 ? cols : 128);
-        set_chunks(&p, s, 4, 1 << 20);
+        set_chunks(&p, s, 4, kFlush * kFlush);
     }
     p.lds = ((backward ? 2 : 3) * (size_t)p.parts + 4) * p.cb * sizeof(float);
     const size_t lists = (size_t)s.N * p.chunks * s.C, all = (size_t)s.N * s.C, groups = (size_t)s.N * s.G * 2;
