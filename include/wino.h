@@ -342,8 +342,9 @@ int wino_conv2d_nhwc(const float* x, const float* U, float* y,
  *   whatever its length.  Outputs must not overlap each other or any input.  Tensors
  *   may have any address that suits their element type (16-byte ones run faster);
  *   checkpoints and workspaces must be on 16-byte addresses, else
- *   WINO_ERR_INVALID_ARG.  At most 2^40 elements a tensor (INVALID_ARG) and 2^30 workgroups' shares of one
- *   (UNSUPPORTED; reached only by more than 2^30 images of a few values). */
+ *   WINO_ERR_INVALID_ARG.  At most 2^40 elements a tensor (INVALID_ARG), 2^30 channels
+ *   and 2^30 workgroups' shares of a tensor (UNSUPPORTED; the latter reached only by
+ *   more than 2^30 images of a few values). */
 #define WINO_FLAG_SILU     0x002u   /* y = z * sigmoid(z) (group norm and the calls that undo it) */
 #define WINO_FLAG_ACT8     0x004u   /* x is an 8-bit checkpoint */
 #define WINO_IO_F16        0x040u   /* tensors are fp16 */

@@ -9,6 +9,9 @@ using namespace wino;
 
 namespace {
 
+// Channel numbers are 32-bit, and a workgroup's columns run up to 1024 channels on.
+constexpr int kMaxChannels = 1 << 30;
+
 // The element type and activation of the flags, the others being `more`.
 int flags_of(unsigned flags, unsigned more, Io* io, Act* act) {
     if (flags & ~(WINO_FLAG_RELU | WINO_FLAG_SILU | WINO_IO_MASK | more)) return WINO_ERR_UNSUPPORTED;
@@ -23,6 +26,7 @@ int make_shape(int N, int C, int H, int W, int G, unsigned flags, unsigned more,
     if (N <= 0 || C <= 0 || H <= 0 || W <= 0 || G <= 0 || C % G) return WINO_ERR_INVALID_ARG;
     int64_t e;
     if (!mul_ok(H, W, &s->P) || !mul_ok(s->P, C, &e) || !mul_ok(e, N, &e)) return WINO_ERR_INVALID_ARG;
+    if (C > kMaxChannels) return WINO_ERR_UNSUPPORTED;
     s->N = N; s->C = C; s->G = G; s->D = C / G;
     return flags_of(flags, more, &s->io, &s->act);
 }
