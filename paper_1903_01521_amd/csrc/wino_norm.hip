@@ -1014,7 +1014,7 @@ NormPlan norm_plan(const NormShape& s, bool backward, bool aligned) {
     const int64_t unit = (int64_t)s.D / gcd(s.D, p.vec) * p.vec;
     for (int64_t cb = unit; !p.one && cb <= 512 && cb <= s.C; cb += unit) {
         const bool wide = cb * io_size(s.io) >= 64 || cb == s.C;
-        if (s.C % cb || cb / p.vec > kMaxThreads || (!wide && s.N > 128 / (s.C / cb))) continue;
+        if (s.C % cb || cb / p.vec > kMaxThreads || (!wide && s.N * (s.C / cb) > 128)) continue;
         for (int threads = 256; threads <= kMaxThreads && !p.one; threads *= 2)
             for (int many = 0; many < 2 && !p.one && cb / p.vec <= threads; ++many) {
                 set_rows(&p, threads, (int)(cb / p.vec));
