@@ -420,7 +420,8 @@ int wino_group_norm_backward_nhwc(const void* dy, const void* x, const float* st
  *   less than 2^-39 of it below.  Sums are fp32.  Values that are not finite give results
  *   that are not (NaN where fp32 would give infinities), in their channel or filter.
  *   N*Ho*Wo must be below 2^31 (INVALID_ARG), and (H + 2*pad + 16)*W*C and
- *   (H + 2*pad + 16)*Wo*K below 2^29 (UNSUPPORTED). */
+ *   (H + 2*pad + 16)*Wo*K below 2^29 and ceil(C/8)*ceil(K/32)*3 below 2^24
+ *   (UNSUPPORTED). */
 size_t wino_conv2d_wgrad_workspace_bytes(int N, int C, int H, int W, int K, int pad, unsigned flags);
 int wino_conv2d_wgrad_nhwc(const void* x, const void* dy, float* dg, const float* stats, const float* gamma,
                            const float* beta, int G, int N, int C, int H, int W, int K, int pad, unsigned flags,

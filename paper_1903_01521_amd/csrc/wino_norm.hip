@@ -876,40 +876,44 @@ __global__ __launch_bounds__(256) void k_norm_back_apply(BwdArgs a, Cut k) {
     }
 }
 
-// dgamma, dbeta: every image's sums, 32 channels a workgroup.
+// dgamma, dbeta: every image's sums, 32 channels a workgroup at a time.
 __global__ __launch_bounds__(256) void k_norm_params(const float* __restrict__ sums, float* __restrict__ dgamma,
                                                      float* __restrict__ dbeta, int N, int C) {
     __shared__ double acc[2][8][32];
-    const int c = blockIdx.x * 32 + (threadIdx.x & 31), row = threadIdx.x >> 5;
-    double z = 0.0, n = 0.0;
-    if (c < C) {
-        int i = row;
-        for (; i + 24 < N; i += 32) {         // four loads in flight
-            Raw<float, 2> p[4];
+    const int lane = threadIdx.x & 31, row = threadIdx.x >> 5;
+    for (int c0 = blockIdx.x * 32; c0 < C; c0 += gridDim.x * 32) {
+        const int c = c0 + lane;
+        double z = 0.0, n = 0.0;
+        if (c < C) {
+            int i = row;
+            for (; i + 24 < N; i += 32) {     // four loads in flight
+                Raw<float, 2> p[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) p[u] = *(const Raw<float, 2>*)(sums + ((size_t)(i + u * 8) * C + c) * 2);
+                for (int u = 0; u < 4; ++u) p[u] = *(const Raw<float, 2>*)(sums + ((size_t)(i + u * 8) * C + c) * 2);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                z += p[u].v[0];
-                n += p[u].v[1];
+                for (int u = 0; u < 4; ++u) {
+                    z += p[u].v[0];
+                    n += p[u].v[1];
+                }
+            }
+            for (; i < N; i += 8) {
+                const Raw<float, 2> p = *(const Raw<float, 2>*)(sums + ((size_t)i * C + c) * 2);
+                z += p.v[0];
+                n += p.v[1];
             }
         }
-        for (; i < N; i += 8) {
-            const Raw<float, 2> p = *(const Raw<float, 2>*)(sums + ((size_t)i * C + c) * 2);
-            z += p.v[0];
-            n += p.v[1];
+        acc[0][row][lane] = z;
+        acc[1][row][lane] = n;
+        __syncthreads();
+        if (row == 0 && c < C) {
+            for (int r = 1; r < 8; ++r) {
+                z += acc[0][r][lane];
+                n += acc[1][r][lane];
+            }
+            if (dbeta) dbeta[c] = (float)z;
+            if (dgamma) dgamma[c] = (float)n;
         }
-    }
-    acc[0][row][threadIdx.x & 31] = z;
-    acc[1][row][threadIdx.x & 31] = n;
-    __syncthreads();
-    if (row == 0 && c < C) {
-        for (int r = 1; r < 8; ++r) {
-            z += acc[0][r][threadIdx.x];
-            n += acc[1][r][threadIdx.x];
-        }
-        if (dbeta) dbeta[c] = (float)z;
-        if (dgamma) dgamma[c] = (float)n;
+        __syncthreads();
     }
 }
 
@@ -1125,7 +1129,7 @@ hipError_t launch_norm_backward(const NormBwd& a, const NormShape& s, const Norm
         else go(std::false_type());
     });
     if (e != hipSuccess || (!a.dgamma && !a.dbeta)) return e;
-    k_norm_params<<<(s.C + 31) / 32, 256, 0, st>>>(sums, a.dgamma, a.dbeta, s.N, s.C);
+    k_norm_params<<<blocks_of((s.C + 31) / 32), 256, 0, st>>>(sums, a.dgamma, a.dbeta, s.N, s.C);
     return hipGetLastError();
 }
 

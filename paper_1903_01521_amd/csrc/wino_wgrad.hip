@@ -713,6 +713,9 @@ Walk walk_of(const WgradShape& s, int form, int slices) {
     return w;
 }
 
+// Workgroups of k_wgrad_sum.
+int64_t sum_blocks(const WgradShape& s) { return (int64_t)((s.K + 31) / 32) * ((s.C + 7) / 8) * 3; }
+
 // Products on the matrix cores that one product of the operands takes.
 int products_of(const WgradShape& s) { return s.io == Io::F32 ? 3 : s.norm || s.x8 ? 2 : 1; }
 
@@ -779,7 +782,9 @@ bool wgrad_fits(const WgradShape& s) {
     if (high >= top || s.W >= top / high || s.C >= top / high / s.W || s.Wo >= top / high || s.K >= top / high / s.Wo)
         return false;
     const Walk w = walk_of(s, 2, 1);
-    return s.N < count && w.rows < count && (int64_t)w.ctiles * w.ktiles < count;
+    // a launch has fewer than 2^32 threads
+    return s.N < count && w.rows < count && (int64_t)w.ctiles * w.ktiles * 512 < (int64_t)1 << 31 &&
+           sum_blocks(s) * 256 < (int64_t)1 << 32;
 }
 
 size_t wgrad_workspace(const WgradShape& s) {
@@ -819,8 +824,7 @@ hipError_t launch_wgrad(const WgradArgs& a, const WgradShape& s, void* ws, hipSt
     else with(__bf16());
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const unsigned blocks3 = (unsigned)((s.K + 31) / 32) * ((s.C + 7) / 8) * 3;
-    k_wgrad_sum<<<blocks3, 256, 0, st>>>((const float*)ws, a.dg, s.C, s.K, g.w.slices);
+    k_wgrad_sum<<<(unsigned)sum_blocks(s), 256, 0, st>>>((const float*)ws, a.dg, s.C, s.K, g.w.slices);
     return hipGetLastError();
 }
 
