@@ -92,13 +92,22 @@ def log(*a):
     print(*a, file=sys.stderr, flush=True)
 
 
+# Sources of the training calls, which no workload here runs.
+TRAINING_SOURCES = ("wino_norm", "wino_wgrad", "wino_train")
+
+
+def layer_sources() -> list[str]:
+    """The HIP sources and host planner that define the measured kernels and launches."""
+    return [f for f in sorted(glob.glob(os.path.join(CSRC, "*")))
+            if f.endswith((".hip", ".h", ".cpp")) and not os.path.basename(f).startswith(TRAINING_SOURCES)]
+
+
 def sources_hash() -> str:
-    """sha256 over the HIP sources and host planner that define the kernels and launches."""
+    """sha256 over those sources."""
     h = hashlib.sha256()
-    for f in sorted(glob.glob(os.path.join(CSRC, "*"))):
-        if f.endswith((".hip", ".h", ".cpp")):
-            h.update(os.path.basename(f).encode())
-            h.update(open(f, "rb").read())
+    for f in layer_sources():
+        h.update(os.path.basename(f).encode())
+        h.update(open(f, "rb").read())
     return h.hexdigest()[:16]
 
 
