@@ -362,7 +362,7 @@ __global__ __launch_bounds__(kMaxThreads) void k_norm(FwdArgs a, Cut k) {
 // time: a mean far from zero costs nothing, and a first value far from the others no more
 // than in one such part (all of 4096 values about it: 12% of the variance).  Threads are
 // joined as means, about the chunk's first value, and squares about the chunk's mean.
-// Bound by memory: 411 MB (N = 32, 64 channels at 224x224, fp32) in 70 us, 5.9 TB/s.
+// Bound by memory: 411 MB (N = 32, 64 channels at 224x224, fp32) in 72 us, 5.7 TB/s.
 template <typename T, int VEC, bool CODES>
 __global__ __launch_bounds__(256) void k_norm_part(FwdArgs a, Cut k) {
     constexpr int U = VEC == 1 ? 16 : 8;      // loads in flight
@@ -531,7 +531,7 @@ struct ApplyArgs {
 };
 
 // The second pass: y (and the codes) from x or codes and the statistics.  Bound by
-// memory: 822 MB of the same tensor in 120 us, 6.8 TB/s.
+// memory: 822 MB of the same tensor in 121 us, 6.8 TB/s.
 template <typename T, int VEC, bool X8, bool SILU>
 __global__ __launch_bounds__(256) void k_norm_apply(ApplyArgs a, Cut k) {
     constexpr int U = VEC == 1 ? 8 : 4;       // loads in flight
@@ -707,7 +707,7 @@ __global__ __launch_bounds__(kMaxThreads) void k_norm_back(BwdArgs a, Cut k) {
 
 // The parts of the sums of a chunk of an image.  Bound by memory and, in 16 bits, by
 // SiLU's exponential and reciprocal too: 514 MB (N = 32, 64 channels at 224x224, fp32
-// dy and codes) in 91 us, 5.6 TB/s; 206 MB (N = 64, 256 at 56x56, bf16) in 39, 5.2.
+// dy and codes) in 93 us, 5.5 TB/s; 206 MB (N = 64, 256 at 56x56, bf16) in 41, 5.0.
 template <typename T, int VEC, bool X8, bool SILU>
 __global__ __launch_bounds__(256) void k_norm_back_part(BwdArgs a, Cut k) {
     constexpr int U = VEC == 1 ? 8 : 4;
@@ -826,7 +826,7 @@ __global__ __launch_bounds__(256) void k_norm_back_join(const float* __restrict_
     }
 }
 
-// The second pass: dx.  925 MB of the first of these tensors in 144 us, 6.4 TB/s.
+// The second pass: dx.  925 MB of the first of these tensors in 148 us, 6.3 TB/s.
 template <typename T, int VEC, bool X8, bool SILU>
 __global__ __launch_bounds__(256) void k_norm_back_apply(BwdArgs a, Cut k) {
     constexpr int U = VEC == 1 ? 8 : 4;

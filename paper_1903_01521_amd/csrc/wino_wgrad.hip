@@ -525,7 +525,7 @@ struct Wgrad {
 // row `block` of `blocks`.  16 bytes a load of whichever C: a run of C / gcd(C, V) vectors
 // is whole pixels, so a thread that moves on by whole runs keeps its V channels.  (One
 // value a load, each thread a channel, for tensors off 16-byte addresses and for more runs'
-// vectors than threads.)  205 MB in 33 us, 6.3 TB/s.
+// vectors than threads.)  205 MB in 33 us, 6.2 TB/s.
 template <typename T>
 __device__ __forceinline__ void most_of(const T* p, int64_t n, int C, int block, int blocks, uint32_t* lds, uint8_t* out) {
     constexpr int V = 16 / sizeof(T), threads = kMostThreads;
@@ -622,9 +622,11 @@ __global__ __launch_bounds__(kMostThreads) void k_wgrad_most(Args g) {
 // same slice run on one XCD, so that they share its rows in L2.  144 accumulators a lane
 // hold the nine taps of 16 channels by 64 filters: a step reads 18 words of the input and
 // 8 of dy from LDS for 108 products, so the matrix cores bound it (N = 64, 256 -> 256 at
-// 56x56, fp32: 495 us, 1.43 PFLOP/s of fp16 products; formed from the checkpoint with
-// SiLU 560, the matrix cores 60% busy; bf16, one product of each, 285 us, 0.83 PFLOP/s,
-// bound by the loads of two bytes a lane).  Small layers are a chain of steps of 1.3 us.
+// 56x56 in calls in a row, less the other launches: fp32 495 to 533 us, 1.34 to 1.43
+// PFLOP/s of fp16 products; formed from the checkpoint with SiLU 527 to 573, the matrix
+// cores 59% busy; bf16, one product of each, 277 to 282, 0.84, bound by the loads of two
+// bytes a lane; a kernel trace shows 10 to 23% more).  Small layers are a chain of steps
+// of 1.3 us.
 template <typename T, bool X8, bool NORM, int WC, int KW, int KS>
 __global__ __launch_bounds__(WC* KW* KS * 64, WC* KW* KS / 4) void k_wgrad(Args g) {
     typedef Wgrad<T, X8, NORM, WC, KW, KS> W;
@@ -731,7 +733,8 @@ double step_of(const WgradShape& s, int form) {
 // the first loads and the last stores; a step for every row of a slice and two for
 // every strip that it enters; the slices' parts, 72 bytes a filter and channel, written
 // and read at 8 TB/s.  (The launch for the scale is the same for all.)  Against every
-// form at 4 to 224 slices its choice was within 6% of the best (us): N = 8, 128 -> 128 at
+// form at 4 to 224 slices its choice was within 6% of the best (us, with one scale a
+// tensor; the channels' own add 1 to 2 to all): N = 8, 128 -> 128 at
 // 28x28 31.4 (third form, 28 slices; first form 35.7 at best); N = 1, 256 -> 256 at 56x56
 // 37.4 (second, 13; 36.1 at 16); N = 32, 512 -> 512 at 14x14 97.5 (second, 4; 97.3);
 // N = 32, 256 -> 256 at 28x28 in bf16 59.3 (59.5).
