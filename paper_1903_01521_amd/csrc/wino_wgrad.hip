@@ -521,6 +521,30 @@ struct Wgrad {
     }
 };
 
+// The exponents of the largest of `rows` values of each channel, value(row, channel) as
+// magnitude bits: row `block` of `blocks`, a thread a channel.
+template <typename F>
+__device__ __forceinline__ void most_by_channel(int64_t rows, int C, int block, int blocks, uint32_t* lds, uint8_t* out,
+                                                F value) {
+    constexpr int threads = kMostThreads;
+    const int t = threadIdx.x, wide = C < threads ? C : threads, per = threads / wide, row = t / wide;
+    for (int c0 = 0; c0 < C; c0 += threads) {
+        const int c = c0 + t % wide;
+        uint32_t m = 0;
+        if (c < C && row < per)
+            for (int64_t i = (int64_t)block * per + row; i < rows; i += (int64_t)blocks * per) {
+                const uint32_t v = value(i, c);
+                m = v > m ? v : m;
+            }
+        lds[t] = 0;
+        __syncthreads();
+        if (c < C && row < per) atomicMax(lds + (c - c0), m);
+        __syncthreads();
+        if (c0 + t < C) out[c0 + t] = (uint8_t)(lds[t] >> 23);
+        __syncthreads();
+    }
+}
+
 // The exponents of a channel-last tensor's largest magnitudes, n values of C channels:
 // row `block` of `blocks`.  16 bytes a load of whichever C: a run of C / gcd(C, V) vectors
 // is whole pixels, so a thread that moves on by whole runs keeps its V channels.  (One
@@ -532,21 +556,7 @@ __device__ __forceinline__ void most_of(const T* p, int64_t n, int C, int block,
     const int g = C % V == 0 ? V : C % 4 == 0 ? 4 : C % 2 == 0 ? 2 : 1;      // gcd(C, V): V is 4 or 8
     const int t = threadIdx.x, run = C / g;
     if (((uintptr_t)p & 15) || run > threads) {
-        const int64_t pixels = n / C;
-        const int per = C < threads ? threads / C : 1;
-        for (int c0 = 0; c0 < C; c0 += threads) {
-            const int c = c0 + t % (C < threads ? C : threads), row = C < threads ? t / C : 0;
-            uint32_t m = 0;
-            if (c < C && row < per)
-                for (int64_t i = (int64_t)block * per + row; i < pixels; i += (int64_t)blocks * per)
-                    m = larger(m, (float)p[i * C + c]);
-            lds[t] = 0;
-            __syncthreads();
-            if (c < C && row < per) atomicMax(lds + (c - c0), m);
-            __syncthreads();
-            if (c0 + t < C) out[c0 + t] = (uint8_t)(lds[t] >> 23);
-            __syncthreads();
-        }
+        most_by_channel(n / C, C, block, blocks, lds, out, [&](int64_t i, int c) { return larger(0, (float)p[i * C + c]); });
         return;
     }
     const int per = threads / run, col = t % run, row = t / run;
@@ -595,18 +605,16 @@ __global__ __launch_bounds__(kMostThreads) void k_wgrad_most(Args g) {
         out = g.most + (size_t)g.nx * most_row(C) + (size_t)(b - g.nx) * most_row(g.s.K);
         most_of((const T*)g.a.dy, (int64_t)g.s.N * g.s.Ho * g.s.Wo * g.s.K, g.s.K, b - g.nx, g.nd, lds, out);
     } else if (g.s.x8) {
-        for (int c = threadIdx.x; c < C; c += kMostThreads) {
-            uint32_t m = 0;
-            const float gamma = g.s.norm && g.a.gamma ? fabsf(g.a.gamma[c]) : 1.0f;
-            const float beta = g.s.norm && g.a.beta ? fabsf(g.a.beta[c]) : 0.0f;
-            for (int n = b; n < g.s.N; n += g.nx) {
-                const float* r = g.a.rows + ((size_t)n * C + c) * 2;
-                const float* st = g.s.norm ? g.a.stats + ((size_t)n * g.s.G + c / g.s.D) * 2 : nullptr;
-                const float reach = (fabsf(r[0] - (st ? st[0] : 0.0f)) + kCodes * r[1]) * (st ? st[1] : 1.0f);
-                m = larger(m, reach * gamma + beta > top ? top : reach * gamma + beta);
+        most_by_channel(g.s.N, C, b, g.nx, lds, out, [&](int64_t n, int c) {
+            const float* r = g.a.rows + ((size_t)n * C + c) * 2;
+            float v = fabsf(r[0]) + kCodes * r[1];
+            if (g.s.norm) {
+                const float* st = g.a.stats + ((size_t)n * g.s.G + c / g.s.D) * 2;
+                v = (fabsf(r[0] - st[0]) + kCodes * r[1]) * st[1] * fabsf(g.a.gamma ? g.a.gamma[c] : 1.0f) +
+                    fabsf(g.a.beta ? g.a.beta[c] : 0.0f);
             }
-            out[c] = (uint8_t)(m >> 23);
-        }
+            return larger(0, v > top ? top : v);
+        });
     } else if (g.s.norm) {
         const float bound = 2.0f * sqrtf((float)g.s.D * (float)g.s.H * (float)g.s.W);
         for (int c = threadIdx.x; c < C; c += kMostThreads) {
@@ -769,7 +777,7 @@ struct Scales {
 Scales scales_of(const WgradShape& s) {
     auto blocks = [](int64_t n) { return (int)(n > (int64_t)kMost * 8192 ? kMost : (n + 8191) / 8192); };
     Scales m = {0, 0};
-    if (s.x8) m.nx = s.N < kMost ? s.N : kMost;
+    if (s.x8) m.nx = blocks((int64_t)s.N * s.C * 8);      // a value a thread
     else if (s.norm) m.nx = 1;
     else if (s.io == Io::F32) m.nx = blocks((int64_t)s.N * s.H * s.W * s.C);
     if (s.io == Io::F32 || (s.io == Io::BF16 && m.nx)) m.nd = blocks((int64_t)s.N * s.Ho * s.Wo * s.K);
