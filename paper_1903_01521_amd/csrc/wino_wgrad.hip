@@ -14,8 +14,9 @@
 // fp32 operands are held in two fp16 terms, 22 significand bits, and three of the four
 // products are summed in fp32: a product is off by less than 2^-20 (2^-22 from each
 // operand and from the term left out), and results of many products as near the exact
-// ones as fp32 sums are (two bf16 terms, 16 bits, gave 4.5e-6 of the norm where these
-// give 2e-7).  For fp16's range every channel of the input and every filter of dy is
+// ones as fp32 sums are (two bf16 terms, 16 bits, gave 4.5e-6 of the norm at N = 8,
+// 128 -> 128, 28x28, where these give 2e-7; 1.2e-6 at N = 64, 256 -> 256, 56x56, from the
+// fp32 sums of 200704 products, torch's 4.2e-6).  For fp16's range every channel of the input and every filter of dy is
 // scaled by a power of two of its own, which takes the largest finite value that it
 // holds to 2^14, found by a launch before: values below 2^-17 of that lose bits, in all
 // less than 2^-39 of it.  dg has one channel and one filter an element, so what the others
