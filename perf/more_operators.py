@@ -253,8 +253,11 @@ def _plan(case, d):
             out["dk"], out["dv"] = out["dkv"][:, :, 0], out["dkv"][:, :, 1]
             ws = B.wino_cross_attention_backward_workspace_bytes(*size)
     assert 0 <= ws < 1 << 40
-    return {"out": out, "flags": flags, "space": torch.empty(ws, dtype=torch.int8, device="cuda") if ws else None,
+    plan = {"out": out, "flags": flags, "space": torch.empty(ws, dtype=torch.int8, device="cuda") if ws else None,
             "bytes": ws}
+    if op == "aback":
+        plan["y"] = d["y"].contiguous()         # as the forward call wrote it
+    return plan
 
 
 def _call(s):
