@@ -347,6 +347,7 @@ int wino_conv2d_nhwc(const float* x, const float* U, float* y,
  *   more than 2^30 images of a few values). */
 #define WINO_FLAG_SILU     0x002u   /* y = z * sigmoid(z) (group norm and the calls that undo it) */
 #define WINO_FLAG_ACT8     0x004u   /* x is an 8-bit checkpoint */
+#define WINO_FLAG_PAIRS    0x008u   /* rotations of channels (2i, 2i+1), else (i, i + R/2) */
 #define WINO_IO_F16        0x040u   /* tensors are fp16 */
 #define WINO_IO_BF16       0x080u   /* tensors are bf16 */
 #define WINO_IO_MASK       0x0C0u
@@ -426,6 +427,103 @@ size_t wino_conv2d_wgrad_workspace_bytes(int N, int C, int H, int W, int K, int 
 int wino_conv2d_wgrad_nhwc(const void* x, const void* dy, float* dg, const float* stats, const float* gamma,
                            const float* beta, int G, int N, int C, int H, int W, int K, int pad, unsigned flags,
                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- attention and gated layers on channel-last tensors ----------------------
+ * The other half of a block that is conditioned on an encoder's output: queries from
+ * the pixels [N][H][W][C] (tokens, L = H*W, C = heads * D), keys and values from the
+ * encoder's states, of another length, or from the pixels themselves.
+ *   Tensors are of fp32, or fp16 / bf16 with WINO_IO_F16 / WINO_IO_BF16; gammas,
+ *   biases, tables, statistics and gradients of gammas and biases fp32.  Sums are in a
+ *   fixed order and held in fp32.  q, k, v and their gradients are
+ *   [N][L][heads][D] with a token's heads together and tokens ld elements apart
+ *   (ld >= heads * D; images L * ld apart), so that they may lie in one projection's
+ *   tensor; a gradient has the ld of its tensor, and only its own elements are written.
+ *   All others are dense.  Outputs must not overlap each other or any input (rows
+ *   of equal ld that lie between each other do not overlap).  D <= 128 (UNSUPPORTED
+ *   past it).  Tensors may have any address that suits their element type; 16-byte
+ *   addresses, and D and ld of whole 16-byte words, run faster.  Workspaces on
+ *   16-byte addresses, else WINO_ERR_INVALID_ARG; they may be NULL where their size is
+ *   0; (size_t)-1 on invalid arguments. */
+
+/* Each head of queries and keys over its root mean square, scaled and turned by its
+ * token's position, one launch for both tensors:
+ *   n = x / sqrt(mean_d x^2 + eps), z = n * gamma[d],
+ *   y = z with the pairs (a, b) of its first R channels turned to
+ *       (a cos - b sin, b cos + a sin); the pairs are channels (i, i + R/2), or with
+ *       WINO_FLAG_PAIRS (2i, 2i+1), i < R/2.
+ *   q : [N][Lq][Hq][D], ldq; k : [N][Lk][Hk][D], ldk, or NULL (then nothing of k's is
+ *       read: gk, kpos, yk, Lk, Hk, ldk, and backward dyk, dk, dgk).
+ *   gq, gk : [D] or NULL (1).      eps >= 0.
+ *   rot : [T][R/2][2] of (cos, sin), one row for each position.  R even, 0 <= R <= D; with
+ *       R = 0 rot, T, qpos and kpos are not read.
+ *   qpos, kpos : [N][Lq], [N][Lk] rows of the table for each token, or NULL: token t of
+ *       every image is at row t (L <= T, else INVALID_ARG).  A token whose position is
+ *       not below T, or negative, gets NaN in its turned channels (and backward in its
+ *       heads' gradients and in dgamma).
+ *   yq, yk : [N][Lq][Hq][D], [N][Lk][Hk][D], dense.
+ * N * L * ceil(heads / 4) must be below 2^31 (UNSUPPORTED). */
+int wino_qk_norm_nhwc(const void* q, const void* k, const float* gq, const float* gk, const float* rot,
+                      const int* qpos, const int* kpos, void* yq, void* yk, int N, int Lq, int Lk, int Hq, int Hk,
+                      int D, int R, int T, int ldq, int ldk, float eps, unsigned flags, void* stream);
+/* Its backward pass, from dyq, dyk (dense) and what the forward pass read: dq, dk (as q
+ * and k), dgq, dgk : [D], either may be NULL (the workspace is needed only for these). */
+size_t wino_qk_norm_backward_workspace_bytes(int N, int Lq, int Lk, int Hq, int Hk, int D, unsigned flags);
+int wino_qk_norm_backward_nhwc(const void* dyq, const void* dyk, const void* q, const void* k, const float* gq,
+                               const float* gk, const float* rot, const int* qpos, const int* kpos, void* dq, void* dk,
+                               float* dgq, float* dgk, int N, int Lq, int Lk, int Hq, int Hk, int D, int R, int T,
+                               int ldq, int ldk, float eps, unsigned flags, void* workspace, size_t workspace_bytes,
+                               void* stream);
+
+/* Attention of Lq tokens to Lk keys of the same image, for query head h over key head
+ * h / (Hq / Hk) (Hq % Hk == 0):
+ *   S = scale * q k^T, y = softmax(S) v over the keys that klen and mask leave.
+ *   k, v : [N][Lk][Hk][D], ldk, ldv.   scale > 0 and finite.
+ *   klen : [N] lengths, keys from klen[n] on are left out (values outside 0..Lk are taken
+ *          as 0 or Lk), or NULL.
+ *   mask : [N][Lk] bytes, keys of zero bytes are left out, or NULL.
+ *   y    : [N][Lq][Hq][D], dense.
+ *   lse  : [N][Hq][Lq], log of the sum of exp(S), for the backward pass, or NULL.
+ * What a key that is left out holds is not read.  An image without keys gives y = 0,
+ * lse = -infinity.  Products of fp32 tensors are summed on fp32 MFMA; of 16-bit tensors
+ * exactly, exp(S - a running maximum) being rounded to the tensors' type once. */
+size_t wino_cross_attention_workspace_bytes(int N, int Lq, int Lk, int Hq, int Hk, int D, unsigned flags);
+int wino_cross_attention_nhwc(const void* q, const void* k, const void* v, const int* klen, const unsigned char* mask,
+                              void* y, float* lse, int N, int Lq, int Lk, int Hq, int Hk, int D, int ldq, int ldk,
+                              int ldv, float scale, unsigned flags, void* workspace, size_t workspace_bytes,
+                              void* stream);
+/* Its backward pass, from dy (dense), the inputs, and y and lse as the forward pass wrote
+ * them: with P = exp(S - lse), dP = dy v^T, dS = P * (dP - sum_d dy y):
+ *   dq = scale * dS k, dk = scale * dS^T q, dv = P^T dy
+ * summed over the query heads that share a key head.  Every key's gradient is written, zeros
+ * where it is left out, and zeros in dq of an image without keys.  P and dS of 16-bit tensors
+ * are rounded to their type once (fp16: times powers of two that keep them in its range). */
+size_t wino_cross_attention_backward_workspace_bytes(int N, int Lq, int Lk, int Hq, int Hk, int D, unsigned flags);
+int wino_cross_attention_backward_nhwc(const void* dy, const void* q, const void* k, const void* v, const void* y,
+                                       const float* lse, const int* klen, const unsigned char* mask, void* dq, void* dk,
+                                       void* dv, int N, int Lq, int Lk, int Hq, int Hk, int D, int ldq, int ldk,
+                                       int ldv, float scale, unsigned flags, void* workspace, size_t workspace_bytes,
+                                       void* stream);
+
+/* The gated layer: two 1x1 layers of x [N][H][W][C], one through the activation, and
+ * their product, in one launch:
+ *   y = act(x w[0]^T + bias[0]) * (x w[1]^T + bias[1])
+ *   w    : [2][K][C], of the tensors' type.    bias : [2][K] fp32 or NULL (0).
+ *   y    : [N][H][W][K].
+ *   flags: WINO_FLAG_RELU or WINO_FLAG_SILU or neither; WINO_IO_*. */
+size_t wino_gated_layer_workspace_bytes(int N, int C, int H, int W, int K, unsigned flags);
+int wino_gated_layer_nhwc(const void* x, const void* w, const float* bias, void* y, int N, int C, int H, int W, int K,
+                          unsigned flags, void* workspace, size_t workspace_bytes, void* stream);
+/* Its backward pass, from dy [N][H][W][K] and the inputs: zg and zu, the two layers'
+ * results, are formed again, and with dzg = dy * zu * act'(zg), dzu = dy * act(zg) (ReLU:
+ * 0 at zg <= 0):
+ *   dx = dzg w[0] + dzu w[1], dw = (dzg^T x, dzu^T x), dbias = (sum dzg, sum dzu).
+ *   dx : as x; dw : as w; dbias : [2][K] fp32.  Each may be NULL, not all (INVALID_ARG).
+ * dzg and dzu go through the workspace in the tensors' type, one rounding; dbias is summed
+ * before it.  N*H*W and 2*K must be below 2^31, K*C below 2^37 (UNSUPPORTED). */
+size_t wino_gated_layer_backward_workspace_bytes(int N, int C, int H, int W, int K, unsigned flags);
+int wino_gated_layer_backward_nhwc(const void* dy, const void* x, const void* w, const float* bias, void* dx, void* dw,
+                                   float* dbias, int N, int C, int H, int W, int K, unsigned flags, void* workspace,
+                                   size_t workspace_bytes, void* stream);
 
 /* ---- allocation-free variant ------------------------------------------------
  * For callers that cannot allocate device memory (code under HIP graph

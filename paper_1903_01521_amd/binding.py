@@ -98,6 +98,18 @@ _SIGS = {
     "wino_group_norm_backward_nhwc": ([_vp] * 8 + [_c_int] * 5 + [_c_uint, _vp, _c_size, _vp], _c_int),
     "wino_conv2d_wgrad_workspace_bytes": ([_c_int] * 6 + [_c_uint], _c_size),
     "wino_conv2d_wgrad_nhwc": ([_vp] * 6 + [_c_int] * 7 + [_c_uint, _vp, _c_size, _vp], _c_int),
+    "wino_qk_norm_nhwc": ([_vp] * 9 + [_c_int] * 10 + [ctypes.c_float, _c_uint, _vp], _c_int),
+    "wino_qk_norm_backward_workspace_bytes": ([_c_int] * 6 + [_c_uint], _c_size),
+    "wino_qk_norm_backward_nhwc": ([_vp] * 13 + [_c_int] * 10 + [ctypes.c_float, _c_uint, _vp, _c_size, _vp], _c_int),
+    "wino_cross_attention_workspace_bytes": ([_c_int] * 6 + [_c_uint], _c_size),
+    "wino_cross_attention_nhwc": ([_vp] * 7 + [_c_int] * 9 + [ctypes.c_float, _c_uint, _vp, _c_size, _vp], _c_int),
+    "wino_cross_attention_backward_workspace_bytes": ([_c_int] * 6 + [_c_uint], _c_size),
+    "wino_cross_attention_backward_nhwc": ([_vp] * 11 + [_c_int] * 9 + [ctypes.c_float, _c_uint, _vp, _c_size, _vp],
+                                           _c_int),
+    "wino_gated_layer_workspace_bytes": ([_c_int] * 5 + [_c_uint], _c_size),
+    "wino_gated_layer_nhwc": ([_vp] * 4 + [_c_int] * 5 + [_c_uint, _vp, _c_size, _vp], _c_int),
+    "wino_gated_layer_backward_workspace_bytes": ([_c_int] * 5 + [_c_uint], _c_size),
+    "wino_gated_layer_backward_nhwc": ([_vp] * 7 + [_c_int] * 5 + [_c_uint, _vp, _c_size, _vp], _c_int),
     "wino_conv2d_noalloc": ([_vp, _vp, _vp] + [_c_int] * 7 + [_c_uint, _vp], _c_int),
 }
 
@@ -424,6 +436,112 @@ def wino_conv2d_wgrad_nhwc(x, dy, dg, stats, gamma, beta, G, N, C, H, W, K, pad,
     return lib().wino_conv2d_wgrad_nhwc(_xptr(x, flags), _tptr(dy, flags), _fptr(dg), _fptr(stats), _fptr(gamma),
                                         _fptr(beta), G, N, C, H, W, K, pad, flags, _ptr(workspace), workspace_bytes,
                                         _stream(stream))
+
+
+WINO_FLAG_PAIRS = 0x008
+
+
+def _rows(t, flags, ld):
+    """[N][L][heads][D] of the element type that WINO_IO_* names, tokens ld elements apart:
+    a dense tensor, or a view of one projection's."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.is_contiguous():
+        p = _tptr(t, flags)
+        if t.dim() == 4 and t.shape[0] * t.shape[1] > 1 and t.stride(1) != ld:
+            raise ValueError("a tensor's tokens must be ld elements apart")
+        return p
+    if t.dim() != 4:
+        raise ValueError("device buffers must be contiguous, or views [N][L][heads][D]")
+    (N, L, H, D), (sn, sl, sh, sd) = t.shape, t.stride()
+    if (D > 1 and sd != 1) or (H > 1 and sh != D) or (L > 1 and sl != ld) or (N > 1 and sn != L * ld):
+        raise ValueError("a token's heads must lie together, tokens ld elements apart and images L * ld")
+    if not t.is_cuda:
+        raise ValueError("device buffers must be CUDA (HIP) tensors")
+    if _io_dtypes is None:
+        _tptr(t.new_empty(0), flags)
+    if t.dtype is not _io_dtypes.get(flags & WINO_IO_MASK):
+        raise ValueError("tensors must have the element type that the flags name")
+    return t.data_ptr()
+
+
+def _iptr(t):
+    if t is None or isinstance(t, int):
+        return t
+    if t.dtype is not (_torch or _import_torch()).int32:
+        raise ValueError("positions and lengths must be int32")
+    return _ptr(t)
+
+
+def _mptr(t):
+    if t is None or isinstance(t, int):
+        return t
+    if t.element_size() != 1:
+        raise ValueError("masks must be tensors of bytes")
+    return _ptr(t)
+
+
+def wino_qk_norm_nhwc(q, k, gq, gk, rot, qpos, kpos, yq, yk, N, Lq, Lk, Hq, Hk, D, R, T, ldq, ldk, eps, flags=0,
+                      stream=None) -> int:
+    return lib().wino_qk_norm_nhwc(_rows(q, flags, ldq), _rows(k, flags, ldk), _fptr(gq), _fptr(gk), _fptr(rot),
+                                   _iptr(qpos), _iptr(kpos), _tptr(yq, flags), _tptr(yk, flags), N, Lq, Lk, Hq, Hk, D,
+                                   R, T, ldq, ldk, eps, flags, _stream(stream))
+
+
+def wino_qk_norm_backward_workspace_bytes(N, Lq, Lk, Hq, Hk, D, flags=0) -> int:
+    return lib().wino_qk_norm_backward_workspace_bytes(N, Lq, Lk, Hq, Hk, D, flags)
+
+
+def wino_qk_norm_backward_nhwc(dyq, dyk, q, k, gq, gk, rot, qpos, kpos, dq, dk, dgq, dgk, N, Lq, Lk, Hq, Hk, D, R, T,
+                               ldq, ldk, eps, flags=0, workspace=None, workspace_bytes=0, stream=None) -> int:
+    return lib().wino_qk_norm_backward_nhwc(
+        _tptr(dyq, flags), _tptr(dyk, flags), _rows(q, flags, ldq), _rows(k, flags, ldk), _fptr(gq), _fptr(gk),
+        _fptr(rot), _iptr(qpos), _iptr(kpos), _rows(dq, flags, ldq), _rows(dk, flags, ldk), _fptr(dgq), _fptr(dgk), N,
+        Lq, Lk, Hq, Hk, D, R, T, ldq, ldk, eps, flags, _ptr(workspace), workspace_bytes, _stream(stream))
+
+
+def wino_cross_attention_workspace_bytes(N, Lq, Lk, Hq, Hk, D, flags=0) -> int:
+    return lib().wino_cross_attention_workspace_bytes(N, Lq, Lk, Hq, Hk, D, flags)
+
+
+def wino_cross_attention_nhwc(q, k, v, klen, mask, y, lse, N, Lq, Lk, Hq, Hk, D, ldq, ldk, ldv, scale, flags=0,
+                              workspace=None, workspace_bytes=0, stream=None) -> int:
+    return lib().wino_cross_attention_nhwc(_rows(q, flags, ldq), _rows(k, flags, ldk), _rows(v, flags, ldv),
+                                           _iptr(klen), _mptr(mask), _tptr(y, flags), _fptr(lse), N, Lq, Lk, Hq, Hk, D,
+                                           ldq, ldk, ldv, scale, flags, _ptr(workspace), workspace_bytes,
+                                           _stream(stream))
+
+
+def wino_cross_attention_backward_workspace_bytes(N, Lq, Lk, Hq, Hk, D, flags=0) -> int:
+    return lib().wino_cross_attention_backward_workspace_bytes(N, Lq, Lk, Hq, Hk, D, flags)
+
+
+def wino_cross_attention_backward_nhwc(dy, q, k, v, y, lse, klen, mask, dq, dk, dv, N, Lq, Lk, Hq, Hk, D, ldq, ldk,
+                                       ldv, scale, flags=0, workspace=None, workspace_bytes=0, stream=None) -> int:
+    return lib().wino_cross_attention_backward_nhwc(
+        _tptr(dy, flags), _rows(q, flags, ldq), _rows(k, flags, ldk), _rows(v, flags, ldv), _tptr(y, flags),
+        _fptr(lse), _iptr(klen), _mptr(mask), _rows(dq, flags, ldq), _rows(dk, flags, ldk), _rows(dv, flags, ldv), N,
+        Lq, Lk, Hq, Hk, D, ldq, ldk, ldv, scale, flags, _ptr(workspace), workspace_bytes, _stream(stream))
+
+
+def wino_gated_layer_workspace_bytes(N, C, H, W, K, flags=0) -> int:
+    return lib().wino_gated_layer_workspace_bytes(N, C, H, W, K, flags)
+
+
+def wino_gated_layer_nhwc(x, w, bias, y, N, C, H, W, K, flags=0, workspace=None, workspace_bytes=0, stream=None) -> int:
+    return lib().wino_gated_layer_nhwc(_tptr(x, flags), _tptr(w, flags), _fptr(bias), _tptr(y, flags), N, C, H, W, K,
+                                       flags, _ptr(workspace), workspace_bytes, _stream(stream))
+
+
+def wino_gated_layer_backward_workspace_bytes(N, C, H, W, K, flags=0) -> int:
+    return lib().wino_gated_layer_backward_workspace_bytes(N, C, H, W, K, flags)
+
+
+def wino_gated_layer_backward_nhwc(dy, x, w, bias, dx, dw, dbias, N, C, H, W, K, flags=0, workspace=None,
+                                   workspace_bytes=0, stream=None) -> int:
+    return lib().wino_gated_layer_backward_nhwc(_tptr(dy, flags), _tptr(x, flags), _tptr(w, flags), _fptr(bias),
+                                                _tptr(dx, flags), _tptr(dw, flags), _fptr(dbias), N, C, H, W, K, flags,
+                                                _ptr(workspace), workspace_bytes, _stream(stream))
 
 
 def check(status: int, where: str = "wino") -> None:

@@ -16,10 +16,12 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libwino.so")
 KERNELS = [os.path.join(CSRC, f) for f in ("wino_kernels.hip", "wino_bf3.hip", "wino_bf3_1d.hip", "wino_gemm3.hip",
-                                          "wino_norm.hip", "wino_wgrad.hip")]
-SOURCES = KERNELS + [os.path.join(CSRC, f) for f in ("wino_api.cpp", "wino_train_api.cpp")]
+                                          "wino_norm.hip", "wino_wgrad.hip", "wino_qknorm.hip", "wino_attn_f32.hip",
+                                          "wino_attn_f16.hip", "wino_attn_bf16.hip", "wino_attn.hip", "wino_gated.hip")]
+SOURCES = KERNELS + [os.path.join(CSRC, f) for f in ("wino_api.cpp", "wino_train_api.cpp", "wino_block_api.cpp")]
 HEADERS = [os.path.join(CSRC, f) for f in ("wino_device.h", "wino_transforms.h", "wino_internal.h", "wino_checks.h",
-                                           "wino_fastdiv.h", "wino_norm.h", "wino_norm_device.h", "wino_wgrad.h")] + [
+                                           "wino_fastdiv.h", "wino_norm.h", "wino_norm_device.h", "wino_wgrad.h",
+                                           "wino_qknorm.h", "wino_attn.h", "wino_attn_device.h", "wino_gated.h")] + [
     os.path.join(ROOT, "include", "wino.h")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -1,0 +1,84 @@
+// Attention: plans, and the launches by element type.
+#include "wino_attn_device.h"
+#include "wino_checks.h"
+
+namespace wino {
+
+namespace {
+
+constexpr int64_t kMostItems = (int64_t)1 << 30;
+// Workgroups that fill the card: two on each of 256 CUs.
+constexpr int64_t kFill = 512;
+
+// Parts of `length` (steps of `step`, two at least a part) that fill the card.
+int splits_of(int64_t groups, int64_t length, int step) {
+    const int64_t want = (kFill + groups - 1) / groups, most = length / (2 * (int64_t)step);
+    const int64_t s = want < most ? want : most;
+    return s < 1 ? 1 : s > 64 ? 64 : (int)s;
+}
+
+bool all16(const AttnShape& s, std::initializer_list<const void*> ps) {
+    const int z = io_size(s.io);
+    if (s.D * z % 16 || (int64_t)s.ldq * z % 16 || (int64_t)s.ldk * z % 16 || (int64_t)s.ldv * z % 16) return false;
+    for (const void* p : ps)
+        if (!aligned16(p)) return false;
+    return true;
+}
+
+hipError_t run(const AttnK& g, const AttnPlan& p, bool backward, hipStream_t st) {
+    if (g.s.io == Io::F32) return attn_f32(g, p, backward, st);
+    return g.s.io == Io::F16 ? attn_f16(g, p, backward, st) : attn_bf16(g, p, backward, st);
+}
+
+}  // namespace
+
+AttnPlan attn_plan(const AttnShape& s, bool backward) {
+    AttnPlan p{};
+    const int64_t pairs = (int64_t)s.N * s.Hk;
+    p.few = !backward && s.rows <= 32;
+    const int per = p.few ? 32 : 128;
+    p.rows.tiles = (s.rows + per - 1) / per;
+    p.rows.splits = splits_of(pairs * p.rows.tiles, s.Lk, p.few ? 128 : 64);
+    const int64_t all = pairs * s.rows;
+    p.keys.tiles = (s.Lk + 127) / 128;
+    p.keys.splits = splits_of(pairs * p.keys.tiles, s.rows, 64);
+    // elementwise joins have a workgroup for 256 values of one part
+    p.fits = pairs * p.rows.tiles * p.rows.splits <= kMostItems && pairs * p.keys.tiles * p.keys.splits <= kMostItems &&
+             s.rows <= INT32_MAX;
+    if (!p.fits) return p;
+    size_t part = p.rows.splits > 1 ? (size_t)p.rows.splits * all * s.D * 4 : 0;
+    if (backward) {
+        p.delta = round_up((size_t)all * 4, 16);
+        const size_t keys = p.keys.splits > 1 ? (size_t)p.keys.splits * pairs * s.Lk * s.D * 8 : 0;
+        part = part > keys ? part : keys;
+    } else if (p.rows.splits > 1) {
+        p.stat = round_up((size_t)p.rows.splits * all * 8, 16);
+    }
+    p.part = round_up(part, 16);
+    p.need = p.delta + p.part + p.stat;
+    return p;
+}
+
+hipError_t launch_attn(const AttnArgs& a, const AttnShape& s, const AttnPlan& p, void* ws, hipStream_t st) {
+    AttnK g{};
+    g.s = s;
+    g.a = a;
+    g.vec = all16(s, {a.q, a.k, a.v, a.y});
+    g.rep = make_fastdiv((uint32_t)s.rep);
+    g.part = (float*)ws;
+    g.stat = (float*)((char*)ws + p.part);
+    return run(g, p, false, st);
+}
+
+hipError_t launch_attn_backward(const AttnBwd& b, const AttnShape& s, const AttnPlan& p, void* ws, hipStream_t st) {
+    AttnK g{};
+    g.s = s;
+    g.b = b;
+    g.vec = all16(s, {b.dy, b.q, b.k, b.v, b.y, b.dq, b.dk, b.dv});
+    g.rep = make_fastdiv((uint32_t)s.rep);
+    g.delta = (float*)ws;
+    g.part = (float*)((char*)ws + p.delta);
+    return run(g, p, true, st);
+}
+
+}  // namespace wino

@@ -1,0 +1,36 @@
+// The gated layer of channel-last tensors and its backward pass: shapes, plan, launchers.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "wino_norm.h"
+
+namespace wino {
+
+// y[m][f] = act(x w0^T + b0) * (x w1^T + b1); x [M][C], w [2][K][C], b [2][K].
+struct GatedShape {
+    int64_t M;
+    int C, K;
+    Io io;
+    Act act;
+};
+struct GatedArgs {
+    const void *dy, *x, *w;
+    const float* bias;                       // or null
+    void *y, *dx, *dw;                       // dx, dw, dbias: null if not wanted
+    float* dbias;
+};
+struct GatedPlan {
+    bool fits;
+    bool few;                                // forward: a wave for each unit, no tiles
+    int splits;                              // of the sum over tokens in dw
+    size_t dz, dbias, part, need;            // workspace: bytes of each region
+};
+// want_*: what a backward call asks for (all, for the size that is reported)
+GatedPlan gated_plan(const GatedShape& s, bool backward);
+hipError_t launch_gated(const GatedArgs& a, const GatedShape& s, const GatedPlan& p, hipStream_t st);
+hipError_t launch_gated_backward(const GatedArgs& a, const GatedShape& s, const GatedPlan& p, void* ws, hipStream_t st);
+
+}  // namespace wino
