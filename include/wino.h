@@ -434,7 +434,11 @@ int wino_conv2d_wgrad_nhwc(const void* x, const void* dy, float* dg, const float
  * encoder's states, of another length, or from the pixels themselves.
  *   Tensors are of fp32, or fp16 / bf16 with WINO_IO_F16 / WINO_IO_BF16; gammas,
  *   biases, tables, statistics and gradients of gammas and biases fp32.  Sums are in a
- *   fixed order and held in fp32.  q, k, v and their gradients are
+ *   fixed order and held in fp32.  Matrix products of 16-bit operands are exact; fp32
+ *   operands are held as three bf16 terms each (exact down to 2^-110) and the six largest
+ *   of their nine products summed: off by less than 2^-20 of a product, and where a value is
+ *   not finite the results that it enters are not (NaN where fp32 might give
+ *   infinities).  q, k, v and their gradients are
  *   [N][L][heads][D] with a token's heads together and tokens ld elements apart
  *   (ld >= heads * D; images L * ld apart), so that they may lie in one projection's
  *   tensor; a gradient has the ld of its tensor, and only its own elements are written.
@@ -484,19 +488,19 @@ int wino_qk_norm_backward_nhwc(const void* dyq, const void* dyk, const void* q, 
  *   y    : [N][Lq][Hq][D], dense.
  *   lse  : [N][Hq][Lq], log of the sum of exp(S), for the backward pass, or NULL.
  * What a key that is left out holds is not read.  An image without keys gives y = 0,
- * lse = -infinity.  Products of fp32 tensors are summed on fp32 MFMA; of 16-bit tensors
- * exactly, exp(S - a running maximum) being rounded to the tensors' type once. */
+ * lse = -infinity.  exp(S - a running maximum) is rounded to 16-bit tensors' type once. */
 size_t wino_cross_attention_workspace_bytes(int N, int Lq, int Lk, int Hq, int Hk, int D, unsigned flags);
 int wino_cross_attention_nhwc(const void* q, const void* k, const void* v, const int* klen, const unsigned char* mask,
                               void* y, float* lse, int N, int Lq, int Lk, int Hq, int Hk, int D, int ldq, int ldk,
                               int ldv, float scale, unsigned flags, void* workspace, size_t workspace_bytes,
                               void* stream);
 /* Its backward pass, from dy (dense), the inputs, and y and lse as the forward pass wrote
- * them: with P = exp(S - lse), dP = dy v^T, dS = P * (dP - sum_d dy y):
+ * them: with P = exp(S - lse), dP = dy v^T, dS = P * (dP - sum_keys P dP):
  *   dq = scale * dS k, dk = scale * dS^T q, dv = P^T dy
  * summed over the query heads that share a key head.  Every key's gradient is written, zeros
- * where it is left out, and zeros in dq of an image without keys.  P and dS of 16-bit tensors
- * are rounded to their type once (fp16: times powers of two that keep them in its range). */
+ * where it is left out, and zeros in dq of an image without keys.  The sum in dS is that of
+ * dy y, the rounding of a 16-bit y taken out again.  P and dS of 16-bit tensors are rounded to
+ * their type once (fp16: times powers of two that keep them in its range). */
 size_t wino_cross_attention_backward_workspace_bytes(int N, int Lq, int Lk, int Hq, int Hk, int D, unsigned flags);
 int wino_cross_attention_backward_nhwc(const void* dy, const void* q, const void* k, const void* v, const void* y,
                                        const float* lse, const int* klen, const unsigned char* mask, void* dq, void* dk,

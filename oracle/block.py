@@ -88,7 +88,8 @@ def attention(q, k, v, scale, kept):
 
 
 def attention_backward(dy, q, k, v, y, lse, scale, kept):
-    """dq, dk, dv from what the forward pass left, and the intermediates that bound rounding."""
+    """dq, dk, dv with the rows' log sums that the forward pass left, and the intermediates
+    that bound rounding (y is one of them only)."""
     N, Lk, Hk, D = k.shape
     rep = q.shape[2] // Hk
     k, v = _heads(_drop(k, kept), rep), _heads(_drop(v, kept), rep)
@@ -97,7 +98,7 @@ def attention_backward(dy, q, k, v, y, lse, scale, kept):
     with np.errstate(invalid="ignore", over="ignore"):
         p = np.where(kept[:, None, None], np.exp(s - lse[..., None]), 0.0)
     dp = dy @ v.transpose(0, 1, 3, 2)
-    delta = (dy * y).sum(-1, keepdims=True)
+    delta = (p * dp).sum(-1, keepdims=True)
     ds = p * (dp - delta)
 
     def shared(g):

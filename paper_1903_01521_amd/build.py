@@ -49,7 +49,7 @@ def build(verbose: bool = False) -> str:
             subprocess.check_call(cmd)
             return obj
         objects = _each(compile_one, SOURCES)
-        subprocess.check_call([HIPCC, "--offload-arch=" + ARCH, "-shared", "-o", tmp] + objects)
+        subprocess.check_call([HIPCC, "--offload-arch=" + ARCH, "-shared", "-Wl,-z,defs", "-o", tmp] + objects)
     os.replace(tmp, LIB)
     return LIB
 

@@ -40,18 +40,21 @@ AttnPlan attn_plan(const AttnShape& s, bool backward) {
     p.rows.tiles = (s.rows + per - 1) / per;
     p.rows.splits = splits_of(pairs * p.rows.tiles, s.Lk, p.few ? 128 : 64);
     const int64_t all = pairs * s.rows;
-    p.keys.tiles = (s.Lk + 127) / 128;
+    p.keys.tiles = (s.Lk + kOwnKeys - 1) / kOwnKeys;
     p.keys.splits = splits_of(pairs * p.keys.tiles, s.rows, 64);
-    // elementwise joins have a workgroup for 256 values of one part
-    p.fits = pairs * p.rows.tiles * p.rows.splits <= kMostItems && pairs * p.keys.tiles * p.keys.splits <= kMostItems &&
-             s.rows <= INT32_MAX;
+    // pairs are rounded up to eight; a row of a tile past 2^31 would pass 32 bits
+    const int64_t eights = (pairs + 7) / 8 * 8;
+    p.fits = eights * p.rows.tiles * p.rows.splits <= kMostItems && eights * p.keys.tiles * p.keys.splits <= kMostItems &&
+             s.rows <= INT32_MAX - 128;
     if (!p.fits) return p;
-    size_t part = p.rows.splits > 1 ? (size_t)p.rows.splits * all * s.D * 4 : 0;
+    const bool parts = p.rows.splits > 1;
+    size_t part = parts ? (size_t)p.rows.splits * all * s.D * (backward ? 8 : 4) : 0;
     if (backward) {
-        p.delta = round_up((size_t)all * 4, 16);
+        p.delta = round_up((size_t)all * 4, 16) * (s.io == Io::F32 ? 2 : 1);   // with P's sums
+        p.stat = parts ? round_up((size_t)p.rows.splits * all * 8, 16) : 0;
         const size_t keys = p.keys.splits > 1 ? (size_t)p.keys.splits * pairs * s.Lk * s.D * 8 : 0;
         part = part > keys ? part : keys;
-    } else if (p.rows.splits > 1) {
+    } else if (parts) {
         p.stat = round_up((size_t)p.rows.splits * all * 8, 16);
     }
     p.part = round_up(part, 16);
@@ -77,7 +80,9 @@ hipError_t launch_attn_backward(const AttnBwd& b, const AttnShape& s, const Attn
     g.vec = all16(s, {b.dy, b.q, b.k, b.v, b.y, b.dq, b.dk, b.dv});
     g.rep = make_fastdiv((uint32_t)s.rep);
     g.delta = (float*)ws;
+    g.share = (float*)((char*)ws + p.delta / 2);
     g.part = (float*)((char*)ws + p.delta);
+    g.stat = (float*)((char*)ws + p.delta + p.part);
     return run(g, p, true, st);
 }
 

@@ -47,48 +47,106 @@ __device__ __forceinline__ float add_halves(float x) {
 // ---------------------------------------------------------------- operands
 // Eight values of a lane: 16 terms of a product, eight each in the wave's halves.
 
+// fp32 operands are three bf16 terms each, h + m + l, eight significand bits a term (their
+// split is exact down to 2^-110), and a product is the sum of the six largest of nine,
+// 2.67 times the fp32 matrix rate; what is dropped is below 2^-20 of the product.  A value
+// that is not finite makes its sums NaN.
+
 template <typename T>
 struct Frag {
     typedef T V __attribute__((ext_vector_type(8)));
     V v;
 };
+typedef __bf16 b16x8 __attribute__((ext_vector_type(8)));
 template <>
 struct Frag<float> {
-    float v[8];
+    b16x8 h, m, l;
 };
 
-__device__ __forceinline__ f32x16 mma(const Frag<__bf16>& a, const Frag<__bf16>& b, f32x16 c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, c, 0, 0, 0);
-}
 __device__ __forceinline__ f32x16 mma(const Frag<_Float16>& a, const Frag<_Float16>& b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a.v, b.v, c, 0, 0, 0);
 }
+__device__ __forceinline__ f32x16 mma(b16x8 a, b16x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma(const Frag<__bf16>& a, const Frag<__bf16>& b, f32x16 c) { return mma(a.v, b.v, c); }
 __device__ __forceinline__ f32x16 mma(const Frag<float>& a, const Frag<float>& b, f32x16 c) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[j], b.v[j], c, 0, 0, 0);
-    return c;
+    c = mma(a.l, b.h, c);
+    c = mma(a.h, b.l, c);
+    c = mma(a.m, b.m, c);
+    c = mma(a.m, b.h, c);
+    c = mma(a.h, b.m, c);
+    return mma(a.h, b.h, c);
 }
 
-// Values 8 at .. 8 at + 7 of a result as an operand, rounded once to T.
+// The terms of two values, a word of each: h and m cut off towards zero, l what is left.
+__device__ __forceinline__ void split_two(float a, float b, uint32_t& h, uint32_t& m, uint32_t& l) {
+    constexpr uint32_t kHigh = 0xffff0000u, kTake = 0x07060302u;
+    const uint32_t ab = __float_as_uint(a), bb = __float_as_uint(b);
+    const float a1 = a - __uint_as_float(ab & kHigh), b1 = b - __uint_as_float(bb & kHigh);
+    const uint32_t a1b = __float_as_uint(a1), b1b = __float_as_uint(b1);
+    const float a2 = a1 - __uint_as_float(a1b & kHigh), b2 = b1 - __uint_as_float(b1b & kHigh);
+    h = __builtin_amdgcn_perm(bb, ab, kTake);
+    m = __builtin_amdgcn_perm(b1b, a1b, kTake);
+    l = __builtin_amdgcn_perm(__float_as_uint(b2), __float_as_uint(a2), kTake);
+}
+
+// Eight values as an operand, rounded once to T.
 template <typename T>
-__device__ __forceinline__ Frag<T> pack(const f32x16& s, int at) {
+__device__ __forceinline__ Frag<T> frag_of(const float (&x)[8]) {
     Frag<T> f;
+    if constexpr (sizeof(T) == 4) {
+        uint32_t h[4], m[4], l[4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f.v[j] = (T)s[8 * at + j];
+        for (int j = 0; j < 4; ++j) split_two(x[2 * j], x[2 * j + 1], h[j], m[j], l[j]);
+        __builtin_memcpy(&f.h, h, 16);
+        __builtin_memcpy(&f.m, m, 16);
+        __builtin_memcpy(&f.l, l, 16);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f.v[j] = (T)x[j];
+    }
     return f;
 }
 
-// ---------------------------------------------------------------- tiles in LDS
-// Rows of W = 16 D16 values (up to a power of two), in 16-byte chunks whose place is
-// xored with bits of the row, so that 16 rows' chunk of the same number lie in
-// different banks (read(), a row for each lane) and four rows' 64 bytes too (turned(),
-// the transposing read of four rows by 16 columns).
+// Values 8 at .. 8 at + 7 of a result as an operand.
+template <typename T>
+__device__ __forceinline__ Frag<T> pack(const f32x16& s, int at) {
+    float x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = s[8 * at + j];
+    return frag_of<T>(x);
+}
 
-template <typename T, int D16>
+// c + the sum of an operand's eight values as they are rounded (16-bit types).
+__device__ __forceinline__ float sum_of(const Frag<_Float16>& f, float c) {
+    typedef _Float16 V2 __attribute__((ext_vector_type(2)));
+    const V2 one = {(_Float16)1.0f, (_Float16)1.0f};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_fdot2(V2{f.v[2 * j], f.v[2 * j + 1]}, one, c, false);
+    return c;
+}
+__device__ __forceinline__ float sum_of(const Frag<__bf16>& f, float c) {
+    typedef __bf16 V2 __attribute__((ext_vector_type(2)));
+    const V2 one = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_fdot2_f32_bf16(V2{f.v[2 * j], f.v[2 * j + 1]}, one, c, false);
+    return c;
+}
+
+// ---------------------------------------------------------------- tiles in LDS
+// R rows of W = 16 D16 16-bit values (up to a power of two), in 16-byte chunks whose place
+// is xored with bits of the row, so that 16 rows' chunk of the same number lie in
+// different banks (read(), a row for each lane) and four rows' 64 bytes too (turned(),
+// the transposing read of four rows by 16 columns).  fp32 tiles are three such planes.
+
+template <typename T, int D16, int R>
 struct Tile {
     static constexpr int kP2 = D16 <= 2 ? 2 : D16 <= 4 ? 4 : 8;
-    static constexpr int kRow = kP2 * 16 * (int)sizeof(T);          // bytes
-    static constexpr int kChunks = D16 * (int)sizeof(T);            // used 16-byte chunks of a row
+    static constexpr int kRow = kP2 * 32;                           // bytes
+    static constexpr int kPlane = R * kRow;
+    static constexpr int kBytes = kPlane * (sizeof(T) == 4 ? 3 : 1);
+    static constexpr int kChunks = D16 * (int)sizeof(T);            // 16-byte chunks of a row in memory
     static constexpr int kEach = 16 / (int)sizeof(T);               // values of a chunk
 
     __device__ static __forceinline__ int twist(int row) {
@@ -98,19 +156,31 @@ struct Tile {
     }
     __device__ static __forceinline__ int at(int row, int chunk) { return row * kRow + ((chunk ^ twist(row)) << 4); }
 
+    // a chunk of memory, to its place
+    __device__ static __forceinline__ void store(char* t, int row, int ch, uint4 w) {
+        if constexpr (sizeof(T) == 2) {
+            *(uint4*)(t + at(row, ch)) = w;
+        } else {
+            uint2 h, m, l;
+            split_two(__uint_as_float(w.x), __uint_as_float(w.y), h.x, m.x, l.x);
+            split_two(__uint_as_float(w.z), __uint_as_float(w.w), h.y, m.y, l.y);
+            char* p = t + at(row, ch >> 1) + (ch & 1) * 8;
+            *(uint2*)p = h;
+            *(uint2*)(p + kPlane) = m;
+            *(uint2*)(p + 2 * kPlane) = l;
+        }
+    }
+
     // values 16 c + 8 h .. + 7 of row `row`
     __device__ static __forceinline__ Frag<T> read(const char* t, int row, int c, int h) {
         Frag<T> f;
+        const char* p = t + at(row, 2 * c + h);
         if constexpr (sizeof(T) == 2) {
-            f.v = __builtin_bit_cast(typename Frag<T>::V, *(const uint4*)(t + at(row, 2 * c + h)));
+            f.v = *(const typename Frag<T>::V*)p;
         } else {
-            const f32x4v a = *(const f32x4v*)(t + at(row, 4 * c + 2 * h));
-            const f32x4v b = *(const f32x4v*)(t + at(row, 4 * c + 2 * h + 1));
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                f.v[j] = a[j];
-                f.v[4 + j] = b[j];
-            }
+            f.h = *(const b16x8*)p;
+            f.m = *(const b16x8*)(p + kPlane);
+            f.l = *(const b16x8*)(p + 2 * kPlane);
         }
         return f;
     }
@@ -125,20 +195,21 @@ struct Tile {
     template <int HALF, int NEXT>
     __device__ static __forceinline__ Frag<T> turned_by(const char* t, int r, int db, int lane) {
         Frag<T> f;
-        const int h = lane >> 5;
-        if constexpr (sizeof(T) == 2) {
-            const int row = r + HALF * h + ((lane >> 2) & 3), chunk = 4 * db + ((lane >> 3) & 2) + ((lane >> 1) & 1);
-            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(t + at(row, chunk) + (lane & 1) * 8));
-            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(t + at(row + NEXT, chunk) + (lane & 1) * 8));
+        const int row = r + HALF * (lane >> 5) + ((lane >> 2) & 3);
+        const int chunk = 4 * db + ((lane >> 3) & 2) + ((lane >> 1) & 1), low = (lane & 1) * 8;
+        const char *p = t + at(row, chunk) + low, *q = t + at(row + NEXT, chunk) + low;
+        auto two = [&](int plane) {
+            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + plane * kPlane));
+            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(q + plane * kPlane));
             typedef short s16x8 __attribute__((ext_vector_type(8)));
-            f.v = __builtin_bit_cast(typename Frag<T>::V, (s16x8)__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+            return (s16x8)__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+        };
+        if constexpr (sizeof(T) == 2) {
+            f.v = __builtin_bit_cast(typename Frag<T>::V, two(0));
         } else {
-            const int c = 32 * db + (lane & 31);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int row = r + HALF * h + (j & 3) + NEXT * (j >> 2);
-                f.v[j] = *(const float*)(t + at(row, c >> 2) + (c & 3) * 4);
-            }
+            f.h = __builtin_bit_cast(b16x8, two(0));
+            f.m = __builtin_bit_cast(b16x8, two(1));
+            f.l = __builtin_bit_cast(b16x8, two(2));
         }
         return f;
     }
@@ -162,15 +233,26 @@ __device__ __forceinline__ uint4 load_chunk(const T* p, int d, int D, bool vec) 
 
 // Values 16 c + 8 h .. + 7 of the vector at p; zeros where p is null.
 template <typename T>
-__device__ __forceinline__ Frag<T> load_frag(const T* p, int c, int h, int D, bool vec) {
-    uint4 r[sizeof(T) / 2];
-    constexpr int kEach = 16 / (int)sizeof(T);
+struct Eight {
+    T v[8];
+    __device__ __forceinline__ Eight(const T* p, int c, int h, int D, bool vec) {
+        constexpr int kEach = 16 / (int)sizeof(T);
+        uint4 r[sizeof(T) / 2];
 #pragma unroll
-    for (int j = 0; j < (int)sizeof(T) / 2; ++j)
-        r[j] = p ? load_chunk(p, 16 * c + 8 * h + j * kEach, D, vec) : make_uint4(0, 0, 0, 0);
-    Frag<T> f;
-    __builtin_memcpy(&f.v, r, sizeof(r));
-    return f;
+        for (int j = 0; j < (int)sizeof(T) / 2; ++j)
+            r[j] = p ? load_chunk(p, 16 * c + 8 * h + j * kEach, D, vec) : make_uint4(0, 0, 0, 0);
+        __builtin_memcpy(v, r, sizeof(r));
+    }
+    __device__ __forceinline__ Frag<T> frag() const {
+        Frag<T> f;
+        if constexpr (sizeof(T) == 4) f = frag_of<float>(v);
+        else __builtin_memcpy(&f.v, v, 16);
+        return f;
+    }
+};
+template <typename T>
+__device__ __forceinline__ Frag<T> load_frag(const T* p, int c, int h, int D, bool vec) {
+    return Eight<T>(p, c, h, D, vec).frag();
 }
 
 // Four neighbouring values of a result to p + d, those below D.
@@ -189,7 +271,7 @@ __device__ __forceinline__ void store4(T* p, int d, int D, bool vec, float a, fl
 // A tile of `R` rows on its way: loaded to registers while the one before is worked on.
 template <typename T, int D16, int R, int NT>
 struct Moving {
-    using Tl = Tile<T, D16>;
+    using Tl = Tile<T, D16, R>;
     static constexpr int kAll = R * Tl::kChunks, kMine = (kAll + NT - 1) / NT;
     uint4 w[kMine];
     // ptr(row): the row's vector, or null for zeros
@@ -206,27 +288,53 @@ struct Moving {
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
             const int idx = threadIdx.x + i * NT, row = idx / Tl::kChunks, ch = idx % Tl::kChunks;
-            if (kAll % NT == 0 || idx < kAll) *(uint4*)(t + Tl::at(row, ch)) = w[i];
+            if (kAll % NT == 0 || idx < kAll) Tl::store(t, row, ch, w[i]);
         }
     }
 };
 
-// ---------------------------------------------------------------- work
+// A tile of R rows from memory straight to LDS, 16 bytes a lane, whose place is fixed there:
+// a lane takes the chunk that belongs to it.  Offsets past 2^31 read zeros, as do rows past
+// the buffer's end; they are the same for every tile.  (In place of Moving: 64 keys of 64
+// channels a step cost 80 of 285 vector instructions and 16 registers less.)
+template <typename Tl, int R, int NT>
+struct Direct {
+    static constexpr int kRowChunks = Tl::kRow / 16, kN = R * kRowChunks / NT;
+    static_assert(R * kRowChunks % NT == 0);
+    uint32_t off[kN];
+    // offset(row, chunk) in bytes; the chunk is one past the row's values: none
+    template <typename F>
+    __device__ __forceinline__ void init(int used, F offset) {
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            const int at = threadIdx.x + i * NT, row = at / kRowChunks, chunk = (at % kRowChunks) ^ Tl::twist(row);
+            off[i] = chunk < used ? offset(row, chunk) : 0x80000000u;
+        }
+    }
+    // to the tile at t; bytes: of the buffer at p
+    __device__ __forceinline__ void issue(char* t, const void* p, uint32_t bytes) const {
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, bytes, 0x00020000);
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+        for (int i = 0; i < kN; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                r, (__attribute__((address_space(3))) void*)(t + (i * NT + wave * 64) * 16), 16, off[i], 0, 0, 0);
+    }
+};
+// Every load to LDS of this wave has arrived.
+__device__ __forceinline__ void arrived() { __builtin_amdgcn_s_waitcnt(0x0F70); }
 
-// Workgroups that share an image's keys (or rows) follow each other on one XCD, whose
-// L2 then holds them: workgroup ids go round the eight XCDs.  Item of `all`, or -1.
-__device__ __forceinline__ int64_t item_of(int64_t all) {
-    const int64_t each = (all + 7) / 8, i = (int64_t)(blockIdx.x & 7) * each + (blockIdx.x >> 3);
-    return (blockIdx.x >> 3) < each && i < all ? i : -1;
-}
+// ---------------------------------------------------------------- work
 
 struct AttnK {
     AttnShape s;
     AttnArgs a;
     AttnBwd b;
-    int64_t items, tiles;                    // of this launch; item = (pair * tiles + tile) * splits + split
+    int64_t tiles;                           // of a pair in this launch, each in `splits` parts
     int splits;
-    float *delta, *part, *part2, *stat;
+    bool by_xcd;
+    FastDiv per_pair, per_tile;              // by tiles * splits, by splits
+    float *delta, *share, *part, *part2, *stat;
     bool vec;
     FastDiv rep;                             // by s.rep; rows are below 2^31
 };
@@ -241,6 +349,29 @@ __device__ __forceinline__ RowAt row_at(const AttnK& g, int n, int hk, int64_t r
     return {(int64_t)n * g.s.Lq + t, t, hk * g.s.rep + (int)row - t * g.s.rep};
 }
 
+// A workgroup's (image, key head) pair, tile and part.  Workgroup ids go round the eight
+// XCDs; with by_xcd all workgroups of a pair are on one, whose L2 then holds the pair's
+// keys (or rows), and the pairs go round, so that images of different lengths spread (16
+// images of 0 to 2048 keys, 8 heads: 248 us with runs of pairs on an XCD).  Without, for few pairs, an
+// XCD would be left with less: workgroups as they come.
+struct Work {
+    int n, hk, split;
+    int64_t pair, tile;
+    bool none;
+};
+__device__ __forceinline__ Work work_of(const AttnK& g) {
+    const uint32_t id = blockIdx.x, per = (uint32_t)(g.tiles * g.splits), j = g.by_xcd ? id >> 3 : id;
+    const uint32_t p = fdiv(j, g.per_pair), at = j - p * per, tile = fdiv(at, g.per_tile);
+    Work w;
+    w.pair = g.by_xcd ? p * 8 + (id & 7) : p;
+    w.none = w.pair >= (int64_t)g.s.N * g.s.Hk;
+    w.n = (int)(w.pair / g.s.Hk);
+    w.hk = (int)(w.pair - (int64_t)w.n * g.s.Hk);
+    w.tile = tile;
+    w.split = (int)(at - tile * (uint32_t)g.splits);
+    return w;
+}
+
 // keys of image n
 __device__ __forceinline__ int keys_of(const int* klen, int n, int Lk) {
     return klen ? min(max(klen[n], 0), Lk) : Lk;
@@ -252,6 +383,83 @@ __device__ __forceinline__ void part_of(int64_t n, int step, int split, int spli
     lo = min(each * split, n);
     hi = min(lo + each, n);
 }
+
+// Waves a SIMD that a kernel's registers are held to.  With two (256 registers a wave) no
+// result lies in accumulation registers, from where every step would have to copy it; heads
+// wider than 16 `most` would spill.
+template <typename T, int D16>
+constexpr int waves_of(int most) {
+    return sizeof(T) == 2 && D16 <= most ? 2 : 1;
+}
+
+// Copies of the tiles in LDS: with two, a step has one barrier, and the next tile is
+// stored while slower waves still read this one.  fp32 tiles are too large.
+template <typename T>
+constexpr int kCopies = sizeof(T) == 2 ? 2 : 1;
+
+// The keys' and values' tiles of a walk over keys up to hi.
+template <typename T, int D16, int KT, int NT, bool kDirect>
+struct KeyTiles {                            // by way of registers: any address, type and mask
+    Moving<T, D16, KT, NT> mk, mv;
+    float mb;
+    const AttnShape* s;
+    bool vec;
+    const T *kbase, *vbase;
+    const uint8_t* mask;
+    int64_t hi;
+    __device__ __forceinline__ void init(const AttnShape& s_, bool vec_, const T* k, const T* v, const uint8_t* mask_,
+                                         int64_t hi_) {
+        s = &s_; vec = vec_; kbase = k; vbase = v; mask = mask_; hi = hi_;
+        mb = 0.0f;
+    }
+    __device__ __forceinline__ void load(int64_t k0) {
+        auto kept = [&](int r) { return k0 + r < hi && (!mask || mask[k0 + r]); };
+        mk.load([&](int r) { return kept(r) ? kbase + (k0 + r) * s->ldk : nullptr; }, s->D, vec);
+        mv.load([&](int r) { return kept(r) ? vbase + (k0 + r) * s->ldv : nullptr; }, s->D, vec);
+        if (threadIdx.x < KT) mb = kept(threadIdx.x) ? 0.0f : -INFINITY;
+    }
+    __device__ __forceinline__ void first(char*, char*, int64_t k0) { load(k0); }
+    // the tile at k0 to LDS, the next one on its way
+    __device__ __forceinline__ void step(char* sk, char* sv, float* bias, char*, char*, int64_t k0) {
+        if (kCopies<T> == 1) __syncthreads();
+        mk.store(sk);
+        mv.store(sv);
+        if (threadIdx.x < KT) bias[threadIdx.x] = mb;
+        __syncthreads();
+        if (k0 + KT < hi) load(k0 + KT);
+    }
+    // what is added to the scores of keys at .. at + 3 of the tile at k0
+    __device__ __forceinline__ f32x4v left_out(const float* bias, int at, int64_t) const { return *(const f32x4v*)&bias[at]; }
+};
+template <typename T, int D16, int KT, int NT>
+struct KeyTiles<T, D16, KT, NT, true> {      // straight to LDS: 16-bit, 16-byte words, no mask
+    using Tl = Tile<T, D16, KT>;
+    Direct<Tl, KT, NT> dk, dv;
+    const T *kbase, *vbase;
+    int64_t hi;
+    int ldk, ldv, D;
+    __device__ __forceinline__ void init(const AttnShape& s, bool, const T* k, const T* v, const uint8_t*, int64_t hi_) {
+        kbase = k; vbase = v; hi = hi_; ldk = s.ldk; ldv = s.ldv; D = s.D;
+        dk.init(D / 8, [&](int row, int chunk) { return (uint32_t)row * (uint32_t)s.ldk * 2 + chunk * 16; });
+        dv.init(D / 8, [&](int row, int chunk) { return (uint32_t)row * (uint32_t)s.ldv * 2 + chunk * 16; });
+    }
+    __device__ __forceinline__ void first(char* sk, char* sv, int64_t k0) {
+        const uint32_t last = (uint32_t)min((int64_t)KT, hi - k0) - 1;
+        dk.issue(sk, kbase + k0 * ldk, (last * (uint32_t)ldk + (uint32_t)D) * 2);
+        dv.issue(sv, vbase + k0 * ldv, (last * (uint32_t)ldv + (uint32_t)D) * 2);
+    }
+    __device__ __forceinline__ void step(char*, char*, float*, char* nk, char* nv, int64_t k0) {
+        arrived();
+        __syncthreads();
+        if (k0 + KT < hi) first(nk, nv, k0 + KT);
+    }
+    __device__ __forceinline__ f32x4v left_out(const float*, int at, int64_t k0) const {
+        f32x4v m;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m[i] = k0 + at + i < hi ? 0.0f : -INFINITY;
+        return m;
+    }
+};
 
 // ---------------------------------------------------------------- forward
 // One pass over the keys with a running maximum and sum.  The maximum moves, and what
@@ -267,21 +475,20 @@ struct FwdCut {
     static constexpr int kThreads = 64 * kWaves;
 };
 
-template <typename T, int D16, bool kFew>
-__global__ __launch_bounds__((FwdCut<T, D16, kFew>::kThreads)) void k_attn(AttnK g) {
+template <typename T, int D16, bool kFew, bool kDirect>
+__global__ __launch_bounds__((FwdCut<T, D16, kFew>::kThreads), (waves_of<T, D16>(kFew && !kDirect ? 6 : 8))) void k_attn(AttnK g) {
     using Cut = FwdCut<T, D16, kFew>;
-    using Tl = Tile<T, D16>;
     constexpr int NT = Cut::kThreads, KT = Cut::kKeys, KB = kFew ? 1 : KT / 32, DB = (D16 + 1) / 2;
-    __shared__ alignas(16) char sk[KT * Tl::kRow];
-    __shared__ alignas(16) char sv[KT * Tl::kRow];
-    __shared__ alignas(16) float bias[KT];
+    using Tl = Tile<T, D16, KT>;
+    __shared__ alignas(16) char tk[kCopies<T>][Tl::kBytes];
+    __shared__ alignas(16) char tv[kCopies<T>][Tl::kBytes];
+    __shared__ alignas(16) float biases[kCopies<T>][KT];
     const AttnShape& s = g.s;
-    const int64_t item = item_of(g.items);
-    if (item < 0) return;
+    const Work wk = work_of(g);
+    if (wk.none) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-    const int split = (int)(item % g.splits);
-    const int64_t tile = item / g.splits % g.tiles, pair = item / g.splits / g.tiles;
-    const int n = (int)(pair / s.Hk), hk = (int)(pair % s.Hk);
+    const int split = wk.split, n = wk.n, hk = wk.hk;
+    const int64_t tile = wk.tile, pair = wk.pair;
     const int64_t row = tile * Cut::kRows + (kFew ? 0 : wave * 32) + (lane & 31);
     const bool live = row < s.rows;
     const RowAt me = row_at(g, n, hk, row);
@@ -297,29 +504,23 @@ __global__ __launch_bounds__((FwdCut<T, D16, kFew>::kThreads)) void k_attn(AttnK
     const T* vbase = (const T*)g.a.v + (int64_t)n * s.Lk * s.ldv + (int64_t)hk * s.D;
     const uint8_t* mask = g.a.mask ? g.a.mask + (int64_t)n * s.Lk : nullptr;
 
-    Moving<T, D16, KT, NT> mk, mv;
-    float mb = 0.0f;
-    auto load = [&](int64_t k0) {
-        auto kept = [&](int r) { return k0 + r < hi && (!mask || mask[k0 + r]); };
-        mk.load([&](int r) { return kept(r) ? kbase + (k0 + r) * s.ldk : nullptr; }, s.D, g.vec);
-        mv.load([&](int r) { return kept(r) ? vbase + (k0 + r) * s.ldv : nullptr; }, s.D, g.vec);
-        if (threadIdx.x < KT) mb = kept(threadIdx.x) ? 0.0f : -INFINITY;
-    };
+    KeyTiles<T, D16, KT, NT, kDirect> in;
+    in.init(s, g.vec, kbase, vbase, mask, hi);
 
     const float c2 = s.scale * kLog2e, slack = fminf(8.0f / c2, 0x1p127f);
     float top = -INFINITY, sum = 0.0f;
     f32x16 o[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d) o[d] = f32x16{};
-    if (lo < hi) load(lo);
+    if (lo < hi) in.first(tk[0], tv[0], lo);
+    int copy = 0;
     for (int64_t k0 = lo; k0 < hi; k0 += KT) {
-        __syncthreads();
-        mk.store(sk);
-        mv.store(sv);
-        if (threadIdx.x < KT) bias[threadIdx.x] = mb;
-        __syncthreads();
+        const char *sk = tk[copy], *sv = tv[copy];
+        const float* bias = biases[copy];
+        const int next = kCopies<T> == 1 ? 0 : copy ^ 1;
+        in.step(tk[copy], tv[copy], biases[copy], tk[next], tv[next], k0);
+        copy = next;
         const bool whole = !mask && k0 + KT <= hi;
-        if (k0 + KT < hi) load(k0 + KT);
         const int kb0 = kFew ? wave : 0;
         f32x16 p[KB];
 #pragma unroll
@@ -333,7 +534,7 @@ __global__ __launch_bounds__((FwdCut<T, D16, kFew>::kThreads)) void k_attn(AttnK
             for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
-                    const f32x4v m = *(const f32x4v*)&bias[(kb0 + kb) * 32 + 8 * b + 4 * h];
+                    const f32x4v m = in.left_out(bias, (kb0 + kb) * 32 + 8 * b + 4 * h, k0);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) p[kb][4 * b + i] += m[i];
                 }
@@ -372,9 +573,9 @@ __global__ __launch_bounds__((FwdCut<T, D16, kFew>::kThreads)) void k_attn(AttnK
     }
     sum = add_halves(sum);
     if constexpr (kFew) {
-        // the waves' sums over their keys, by way of LDS: sk holds a wave's 32 rows at a time
+        // the waves' sums over their keys, by way of LDS: a wave's 32 rows at a time
         __shared__ float st[Cut::kWaves][32][2];
-        static_assert(sizeof(sk) >= 32 * 32 * sizeof(float));
+        static_assert(Tl::kBytes >= 32 * 32 * sizeof(float));
         if (h == 0) {
             st[wave][lane][0] = top;
             st[wave][lane][1] = sum;
@@ -390,7 +591,7 @@ __global__ __launch_bounds__((FwdCut<T, D16, kFew>::kThreads)) void k_attn(AttnK
             sum += st[w][lane & 31][1] * __builtin_amdgcn_exp2f((st[w][lane & 31][0] - base) * c2);
         const float a = __builtin_amdgcn_exp2f((top - base) * c2);
         top = all;
-        float* x = (float*)sk;
+        float* x = (float*)tk[0];
 #pragma unroll
         for (int d = 0; d < DB; ++d)
             for (int w = 0; w < Cut::kWaves; ++w) {
@@ -472,15 +673,27 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnK g) {
 // keys, each forming S and dP again, so that every sum has one owner and a fixed
 // order; the first also leaves delta for the second.
 //
+// y of 16-bit tensors is rounded, which moves delta by up to 2^-9 |dy| |y|: where one key
+// has most of a row, dS is the small difference of dP and delta and loses most of its bits
+// (gradients of a head of 64, 1024 keys, scores of deviation 2: 3.0e-3 off instead of 2.3e-3;
+// sharper rows far more).  With dS' formed from that delta, e = sum dS' is what it lacks:
+// delta + e is exact, and dq = scale (sum dS' k - e sum P k), one more product.  There e is
+// summed from dS' as rounded, so that what keys have in common, which dS (its sum is zero)
+// does not see, takes no part in the rounding either.
+//
+// fp32: lse's own rounding, and that of its product with log2 e, move all of a row's P by some
+// 2^-21; the first launch sums P and both divide by it.
+//
 // fp16 operands: P is held 2^12 times as large (a row's share of 2^-24 keeps its bits),
 // dS times a power of two for each column of the result, which falls, with what is
 // summed, where a larger dS than fp16 holds comes by.
 
 constexpr float kPUp = 4096.0f;
 
-// dS of a lane's column to operands' range: s *= up; up falls first if it must.
+// Lets up fall where a lane's column of dS times up would pass fp16's range, and what is
+// summed with it.
 template <int NB, int DB>
-__device__ __forceinline__ void keep_range(const f32x16 (&ds)[NB], float& up, f32x16 (&acc)[DB]) {
+__device__ __forceinline__ void keep_range(const f32x16 (&ds)[NB], float& up, f32x16 (&acc)[DB], float& round) {
     float mx = 0.0f;
 #pragma unroll
     for (int k = 0; k < NB; ++k)
@@ -493,6 +706,7 @@ __device__ __forceinline__ void keep_range(const f32x16 (&ds)[NB], float& up, f3
         const float to = fminf(up, __uint_as_float((uint32_t)(min(max(14 - e, -126), 100) + 127) << 23));
         const float a = to / up;
         up = to;
+        round *= a;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -500,22 +714,24 @@ __device__ __forceinline__ void keep_range(const f32x16 (&ds)[NB], float& up, f3
     }
 }
 
+// 1 over a row's sum of P; 0 for a row without keys.
+__device__ __forceinline__ float share_of(float sum) { return sum == 0.0f ? 0.0f : 1.0f / sum; }
+
 // dq of 128 rows, and delta.
-template <typename T, int D16>
-__global__ __launch_bounds__(256) void k_attn_dq(AttnK g) {
-    using Tl = Tile<T, D16>;
+template <typename T, int D16, bool kDirect>
+__global__ __launch_bounds__(256, (waves_of<T, D16>(4))) void k_attn_dq(AttnK g) {
     constexpr int NT = 256, KT = 64, KB = 2, DB = (D16 + 1) / 2;
-    constexpr bool kHalf = std::is_same_v<T, _Float16>;
-    __shared__ alignas(16) char sk[KT * Tl::kRow];
-    __shared__ alignas(16) char sv[KT * Tl::kRow];
-    __shared__ alignas(16) float bias[KT];
+    constexpr bool kHalf = std::is_same_v<T, _Float16>, kFix = sizeof(T) == 2;
+    using Tl = Tile<T, D16, KT>;
+    __shared__ alignas(16) char tk[kCopies<T>][Tl::kBytes];
+    __shared__ alignas(16) char tv[kCopies<T>][Tl::kBytes];
+    __shared__ alignas(16) float biases[kCopies<T>][KT];
     const AttnShape& s = g.s;
-    const int64_t item = item_of(g.items);
-    if (item < 0) return;
+    const Work wk = work_of(g);
+    if (wk.none) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-    const int split = (int)(item % g.splits);
-    const int64_t tile = item / g.splits % g.tiles, pair = item / g.splits / g.tiles;
-    const int n = (int)(pair / s.Hk), hk = (int)(pair % s.Hk);
+    const int split = wk.split, n = wk.n, hk = wk.hk;
+    const int64_t tile = wk.tile, pair = wk.pair;
     const int64_t row = tile * 128 + wave * 32 + (lane & 31);
     const bool live = row < s.rows;
     const RowAt me = row_at(g, n, hk, row);
@@ -528,13 +744,12 @@ __global__ __launch_bounds__(256) void k_attn_dq(AttnK g) {
 #pragma unroll
     for (int c = 0; c < D16; ++c) {
         fq[c] = load_frag(q, c, h, s.D, g.vec);
-        fo[c] = load_frag(dy, c, h, s.D, g.vec);
-        const Frag<T> fy = load_frag(y, c, h, s.D, g.vec);
+        const Eight<T> ed(dy, c, h, s.D, g.vec), ey(y, c, h, s.D, g.vec);
+        fo[c] = ed.frag();
 #pragma unroll
-        for (int j = 0; j < 8; ++j) delta = __builtin_fmaf((float)fo[c].v[j], (float)fy.v[j], delta);
+        for (int j = 0; j < 8; ++j) delta = __builtin_fmaf((float)ed.v[j], (float)ey.v[j], delta);
     }
     delta = add_halves(delta);
-    if (live && h == 0 && split == 0) g.delta[stat] = delta;
     const float lse = live ? g.b.lse[stat] : -INFINITY;
     const float off = lse == -INFINITY ? -INFINITY : -lse * kLog2e;
 
@@ -544,30 +759,24 @@ __global__ __launch_bounds__(256) void k_attn_dq(AttnK g) {
     const T* kbase = (const T*)g.b.k + (int64_t)n * s.Lk * s.ldk + (int64_t)hk * s.D;
     const T* vbase = (const T*)g.b.v + (int64_t)n * s.Lk * s.ldv + (int64_t)hk * s.D;
     const uint8_t* mask = g.b.mask ? g.b.mask + (int64_t)n * s.Lk : nullptr;
-    Moving<T, D16, KT, NT> mk, mv;
-    float mb = 0.0f;
-    auto load = [&](int64_t k0) {
-        auto kept = [&](int r) { return k0 + r < hi && (!mask || mask[k0 + r]); };
-        mk.load([&](int r) { return kept(r) ? kbase + (k0 + r) * s.ldk : nullptr; }, s.D, g.vec);
-        mv.load([&](int r) { return kept(r) ? vbase + (k0 + r) * s.ldv : nullptr; }, s.D, g.vec);
-        if (threadIdx.x < KT) mb = kept(threadIdx.x) ? 0.0f : -INFINITY;
-    };
+    KeyTiles<T, D16, KT, NT, kDirect> in;
+    in.init(s, g.vec, kbase, vbase, mask, hi);
 
     const float c2 = s.scale * kLog2e;
-    float up = kHalf ? 0x1p100f : 1.0f;
-    f32x16 acc[DB];
+    float up = kHalf ? 0x1p100f : 1.0f, lack = 0.0f, round = 0.0f;
+    f32x16 acc[DB], mean[DB];                // mean: sum P k
 #pragma unroll
-    for (int d = 0; d < DB; ++d) acc[d] = f32x16{};
-    if (lo < hi) load(lo);
+    for (int d = 0; d < DB; ++d) acc[d] = mean[d] = f32x16{};
+    if (lo < hi) in.first(tk[0], tv[0], lo);
+    int copy = 0;
     for (int64_t k0 = lo; k0 < hi; k0 += KT) {
-        __syncthreads();
-        mk.store(sk);
-        mv.store(sv);
-        if (threadIdx.x < KT) bias[threadIdx.x] = mb;
-        __syncthreads();
+        const char *sk = tk[copy], *sv = tv[copy];
+        const float* bias = biases[copy];
+        const int next = kCopies<T> == 1 ? 0 : copy ^ 1;
+        in.step(tk[copy], tv[copy], biases[copy], tk[next], tv[next], k0);
+        copy = next;
         const bool whole = !mask && k0 + KT <= hi;
-        if (k0 + KT < hi) load(k0 + KT);
-        f32x16 ds[KB];
+        f32x16 ds[KB], ps[KB];
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
             f32x16 p{}, dp{};
@@ -579,17 +788,25 @@ __global__ __launch_bounds__(256) void k_attn_dq(AttnK g) {
             if (!whole) {
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
-                    const f32x4v m = *(const f32x4v*)&bias[kb * 32 + 8 * b + 4 * h];
+                    const f32x4v m = in.left_out(bias, kb * 32 + 8 * b + 4 * h, k0);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) p[4 * b + i] += m[i];
                 }
             }
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                ds[kb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c2, off)) * (dp[i] - delta);
+            for (int i = 0; i < 16; ++i) {
+                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c2, off));
+                ds[kb][i] = x * (dp[i] - delta);
+                if constexpr (kFix) {
+                    lack += ds[kb][i];
+                    ps[kb][i] = kHalf ? x * kPUp : x;
+                } else {
+                    lack += x;
+                }
+            }
         }
         if constexpr (kHalf) {
-            keep_range(ds, up, acc);
+            keep_range(ds, up, acc, round);
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -600,50 +817,183 @@ __global__ __launch_bounds__(256) void k_attn_dq(AttnK g) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const Frag<T> f = pack<T>(ds[kb], e);
+                Frag<T> fp;
+                if constexpr (kFix) {
+                    fp = pack<T>(ps[kb], e);
+                    round = sum_of(f, round);
+                }
 #pragma unroll
-                for (int d = 0; d < DB; ++d) acc[d] = mma(Tl::turned(sk, kb * 32 + 16 * e, d, lane), f, acc[d]);
+                for (int d = 0; d < DB; ++d) {
+                    const Frag<T> t = Tl::turned(sk, kb * 32 + 16 * e, d, lane);
+                    acc[d] = mma(t, f, acc[d]);
+                    if constexpr (kFix) mean[d] = mma(t, fp, mean[d]);
+                }
             }
     }
+    lack = add_halves(lack);
+    round = add_halves(round) / up;
     if (!live) return;
-    const float f = s.scale / up;
+    const float share = kFix || g.splits > 1 ? 1.0f : share_of(lack);
+    const float f = s.scale * share / up, fm = s.scale * (kHalf ? 1.0f / kPUp : 1.0f);
     if (g.splits > 1) {
-        float* part = g.part + (((int64_t)split * s.N * s.Hk + pair) * s.rows + row) * s.D;
+        // parts: what dq and the sums P k are so far, and what delta lacks
+        const int64_t id = ((int64_t)split * s.N * s.Hk + pair) * s.rows + row;
+        float *part = g.part + id * s.D, *part2 = g.part2 + id * s.D;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
+            for (int b = 0; b < 4; ++b) {
                 store4(part, 32 * d + 8 * b + 4 * h, s.D, (s.D & 3) == 0, acc[d][4 * b] * f, acc[d][4 * b + 1] * f,
                        acc[d][4 * b + 2] * f, acc[d][4 * b + 3] * f);
+                if constexpr (kFix)
+                    store4(part2, 32 * d + 8 * b + 4 * h, s.D, (s.D & 3) == 0, mean[d][4 * b] * fm,
+                           mean[d][4 * b + 1] * fm, mean[d][4 * b + 2] * fm, mean[d][4 * b + 3] * fm);
+            }
+        if (h == 0) {
+            g.stat[id * 2] = lack;
+            g.stat[id * 2 + 1] = round;
+            if (split == 0) g.delta[stat] = delta;
+        }
         return;
     }
+    if (h == 0) {
+        g.delta[stat] = kFix ? delta + lack : delta;
+        if constexpr (!kFix) g.share[stat] = share;
+    }
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            acc[d][i] *= f;
+            if constexpr (kFix) acc[d][i] -= round * (mean[d][i] * fm);
+        }
     T* dq = (T*)g.b.dq + me.tok * s.ldq + (int64_t)me.head * s.D;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int b = 0; b < 4; ++b)
-            store4(dq, 32 * d + 8 * b + 4 * h, s.D, g.vec, acc[d][4 * b] * f, acc[d][4 * b + 1] * f, acc[d][4 * b + 2] * f,
-                   acc[d][4 * b + 3] * f);
+            store4(dq, 32 * d + 8 * b + 4 * h, s.D, g.vec, acc[d][4 * b], acc[d][4 * b + 1], acc[d][4 * b + 2],
+                   acc[d][4 * b + 3]);
 }
 
-// dk and dv of 128 keys: a wave owns 32 of them and walks the pair's rows.  Keys that
-// are left out are columns of their own, so what they hold goes nowhere.
-template <typename T, int D16>
-__global__ __launch_bounds__(256) void k_attn_dkv(AttnK g) {
-    using Tl = Tile<T, D16>;
-    constexpr int NT = 256, RT = 32, DB = (D16 + 1) / 2;
-    constexpr bool kHalf = std::is_same_v<T, _Float16>;
-    __shared__ alignas(16) char sq[RT * Tl::kRow];
-    __shared__ alignas(16) char so[RT * Tl::kRow];
-    __shared__ alignas(16) float offs[RT], deltas[RT];
+// dq of rows whose keys were taken in parts, and their delta.
+template <typename T>
+__global__ __launch_bounds__(256) void k_attn_dq_join(AttnK g) {
     const AttnShape& s = g.s;
-    const int64_t item = item_of(g.items);
-    if (item < 0) return;
+    const int64_t rows = (int64_t)s.N * s.Hk * s.rows, i = (int64_t)blockIdx.x * 256 + threadIdx.x, id = i / s.D;
+    if (id >= rows) return;
+    const int d = (int)(i - id * s.D);
+    float sum = 0.0f, mean = 0.0f, lack = 0.0f, round = 0.0f;
+    for (int k = 0; k < g.splits; ++k) {
+        const int64_t at = k * rows + id;
+        sum += g.part[at * s.D + d];
+        lack += g.stat[at * 2];
+        if constexpr (sizeof(T) == 2) {
+            mean += g.part2[at * s.D + d];
+            round += g.stat[at * 2 + 1];
+        }
+    }
+    const int64_t pair = id / s.rows, row = id - pair * s.rows;
+    const int n = (int)(pair / s.Hk);
+    const RowAt me = row_at(g, n, (int)(pair - (int64_t)n * s.Hk), row);
+    const int64_t stat = ((int64_t)n * s.Hq + me.head) * s.Lq + me.t;
+    T* dq = (T*)g.b.dq + me.tok * s.ldq + (int64_t)me.head * s.D;
+    if constexpr (sizeof(T) == 2) {
+        dq[d] = (T)(sum - round * mean);
+        if (d == 0) g.delta[stat] += lack;
+    } else {
+        dq[d] = sum * share_of(lack);
+        if (d == 0) g.share[stat] = share_of(lack);
+    }
+}
+
+// The rows' tiles, of q and dy, of a walk over a pair's rows up to hi.
+template <typename T, int D16, int RT, int NT, bool kDirect>
+struct RowTiles {
+    Moving<T, D16, RT, NT> mq, mo;
+    const AttnK* g;
+    int n, hk;
+    int64_t hi;
+    __device__ __forceinline__ void init(const AttnK& g_, int n_, int hk_, int64_t hi_) {
+        g = &g_; n = n_; hk = hk_; hi = hi_;
+    }
+    __device__ __forceinline__ void load(int64_t r0, char*, char*) {
+        const AttnShape& s = g->s;
+        mq.load([&](int r) {
+            const RowAt x = row_at(*g, n, hk, r0 + r);
+            return r0 + r < hi ? (const T*)g->b.q + x.tok * s.ldq + (int64_t)x.head * s.D : nullptr;
+        }, s.D, g->vec);
+        mo.load([&](int r) {
+            const RowAt x = row_at(*g, n, hk, r0 + r);
+            return r0 + r < hi ? (const T*)g->b.dy + (x.tok * s.Hq + x.head) * s.D : nullptr;
+        }, s.D, g->vec);
+    }
+    __device__ __forceinline__ void store(char* sq, char* so) const {
+        mq.store(sq);
+        mo.store(so);
+    }
+};
+// Straight to LDS.  rep divides a tile's rows: its tokens are whole, and offsets the same in
+// every tile.
+template <typename T, int D16, int RT, int NT>
+struct RowTiles<T, D16, RT, NT, true> {
+    using Tl = Tile<T, D16, RT>;
+    Direct<Tl, RT, NT> mq, mo;
+    const T *q, *dy;
+    FastDiv rep;
+    int64_t hi;
+    uint32_t ldq, ldo, row;
+    __device__ __forceinline__ void init(const AttnK& g, int n, int hk, int64_t hi_) {
+        const AttnShape& s = g.s;
+        const RowAt x = row_at(g, n, hk, 0);
+        hi = hi_;
+        rep = g.rep;
+        ldq = s.ldq;
+        ldo = s.Hq * s.D;
+        row = s.rep * s.D;
+        q = (const T*)g.b.q + x.tok * s.ldq + (int64_t)x.head * s.D;
+        dy = (const T*)g.b.dy + (x.tok * s.Hq + x.head) * s.D;
+        auto place = [&](Direct<Tl, RT, NT>& m, uint32_t ld) {
+            m.init(s.D / 8, [&](int r, int chunk) {
+                const uint32_t t = fdiv((uint32_t)r, g.rep);
+                return (t * ld + ((uint32_t)r - t * s.rep) * s.D) * 2 + chunk * 16;
+            });
+        };
+        place(mq, ldq);
+        place(mo, ldo);
+    }
+    __device__ __forceinline__ void load(int64_t r0, char* sq, char* so) {
+        const int64_t left = hi - r0, t = fdiv((uint32_t)r0, rep);
+        const uint32_t last = fdiv((uint32_t)(left < RT ? left : RT), rep) - 1;
+        mq.issue(sq, q + t * ldq, (last * ldq + row) * 2);
+        mo.issue(so, dy + t * ldo, (last * ldo + row) * 2);
+    }
+    __device__ __forceinline__ void store(char*, char*) const { arrived(); }
+};
+
+// dk and dv of 64 keys: a wave owns 32 of them and every other 32 of the pair's rows, and
+// the two waves of 32 keys join at the end (128 keys a workgroup, a wave to 32: half as many
+// workgroups, each twice as long, one wave a SIMD where lengths are ragged, 288 us in place
+// of 225 for 16 images of 3136 by 0 to 1024 tokens, 8 and 4 heads of 64, bf16).  Keys that are
+// left out are columns of their own, so what they hold goes nowhere.
+constexpr int kOwnKeys = 64;
+template <typename T, int D16, bool kDirect>
+__global__ __launch_bounds__(256, (waves_of<T, D16>(kDirect ? 6 : 4))) void k_attn_dkv(AttnK g) {
+    constexpr int NT = 256, RT = 64, DB = (D16 + 1) / 2, CP = kCopies<T>;
+    constexpr bool kHalf = std::is_same_v<T, _Float16>, kShare = sizeof(T) == 4;
+    using Tl = Tile<T, D16, RT>;
+    __shared__ alignas(16) char tq[CP][Tl::kBytes];
+    __shared__ alignas(16) char to[CP][Tl::kBytes];
+    __shared__ alignas(16) float toff[CP][RT], tdel[CP][RT], tshare[CP][kShare ? RT : 4];
+    const AttnShape& s = g.s;
+    const Work wk = work_of(g);
+    if (wk.none) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-    const int split = (int)(item % g.splits);
-    const int64_t tile = item / g.splits % g.tiles, pair = item / g.splits / g.tiles;
-    const int n = (int)(pair / s.Hk), hk = (int)(pair % s.Hk);
+    const int split = wk.split, n = wk.n, hk = wk.hk;
+    const int64_t tile = wk.tile, pair = wk.pair;
     const int len = keys_of(g.b.klen, n, s.Lk);
-    const int64_t key = tile * 128 + wave * 32 + (lane & 31);
+    const int64_t key = tile * kOwnKeys + (wave & 1) * 32 + (lane & 31);
+    const int mine = (wave >> 1) * 32;       // of a tile's rows
     const bool kept = key < len && (!g.b.mask || g.b.mask[(int64_t)n * s.Lk + key]);
     const int64_t tok = (int64_t)n * s.Lk + key;
     const T* k = kept ? (const T*)g.b.k + tok * s.ldk + (int64_t)hk * s.D : nullptr;
@@ -655,62 +1005,65 @@ __global__ __launch_bounds__(256) void k_attn_dkv(AttnK g) {
         fv[c] = load_frag(v, c, h, s.D, g.vec);
     }
     int64_t lo, hi;
-    part_of(tile * 128 < len ? s.rows : 0, RT, split, g.splits, lo, hi);
-    Moving<T, D16, RT, NT> mq, mo;
-    float moff = 0.0f, mdel = 0.0f;
-    auto load = [&](int64_t r0) {
-        mq.load([&](int r) {
-            const RowAt x = row_at(g, n, hk, r0 + r);
-            return r0 + r < hi ? (const T*)g.b.q + x.tok * s.ldq + (int64_t)x.head * s.D : nullptr;
-        }, s.D, g.vec);
-        mo.load([&](int r) {
-            const RowAt x = row_at(g, n, hk, r0 + r);
-            return r0 + r < hi ? (const T*)g.b.dy + (x.tok * s.Hq + x.head) * s.D : nullptr;
-        }, s.D, g.vec);
+    part_of(tile * kOwnKeys < len ? s.rows : 0, RT, split, g.splits, lo, hi);
+    RowTiles<T, D16, RT, NT, kDirect> in;
+    in.init(g, n, hk, hi);
+    float moff = 0.0f, mdel = 0.0f, mshare = 0.0f;
+    auto load = [&](int64_t r0, char* sq, char* so) {
+        in.load(r0, sq, so);
         if (threadIdx.x < RT) {
-            const bool in = r0 + threadIdx.x < hi;
+            const bool inside = r0 + threadIdx.x < hi;
             const RowAt x = row_at(g, n, hk, r0 + threadIdx.x);
-            const int64_t at = in ? ((int64_t)n * s.Hq + x.head) * s.Lq + x.t : 0;
-            const float l = in ? g.b.lse[at] : -INFINITY;
+            const int64_t at = inside ? ((int64_t)n * s.Hq + x.head) * s.Lq + x.t : 0;
+            const float l = inside ? g.b.lse[at] : -INFINITY;
             moff = l == -INFINITY ? -INFINITY : -l * kLog2e;
-            mdel = in ? g.delta[at] : 0.0f;
+            mdel = inside ? g.delta[at] : 0.0f;
+            if constexpr (kShare) mshare = inside ? g.share[at] : 0.0f;
         }
     };
 
     const float c2 = s.scale * kLog2e;
-    float up = kHalf ? 0x1p100f : 1.0f;
+    float up = kHalf ? 0x1p100f : 1.0f, none = 0.0f;
     f32x16 ak[DB], av[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d) ak[d] = av[d] = f32x16{};
-    if (lo < hi) load(lo);
+    if (lo < hi) load(lo, tq[0], to[0]);
+    int copy = 0;
     for (int64_t r0 = lo; r0 < hi; r0 += RT) {
-        __syncthreads();
-        mq.store(sq);
-        mo.store(so);
+        char *sq = tq[copy], *so = to[copy];
+        float *offs = toff[copy], *deltas = tdel[copy], *shares = tshare[copy];
+        if (CP == 1) __syncthreads();
+        else copy ^= 1;
+        in.store(sq, so);
         if (threadIdx.x < RT) {
             offs[threadIdx.x] = moff;
             deltas[threadIdx.x] = mdel;
+            if constexpr (kShare) shares[threadIdx.x] = mshare;
         }
         __syncthreads();
-        if (r0 + RT < hi) load(r0 + RT);
+        if (r0 + RT < hi) load(r0 + RT, tq[copy], to[copy]);
         f32x16 p{}, ds[1] = {f32x16{}};
 #pragma unroll
         for (int c = 0; c < D16; ++c) {
-            p = mma(Tl::read(sq, lane & 31, c, h), fk[c], p);
-            ds[0] = mma(Tl::read(so, lane & 31, c, h), fv[c], ds[0]);
+            p = mma(Tl::read(sq, mine + (lane & 31), c, h), fk[c], p);
+            ds[0] = mma(Tl::read(so, mine + (lane & 31), c, h), fv[c], ds[0]);
         }
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-            const f32x4v o4 = *(const f32x4v*)&offs[8 * b + 4 * h], d4 = *(const f32x4v*)&deltas[8 * b + 4 * h];
+            const int at = mine + 8 * b + 4 * h;
+            const f32x4v o4 = *(const f32x4v*)&offs[at], d4 = *(const f32x4v*)&deltas[at];
+            f32x4v s4{};
+            if constexpr (kShare) s4 = *(const f32x4v*)&shares[at];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(p[4 * b + i], c2, o4[i]));
+                float x = __builtin_amdgcn_exp2f(__builtin_fmaf(p[4 * b + i], c2, o4[i]));
+                if constexpr (kShare) x *= s4[i];
                 ds[0][4 * b + i] = x * (ds[0][4 * b + i] - d4[i]);
                 p[4 * b + i] = kHalf ? x * kPUp : x;
             }
         }
         if constexpr (kHalf) {
-            keep_range(ds, up, ak);
+            keep_range(ds, up, ak, none);
 #pragma unroll
             for (int i = 0; i < 16; ++i) ds[0][i] *= up;
         }
@@ -719,13 +1072,42 @@ __global__ __launch_bounds__(256) void k_attn_dkv(AttnK g) {
             const Frag<T> fp = pack<T>(p, e), fd = pack<T>(ds[0], e);
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
-                av[d] = mma(Tl::turned(so, 16 * e, d, lane), fp, av[d]);
-                ak[d] = mma(Tl::turned(sq, 16 * e, d, lane), fd, ak[d]);
+                av[d] = mma(Tl::turned(so, mine + 16 * e, d, lane), fp, av[d]);
+                ak[d] = mma(Tl::turned(sq, mine + 16 * e, d, lane), fd, ak[d]);
             }
         }
     }
-    if (key >= s.Lk) return;
     const float f = s.scale / up, fvv = kHalf ? 1.0f / kPUp : 1.0f;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            ak[d][i] *= f;
+            av[d][i] *= fvv;
+        }
+    // the second half of the rows, by way of LDS, 32 channels at a time
+    static_assert(sizeof(tq) >= 2 * 16 * 64 * sizeof(float));
+    float *xk = (float*)tq[0] + (wave & 1) * 1024, *xv = (float*)to[0] + (wave & 1) * 1024;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) {
+        __syncthreads();
+        if (mine) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                xk[i * 64 + lane] = ak[d][i];
+                xv[i * 64 + lane] = av[d][i];
+            }
+        }
+        __syncthreads();
+        if (!mine) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                ak[d][i] += xk[i * 64 + lane];
+                av[d][i] += xv[i * 64 + lane];
+            }
+        }
+    }
+    if (mine || key >= s.Lk) return;
     auto put = [&](auto* dk, auto* dv, bool vec) {
 #pragma unroll
         for (int d = 0; d < DB; ++d)
@@ -734,8 +1116,8 @@ __global__ __launch_bounds__(256) void k_attn_dkv(AttnK g) {
                 float x[8];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    x[i] = kept ? ak[d][4 * b + i] * f : 0.0f;
-                    x[4 + i] = kept ? av[d][4 * b + i] * fvv : 0.0f;
+                    x[i] = kept ? ak[d][4 * b + i] : 0.0f;
+                    x[4 + i] = kept ? av[d][4 * b + i] : 0.0f;
                 }
                 store4(dk, 32 * d + 8 * b + 4 * h, s.D, vec, x[0], x[1], x[2], x[3]);
                 store4(dv, 32 * d + 8 * b + 4 * h, s.D, vec, x[4], x[5], x[6], x[7]);
@@ -749,65 +1131,86 @@ __global__ __launch_bounds__(256) void k_attn_dkv(AttnK g) {
     }
 }
 
-// Sum of `splits` partial gradients [pairs][rows][D], to tokens ld elements apart.
-struct AttnSum {
-    const float *a, *b;                      // b: a second tensor, or null
-    void *x, *y;
-    int64_t pairs, rows;
-    int Hk, rep, L, D, ldx, ldy, splits;
-};
+// dk (blockIdx.y 0) or dv of keys whose rows were taken in parts.
 template <typename T>
-__global__ __launch_bounds__(256) void k_attn_sum(AttnSum g) {
-    const int64_t all = g.pairs * g.rows * g.D, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+__global__ __launch_bounds__(256) void k_attn_sum(AttnK g) {
+    const AttnShape& s = g.s;
+    const int64_t all = (int64_t)s.N * s.Hk * s.Lk * s.D, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= all) return;
-    const float* p = blockIdx.y ? g.b : g.a;
+    const float* p = blockIdx.y ? g.part2 : g.part;
     float sum = 0.0f;
     for (int k = 0; k < g.splits; ++k) sum += p[k * all + i];
-    const int d = (int)(i % g.D);
-    const int64_t id = i / g.D, pair = id / g.rows, row = id % g.rows;
-    const int64_t tok = pair / g.Hk * g.L + row / g.rep;
-    const int head = (int)(pair % g.Hk) * g.rep + (int)(row % g.rep);
-    ((T*)(blockIdx.y ? g.y : g.x))[tok * (blockIdx.y ? g.ldy : g.ldx) + (int64_t)head * g.D + d] = (T)sum;
+    const int64_t id = i / s.D, pair = id / s.Lk, n = pair / s.Hk;
+    const int64_t tok = n * s.Lk + (id - pair * s.Lk);
+    T* x = (T*)(blockIdx.y ? g.b.dv : g.b.dk) + tok * (blockIdx.y ? s.ldv : s.ldk);
+    x[(pair - n * s.Hk) * s.D + (i - id * s.D)] = (T)sum;
 }
 
 // ---------------------------------------------------------------- launches
 
-inline unsigned grid_of(int64_t items) { return (unsigned)((items + 7) / 8 * 8); }
+// Sets a launch's cut; the number of its workgroups (below 2^31: attn_plan).
+inline unsigned cut(AttnK& a, const AttnCut& c) {
+    const int64_t pairs = (int64_t)a.s.N * a.s.Hk;
+    a.tiles = c.tiles;
+    a.splits = c.splits;
+    a.per_pair = make_fastdiv((uint32_t)(c.tiles * c.splits));
+    a.per_tile = make_fastdiv((uint32_t)c.splits);
+    a.by_xcd = pairs % 8 == 0 || pairs >= 64;
+    return (unsigned)((a.by_xcd ? (pairs + 7) / 8 * 8 : pairs) * c.tiles * c.splits);
+}
 
-template <typename T, int D16>
-hipError_t attn_run(const AttnK& g, const AttnPlan& p, bool backward, hipStream_t st) {
+template <typename T, int D16, bool kDirect>
+hipError_t attn_run_by(const AttnK& g, const AttnPlan& p, bool backward, hipStream_t st) {
     AttnK a = g;
     const AttnShape& s = g.s;
     const int64_t pairs = (int64_t)s.N * s.Hk;
-    a.tiles = p.rows.tiles;
-    a.splits = p.rows.splits;
-    a.items = pairs * a.tiles * a.splits;
+    unsigned blocks = cut(a, p.rows);
     if (!backward) {
         if (p.few)
-            k_attn<T, D16, true><<<grid_of(a.items), FwdCut<T, D16, true>::kThreads, 0, st>>>(a);
+            k_attn<T, D16, true, kDirect><<<blocks, FwdCut<T, D16, true>::kThreads, 0, st>>>(a);
         else
-            k_attn<T, D16, false><<<grid_of(a.items), FwdCut<T, D16, false>::kThreads, 0, st>>>(a);
+            k_attn<T, D16, false, kDirect><<<blocks, FwdCut<T, D16, false>::kThreads, 0, st>>>(a);
         if (a.splits > 1) {
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
             const int per = 256 / s.D;
             k_attn_join<T><<<(unsigned)((pairs * s.rows + per - 1) / per), 256, 0, st>>>(a);
         }
         return hipGetLastError();
     }
-    k_attn_dq<T, D16><<<grid_of(a.items), 256, 0, st>>>(a);
+    a.part2 = a.part + (size_t)a.splits * pairs * s.rows * s.D;
+    k_attn_dq<T, D16, kDirect><<<blocks, 256, 0, st>>>(a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
     if (a.splits > 1) {
-        const AttnSum m{a.part, nullptr, a.b.dq, nullptr, pairs, s.rows, s.Hk, s.rep, s.Lq, s.D, s.ldq, 0, a.splits};
-        k_attn_sum<T><<<(unsigned)((pairs * s.rows * s.D + 255) / 256), 256, 0, st>>>(m);
+        k_attn_dq_join<T><<<(unsigned)((pairs * s.rows * s.D + 255) / 256), 256, 0, st>>>(a);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    a.tiles = p.keys.tiles;
-    a.splits = p.keys.splits;
-    a.items = pairs * a.tiles * a.splits;
+    blocks = cut(a, p.keys);
     a.part2 = a.part + (size_t)a.splits * pairs * s.Lk * s.D;
-    k_attn_dkv<T, D16><<<grid_of(a.items), 256, 0, st>>>(a);
-    if (a.splits > 1) {
-        const AttnSum m{a.part, a.part2, a.b.dk, a.b.dv, pairs, s.Lk, s.Hk, 1, s.Lk, s.D, s.ldk, s.ldv, a.splits};
-        k_attn_sum<T><<<dim3((unsigned)((pairs * s.Lk * s.D + 255) / 256), 2), 256, 0, st>>>(m);
+    bool direct = false;
+    if constexpr (kDirect) {
+        direct = 64 % s.rep == 0;
+        if (direct) k_attn_dkv<T, D16, true><<<blocks, 256, 0, st>>>(a);
     }
+    if (!direct) k_attn_dkv<T, D16, false><<<blocks, 256, 0, st>>>(a);
+    e = hipGetLastError();
+    if (e != hipSuccess || a.splits == 1) return e;
+    k_attn_sum<T><<<dim3((unsigned)((pairs * s.Lk * s.D + 255) / 256), 2), 256, 0, st>>>(a);
     return hipGetLastError();
+}
+
+// Tiles go straight to LDS where words and offsets allow: 16-byte words, and the rows of a
+// tile, 128 of them at most, within 2^31 bytes.
+template <typename T, int D16>
+hipError_t attn_run(const AttnK& g, const AttnPlan& p, bool backward, hipStream_t st) {
+    constexpr int kMost = 1 << 22;
+    if constexpr (sizeof(T) == 2) {
+        const AttnShape& s = g.s;
+        if (g.vec && !g.a.mask && !g.b.mask && s.ldq <= kMost && s.ldk <= kMost && s.ldv <= kMost && s.Hq * s.D <= kMost)
+            return attn_run_by<T, D16, true>(g, p, backward, st);
+    }
+    return attn_run_by<T, D16, false>(g, p, backward, st);
 }
 
 template <typename T>

@@ -36,11 +36,11 @@ struct GatedK {
 // is [sum][index], else [index][sum].
 template <typename T, bool T_>
 struct Side {
-    static constexpr int kBk = 128 / (int)sizeof(T);
+    static constexpr int kBk = sizeof(T) == 4 ? 32 : 64;
     static constexpr int kRows = T_ ? kBk : kTile;
     static constexpr int kD16 = T_ ? kTile / 16 : kBk / 16;
-    using Tl = Tile<T, kD16>;
-    static constexpr int kBytes = kRows * Tl::kRow;
+    using Tl = Tile<T, kD16, kRows>;
+    static constexpr int kBytes = Tl::kBytes;
     // terms 16 c .. of indices 32 blk ..
     __device__ static __forceinline__ Frag<T> read(const char* t, int blk, int c, int lane) {
         if constexpr (T_) return Tl::turned8(t, 16 * c, blk, lane);
@@ -90,6 +90,14 @@ __device__ __forceinline__ void product(f32x16 (&acc)[2][2], char* sa, char* sb,
         }
     }
 }
+
+// Workgroups that share a tile's tokens follow each other on one XCD, whose L2 then holds
+// them: workgroup ids go round the eight XCDs.  Item of `all`, or -1.
+__device__ __forceinline__ int64_t item_of(int64_t all) {
+    const int64_t each = (all + 7) / 8, i = (int64_t)(blockIdx.x & 7) * each + (blockIdx.x >> 3);
+    return (blockIdx.x >> 3) < each && i < all ? i : -1;
+}
+inline unsigned grid_of(int64_t items) { return (unsigned)((items + 7) / 8 * 8); }
 
 __device__ __forceinline__ float sigmoid(float z) {
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-z * kLog2e));

@@ -7,6 +7,12 @@ from oracle import block as O
 from paper_1903_01521_amd import binding as B
 from train_helpers import ACT, DEV, DTYPE, HALF_ULP, IO, U32, dev, host, space
 
+# Roundings that a sum of n products counts for, of the absolute products: one each, some
+# more, and for fp32 the terms of the operands' split that are dropped, 2^-20.
+def sums(n, dtype):
+    return (n + 16 + (16 if dtype == "f32" else 0)) * U32
+
+
 TINY = {"f32": 2.0 ** -126, "f16": 2.0 ** -25, "bf16": 2.0 ** -126}     # half a step at the range's lower end
 
 
@@ -88,9 +94,9 @@ def attend(q, k, v, scale, dtype="f32", klen=None, mask=None, lse=True, ld=(None
     return y, st
 
 
-def score_error(q, k, scale, D):
+def score_error(q, k, scale, D, dtype):
     """Bound of |S| errors [N][Hq][Lq][Lk] for heads [..][L][D]: a sum of D products, scaled."""
-    return (D + 4) * U32 * scale * (np.abs(q) @ np.abs(k).transpose(0, 1, 3, 2))
+    return sums(D, dtype) * scale * (np.abs(q) @ np.abs(k).transpose(0, 1, 3, 2))
 
 
 def attend_tol(q, k, v, scale, kept, p, y, lse, dtype):
@@ -102,12 +108,12 @@ def attend_tol(q, k, v, scale, kept, p, y, lse, dtype):
     kk = np.repeat(O._drop(k, kept).transpose(0, 2, 1, 3), rep, 1)
     vv = np.repeat(O._drop(v, kept).transpose(0, 2, 1, 3), rep, 1)
     qq = q.transpose(0, 2, 1, 3)
-    es = score_error(qq, kk, scale, D)
+    es = score_error(qq, kk, scale, D, dtype)
     s = scale * np.abs(qq @ kk.transpose(0, 1, 3, 2)) * kept[:, None, None]
     big = s.max(-1, keepdims=True)
     arg = es + 6 * U32 * (s + big) + 8 * U32                 # of a term's exponent
     worst = np.where(kept[:, None, None], arg, 0).max(-1, keepdims=True)
-    rel = arg + worst + HALF_ULP[dtype] + (Lk + 32) * U32
+    rel = arg + worst + HALF_ULP[dtype] + sums(Lk + 16, dtype)
     ty = (p * rel) @ np.abs(vv) + 2 * TINY["f16"] * (dtype == "f16") * np.abs(vv).sum(2, keepdims=True)
     tl = worst[..., 0] + (Lk + 32) * U32 + 4 * U32 * np.abs(np.where(np.isinf(lse), 0, lse))
     return stored(y, ty.transpose(0, 2, 1, 3), dtype), tl
@@ -130,26 +136,31 @@ def attend_back(dy, q, k, v, y, lse, scale, dtype="f32", klen=None, mask=None, l
 
 def attend_back_tol(m, scale, kept, D, dtype, dq, dk, dv, lse):
     """Bounds of dq, dk, dv from attention_backward's intermediates: errors of S, dP and
-    delta, dS's and P's rounding, and the sums."""
+    delta, dS's and P's rounding, and the sums.  dS is rounded while delta still has the
+    rounding of y, h sum |dy y|, which is then taken off with P's: h of that again, twice.
+    dS's roundings r_j enter dq as sum r_j k_j - (sum r_j) sum P k, so |r_j| <= h |dS_j| counts
+    with |k_j| + sum P |k|."""
     a = {n: np.abs(m[n]) for n in ("q", "k", "v", "dy", "y")}
     finite = np.where(np.isinf(lse), 0, np.abs(lse))[..., None]
-    ep = score_error(a["q"], a["k"], scale, D) + 6 * U32 * (np.abs(m["s"]) + finite) + 8 * U32
-    edp = (D + 4) * U32 * (a["dy"] @ a["v"].transpose(0, 1, 3, 2))
-    edelta = (D + 4) * U32 * (a["dy"] * a["y"]).sum(-1, keepdims=True)
-    h = HALF_ULP[dtype]
+    ep = score_error(a["q"], a["k"], scale, D, dtype) + 6 * U32 * (np.abs(m["s"]) + finite) + 8 * U32
+    edp = sums(D, dtype) * (a["dy"] @ a["v"].transpose(0, 1, 3, 2))
+    Lq, Lk = m["p"].shape[-2:]
+    h, dyy = HALF_ULP[dtype], (a["dy"] * a["y"]).sum(-1, keepdims=True)
+    edelta = (D + 4) * U32 * dyy + (Lk + 16) * U32 * (m["p"] * (np.abs(m["dp"]) + np.abs(m["delta"]))).sum(
+        -1, keepdims=True) + 3 * h * h * dyy + (m["p"] * (ep + edp)).sum(-1, keepdims=True) * h
     eds = m["p"] * (ep * (1 + ep) * np.abs(m["dp"] - m["delta"]) + edp + edelta) + (h + 8 * U32) * np.abs(m["ds"])
     epv = m["p"] * (ep * (1 + ep) + h + 4 * U32)
     if dtype == "f16":          # what falls below fp16's range, P held 2^12 up, dS near 2^14 of its column's largest
         epv = epv + 2.0 ** -36
         most = np.maximum(np.abs(m["ds"]).max(-1, keepdims=True), np.abs(m["ds"]).max(-2, keepdims=True))
         eds = eds + 2.0 ** -36 * most
-    Lq, Lk = m["p"].shape[-2:]
     ads = np.abs(m["ds"])
-    tq = scale * (eds @ a["k"] + (Lk + 16) * U32 * (ads @ a["k"]))
-    rows = Lq * (m["q"].shape[1] // dk.shape[2]) + 16
+    mean = m["p"] @ a["k"]
+    tq = scale * (eds @ a["k"] + (h * ads).sum(-1, keepdims=True) * mean + sums(Lk, dtype) * (ads @ a["k"]))
+    rows = sums(Lq * (m["q"].shape[1] // dk.shape[2]), dtype)
     t = lambda x: x.transpose(0, 1, 3, 2)  # noqa: E731
-    tk = m["shared"](scale * (t(eds) @ a["q"] + rows * U32 * (t(ads) @ a["q"])))
-    tv = m["shared"](t(epv) @ a["dy"] + rows * U32 * (t(m["p"]) @ a["dy"]))
+    tk = m["shared"](scale * (t(eds) @ a["q"] + rows * (t(ads) @ a["q"])))
+    tv = m["shared"](t(epv) @ a["dy"] + rows * (t(m["p"]) @ a["dy"]))
     return (stored(dq, tq.transpose(0, 2, 1, 3), dtype), stored(dk, tk, dtype), stored(dv, tv, dtype))
 
 
@@ -180,11 +191,10 @@ def gated_back(dy, x, w, bias, dtype="f32", act="none", offset=0, want=(True, Tr
     return outs
 
 
-def layers_tol(x, w, bias):
+def layers_tol(x, w, bias, dtype):
     """Bound of zg's and zu's errors [2][M][K]: sums of C products and the bias."""
-    C = x.shape[-1]
     a = np.stack([np.abs(x) @ np.abs(w[i]).T for i in (0, 1)])
-    return (C + 4) * U32 * (a if bias is None else a + np.abs(bias)[:, None])
+    return sums(x.shape[-1], dtype) * (a if bias is None else a + np.abs(bias)[:, None])
 
 
 # Sigmoid: its exponent is off by a few roundings of |z|, exp2, sum and reciprocal by some more.
@@ -193,7 +203,7 @@ def _sig_error(z):
 
 
 def gated_tol(x, w, bias, act, y, zg, zu, dtype):
-    ez = layers_tol(x, w, bias)
+    ez = layers_tol(x, w, bias, dtype)
     v, _ = O.act_slope(zg, act)
     top = 1.1 if act == "silu" else 1.0                          # of |act'|
     es = _sig_error(zg) if act == "silu" else 0.0
@@ -205,7 +215,7 @@ def gated_back_tol(dy, x, w, bias, act, dz, got_like, dtype):
     """Bounds of dx, dw, dbias.  act'' of SiLU is below 0.5; where zg is within its error
     of zero ReLU's slope may be either."""
     _, zg, zu = O.gated(x, w, bias, act)
-    ez = layers_tol(x, w, bias)
+    ez = layers_tol(x, w, bias, dtype)
     v, d = O.act_slope(zg, act)
     top, curve = (1.1, 0.5) if act == "silu" else (1.0, 0.0)
     es = _sig_error(zg) if act == "silu" else 0.0
@@ -218,8 +228,8 @@ def gated_back_tol(dy, x, w, bias, act, dz, got_like, dtype):
     M, C, K = x.shape[0], x.shape[1], w.shape[1]
     a = np.abs(dz) + kept
     aw, ax = np.abs(w), np.abs(x)
-    tx = sum(kept[i] @ aw[i] + (2 * K + 16) * U32 * (a[i] @ aw[i]) for i in (0, 1))
-    tw = np.stack([kept[i].T @ ax + (M + 16) * U32 * (a[i].T @ ax) for i in (0, 1)])
+    tx = sum(kept[i] @ aw[i] + sums(2 * K, dtype) * (a[i] @ aw[i]) for i in (0, 1))
+    tw = np.stack([kept[i].T @ ax + sums(M, dtype) * (a[i].T @ ax) for i in (0, 1)])
     tb = e.sum(1) + (M + 16) * U32 * np.abs(dz).sum(1)
     dx, dw, _ = got_like
     return stored(dx, tx, dtype), stored(dw, tw, dtype), tb
