@@ -320,6 +320,16 @@ struct Direct {
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
                 r, (__attribute__((address_space(3))) void*)(t + (i * NT + wave * 64) * 16), 16, off[i], 0, 0, 0);
     }
+    // the same, of each row `used` chunks
+    __device__ __forceinline__ void issue_part(char* t, const void* p, uint32_t bytes, int used) const {
+        Direct d;
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            const int at = threadIdx.x + i * NT, row = at / kRowChunks;
+            d.off[i] = ((at % kRowChunks) ^ Tl::twist(row)) < used ? off[i] : 0x80000000u;
+        }
+        d.issue(t, p, bytes);
+    }
 };
 // Every load to LDS of this wave has arrived.
 __device__ __forceinline__ void arrived() { __builtin_amdgcn_s_waitcnt(0x0F70); }

@@ -24,11 +24,10 @@ struct GatedArgs {
 };
 struct GatedPlan {
     bool fits;
-    bool few;                                // forward: a wave for each unit, no tiles
+    int first, dx, dw;                       // tile shapes of the products
     int splits;                              // of the sum over tokens in dw
     size_t dz, dbias, part, need;            // workspace: bytes of each region
 };
-// want_*: what a backward call asks for (all, for the size that is reported)
 GatedPlan gated_plan(const GatedShape& s, bool backward);
 hipError_t launch_gated(const GatedArgs& a, const GatedShape& s, const GatedPlan& p, hipStream_t st);
 hipError_t launch_gated_backward(const GatedArgs& a, const GatedShape& s, const GatedPlan& p, void* ws, hipStream_t st);

@@ -18,8 +18,6 @@ namespace wino {
 
 namespace {
 
-constexpr int kTile = 128, kUnits = 64;
-
 struct GatedK {
     GatedArgs a;
     int64_t M;
@@ -32,63 +30,216 @@ struct GatedK {
     int splits;
 };
 
-// One operand of a product: a tile of 128 indices by BK terms of the sum.  T_: its memory
-// is [sum][index], else [index][sum].
-template <typename T, bool T_>
+// How a workgroup's four waves share a tile: WA by WB of them, each AB by BB blocks of 32
+// by 32 results.  A block's step reads AB + BB operands from LDS for AB * BB products, so
+// wide tiles need the least of LDS, whose 128 bytes a cycle the 64x64 ones of a wave just
+// fill; narrow ones fill the card where results are few.
+template <int AB_, int BB_, int WA_, int WB_>
+struct Shape {
+    static constexpr int AB = AB_, BB = BB_, WA = WA_, WB = WB_;
+    static constexpr int kA = 32 * AB * WA, kB = 32 * BB * WB;      // indices of a tile
+};
+using Wide = Shape<4, 2, 1, 4>;              // 128 x 256
+using Square = Shape<2, 2, 2, 2>;            // 128 x 128
+using Narrow = Shape<2, 1, 1, 4>;            // 64 x 128
+
+constexpr int kBk = 32;                      // terms of a step
+
+// A matrix in memory, [index][sum], or [sum][index] (T_): `rows` rows of `cols` values, ld
+// apart.  Rows from `split` on lie `jump` further.
+template <typename T>
+struct Source {
+    const T* p;
+    int64_t rows;
+    int cols, ld, split, jump;
+};
+
+// One operand's tile of I indices by kBk terms.
+template <typename T, int I, bool T_, bool kDirect>
 struct Side {
-    static constexpr int kBk = sizeof(T) == 4 ? 32 : 64;
-    static constexpr int kRows = T_ ? kBk : kTile;
-    static constexpr int kD16 = T_ ? kTile / 16 : kBk / 16;
-    using Tl = Tile<T, kD16, kRows>;
-    static constexpr int kBytes = Tl::kBytes;
+    static constexpr int kRows = T_ ? kBk : I;
+    // rows of more than 128 values in halves of 128, each a tile
+    static constexpr int kCols = T_ ? (I < 128 ? I : 128) : kBk, kParts = T_ ? I / kCols : 1;
+    using Tl = Tile<T, kCols / 16, kRows>;
+    static constexpr int kBytes = Tl::kBytes * kParts;
+    Source<T> s;
+    bool vec;
+    Moving<T, kCols / 16, kRows, 256> m[kParts];
+
+    __device__ __forceinline__ void init(const Source<T>& s_, bool vec_) {
+        s = s_;
+        vec = vec_;
+    }
+    __device__ __forceinline__ void load(char*, int64_t k, int64_t hi) {
+#pragma unroll
+        for (int i = 0; i < kParts; ++i)
+            m[i].load([&](int r) {
+                if constexpr (T_) {
+                    return k + r < hi ? s.p + (k + r) * s.ld + i * kCols : nullptr;
+                } else {
+                    const int64_t row = r + (r >= s.split ? s.jump : 0);
+                    return row < s.rows ? s.p + row * s.ld + k : nullptr;
+                }
+            }, T_ ? s.cols - i * kCols : (int)(hi - k), vec);
+    }
+    __device__ __forceinline__ void store(char* t) const {
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) m[i].store(t + i * Tl::kBytes);
+    }
     // terms 16 c .. of indices 32 blk ..
     __device__ static __forceinline__ Frag<T> read(const char* t, int blk, int c, int lane) {
-        if constexpr (T_) return Tl::turned8(t, 16 * c, blk, lane);
+        if constexpr (T_) return Tl::turned8(t + blk / (kCols / 32) * Tl::kBytes, 16 * c, blk % (kCols / 32), lane);
         else return Tl::read(t, 32 * blk + (lane & 31), c, lane >> 5);
     }
 };
-
-// acc[i][j] = products of left block a0 + i * da and right block b0 + j, over the terms
-// lo .. hi.  left(r, k), right(r, k): the memory row r of a tile at term k, or null; the
-// values that a row holds from there on are limit_left(k), limit_right(k).
-template <typename T, bool AT, bool BT, typename L, typename R, typename LL, typename LR>
-__device__ __forceinline__ void product(f32x16 (&acc)[2][2], char* sa, char* sb, int64_t lo, int64_t hi, int a0, int da,
-                                        int b0, bool vec, L left, R right, LL limit_left, LR limit_right) {
-    using A = Side<T, AT>;
-    using B = Side<T, BT>;
-    constexpr int BK = A::kBk;
-    const int lane = threadIdx.x & 63;
-    Moving<T, A::kD16, A::kRows, 256> ma;
-    Moving<T, B::kD16, B::kRows, 256> mb;
-    auto load = [&](int64_t k) {
-        ma.load([&](int r) { return left(r, k); }, limit_left(k), vec);
-        mb.load([&](int r) { return right(r, k); }, limit_right(k), vec);
-    };
+// Straight to LDS: 16-bit values in whole 16-byte words, a tile within 2^31 bytes.
+template <typename T, int I, bool T_>
+struct Side<T, I, T_, true> : Side<T, I, T_, false> {
+    using Base = Side<T, I, T_, false>;
+    using Tl = typename Base::Tl;
+    using Dir = Direct<Tl, Base::kRows, 256>;
+    Dir d[Base::kParts];
+    __device__ __forceinline__ void init(const Source<T>& s, bool) {
+        this->s = s;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < Base::kParts; ++i)
+            d[i].init(T_ ? (s.cols - i * Base::kCols + 7) / 8 : 1 << 20, [&](int r, int chunk) {
+                const uint32_t row = (uint32_t)r + (!T_ && r >= s.split ? (uint32_t)s.jump : 0u);
+                return row * (uint32_t)s.ld * 2 + chunk * 16 + i * Base::kCols * 2;
+            });
+    }
+    __device__ __forceinline__ void load(char* t, int64_t k, int64_t hi) {
+        const Source<T>& s = this->s;
+        if constexpr (T_) {
+            const int64_t left = hi - k;
+            const uint32_t last = (uint32_t)(left < kBk ? left : kBk) - 1;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) acc[i][j] = f32x16{};
-    if (lo < hi) load(lo);
-    for (int64_t k = lo; k < hi; k += BK) {
-        __syncthreads();
-        ma.store(sa);
-        mb.store(sb);
-        __syncthreads();
-        if (k + BK < hi) load(k + BK);
-#pragma unroll
-        for (int c = 0; c < BK / 16; ++c) {
-            Frag<T> a[2], b[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                a[i] = A::read(sa, a0 + i * da, c, lane);
-                b[i] = B::read(sb, b0 + i, c, lane);
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) acc[i][j] = mma(a[i], b[j], acc[i][j]);
+            for (int i = 0; i < Base::kParts; ++i)
+                d[i].issue(t + i * Tl::kBytes, s.p + k * s.ld, (last * (uint32_t)s.ld + (uint32_t)s.cols) * 2);
+        } else {
+            const int64_t bytes = ((s.rows - 1) * s.ld + (s.cols - k)) * 2;
+            const uint32_t n = bytes < 0x7fffffff ? (uint32_t)bytes : 0x7fffffffu;
+            if (hi - k >= kBk) d[0].issue(t, s.p + k, n);
+            else d[0].issue_part(t, s.p + k, n, (int)(hi - k + 7) / 8);
         }
     }
+    __device__ __forceinline__ void store(char*) const {}
+};
+
+// acc[i][j] = products of the wave's left block i and right block j, over the terms lo .. hi.
+// Left block i of wave column wa: i * WA + wa.
+template <typename S, typename A, typename B>
+__device__ __forceinline__ void product(f32x16 (&acc)[S::AB][S::BB], A& a, B& b, char* lds, int64_t lo, int64_t hi,
+                                        bool direct) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wa = wave % S::WA, wb = wave / S::WA;
+    constexpr int kBoth = A::kBytes + B::kBytes;
+#pragma unroll
+    for (int i = 0; i < S::AB; ++i)
+#pragma unroll
+        for (int j = 0; j < S::BB; ++j) acc[i][j] = f32x16{};
+    int copy = 0;
+    if (lo < hi) {
+        a.load(lds, lo, hi);
+        b.load(lds + A::kBytes, lo, hi);
+    }
+    for (int64_t k = lo; k < hi; k += kBk) {
+        char* t = lds + copy * kBoth;
+        if (direct) {
+            copy ^= 1;
+            arrived();
+        } else {
+            __syncthreads();
+            a.store(t);
+            b.store(t + A::kBytes);
+        }
+        __syncthreads();
+        if (k + kBk < hi) {
+            a.load(lds + copy * kBoth, k + kBk, hi);
+            b.load(lds + copy * kBoth + A::kBytes, k + kBk, hi);
+        }
+#pragma unroll
+        for (int c = 0; c < kBk / 16; ++c) {
+            decltype(A::read(t, 0, 0, 0)) fa[S::AB], fb[S::BB];
+#pragma unroll
+            for (int i = 0; i < S::AB; ++i) fa[i] = A::read(t, i * S::WA + wa, c, lane);
+#pragma unroll
+            for (int j = 0; j < S::BB; ++j) fb[j] = B::read(t + A::kBytes, wb * S::BB + j, c, lane);
+#pragma unroll
+            for (int i = 0; i < S::AB; ++i)
+#pragma unroll
+                for (int j = 0; j < S::BB; ++j) acc[i][j] = mma(fa[i], fb[j], acc[i][j]);
+        }
+    }
+    __syncthreads();                         // the tiles' LDS is free
+}
+
+// A wave's 32 rows by 64 columns on their way between a lane's order (a row; columns 32 w
+// + 8 b + 4 h + i) and memory's (16 bytes a lane, whole rows in turn), by way of LDS.
+template <typename O>
+struct Rows64 {
+    static constexpr int kEach = 16 / (int)sizeof(O), kRow = 64 * (int)sizeof(O) + 16, kBytes = 32 * kRow;
+    static constexpr int kLanes = 64 / kEach;                       // of a row
+    char* t;                                                        // the wave's own kBytes
+    // four values of the lane's row, to columns c .. c + 3
+    __device__ __forceinline__ void put4(int c, float a, float b, float d, float e) const {
+        const O v[4] = {(O)a, (O)b, (O)d, (O)e};
+        __builtin_memcpy(__builtin_assume_aligned(t + (threadIdx.x & 31) * kRow + c * (int)sizeof(O), 8), v, sizeof(v));
+    }
+    __device__ __forceinline__ void get4(int c, float (&v)[4]) const {
+        O o[4];
+        __builtin_memcpy(o, __builtin_assume_aligned(t + (threadIdx.x & 31) * kRow + c * (int)sizeof(O), 8), sizeof(o));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = (float)o[i];
+    }
+    // rows r < rows, columns c < cols (of 64), to or from p + r * ld + c
+    template <bool kStore>
+    __device__ __forceinline__ void move(std::conditional_t<kStore, O, const O>* p, int64_t ld, int rows, int cols,
+                                         bool vec) const {
+        const int lane = threadIdx.x & 63, c = lane % kLanes * kEach;
+#pragma unroll
+        for (int r0 = 0; r0 < 32; r0 += 64 / kLanes) {
+            const int r = r0 + lane / kLanes;
+            char* q = t + r * kRow + c * (int)sizeof(O);
+            if (r >= rows) continue;
+            if (vec) {
+                if (c >= cols) continue;
+                if constexpr (kStore) *(uint4*)(p + r * ld + c) = *(const uint4*)q;
+                else *(uint4*)q = *(const uint4*)(p + r * ld + c);
+            } else {
+                for (int i = 0; i < kEach; ++i) {
+                    if (c + i >= cols) break;
+                    if constexpr (kStore) p[r * ld + c + i] = ((const O*)q)[i];
+                    else ((O*)q)[i] = p[r * ld + c + i];
+                }
+            }
+        }
+    }
+};
+// LDS of one wave is read as it was written.
+__device__ __forceinline__ void wave_sync() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); }
+
+// The sum of each of 16 values over the 32 lanes of a half: value 8 b4 + 4 b3 + 2 b2 + b1 of
+// lane bits b.  Each exchange halves the values.
+__device__ __forceinline__ float sum16(float (&v)[16]) {
+    const int lane = threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i + 8]), false, false);
+        v[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    auto fold = [&](auto dpp, int bit, int n) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (i >= n) break;
+            const float keep = lane & bit ? v[i + n] : v[i], give = lane & bit ? v[i] : v[i + n];
+            v[i] = keep + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(give), decltype(dpp)::value, 15, 15, true));
+        }
+    };
+    fold(std::integral_constant<int, 0x128>(), 8, 4);       // row_ror:8
+    fold(std::integral_constant<int, 0x141>(), 4, 2);       // row_half_mirror
+    fold(std::integral_constant<int, 0x4e>(), 2, 1);        // quad_perm 2 3 0 1
+    return v[0] + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v[0]), 0xb1, 15, 15, true));
 }
 
 // Workgroups that share a tile's tokens follow each other on one XCD, whose L2 then holds
@@ -133,155 +284,204 @@ __device__ __forceinline__ void load4(const T* p, int d, int D, bool vec, float 
     for (int i = 0; i < 4; ++i) v[i] = d + i < D ? (float)p[d + i] : 0.0f;
 }
 
-// y of 128 tokens by 64 units, or dz of them and the tile's sums of it.
-template <typename T, bool BACK>
-__global__ __launch_bounds__(256) void k_gated(GatedK g) {
-    using S = Side<T, false>;
-    __shared__ alignas(16) char sa[S::kBytes];
-    __shared__ alignas(16) char sb[S::kBytes];
+template <typename S, typename A, typename B>
+constexpr int lds_of(bool direct, int rows_bytes) {
+    const int tiles = (A::kBytes + B::kBytes) * (direct ? 2 : 1), rows = 4 * rows_bytes;
+    return tiles > rows ? tiles : rows;
+}
+
+// y of a tile's tokens and units (its left rows are their gates, then their values, so that
+// both of a unit meet in one lane), or dz of them and the tile's sums of it.
+template <typename T, typename S, bool BACK, bool kDirect>
+__global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void k_gated(GatedK g) {
+    constexpr int kUnits = S::kA / 2, UB = S::AB / 2;
+    using A = Side<T, S::kA, false, kDirect>;
+    using B = Side<T, S::kB, false, kDirect>;
+    using Rows = Rows64<T>;
+    __shared__ alignas(16) char lds[lds_of<S, A, B>(kDirect, Rows::kBytes)];
     const int64_t item = item_of(g.items);
     if (item < 0) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-    const int64_t mt = item / g.tiles, m0 = mt * kTile;
-    const int u0 = (int)(item % g.tiles) * kUnits;
-    const T *x = (const T*)g.a.x, *w = (const T*)g.a.w;
-    f32x16 acc[2][2];                                    // gates and values by two blocks of 32 tokens
-    product<T, false, false>(
-        acc, sa, sb, 0, g.C, wave & 1, 2, wave >> 1 << 1, g.vec,
-        [&](int r, int64_t k) {
-            const int u = u0 + (r & (kUnits - 1));
-            return u < g.K ? w + ((int64_t)(r / kUnits) * g.K + u) * g.C + k : nullptr;
-        },
-        [&](int r, int64_t k) { return m0 + r < g.M ? x + (m0 + r) * g.C + k : nullptr; },
-        [&](int64_t k) { return g.C - (int)k; }, [&](int64_t k) { return g.C - (int)k; });
-    const int ub = u0 + 32 * (wave & 1) + 4 * h;
-    float db[2][16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+    const int64_t mt = item / g.tiles, m0 = mt * S::kB;
+    const int u0 = (int)(item - mt * g.tiles) * kUnits, K = g.K;
+    f32x16 acc[S::AB][S::BB];                            // gates, then values, by blocks of 32 tokens
+    {
+        A a;
+        B b;
+        a.init({(const T*)g.a.w + (int64_t)u0 * g.C, 2 * (int64_t)K - u0, g.C, g.C, kUnits, K - kUnits}, g.vec);
+        b.init({(const T*)g.a.x + m0 * g.C, g.M - m0 < S::kB ? g.M - m0 : S::kB, g.C, g.C, S::kB, 0}, g.vec);
+        product<S>(acc, a, b, lds, 0, g.C, kDirect);
+    }
+    // a wave's 32 tokens by 64 columns at a time: its units' gates, or their values
+    const Rows rows{lds + wave * Rows::kBytes};
+    const int wa = wave % S::WA, wb = wave / S::WA;
+    static_assert(S::AB == 2 || S::WA == 1);
+    // unit of (block i, b, i): blocks of a wave's units are 32 (i WA + wa)
+    const int cols = 32 * UB, ub = u0 + 32 * wa;
+    const int have = K - ub < cols ? K - ub : cols;     // may be negative
+    float db[2][UB][16];
     if constexpr (BACK) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) db[0][i] = db[1][i] = 0.0f;
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+            for (int i = 0; i < UB; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) db[w][i][e] = 0.0f;
     }
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int64_t m = m0 + ((wave >> 1) * 2 + j) * 32 + (lane & 31);
-        if (m >= g.M) continue;
+    for (int j = 0; j < S::BB; ++j) {
+        const int64_t m = m0 + (wb * S::BB + j) * 32;
+        const int left = (int)(g.M - m < 32 ? g.M - m : 32);
+        if (left <= 0) continue;
+        if constexpr (BACK) {
+            rows.template move<false>((const T*)g.a.dy + m * K + ub, K, left, have, g.vec);
+            wave_sync();
+        }
+        float og[UB][16], ou[UB][16];
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const int u = ub + 8 * b;
-            float bg[4] = {0, 0, 0, 0}, bu[4] = {0, 0, 0, 0}, og[4], ou[4], dy[4];
-            if (g.a.bias) {
-                load4(g.a.bias, u, g.K, false, bg);
-                load4(g.a.bias + g.K, u, g.K, false, bu);
-            }
-            if constexpr (BACK) load4((const T*)g.a.dy + m * g.K, u, g.K, g.vec, dy);
+        for (int i = 0; i < UB; ++i)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float zg = acc[0][j][4 * b + i] + bg[i], zu = acc[1][j][4 * b + i] + bu[i];
+            for (int b = 0; b < 4; ++b) {
+                const int c = 32 * i + 8 * b + 4 * h;
+                float bg[4] = {0, 0, 0, 0}, bu[4] = {0, 0, 0, 0}, dy[4];
+                if (g.a.bias) {
+                    load4(g.a.bias, ub + c, K, false, bg);
+                    load4(g.a.bias + K, ub + c, K, false, bu);
+                }
                 if constexpr (BACK) {
-                    float v, d;
-                    gate_slope(zg, g.act, v, d);
-                    og[i] = dy[i] * zu * d;
-                    ou[i] = dy[i] * v;
-                    db[0][4 * b + i] += og[i];
-                    db[1][4 * b + i] += ou[i];
-                } else {
-                    og[i] = gate(zg, g.act) * zu;
+                    rows.get4(c, dy);
+                    // past the tokens LDS holds what was there
+                    if (left < 32 && (lane & 31) >= left) dy[0] = dy[1] = dy[2] = dy[3] = 0.0f;
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float zg = acc[i][j][4 * b + e] + bg[e], zu = acc[UB + i][j][4 * b + e] + bu[e];
+                    if constexpr (BACK) {
+                        float v, d;
+                        gate_slope(zg, g.act, v, d);
+                        og[i][4 * b + e] = dy[e] * zu * d;
+                        ou[i][4 * b + e] = dy[e] * v;
+                        db[0][i][4 * b + e] += og[i][4 * b + e];
+                        db[1][i][4 * b + e] += ou[i][4 * b + e];
+                    } else {
+                        og[i][4 * b + e] = gate(zg, g.act) * zu;
+                    }
                 }
             }
-            if constexpr (BACK) {
-                T* dz = (T*)g.dz + m * 2 * g.K;
-                store4(dz, u, g.K, g.vec, og[0], og[1], og[2], og[3]);
-                store4(dz + g.K, u, g.K, g.vec, ou[0], ou[1], ou[2], ou[3]);
-            } else {
-                store4((T*)g.a.y + m * g.K, u, g.K, g.vec, og[0], og[1], og[2], og[3]);
-            }
+        auto out = [&](const float (&o)[UB][16], T* p, int64_t ld) {
+            wave_sync();
+#pragma unroll
+            for (int i = 0; i < UB; ++i)
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+                    rows.put4(32 * i + 8 * b + 4 * h, o[i][4 * b], o[i][4 * b + 1], o[i][4 * b + 2], o[i][4 * b + 3]);
+            wave_sync();
+            rows.template move<true>(p, ld, left, have, g.vec);
+        };
+        if constexpr (BACK) {
+            T* dz = (T*)g.dz + m * 2 * K + ub;
+            out(og, dz, 2 * (int64_t)K);
+            out(ou, dz + K, 2 * (int64_t)K);
+            wave_sync();
+        } else {
+            out(og, (T*)g.a.y + m * K + ub, K);
+            wave_sync();
         }
     }
     if constexpr (BACK) {
         if (!g.a.dbias) return;
-        // over the 32 lanes of a half, then over the two waves that have these units
-        __shared__ float rows[4][2][2][16];
+        // over the lanes, then over the waves that have these units
+        __shared__ float sums[S::WB][2][kUnits];
 #pragma unroll
-        for (int w2 = 0; w2 < 2; ++w2)
+        for (int w = 0; w < 2; ++w)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                float v = db[w2][i];
-#pragma unroll
-                for (int d = 1; d < 32; d <<= 1) v += __shfl_xor(v, d, 64);
-                if ((lane & 31) == 0) rows[wave][w2][h][i] = v;
+            for (int i = 0; i < UB; ++i) {
+                const float v = sum16(db[w][i]);
+                // value 8 b4 + 4 b3 + 2 b2 + b1: row 8 (value / 4) + 4 h + value % 4 of the block
+                const int val = (lane >> 4 & 1) * 8 + (lane >> 3 & 1) * 4 + (lane >> 2 & 1) * 2 + (lane >> 1 & 1);
+                if (!(lane & 1)) sums[wb][w][32 * (i * S::WA + wa) + 8 * (val >> 2) + 4 * h + (val & 3)] = v;
             }
         __syncthreads();
         if (threadIdx.x < 2 * kUnits) {
-            // value w2, unit 32 wu + 8 b + 4 h + i
-            const int w2 = threadIdx.x >> 6, u = threadIdx.x & 63, wu = u >> 5, hh = (u >> 2) & 1;
-            const int i = ((u & 31) >> 3) * 4 + (u & 3);
-            if (u0 + u < g.K)
-                g.dbias[mt * 2 * g.K + (int64_t)w2 * g.K + u0 + u] = rows[wu][w2][hh][i] + rows[wu + 2][w2][hh][i];
+            const int w = threadIdx.x / kUnits, u = threadIdx.x % kUnits;
+            float v = 0.0f;
+#pragma unroll
+            for (int i = 0; i < S::WB; ++i) v += sums[i][w][u];
+            if (u0 + u < K) g.dbias[mt * 2 * K + (int64_t)w * K + u0 + u] = v;
         }
     }
 }
 
-// Results 32 (wa blocks) of P down, lanes 32 (wb blocks) of Q across, to out[q][p].
-template <typename T, typename O>
-__device__ __forceinline__ void put_tile(const f32x16 (&acc)[2][2], O* out, int p0, int P, int64_t q0, int64_t Q, bool vec) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+// A tile's results to out[q][p], P of p: 64 columns of a wave at a time.
+template <typename S, typename O>
+__device__ __forceinline__ void put_tile(const f32x16 (&acc)[S::AB][S::BB], char* lds, O* out, int p0, int P, int64_t q0,
+                                         int64_t Q, bool vec) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+    const int wa = wave % S::WA, wb = wave / S::WA;
+    const Rows64<O> rows{lds + wave * Rows64<O>::kBytes};
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int64_t q = q0 + ((wave >> 1) * 2 + j) * 32 + (lane & 31);
-        if (q >= Q) continue;
+    for (int j = 0; j < S::BB; ++j) {
+        const int64_t q = q0 + (wb * S::BB + j) * 32;
+        const int left = (int)(Q - q < 32 ? Q - q : 32);
+        if (left <= 0) continue;
+        // with more waves than one a block's columns are not next to the next one's
+        constexpr int each = S::WA == 1 ? 2 : 1;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < S::AB; i += each) {
+            const int p = p0 + 32 * (i * S::WA + wa);
+            wave_sync();
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
-                store4(out + q * P, p0 + ((wave & 1) * 2 + i) * 32 + 8 * b + 4 * h, P, vec, acc[i][j][4 * b],
-                       acc[i][j][4 * b + 1], acc[i][j][4 * b + 2], acc[i][j][4 * b + 3]);
+            for (int e = 0; e < each; ++e)
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+                    rows.put4(32 * e + 8 * b + 4 * h, acc[i + e][j][4 * b], acc[i + e][j][4 * b + 1],
+                              acc[i + e][j][4 * b + 2], acc[i + e][j][4 * b + 3]);
+            wave_sync();
+            rows.template move<true>(out + q * P + p, P, left, P - p < 32 * each ? P - p : 32 * each, vec);
+        }
     }
 }
 
-// dx of 128 tokens by 128 channels: dz [M][2 K] by w [2 K][C].
-template <typename T>
-__global__ __launch_bounds__(256) void k_gated_dx(GatedK g) {
-    __shared__ alignas(16) char sa[Side<T, true>::kBytes];
-    __shared__ alignas(16) char sb[Side<T, false>::kBytes];
+// dx of a tile's tokens and channels: dz [M][2 K] by w [2 K][C].
+template <typename T, typename S, bool kDirect>
+__global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void k_gated_dx(GatedK g) {
+    using A = Side<T, S::kA, true, kDirect>;
+    using B = Side<T, S::kB, false, kDirect>;
+    __shared__ alignas(16) char lds[lds_of<S, A, B>(kDirect, Rows64<T>::kBytes)];
     const int64_t item = item_of(g.items);
     if (item < 0) return;
-    const int wave = threadIdx.x >> 6;
-    const int64_t m0 = item / g.tiles * kTile;
-    const int c0 = (int)(item % g.tiles) * kTile, F = 2 * g.K;
-    const T *dz = (const T*)g.dz, *w = (const T*)g.a.w;
-    f32x16 acc[2][2];
-    product<T, true, false>(
-        acc, sa, sb, 0, F, (wave & 1) * 2, 1, (wave >> 1) * 2, g.vec,
-        [&](int r, int64_t k) { return k + r < F ? w + (k + r) * g.C + c0 : nullptr; },
-        [&](int r, int64_t k) { return m0 + r < g.M ? dz + (m0 + r) * F + k : nullptr; },
-        [&](int64_t) { return g.C - c0; }, [&](int64_t k) { return F - (int)k; });
-    put_tile<T>(acc, (T*)g.a.dx, c0, g.C, m0, g.M, g.vec);
+    const int64_t mt = item / g.tiles, m0 = mt * S::kB;
+    const int c0 = (int)(item - mt * g.tiles) * S::kA, F = 2 * g.K;
+    f32x16 acc[S::AB][S::BB];
+    A a;
+    B b;
+    a.init({(const T*)g.a.w + c0, F, g.C - c0, g.C, kBk, 0}, g.vec);
+    b.init({(const T*)g.dz + m0 * F, g.M - m0 < S::kB ? g.M - m0 : S::kB, F, F, S::kB, 0}, g.vec);
+    product<S>(acc, a, b, lds, 0, F, kDirect);
+    put_tile<S>(acc, lds, (T*)g.a.dx, c0, g.C, m0, g.M, g.vec);
 }
 
-// dw of 128 units by 128 channels, over a part of the tokens: dz^T by x.
-template <typename T>
-__global__ __launch_bounds__(256) void k_gated_dw(GatedK g) {
-    using S = Side<T, true>;
-    __shared__ alignas(16) char sa[S::kBytes];
-    __shared__ alignas(16) char sb[S::kBytes];
+// dw of a tile's units and channels, over a part of the tokens: dz^T by x.
+template <typename T, typename S, bool kDirect>
+__global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void k_gated_dw(GatedK g) {
+    using A = Side<T, S::kA, true, kDirect>;
+    using B = Side<T, S::kB, true, kDirect>;
+    __shared__ alignas(16) char lds[lds_of<S, A, B>(kDirect, Rows64<float>::kBytes)];
     const int64_t item = item_of(g.items);
     if (item < 0) return;
-    const int wave = threadIdx.x >> 6, F = 2 * g.K;
-    const int64_t ft = (F + kTile - 1) / kTile;
-    const int c0 = (int)(item % g.tiles) * kTile, f0 = (int)(item / g.tiles % ft) * kTile;
-    const int split = (int)(item / g.tiles / ft);
-    const T *dz = (const T*)g.dz, *x = (const T*)g.a.x;
+    const int F = 2 * g.K;
+    const int64_t ft = (F + S::kB - 1) / S::kB, at = item / g.tiles;
+    const int c0 = (int)(item - at * g.tiles) * S::kA, split = (int)(at / ft), f0 = (int)(at - split * ft) * S::kB;
     int64_t lo, hi;
-    part_of(g.M, S::kBk, split, g.splits, lo, hi);
-    f32x16 acc[2][2];
-    product<T, true, true>(
-        acc, sa, sb, lo, hi, (wave & 1) * 2, 1, (wave >> 1) * 2, g.vec,
-        [&](int r, int64_t k) { return k + r < hi ? x + (k + r) * g.C + c0 : nullptr; },
-        [&](int r, int64_t k) { return k + r < hi ? dz + (k + r) * F + f0 : nullptr; },
-        [&](int64_t) { return g.C - c0; }, [&](int64_t) { return F - f0; });
-    if (g.splits > 1)
-        put_tile<T>(acc, g.part + (int64_t)split * F * g.C, c0, g.C, f0, F, (g.C & 3) == 0);
-    else
-        put_tile<T>(acc, (T*)g.a.dw, c0, g.C, f0, F, g.vec);
+    part_of(g.M, kBk, split, g.splits, lo, hi);
+    f32x16 acc[S::AB][S::BB];
+    A a;
+    B b;
+    a.init({(const T*)g.a.x + c0, g.M, g.C - c0, g.C, kBk, 0}, g.vec);
+    b.init({(const T*)g.dz + f0, g.M, F - f0, F, kBk, 0}, g.vec);
+    product<S>(acc, a, b, lds, lo, hi, kDirect);
+    if (g.splits > 1) put_tile<S>(acc, lds, g.part + (int64_t)split * F * g.C, c0, g.C, f0, F, (g.C & 3) == 0);
+    else put_tile<S>(acc, lds, (T*)g.a.dw, c0, g.C, f0, F, g.vec);
 }
 
 template <typename T>
@@ -294,9 +494,8 @@ __global__ __launch_bounds__(256) void k_gated_dw_sum(GatedK g) {
 }
 
 // dbias: 16 columns a workgroup, 16 threads a column.
-__global__ __launch_bounds__(256) void k_gated_db(GatedK g) {
+__global__ __launch_bounds__(256) void k_gated_db(GatedK g, int64_t rows) {
     const int F = 2 * g.K, f = blockIdx.x * 16 + (threadIdx.x & 15), i0 = threadIdx.x >> 4;
-    const int64_t rows = (g.M + kTile - 1) / kTile;
     float sum = 0.0f;
     if (f < F)
         for (int64_t i = i0; i < rows; i += 16) sum += g.dbias[i * F + f];
@@ -332,33 +531,76 @@ GatedK args_of(const GatedArgs& a, const GatedShape& s) {
 
 inline int64_t tiles_of(int64_t n, int each) { return (n + each - 1) / each; }
 
+// Shapes for a product of p by q results: the widest whose tiles fill the card twice over
+// (fp32: operands of the wide one pass a wave's registers).
+enum { kWide, kSquare, kNarrow };
+int shape_of(int64_t p, int64_t q, int64_t parts, Io io) {
+    if (io != Io::F32 && tiles_of(p, Wide::kA) * tiles_of(q, Wide::kB) * parts >= 512) return kWide;
+    return tiles_of(p, Square::kA) * tiles_of(q, Square::kB) * parts >= 512 ? kSquare : kNarrow;
+}
+template <typename F>
+auto with_shape(int shape, F f) {
+    return shape == kWide ? f(Wide()) : shape == kSquare ? f(Square()) : f(Narrow());
+}
+
+// f(type, shape, straight to LDS)
+template <typename F>
+hipError_t with_all(const GatedK& g, Io io, int shape, F f) {
+    // offsets of a tile's rows, and from a unit's gate to its value, below 2^31
+    const bool direct = g.vec && io != Io::F32 && g.C <= 1 << 21 && g.K <= 1 << 20 && (int64_t)g.K * g.C < 1 << 28;
+    return with_io(io, [&](auto t) {
+        typedef decltype(t) T;
+        if constexpr (sizeof(T) == 2) {
+            if (direct) return with_shape(shape, [&](auto s) { return f(t, s, std::true_type()); });
+            return with_shape(shape, [&](auto s) { return f(t, s, std::false_type()); });
+        } else {
+            // Wide is not taken
+            return shape == kSquare ? f(t, Square(), std::false_type()) : f(t, Narrow(), std::false_type());
+        }
+    });
+}
+
+int splits_for(const GatedShape& s, int shape) {
+    int64_t tiles = 0;
+    with_shape(shape, [&](auto sh) {
+        tiles = tiles_of(s.C, decltype(sh)::kA) * tiles_of(2 * (int64_t)s.K, decltype(sh)::kB);
+        return 0;
+    });
+    // 512 workgroups fill the card; a part has 256 tokens at least
+    const int64_t want = (512 + tiles - 1) / tiles, most = s.M / 256, n = want < most ? want : most;
+    return n < 1 ? 1 : n > 64 ? 64 : (int)n;
+}
+
 }  // namespace
 
 GatedPlan gated_plan(const GatedShape& s, bool backward) {
     GatedPlan p{};
-    const int64_t mt = tiles_of(s.M, kTile), ut = tiles_of(s.K, kUnits), ct = tiles_of(s.C, kTile);
-    const int64_t ft = tiles_of(2 * (int64_t)s.K, kTile), most = (int64_t)1 << 30;
-    // 512 workgroups fill the card; a part has 256 tokens at least
-    const int64_t want = (512 + ct * ft - 1) / (ct * ft), few = s.M / 256;
-    p.splits = (int)(want < few ? want : few);
-    if (p.splits < 1) p.splits = 1;
-    if (p.splits > 64) p.splits = 64;
-    p.fits = s.M <= INT32_MAX && s.K <= INT32_MAX / 2 && mt * ut <= most && mt * ct <= most && ct * ft * p.splits <= most &&
-             (int64_t)s.K * s.C <= INT32_MAX * (int64_t)64;
-    if (!p.fits || !backward) return p;
-    p.dz = round_up((size_t)s.M * 2 * s.K * io_size(s.io), 16);
-    p.dbias = round_up((size_t)mt * 2 * s.K * 4, 16);
-    p.part = p.splits > 1 ? round_up((size_t)p.splits * 2 * s.K * s.C * 4, 16) : 0;
+    const int64_t most = (int64_t)1 << 30, F = 2 * (int64_t)s.K;
+    // counts of the smallest tiles
+    const int64_t mt = tiles_of(s.M, Narrow::kB), ut = tiles_of(s.K, Narrow::kA / 2), ct = tiles_of(s.C, Narrow::kA);
+    p.fits = s.M <= INT32_MAX && s.K <= INT32_MAX / 2 && mt * ut <= most && mt * ct <= most &&
+             ct * tiles_of(F, Narrow::kB) <= most / 64 && (int64_t)s.K * s.C < (int64_t)1 << 37;
+    if (!p.fits) return p;
+    p.first = shape_of(F, s.M, 1, s.io);
+    if (!backward) return p;
+    p.dx = shape_of(s.C, s.M, 1, s.io);
+    // the sum over tokens is cut as finely as it takes
+    p.dw = s.io != Io::F32 && s.C > Narrow::kA ? kWide : s.C > Narrow::kA ? kSquare : kNarrow;
+    p.splits = splits_for(s, p.dw);
+    p.dz = round_up((size_t)s.M * F * io_size(s.io), 16);
+    p.dbias = round_up((size_t)mt * F * 4, 16);
+    p.part = p.splits > 1 ? round_up((size_t)p.splits * F * s.C * 4, 16) : 0;
     p.need = p.dz + p.dbias + p.part;
     return p;
 }
 
 hipError_t launch_gated(const GatedArgs& a, const GatedShape& s, const GatedPlan& p, hipStream_t st) {
     GatedK g = args_of(a, s);
-    g.tiles = tiles_of(s.K, kUnits);
-    g.items = tiles_of(s.M, kTile) * g.tiles;
-    return with_io(s.io, [&](auto t) {
-        k_gated<decltype(t), false><<<grid_of(g.items), 256, 0, st>>>(g);
+    return with_all(g, s.io, p.first, [&](auto t, auto sh, auto direct) {
+        typedef decltype(sh) S;
+        g.tiles = tiles_of(s.K, S::kA / 2);
+        g.items = tiles_of(s.M, S::kB) * g.tiles;
+        k_gated<decltype(t), S, false, direct.value><<<grid_of(g.items), 256, 0, st>>>(g);
         return hipGetLastError();
     });
 }
@@ -368,31 +610,40 @@ hipError_t launch_gated_backward(const GatedArgs& a, const GatedShape& s, const 
     g.dz = ws;
     g.dbias = (float*)((char*)ws + p.dz);
     g.part = (float*)((char*)ws + p.dz + p.dbias);
-    return with_io(s.io, [&](auto t) {
-        typedef decltype(t) T;
-        g.tiles = tiles_of(s.K, kUnits);
-        g.items = tiles_of(s.M, kTile) * g.tiles;
-        k_gated<T, true><<<grid_of(g.items), 256, 0, st>>>(g);
-        hipError_t e = hipGetLastError();
+    int64_t rows = 0;
+    hipError_t e = with_all(g, s.io, p.first, [&](auto t, auto sh, auto direct) {
+        typedef decltype(sh) S;
+        g.tiles = tiles_of(s.K, S::kA / 2);
+        rows = tiles_of(s.M, S::kB);
+        g.items = rows * g.tiles;
+        k_gated<decltype(t), S, true, direct.value><<<grid_of(g.items), 256, 0, st>>>(g);
+        return hipGetLastError();
+    });
+    if (e != hipSuccess) return e;
+    if (a.dbias) {
+        k_gated_db<<<(unsigned)tiles_of(2 * (int64_t)s.K, 16), 256, 0, st>>>(g, rows);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    if (a.dx) {
+        e = with_all(g, s.io, p.dx, [&](auto t, auto sh, auto direct) {
+            typedef decltype(sh) S;
+            g.tiles = tiles_of(s.C, S::kA);
+            g.items = tiles_of(s.M, S::kB) * g.tiles;
+            k_gated_dx<decltype(t), S, direct.value><<<grid_of(g.items), 256, 0, st>>>(g);
+            return hipGetLastError();
+        });
         if (e != hipSuccess) return e;
-        if (a.dbias) {
-            k_gated_db<<<(unsigned)tiles_of(2 * (int64_t)s.K, 16), 256, 0, st>>>(g);
-            if ((e = hipGetLastError()) != hipSuccess) return e;
-        }
-        g.tiles = tiles_of(s.C, kTile);
-        if (a.dx) {
-            g.items = tiles_of(s.M, kTile) * g.tiles;
-            k_gated_dx<T><<<grid_of(g.items), 256, 0, st>>>(g);
-            if ((e = hipGetLastError()) != hipSuccess) return e;
-        }
-        if (a.dw) {
-            g.splits = p.splits;
-            g.items = g.tiles * tiles_of(2 * (int64_t)s.K, kTile) * g.splits;
-            k_gated_dw<T><<<grid_of(g.items), 256, 0, st>>>(g);
-            if ((e = hipGetLastError()) != hipSuccess) return e;
-            if (g.splits > 1)
-                k_gated_dw_sum<T><<<(unsigned)tiles_of((int64_t)2 * s.K * s.C, 256), 256, 0, st>>>(g);
-        }
+    }
+    if (!a.dw) return hipSuccess;
+    return with_all(g, s.io, p.dw, [&](auto t, auto sh, auto direct) {
+        typedef decltype(sh) S;
+        g.splits = p.splits;
+        g.tiles = tiles_of(s.C, S::kA);
+        g.items = g.tiles * tiles_of(2 * (int64_t)s.K, S::kB) * g.splits;
+        k_gated_dw<decltype(t), S, direct.value><<<grid_of(g.items), 256, 0, st>>>(g);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess || g.splits == 1) return e;
+        k_gated_dw_sum<decltype(t)><<<(unsigned)tiles_of((int64_t)2 * s.K * s.C, 256), 256, 0, st>>>(g);
         return hipGetLastError();
     });
 }
