@@ -50,7 +50,7 @@ AttnPlan attn_plan(const AttnShape& s, bool backward) {
     const bool parts = p.rows.splits > 1;
     size_t part = parts ? (size_t)p.rows.splits * all * s.D * (backward ? 8 : 4) : 0;
     if (backward) {
-        p.delta = round_up((size_t)all * 4, 16) * (s.io == Io::F32 ? 2 : 1);   // with P's sums
+        p.delta = round_up((size_t)all * 4, 16) * (s.io == Io::F32 ? 3 : 2);   // delta, offset, share
         p.stat = parts ? round_up((size_t)p.rows.splits * all * 8, 16) : 0;
         const size_t keys = p.keys.splits > 1 ? (size_t)p.keys.splits * pairs * s.Lk * s.D * 8 : 0;
         part = part > keys ? part : keys;
@@ -80,7 +80,9 @@ hipError_t launch_attn_backward(const AttnBwd& b, const AttnShape& s, const Attn
     g.vec = all16(s, {b.dy, b.q, b.k, b.v, b.y, b.dq, b.dk, b.dv});
     g.rep = make_fastdiv((uint32_t)s.rep);
     g.delta = (float*)ws;
-    g.share = (float*)((char*)ws + p.delta / 2);
+    const size_t each = round_up((size_t)s.N * s.Hk * s.rows * 4, 16);
+    g.offset = (float*)((char*)ws + each);
+    g.share = (float*)((char*)ws + 2 * each);
     g.part = (float*)((char*)ws + p.delta);
     g.stat = (float*)((char*)ws + p.delta + p.part);
     return run(g, p, true, st);

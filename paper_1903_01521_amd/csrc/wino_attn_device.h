@@ -311,14 +311,26 @@ struct Direct {
             off[i] = chunk < used ? offset(row, chunk) : 0x80000000u;
         }
     }
-    // to the tile at t; bytes: of the buffer at p
+    // to the tile at t; bytes: of the buffer at p.  In assembly: the compiler would wait for
+    // every load to LDS before it reads any of LDS, the other copies' tiles too.  What waits for
+    // them is ready().
     __device__ __forceinline__ void issue(char* t, const void* p, uint32_t bytes) const {
-        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, bytes, 0x00020000);
+        typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+        const uint64_t at = (uint64_t)p;
+        const u32x4 r = {(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at),
+                         (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)) & 0xffffu,
+                         (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u};
+        const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)t;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"          // m0 on the clobber list
 #pragma unroll
         for (int i = 0; i < kN; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                r, (__attribute__((address_space(3))) void*)(t + (i * NT + wave * 64) * 16), 16, off[i], 0, 0, 0);
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(
+                             __builtin_amdgcn_readfirstlane(lds + (i * NT + wave * 64) * 16)),
+                         "v"(off[i]), "s"(r)
+                         : "memory", "m0");
+#pragma clang diagnostic pop
     }
     // the same, of each row `used` chunks
     __device__ __forceinline__ void issue_part(char* t, const void* p, uint32_t bytes, int used) const {
@@ -331,8 +343,33 @@ struct Direct {
         d.issue(t, p, bytes);
     }
 };
-// Every load to LDS of this wave has arrived.
-__device__ __forceinline__ void arrived() { __builtin_amdgcn_s_waitcnt(0x0F70); }
+// 64 floats at p, `left` of them and zeros behind, to LDS by one wave.
+__device__ __forceinline__ void load_floats(float* t, const float* p, int64_t left) {
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    const uint64_t at = (uint64_t)p;
+    const u32x4 r = {(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at),
+                     (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)) & 0xffffu,
+                     (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(left < 64 ? left : 64) * 4), 0x00020000u};
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(char*)t;
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(
+                     __builtin_amdgcn_readfirstlane(lds)),
+                 "v"((threadIdx.x & 63) * 4), "s"(r)
+                 : "memory", "m0");
+#pragma clang diagnostic pop
+}
+// This wave's loads to LDS have arrived, but the last n, and its own LDS accesses are
+// done; then so are those of the workgroup's other waves.
+template <int n>
+__device__ __forceinline__ void ready() {
+    static_assert(n < 64);
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(n) : "memory");
+}
+
+// Before a loop with such loads: whatever was loaded to registers is there, or the compiler's
+// wait for it, inside the loop, would wait for the tiles in every step.
+__device__ __forceinline__ void settled() { __builtin_amdgcn_s_waitcnt(0x0F70); }
 
 // ---------------------------------------------------------------- work
 
@@ -344,7 +381,10 @@ struct AttnK {
     int splits;
     bool by_xcd;
     FastDiv per_pair, per_tile;              // by tiles * splits, by splits
-    float *delta, *share, *part, *part2, *stat;
+    // backward, of each pair's rows in turn: delta, the exponent's offset -lse log2 e, and (fp32)
+    // 1 over the sum of P
+    float *delta, *offset, *share;
+    float *part, *part2, *stat;
     bool vec;
     FastDiv rep;                             // by s.rep; rows are below 2^31
 };
@@ -459,8 +499,7 @@ struct KeyTiles<T, D16, KT, NT, true> {      // straight to LDS: 16-bit, 16-byte
         dv.issue(sv, vbase + k0 * ldv, (last * (uint32_t)ldv + (uint32_t)D) * 2);
     }
     __device__ __forceinline__ void step(char*, char*, float*, char* nk, char* nv, int64_t k0) {
-        arrived();
-        __syncthreads();
+        ready<0>();
         if (k0 + KT < hi) first(nk, nv, k0 + KT);
     }
     __device__ __forceinline__ f32x4v left_out(const float*, int at, int64_t k0) const {
@@ -523,6 +562,7 @@ __global__ __launch_bounds__((FwdCut<T, D16, kFew>::kThreads), (waves_of<T, D16>
 #pragma unroll
     for (int d = 0; d < DB; ++d) o[d] = f32x16{};
     if (lo < hi) in.first(tk[0], tv[0], lo);
+    if (kDirect) settled();
     int copy = 0;
     for (int64_t k0 = lo; k0 < hi; k0 += KT) {
         const char *sk = tk[copy], *sv = tv[copy];
@@ -778,6 +818,7 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(4))) void k_attn_dq(AttnK g)
 #pragma unroll
     for (int d = 0; d < DB; ++d) acc[d] = mean[d] = f32x16{};
     if (lo < hi) in.first(tk[0], tv[0], lo);
+    if (kDirect) settled();
     int copy = 0;
     for (int64_t k0 = lo; k0 < hi; k0 += KT) {
         const char *sk = tk[copy], *sv = tv[copy];
@@ -862,13 +903,18 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(4))) void k_attn_dq(AttnK g)
         if (h == 0) {
             g.stat[id * 2] = lack;
             g.stat[id * 2 + 1] = round;
-            if (split == 0) g.delta[stat] = delta;
+            if (split == 0) {
+                g.delta[pair * s.rows + row] = delta;
+                g.offset[pair * s.rows + row] = off;
+            }
         }
         return;
     }
     if (h == 0) {
-        g.delta[stat] = kFix ? delta + lack : delta;
-        if constexpr (!kFix) g.share[stat] = share;
+        const int64_t at = pair * s.rows + row;
+        g.delta[at] = kFix ? delta + lack : delta;
+        g.offset[at] = off;
+        if constexpr (!kFix) g.share[at] = share;
     }
 #pragma unroll
     for (int d = 0; d < DB; ++d)
@@ -906,14 +952,13 @@ __global__ __launch_bounds__(256) void k_attn_dq_join(AttnK g) {
     const int64_t pair = id / s.rows, row = id - pair * s.rows;
     const int n = (int)(pair / s.Hk);
     const RowAt me = row_at(g, n, (int)(pair - (int64_t)n * s.Hk), row);
-    const int64_t stat = ((int64_t)n * s.Hq + me.head) * s.Lq + me.t;
     T* dq = (T*)g.b.dq + me.tok * s.ldq + (int64_t)me.head * s.D;
     if constexpr (sizeof(T) == 2) {
         dq[d] = (T)(sum - round * mean);
-        if (d == 0) g.delta[stat] += lack;
+        if (d == 0) g.delta[id] += lack;
     } else {
         dq[d] = sum * share_of(lack);
-        if (d == 0) g.share[stat] = share_of(lack);
+        if (d == 0) g.share[id] = share_of(lack);
     }
 }
 
@@ -978,7 +1023,7 @@ struct RowTiles<T, D16, RT, NT, true> {
         mq.issue(sq, q + t * ldq, (last * ldq + row) * 2);
         mo.issue(so, dy + t * ldo, (last * ldo + row) * 2);
     }
-    __device__ __forceinline__ void store(char*, char*) const { arrived(); }
+    __device__ __forceinline__ void store(char*, char*) const {}
 };
 
 // dk and dv of 64 keys: a wave owns 32 of them and every other 32 of the pair's rows, and
@@ -998,7 +1043,7 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(kDirect ? 6 : 4))) void k_at
     const AttnShape& s = g.s;
     const Work wk = work_of(g);
     if (wk.none) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     const int split = wk.split, n = wk.n, hk = wk.hk;
     const int64_t tile = wk.tile, pair = wk.pair;
     const int len = keys_of(g.b.klen, n, s.Lk);
@@ -1019,16 +1064,18 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(kDirect ? 6 : 4))) void k_at
     RowTiles<T, D16, RT, NT, kDirect> in;
     in.init(g, n, hk, hi);
     float moff = 0.0f, mdel = 0.0f, mshare = 0.0f;
-    auto load = [&](int64_t r0, char* sq, char* so) {
+    // rows past hi: P = 1, but their q and dy are zeros
+    auto load = [&](int64_t r0, char* sq, char* so, float* offs, float* deltas) {
         in.load(r0, sq, so);
-        if (threadIdx.x < RT) {
+        const int64_t at = pair * s.rows + r0;
+        if constexpr (kDirect) {
+            if (wave == 0) load_floats(offs, g.offset + at, hi - r0);
+            if (wave == 1) load_floats(deltas, g.delta + at, hi - r0);
+        } else if (threadIdx.x < RT) {
             const bool inside = r0 + threadIdx.x < hi;
-            const RowAt x = row_at(g, n, hk, r0 + threadIdx.x);
-            const int64_t at = inside ? ((int64_t)n * s.Hq + x.head) * s.Lq + x.t : 0;
-            const float l = inside ? g.b.lse[at] : -INFINITY;
-            moff = l == -INFINITY ? -INFINITY : -l * kLog2e;
-            mdel = inside ? g.delta[at] : 0.0f;
-            if constexpr (kShare) mshare = inside ? g.share[at] : 0.0f;
+            moff = inside ? g.offset[at + threadIdx.x] : 0.0f;
+            mdel = inside ? g.delta[at + threadIdx.x] : 0.0f;
+            if constexpr (kShare) mshare = inside ? g.share[at + threadIdx.x] : 0.0f;
         }
     };
 
@@ -1037,7 +1084,8 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(kDirect ? 6 : 4))) void k_at
     f32x16 ak[DB], av[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d) ak[d] = av[d] = f32x16{};
-    if (lo < hi) load(lo, tq[0], to[0]);
+    if (lo < hi) load(lo, tq[0], to[0], toff[0], tdel[0]);
+    if (kDirect) settled();
     int copy = 0;
     for (int64_t r0 = lo; r0 < hi; r0 += RT) {
         char *sq = tq[copy], *so = to[copy];
@@ -1045,13 +1093,14 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(kDirect ? 6 : 4))) void k_at
         if (CP == 1) __syncthreads();
         else copy ^= 1;
         in.store(sq, so);
-        if (threadIdx.x < RT) {
+        if (!kDirect && threadIdx.x < RT) {
             offs[threadIdx.x] = moff;
             deltas[threadIdx.x] = mdel;
             if constexpr (kShare) shares[threadIdx.x] = mshare;
         }
-        __syncthreads();
-        if (r0 + RT < hi) load(r0 + RT, tq[copy], to[copy]);
+        if constexpr (kDirect) ready<0>();
+        else __syncthreads();
+        if (r0 + RT < hi) load(r0 + RT, tq[copy], to[copy], toff[copy], tdel[copy]);
         f32x16 p{}, ds[1] = {f32x16{}};
 #pragma unroll
         for (int c = 0; c < D16; ++c) {

@@ -61,7 +61,7 @@ struct Side {
     // rows of more than 128 values in halves of 128, each a tile
     static constexpr int kCols = T_ ? (I < 128 ? I : 128) : kBk, kParts = T_ ? I / kCols : 1;
     using Tl = Tile<T, kCols / 16, kRows>;
-    static constexpr int kBytes = Tl::kBytes * kParts;
+    static constexpr int kBytes = Tl::kBytes * kParts, kLoads = 0;
     Source<T> s;
     bool vec;
     Moving<T, kCols / 16, kRows, 256> m[kParts];
@@ -98,6 +98,7 @@ struct Side<T, I, T_, true> : Side<T, I, T_, false> {
     using Base = Side<T, I, T_, false>;
     using Tl = typename Base::Tl;
     using Dir = Direct<Tl, Base::kRows, 256>;
+    static constexpr int kLoads = Dir::kN * Base::kParts;     // of a lane, a tile
     Dir d[Base::kParts];
     __device__ __forceinline__ void init(const Source<T>& s, bool) {
         this->s = s;
@@ -138,25 +139,27 @@ __device__ __forceinline__ void product(f32x16 (&acc)[S::AB][S::BB], A& a, B& b,
     for (int i = 0; i < S::AB; ++i)
 #pragma unroll
         for (int j = 0; j < S::BB; ++j) acc[i][j] = f32x16{};
+    auto load = [&](int copy, int64_t k) {
+        a.load(lds + copy * kBoth, k, hi);
+        b.load(lds + copy * kBoth + A::kBytes, k, hi);
+    };
+    // straight to LDS: two steps ahead, in three copies
     int copy = 0;
-    if (lo < hi) {
-        a.load(lds, lo, hi);
-        b.load(lds + A::kBytes, lo, hi);
-    }
+    if (lo < hi) load(0, lo);
+    if (direct && lo + kBk < hi) load(1, lo + kBk);
     for (int64_t k = lo; k < hi; k += kBk) {
         char* t = lds + copy * kBoth;
         if (direct) {
-            copy ^= 1;
-            arrived();
+            if (k + kBk < hi) ready<A::kLoads + B::kLoads>();
+            else ready<0>();
+            if (k + 2 * kBk < hi) load(copy == 0 ? 2 : copy - 1, k + 2 * kBk);
+            copy = copy == 2 ? 0 : copy + 1;
         } else {
             __syncthreads();
             a.store(t);
             b.store(t + A::kBytes);
-        }
-        __syncthreads();
-        if (k + kBk < hi) {
-            a.load(lds + copy * kBoth, k + kBk, hi);
-            b.load(lds + copy * kBoth + A::kBytes, k + kBk, hi);
+            __syncthreads();
+            if (k + kBk < hi) load(0, k + kBk);
         }
 #pragma unroll
         for (int c = 0; c < kBk / 16; ++c) {
@@ -286,7 +289,7 @@ __device__ __forceinline__ void load4(const T* p, int d, int D, bool vec, float 
 
 template <typename S, typename A, typename B>
 constexpr int lds_of(bool direct, int rows_bytes) {
-    const int tiles = (A::kBytes + B::kBytes) * (direct ? 2 : 1), rows = 4 * rows_bytes;
+    const int tiles = (A::kBytes + B::kBytes) * (direct ? 3 : 1), rows = 4 * rows_bytes;
     return tiles > rows ? tiles : rows;
 }
 
