@@ -18,6 +18,8 @@ namespace wino {
 
 namespace {
 
+__host__ __device__ inline int64_t tiles_of(int64_t n, int each) { return (n + each - 1) / each; }
+
 struct GatedK {
     GatedArgs a;
     int64_t M;
@@ -128,10 +130,16 @@ struct Side<T, I, T_, true> : Side<T, I, T_, false> {
 };
 
 // acc[i][j] = products of the wave's left block i and right block j, over the terms lo .. hi.
-// Left block i of wave column wa: i * WA + wa.
-template <typename S, typename A, typename B>
+// Left block i of wave column wa: i * WA + wa.  after(i, t), straight to LDS alone: issues
+// kAfter loads to a copy t whose tiles are done with, as the last steps begin (i 0 and 1);
+// they have arrived when their reader is ready().
+struct Nothing {
+    static constexpr int kAfter = 0;
+    __device__ __forceinline__ void operator()(int, char*) const {}
+};
+template <typename S, typename A, typename B, typename F = Nothing>
 __device__ __forceinline__ void product(f32x16 (&acc)[S::AB][S::BB], A& a, B& b, char* lds, int64_t lo, int64_t hi,
-                                        bool direct) {
+                                        bool direct, const F& after = F()) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wa = wave % S::WA, wb = wave / S::WA;
     constexpr int kBoth = A::kBytes + B::kBytes;
@@ -151,9 +159,17 @@ __device__ __forceinline__ void product(f32x16 (&acc)[S::AB][S::BB], A& a, B& b,
         char* t = lds + copy * kBoth;
         if (direct) {
             if (k + kBk < hi) ready<A::kLoads + B::kLoads>();
+            else if (k > lo) ready<F::kAfter>();
             else ready<0>();
-            if (k + 2 * kBk < hi) load(copy == 0 ? 2 : copy - 1, k + 2 * kBk);
+            const int before = copy == 0 ? 2 : copy - 1;
             copy = copy == 2 ? 0 : copy + 1;
+            if (k + 2 * kBk < hi) {
+                load(before, k + 2 * kBk);
+            } else if (F::kAfter > 0) {
+                const bool last = k + kBk >= hi;
+                if (!last || k == lo) after(0, lds + before * kBoth);
+                if (last) after(1, lds + (k == lo ? copy : before) * kBoth);
+            }
         } else {
             __syncthreads();
             a.store(t);
@@ -174,7 +190,8 @@ __device__ __forceinline__ void product(f32x16 (&acc)[S::AB][S::BB], A& a, B& b,
                 for (int j = 0; j < S::BB; ++j) acc[i][j] = mma(fa[i], fb[j], acc[i][j]);
         }
     }
-    __syncthreads();                         // the tiles' LDS is free
+    if (F::kAfter > 0) ready<0>();
+    else __syncthreads();                    // the tiles' LDS is free
 }
 
 // A wave's 32 rows by 64 columns on their way between a lane's order (a row; columns 32 w
@@ -274,24 +291,35 @@ __device__ __forceinline__ void gate_slope(float z, Act act, float& v, float& d)
     }
 }
 
-// Four neighbouring values at p + d, those from D on zero.
-template <typename T>
-__device__ __forceinline__ void load4(const T* p, int d, int D, bool vec, float (&v)[4]) {
-    if (vec) {
-        const Raw<T, 4> r = d < D ? *(const Raw<T, 4>*)(p + d) : Raw<T, 4>{};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = (float)r.v[i];
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = d + i < D ? (float)p[d + i] : 0.0f;
-}
-
 template <typename S, typename A, typename B>
 constexpr int lds_of(bool direct, int rows_bytes) {
     const int tiles = (A::kBytes + B::kBytes) * (direct ? 3 : 1), rows = 4 * rows_bytes;
     return tiles > rows ? tiles : rows;
 }
+
+// dy of 128 tokens (32 of each wave) by 64 units, straight to LDS while a wide tile's last
+// steps run: read afterwards, it held up every workgroup twice (200704 tokens of 256 channels by
+// 1024 units: 620 us).
+template <typename T>
+struct DyTiles {
+    using Tl = Tile<T, 4, 128>;
+    using Dir = Direct<Tl, 128, 256>;
+    static constexpr int kAfter = Dir::kN;
+    Dir d;
+    const T* p;
+    int64_t left;
+    int K, cols;
+    char** at;
+    __device__ __forceinline__ DyTiles(const T* p_, int64_t left_, int K_, int cols_, char** at_)
+        : p(p_), left(left_), K(K_), cols(cols_), at(at_) {
+        d.init((cols + 7) / 8, [&](int r, int chunk) { return (uint32_t)(r / 32 * 64 + r % 32) * (uint32_t)K * 2 + chunk * 16; });
+    }
+    __device__ __forceinline__ void operator()(int i, char* t) const {
+        at[i] = t;
+        const int64_t n = left - 32 * i;             // tokens from this block's first on
+        d.issue(t, p + (int64_t)32 * i * K, n > 0 ? (uint32_t)((n - 1) * K + cols) * 2 : 0);
+    }
+};
 
 // y of a tile's tokens and units (its left rows are their gates, then their values, so that
 // both of a unit meet in one lane), or dz of them and the tile's sums of it.
@@ -307,18 +335,39 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void k_gated(GatedK 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     const int64_t mt = item / g.tiles, m0 = mt * S::kB;
     const int u0 = (int)(item - mt * g.tiles) * kUnits, K = g.K;
+    constexpr bool kAhead = BACK && kDirect && S::AB == 4;
+    // loaded once: a load between stores would wait for them
+    __shared__ alignas(16) float bias[2 * kUnits];
+    if (threadIdx.x < 2 * kUnits) {
+        const int u = u0 + threadIdx.x % kUnits;
+        bias[threadIdx.x] = g.a.bias && u < K ? g.a.bias[threadIdx.x / kUnits * K + u] : 0.0f;
+    }
+    char* dys[2] = {lds, lds};
     f32x16 acc[S::AB][S::BB];                            // gates, then values, by blocks of 32 tokens
     {
         A a;
         B b;
         a.init({(const T*)g.a.w + (int64_t)u0 * g.C, 2 * (int64_t)K - u0, g.C, g.C, kUnits, K - kUnits}, g.vec);
         b.init({(const T*)g.a.x + m0 * g.C, g.M - m0 < S::kB ? g.M - m0 : S::kB, g.C, g.C, S::kB, 0}, g.vec);
-        product<S>(acc, a, b, lds, 0, g.C, kDirect);
+        if constexpr (kAhead) {
+            const DyTiles<T> dy((const T*)g.a.dy + m0 * K + u0, g.M - m0 < S::kB ? g.M - m0 : S::kB, K,
+                                K - u0 < kUnits ? K - u0 : kUnits, dys);
+            product<S>(acc, a, b, lds, 0, g.C, true, dy);
+        } else {
+            product<S>(acc, a, b, lds, 0, g.C, kDirect);
+        }
     }
-    // a wave's 32 tokens by 64 columns at a time: its units' gates, or their values
-    const Rows rows{lds + wave * Rows::kBytes};
+    // a wave's 32 tokens by 64 columns at a time: its units' gates, or their values; where dy
+    // is there already, in the copy that the last step read
+    char* free = lds;
+    if constexpr (kAhead) {
+        constexpr int kBoth = A::kBytes + B::kBytes;
+        static_assert(kBoth >= 4 * Rows::kBytes && kBoth >= DyTiles<T>::Tl::kBytes);
+        free = lds + (tiles_of(g.C, kBk) - 1) % 3 * kBoth;
+    }
+    const Rows rows{free + wave * Rows::kBytes};
     const int wa = wave % S::WA, wb = wave / S::WA;
-    static_assert(S::AB == 2 || S::WA == 1);
+    static_assert(S::AB == 2 || S::WA == 1);   // a wave's units are next to each other
     // unit of (block i, b, i): blocks of a wave's units are 32 (i WA + wa)
     const int cols = 32 * UB, ub = u0 + 32 * wa;
     const int have = K - ub < cols ? K - ub : cols;     // may be negative
@@ -336,7 +385,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void k_gated(GatedK 
         const int64_t m = m0 + (wb * S::BB + j) * 32;
         const int left = (int)(g.M - m < 32 ? g.M - m : 32);
         if (left <= 0) continue;
-        if constexpr (BACK) {
+        if constexpr (BACK && !kAhead) {
             rows.template move<false>((const T*)g.a.dy + m * K + ub, K, left, have, g.vec);
             wave_sync();
         }
@@ -346,12 +395,15 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void k_gated(GatedK 
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
                 const int c = 32 * i + 8 * b + 4 * h;
-                float bg[4] = {0, 0, 0, 0}, bu[4] = {0, 0, 0, 0}, dy[4];
-                if (g.a.bias) {
-                    load4(g.a.bias, ub + c, K, false, bg);
-                    load4(g.a.bias + K, ub + c, K, false, bu);
-                }
-                if constexpr (BACK) {
+                const f32x4v bg = *(const f32x4v*)&bias[32 * wa + c], bu = *(const f32x4v*)&bias[kUnits + 32 * wa + c];
+                float dy[4];
+                if constexpr (kAhead) {
+                    using D = typename DyTiles<T>::Tl;
+                    T o[4];
+                    __builtin_memcpy(o, __builtin_assume_aligned(dys[j] + D::at(wb * 32 + (lane & 31), c >> 3) + 8 * h, 8), 8);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) dy[e] = (float)o[e];
+                } else if constexpr (BACK) {
                     rows.get4(c, dy);
                     // past the tokens LDS holds what was there
                     if (left < 32 && (lane & 31) >= left) dy[0] = dy[1] = dy[2] = dy[3] = 0.0f;
@@ -532,7 +584,6 @@ GatedK args_of(const GatedArgs& a, const GatedShape& s) {
     return g;
 }
 
-inline int64_t tiles_of(int64_t n, int each) { return (n + each - 1) / each; }
 
 // Shapes for a product of p by q results: the widest whose tiles fill the card twice over
 // (fp32: operands of the wide one pass a wave's registers).
