@@ -25,7 +25,7 @@ struct GatedArgs {
 struct GatedPlan {
     bool fits;
     int first, dx, dw;                       // tile shapes of the products
-    int splits;                              // of the sum over tokens in dw
+    int dx_splits, dw_splits;                // parts of the sums over units and over tokens
     size_t dz, dbias, part, need;            // workspace: bytes of each region
 };
 GatedPlan gated_plan(const GatedShape& s, bool backward);

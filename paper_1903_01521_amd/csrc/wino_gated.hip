@@ -44,6 +44,7 @@ struct Shape {
 using Wide = Shape<4, 2, 1, 4>;              // 128 x 256
 using Square = Shape<2, 2, 2, 2>;            // 128 x 128
 using Narrow = Shape<2, 1, 1, 4>;            // 64 x 128
+using Small = Shape<1, 1, 2, 2>;             // 64 x 64
 
 constexpr int kBk = 32;                      // terms of a step
 
@@ -94,39 +95,74 @@ struct Side {
         else return Tl::read(t, 32 * blk + (lane & 31), c, lane >> 5);
     }
 };
-// Straight to LDS: 16-bit values in whole 16-byte words, a tile within 2^31 bytes.
-template <typename T, int I, bool T_>
-struct Side<T, I, T_, true> : Side<T, I, T_, false> {
-    using Base = Side<T, I, T_, false>;
-    using Tl = typename Base::Tl;
-    using Dir = Direct<Tl, Base::kRows, 256>;
-    static constexpr int kLoads = Dir::kN * Base::kParts;     // of a lane, a tile
-    Dir d[Base::kParts];
-    __device__ __forceinline__ void init(const Source<T>& s, bool) {
-        this->s = s;
+// fp32 as it is in memory: R rows of W values.  Operands are split as they are read: 22
+// vector instructions for eight values, beside the 6 products of 32 cycles each that they
+// enter, and the tile is on its way while two others are worked on.
+template <int R, int W>
+struct Whole {
+    static constexpr int kRow = W * 4, kBytes = R * kRow;
+    __device__ static __forceinline__ int twist(int row) { return kRow == 128 ? ((row & 2) << 1) | ((row >> 2) & 3) : 0; }
+    __device__ static __forceinline__ int at(int row, int chunk) { return row * kRow + ((chunk ^ twist(row)) << 4); }
+    __device__ static __forceinline__ Frag<float> read(const char* t, int row, int c, int h) {
+        float x[8];
 #pragma unroll
-        for (int i = 0; i < Base::kParts; ++i)
-            d[i].init(T_ ? (s.cols - i * Base::kCols + 7) / 8 : 1 << 20, [&](int r, int chunk) {
+        for (int e = 0; e < 2; ++e) {
+            const f32x4v v = *(const f32x4v*)(t + at(row, 4 * c + 2 * h + e));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[4 * e + i] = v[i];
+        }
+        return frag_of<float>(x);
+    }
+    // column 32 db + lane % 32 of rows r + 8 h .. + 7
+    __device__ static __forceinline__ Frag<float> turned8(const char* t, int r, int db, int lane) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            x[i] = *(const float*)(t + (r + 8 * (lane >> 5) + i) * kRow + (32 * db + (lane & 31)) * 4);
+        return frag_of<float>(x);
+    }
+};
+
+// Straight to LDS: values in whole 16-byte words, a tile within 2^31 bytes.
+template <typename T, int I, bool T_>
+struct Side<T, I, T_, true> {
+    static constexpr int kRows = T_ ? kBk : I;
+    static constexpr int kCols = T_ ? (I < 128 ? I : 128) : kBk, kParts = T_ ? I / kCols : 1;
+    using Tl = std::conditional_t<sizeof(T) == 4, Whole<kRows, kCols>, Tile<T, kCols / 16, kRows>>;
+    using Dir = Direct<Tl, kRows, 256>;
+    static constexpr int kBytes = Tl::kBytes * kParts, kEach = 16 / (int)sizeof(T), kSize = sizeof(T);
+    static constexpr int kLoads = Dir::kN * kParts;                 // of a lane, a tile
+    Source<T> s;
+    Dir d[kParts];
+    __device__ __forceinline__ void init(const Source<T>& s_, bool) {
+        s = s_;
+#pragma unroll
+        for (int i = 0; i < kParts; ++i)
+            d[i].init(T_ ? (s.cols - i * kCols + kEach - 1) / kEach : 1 << 20, [&](int r, int chunk) {
                 const uint32_t row = (uint32_t)r + (!T_ && r >= s.split ? (uint32_t)s.jump : 0u);
-                return row * (uint32_t)s.ld * 2 + chunk * 16 + i * Base::kCols * 2;
+                return row * (uint32_t)s.ld * kSize + chunk * 16 + i * kCols * kSize;
             });
     }
     __device__ __forceinline__ void load(char* t, int64_t k, int64_t hi) {
-        const Source<T>& s = this->s;
         if constexpr (T_) {
             const int64_t left = hi - k;
             const uint32_t last = (uint32_t)(left < kBk ? left : kBk) - 1;
 #pragma unroll
-            for (int i = 0; i < Base::kParts; ++i)
-                d[i].issue(t + i * Tl::kBytes, s.p + k * s.ld, (last * (uint32_t)s.ld + (uint32_t)s.cols) * 2);
+            for (int i = 0; i < kParts; ++i)
+                d[i].issue(t + i * Tl::kBytes, s.p + k * s.ld, (last * (uint32_t)s.ld + (uint32_t)s.cols) * kSize);
         } else {
-            const int64_t bytes = ((s.rows - 1) * s.ld + (s.cols - k)) * 2;
+            const int64_t bytes = ((s.rows - 1) * s.ld + (s.cols - k)) * kSize;
             const uint32_t n = bytes < 0x7fffffff ? (uint32_t)bytes : 0x7fffffffu;
             if (hi - k >= kBk) d[0].issue(t, s.p + k, n);
-            else d[0].issue_part(t, s.p + k, n, (int)(hi - k + 7) / 8);
+            else d[0].issue_part(t, s.p + k, n, (int)(hi - k + kEach - 1) / kEach);
         }
     }
     __device__ __forceinline__ void store(char*) const {}
+    // terms 16 c .. of indices 32 blk ..
+    __device__ static __forceinline__ Frag<T> read(const char* t, int blk, int c, int lane) {
+        if constexpr (T_) return Tl::turned8(t + blk / (kCols / 32) * Tl::kBytes, 16 * c, blk % (kCols / 32), lane);
+        else return Tl::read(t, 32 * blk + (lane & 31), c, lane >> 5);
+    }
 };
 
 // acc[i][j] = products of the wave's left block i and right block j, over the terms lo .. hi.
@@ -335,7 +371,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void k_gated(GatedK 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     const int64_t mt = item / g.tiles, m0 = mt * S::kB;
     const int u0 = (int)(item - mt * g.tiles) * kUnits, K = g.K;
-    constexpr bool kAhead = BACK && kDirect && S::AB == 4;
+    constexpr bool kAhead = BACK && kDirect && S::AB == 4 && sizeof(T) == 2;
     // loaded once: a load between stores would wait for them
     __shared__ alignas(16) float bias[2 * kUnits];
     if (threadIdx.x < 2 * kUnits) {
@@ -480,7 +516,7 @@ __device__ __forceinline__ void put_tile(const f32x16 (&acc)[S::AB][S::BB], char
         const int left = (int)(Q - q < 32 ? Q - q : 32);
         if (left <= 0) continue;
         // with more waves than one a block's columns are not next to the next one's
-        constexpr int each = S::WA == 1 ? 2 : 1;
+        constexpr int each = S::WA == 1 && S::AB > 1 ? 2 : 1;
 #pragma unroll
         for (int i = 0; i < S::AB; i += each) {
             const int p = p0 + 32 * (i * S::WA + wa);
@@ -497,23 +533,26 @@ __device__ __forceinline__ void put_tile(const f32x16 (&acc)[S::AB][S::BB], char
     }
 }
 
-// dx of a tile's tokens and channels: dz [M][2 K] by w [2 K][C].
+// dx of a tile's tokens and channels: dz [M][2 K] by w [2 K][C], over a part of the units.
 template <typename T, typename S, bool kDirect>
 __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void k_gated_dx(GatedK g) {
     using A = Side<T, S::kA, true, kDirect>;
     using B = Side<T, S::kB, false, kDirect>;
-    __shared__ alignas(16) char lds[lds_of<S, A, B>(kDirect, Rows64<T>::kBytes)];
+    __shared__ alignas(16) char lds[lds_of<S, A, B>(kDirect, Rows64<float>::kBytes)];
     const int64_t item = item_of(g.items);
     if (item < 0) return;
-    const int64_t mt = item / g.tiles, m0 = mt * S::kB;
-    const int c0 = (int)(item - mt * g.tiles) * S::kA, F = 2 * g.K;
+    const int64_t at = item / g.tiles, mt = at / g.splits, m0 = mt * S::kB;
+    const int c0 = (int)(item - at * g.tiles) * S::kA, F = 2 * g.K, split = (int)(at - mt * g.splits);
+    int64_t lo, hi;
+    part_of(F, kBk, split, g.splits, lo, hi);
     f32x16 acc[S::AB][S::BB];
     A a;
     B b;
     a.init({(const T*)g.a.w + c0, F, g.C - c0, g.C, kBk, 0}, g.vec);
     b.init({(const T*)g.dz + m0 * F, g.M - m0 < S::kB ? g.M - m0 : S::kB, F, F, S::kB, 0}, g.vec);
-    product<S>(acc, a, b, lds, 0, F, kDirect);
-    put_tile<S>(acc, lds, (T*)g.a.dx, c0, g.C, m0, g.M, g.vec);
+    product<S>(acc, a, b, lds, lo, hi, kDirect);
+    if (g.splits > 1) put_tile<S>(acc, lds, g.part + split * g.M * g.C, c0, g.C, m0, g.M, (g.C & 3) == 0);
+    else put_tile<S>(acc, lds, (T*)g.a.dx, c0, g.C, m0, g.M, g.vec);
 }
 
 // dw of a tile's units and channels, over a part of the tokens: dz^T by x.
@@ -539,13 +578,14 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void k_gated_dw(Gate
     else put_tile<S>(acc, lds, (T*)g.a.dw, c0, g.C, f0, F, g.vec);
 }
 
+// n sums of `splits` parts.
 template <typename T>
-__global__ __launch_bounds__(256) void k_gated_dw_sum(GatedK g) {
-    const int64_t all = (int64_t)2 * g.K * g.C, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= all) return;
+__global__ __launch_bounds__(256) void k_gated_sum(const float* part, T* out, int64_t n, int splits) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= n) return;
     float sum = 0.0f;
-    for (int k = 0; k < g.splits; ++k) sum += g.part[k * all + i];
-    ((T*)g.a.dw)[i] = (T)sum;
+    for (int k = 0; k < splits; ++k) sum += part[k * n + i];
+    out[i] = (T)sum;
 }
 
 // dbias: 16 columns a workgroup, 16 threads a column.
@@ -585,44 +625,42 @@ GatedK args_of(const GatedArgs& a, const GatedShape& s) {
 }
 
 
-// Shapes for a product of p by q results: the widest whose tiles fill the card twice over
-// (fp32: operands of the wide one pass a wave's registers).
-enum { kWide, kSquare, kNarrow };
+// Shapes for a product of p by q results whose sum may go in `parts` parts: the widest whose
+// tiles fill the card twice over (fp32: operands of the wide one pass a wave's registers).
+enum { kWide, kSquare, kNarrow, kSmall };
 int shape_of(int64_t p, int64_t q, int64_t parts, Io io) {
     if (io != Io::F32 && tiles_of(p, Wide::kA) * tiles_of(q, Wide::kB) * parts >= 512) return kWide;
-    return tiles_of(p, Square::kA) * tiles_of(q, Square::kB) * parts >= 512 ? kSquare : kNarrow;
+    if (tiles_of(p, Square::kA) * tiles_of(q, Square::kB) * parts >= 512) return kSquare;
+    return tiles_of(p, Narrow::kA) * tiles_of(q, Narrow::kB) * parts >= 512 ? kNarrow : kSmall;
 }
-template <typename F>
-auto with_shape(int shape, F f) {
-    return shape == kWide ? f(Wide()) : shape == kSquare ? f(Square()) : f(Narrow());
+int64_t tiles_by(int shape, int64_t p, int64_t q) {
+    return shape == kWide     ? tiles_of(p, Wide::kA) * tiles_of(q, Wide::kB)
+           : shape == kSquare ? tiles_of(p, Square::kA) * tiles_of(q, Square::kB)
+           : shape == kNarrow ? tiles_of(p, Narrow::kA) * tiles_of(q, Narrow::kB)
+                              : tiles_of(p, Small::kA) * tiles_of(q, Small::kB);
+}
+// Parts that fill the card with 512 workgroups, `most` at most.
+int parts_of(int64_t tiles, int64_t most) {
+    const int64_t want = (512 + tiles - 1) / tiles, n = want < most ? want : most;
+    return n < 1 ? 1 : n > 64 ? 64 : (int)n;
 }
 
-// f(type, shape, straight to LDS)
-template <typename F>
+// f(type, shape, straight to LDS); kUnits: a unit's gate and value are to be in one wave
+template <bool kPairs, typename F>
 hipError_t with_all(const GatedK& g, Io io, int shape, F f) {
     // offsets of a tile's rows, and from a unit's gate to its value, below 2^31
-    const bool direct = g.vec && io != Io::F32 && g.C <= 1 << 21 && g.K <= 1 << 20 && (int64_t)g.K * g.C < 1 << 28;
+    const bool direct = g.vec && g.C <= 1 << 20 && g.K <= 1 << 19 && (int64_t)g.K * g.C < 1 << 27;
     return with_io(io, [&](auto t) {
-        typedef decltype(t) T;
-        if constexpr (sizeof(T) == 2) {
-            if (direct) return with_shape(shape, [&](auto s) { return f(t, s, std::true_type()); });
-            return with_shape(shape, [&](auto s) { return f(t, s, std::false_type()); });
-        } else {
-            // Wide is not taken
-            return shape == kSquare ? f(t, Square(), std::false_type()) : f(t, Narrow(), std::false_type());
-        }
+        auto shaped = [&](auto d) {
+            if constexpr (sizeof(t) == 2)
+                if (shape == kWide) return f(t, Wide(), d);
+            if (shape == kSquare) return f(t, Square(), d);
+            if constexpr (!kPairs)
+                if (shape == kSmall) return f(t, Small(), d);
+            return f(t, Narrow(), d);
+        };
+        return direct ? shaped(std::true_type()) : shaped(std::false_type());
     });
-}
-
-int splits_for(const GatedShape& s, int shape) {
-    int64_t tiles = 0;
-    with_shape(shape, [&](auto sh) {
-        tiles = tiles_of(s.C, decltype(sh)::kA) * tiles_of(2 * (int64_t)s.K, decltype(sh)::kB);
-        return 0;
-    });
-    // 512 workgroups fill the card; a part has 256 tokens at least
-    const int64_t want = (512 + tiles - 1) / tiles, most = s.M / 256, n = want < most ? want : most;
-    return n < 1 ? 1 : n > 64 ? 64 : (int)n;
 }
 
 }  // namespace
@@ -631,26 +669,33 @@ GatedPlan gated_plan(const GatedShape& s, bool backward) {
     GatedPlan p{};
     const int64_t most = (int64_t)1 << 30, F = 2 * (int64_t)s.K;
     // counts of the smallest tiles
-    const int64_t mt = tiles_of(s.M, Narrow::kB), ut = tiles_of(s.K, Narrow::kA / 2), ct = tiles_of(s.C, Narrow::kA);
+    const int64_t mt = tiles_of(s.M, Small::kB), ut = tiles_of(s.K, Narrow::kA / 2), ct = tiles_of(s.C, Small::kA);
     p.fits = s.M <= INT32_MAX && s.K <= INT32_MAX / 2 && mt * ut <= most && mt * ct <= most &&
-             ct * tiles_of(F, Narrow::kB) <= most / 64 && (int64_t)s.K * s.C < (int64_t)1 << 37;
+             ct * tiles_of(F, Small::kB) <= most / 64 && (int64_t)s.K * s.C < (int64_t)1 << 37;
     if (!p.fits) return p;
     p.first = shape_of(F, s.M, 1, s.io);
+    if (p.first == kSmall) p.first = kNarrow;
     if (!backward) return p;
+    // parts of 256 units or tokens at least
     p.dx = shape_of(s.C, s.M, 1, s.io);
-    // the sum over tokens is cut as finely as it takes
-    p.dw = s.io != Io::F32 && s.C > Narrow::kA ? kWide : s.C > Narrow::kA ? kSquare : kNarrow;
-    p.splits = splits_for(s, p.dw);
+    p.dx_splits = p.dx == kSmall ? parts_of(tiles_by(kSmall, s.C, s.M), F / 256) : 1;
+    const int64_t parts = s.M / 256 < 1 ? 1 : s.M / 256 < 64 ? s.M / 256 : 64;
+    p.dw = shape_of(s.C, F, parts, s.io);
+    // no wider than the channels are
+    if (p.dw < kNarrow && s.C <= Narrow::kA) p.dw = kNarrow;
+    p.dw_splits = parts_of(tiles_by(p.dw, s.C, F), parts);
     p.dz = round_up((size_t)s.M * F * io_size(s.io), 16);
-    p.dbias = round_up((size_t)mt * F * 4, 16);
-    p.part = p.splits > 1 ? round_up((size_t)p.splits * F * s.C * 4, 16) : 0;
+    p.dbias = round_up((size_t)tiles_of(s.M, Narrow::kB) * F * 4, 16);
+    const size_t x = p.dx_splits > 1 ? (size_t)p.dx_splits * s.M * s.C * 4 : 0;
+    const size_t w = p.dw_splits > 1 ? (size_t)p.dw_splits * F * s.C * 4 : 0;
+    p.part = round_up(x > w ? x : w, 16);
     p.need = p.dz + p.dbias + p.part;
     return p;
 }
 
 hipError_t launch_gated(const GatedArgs& a, const GatedShape& s, const GatedPlan& p, hipStream_t st) {
     GatedK g = args_of(a, s);
-    return with_all(g, s.io, p.first, [&](auto t, auto sh, auto direct) {
+    return with_all<true>(g, s.io, p.first, [&](auto t, auto sh, auto direct) {
         typedef decltype(sh) S;
         g.tiles = tiles_of(s.K, S::kA / 2);
         g.items = tiles_of(s.M, S::kB) * g.tiles;
@@ -661,11 +706,12 @@ hipError_t launch_gated(const GatedArgs& a, const GatedShape& s, const GatedPlan
 
 hipError_t launch_gated_backward(const GatedArgs& a, const GatedShape& s, const GatedPlan& p, void* ws, hipStream_t st) {
     GatedK g = args_of(a, s);
+    const int64_t F = 2 * (int64_t)s.K;
     g.dz = ws;
     g.dbias = (float*)((char*)ws + p.dz);
     g.part = (float*)((char*)ws + p.dz + p.dbias);
     int64_t rows = 0;
-    hipError_t e = with_all(g, s.io, p.first, [&](auto t, auto sh, auto direct) {
+    hipError_t e = with_all<true>(g, s.io, p.first, [&](auto t, auto sh, auto direct) {
         typedef decltype(sh) S;
         g.tiles = tiles_of(s.K, S::kA / 2);
         rows = tiles_of(s.M, S::kB);
@@ -675,30 +721,35 @@ hipError_t launch_gated_backward(const GatedArgs& a, const GatedShape& s, const 
     });
     if (e != hipSuccess) return e;
     if (a.dbias) {
-        k_gated_db<<<(unsigned)tiles_of(2 * (int64_t)s.K, 16), 256, 0, st>>>(g, rows);
+        k_gated_db<<<(unsigned)tiles_of(F, 16), 256, 0, st>>>(g, rows);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
+    auto sum = [&](auto t, void* out, int64_t n) {
+        if (g.splits == 1) return hipSuccess;
+        k_gated_sum<<<(unsigned)tiles_of(n, 256), 256, 0, st>>>(g.part, (decltype(t)*)out, n, g.splits);
+        return hipGetLastError();
+    };
     if (a.dx) {
-        e = with_all(g, s.io, p.dx, [&](auto t, auto sh, auto direct) {
+        e = with_all<false>(g, s.io, p.dx, [&](auto t, auto sh, auto direct) {
             typedef decltype(sh) S;
+            g.splits = p.dx_splits;
             g.tiles = tiles_of(s.C, S::kA);
-            g.items = tiles_of(s.M, S::kB) * g.tiles;
+            g.items = tiles_of(s.M, S::kB) * g.tiles * g.splits;
             k_gated_dx<decltype(t), S, direct.value><<<grid_of(g.items), 256, 0, st>>>(g);
-            return hipGetLastError();
+            const hipError_t e = hipGetLastError();
+            return e != hipSuccess ? e : sum(t, a.dx, s.M * s.C);
         });
         if (e != hipSuccess) return e;
     }
     if (!a.dw) return hipSuccess;
-    return with_all(g, s.io, p.dw, [&](auto t, auto sh, auto direct) {
+    return with_all<false>(g, s.io, p.dw, [&](auto t, auto sh, auto direct) {
         typedef decltype(sh) S;
-        g.splits = p.splits;
+        g.splits = p.dw_splits;
         g.tiles = tiles_of(s.C, S::kA);
-        g.items = g.tiles * tiles_of(2 * (int64_t)s.K, S::kB) * g.splits;
+        g.items = g.tiles * tiles_of(F, S::kB) * g.splits;
         k_gated_dw<decltype(t), S, direct.value><<<grid_of(g.items), 256, 0, st>>>(g);
         const hipError_t e = hipGetLastError();
-        if (e != hipSuccess || g.splits == 1) return e;
-        k_gated_dw_sum<decltype(t)><<<(unsigned)tiles_of((int64_t)2 * s.K * s.C, 256), 256, 0, st>>>(g);
-        return hipGetLastError();
+        return e != hipSuccess ? e : sum(t, a.dw, F * s.C);
     });
 }
 
