@@ -60,6 +60,7 @@ struct Source {
 // One operand's tile of I indices by kBk terms.
 template <typename T, int I, bool T_, bool kDirect>
 struct Side {
+    typedef T Value;
     static constexpr int kRows = T_ ? kBk : I;
     // rows of more than 128 values in halves of 128, each a tile
     static constexpr int kCols = T_ ? (I < 128 ? I : 128) : kBk, kParts = T_ ? I / kCols : 1;
@@ -126,6 +127,7 @@ struct Whole {
 // Straight to LDS: values in whole 16-byte words, a tile within 2^31 bytes.
 template <typename T, int I, bool T_>
 struct Side<T, I, T_, true> {
+    typedef T Value;
     static constexpr int kRows = T_ ? kBk : I;
     static constexpr int kCols = T_ ? (I < 128 ? I : 128) : kBk, kParts = T_ ? I / kCols : 1;
     using Tl = std::conditional_t<sizeof(T) == 4, Whole<kRows, kCols>, Tile<T, kCols / 16, kRows>>;
@@ -165,6 +167,13 @@ struct Side<T, I, T_, true> {
     }
 };
 
+// Copies of the tiles that lie in LDS straight from memory; of fp32's squares two, for two
+// workgroups a CU.
+template <typename T, typename S>
+constexpr int copies_of() {
+    return sizeof(T) == 4 && S::AB * S::BB == 4 ? 2 : 3;
+}
+
 // acc[i][j] = products of the wave's left block i and right block j, over the terms lo .. hi.
 // Left block i of wave column wa: i * WA + wa.  after(i, t), straight to LDS alone: issues
 // kAfter loads to a copy t whose tiles are done with, as the last steps begin (i 0 and 1);
@@ -187,20 +196,21 @@ __device__ __forceinline__ void product(f32x16 (&acc)[S::AB][S::BB], A& a, B& b,
         a.load(lds + copy * kBoth, k, hi);
         b.load(lds + copy * kBoth + A::kBytes, k, hi);
     };
-    // straight to LDS: two steps ahead, in three copies
+    // straight to LDS: one step ahead in two copies, two steps in three
+    constexpr int N = copies_of<typename A::Value, S>();
     int copy = 0;
     if (lo < hi) load(0, lo);
-    if (direct && lo + kBk < hi) load(1, lo + kBk);
+    if (direct && N == 3 && lo + kBk < hi) load(1, lo + kBk);
     for (int64_t k = lo; k < hi; k += kBk) {
         char* t = lds + copy * kBoth;
         if (direct) {
-            if (k + kBk < hi) ready<A::kLoads + B::kLoads>();
-            else if (k > lo) ready<F::kAfter>();
+            if (N == 3 && k + kBk < hi) ready<A::kLoads + B::kLoads>();
+            else if (N == 3 && k > lo) ready<F::kAfter>();
             else ready<0>();
-            const int before = copy == 0 ? 2 : copy - 1;
-            copy = copy == 2 ? 0 : copy + 1;
-            if (k + 2 * kBk < hi) {
-                load(before, k + 2 * kBk);
+            const int before = copy == 0 ? N - 1 : copy - 1;
+            copy = copy == N - 1 ? 0 : copy + 1;
+            if (k + (N - 1) * kBk < hi) {
+                load(before, k + (N - 1) * kBk);
             } else if (F::kAfter > 0) {
                 const bool last = k + kBk >= hi;
                 if (!last || k == lo) after(0, lds + before * kBoth);
@@ -329,7 +339,7 @@ __device__ __forceinline__ void gate_slope(float z, Act act, float& v, float& d)
 
 template <typename S, typename A, typename B>
 constexpr int lds_of(bool direct, int rows_bytes) {
-    const int tiles = (A::kBytes + B::kBytes) * (direct ? 3 : 1), rows = 4 * rows_bytes;
+    const int tiles = (A::kBytes + B::kBytes) * (direct ? copies_of<typename A::Value, S>() : 1), rows = 4 * rows_bytes;
     return tiles > rows ? tiles : rows;
 }
 
@@ -360,7 +370,7 @@ struct DyTiles {
 // y of a tile's tokens and units (its left rows are their gates, then their values, so that
 // both of a unit meet in one lane), or dz of them and the tile's sums of it.
 template <typename T, typename S, bool BACK, bool kDirect>
-__global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void k_gated(GatedK g) {
+__global__ __launch_bounds__(256, 2) void k_gated(GatedK g) {
     constexpr int kUnits = S::kA / 2, UB = S::AB / 2;
     using A = Side<T, S::kA, false, kDirect>;
     using B = Side<T, S::kB, false, kDirect>;
@@ -535,7 +545,7 @@ __device__ __forceinline__ void put_tile(const f32x16 (&acc)[S::AB][S::BB], char
 
 // dx of a tile's tokens and channels: dz [M][2 K] by w [2 K][C], over a part of the units.
 template <typename T, typename S, bool kDirect>
-__global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void k_gated_dx(GatedK g) {
+__global__ __launch_bounds__(256, 2) void k_gated_dx(GatedK g) {
     using A = Side<T, S::kA, true, kDirect>;
     using B = Side<T, S::kB, false, kDirect>;
     __shared__ alignas(16) char lds[lds_of<S, A, B>(kDirect, Rows64<float>::kBytes)];
@@ -557,7 +567,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void k_gated_dx(Gate
 
 // dw of a tile's units and channels, over a part of the tokens: dz^T by x.
 template <typename T, typename S, bool kDirect>
-__global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void k_gated_dw(GatedK g) {
+__global__ __launch_bounds__(256, 2) void k_gated_dw(GatedK g) {
     using A = Side<T, S::kA, true, kDirect>;
     using B = Side<T, S::kB, true, kDirect>;
     __shared__ alignas(16) char lds[lds_of<S, A, B>(kDirect, Rows64<float>::kBytes)];
