@@ -513,6 +513,61 @@ __global__ __launch_bounds__(256, 2) void k_gated(GatedK g) {
     }
 }
 
+// A few tokens: a wave for each unit, its lanes along the channels, eight at a time.  All
+// there is to do is to read the weights once (in tiles of 32 units 2048 of them are 64
+// workgroups: one token of 512 channels 9.1 us).
+constexpr int kFewTokens = 8;
+
+__device__ __forceinline__ float sum64(float x) {
+#define WINO_ROTATED(ctrl) __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), ctrl, 15, 15, true))
+    x += WINO_ROTATED(0x128);                // row_ror:8, 4, 2, 1
+    x += WINO_ROTATED(0x124);
+    x += WINO_ROTATED(0x122);
+    x += WINO_ROTATED(0x121);
+#undef WINO_ROTATED
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return add_halves(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+template <typename T, int MT>
+__global__ __launch_bounds__(256) void k_gated_few(GatedK g) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t u = (int64_t)blockIdx.x * 4 + wave;
+    if (u >= g.K) return;
+    const int C = g.C, M = (int)g.M;
+    const T *w0 = (const T*)g.a.w + u * C, *w1 = w0 + (int64_t)g.K * C, *x = (const T*)g.a.x;
+    float z[2][MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) z[0][m] = z[1][m] = 0.0f;
+    for (int c = lane * 8; c < C; c += 512) {
+        const Eight<T> a(w0 + c, 0, 0, C - c, g.vec), b(w1 + c, 0, 0, C - c, g.vec);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            const Eight<T> v(m < M ? x + (int64_t)m * C + c : nullptr, 0, 0, C - c, g.vec);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                z[0][m] = __builtin_fmaf((float)a.v[i], (float)v.v[i], z[0][m]);
+                z[1][m] = __builtin_fmaf((float)b.v[i], (float)v.v[i], z[1][m]);
+            }
+        }
+    }
+    float zg = 0.0f, zu = 0.0f;              // of token `lane`
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        const float a = sum64(z[0][m]), b = sum64(z[1][m]);
+        if (lane == m) {
+            zg = a;
+            zu = b;
+        }
+    }
+    if (lane >= M) return;
+    if (g.a.bias) {
+        zg += g.a.bias[u];
+        zu += g.a.bias[g.K + u];
+    }
+    ((T*)g.a.y)[(int64_t)lane * g.K + u] = (T)(gate(zg, g.act) * zu);
+}
+
 // A tile's results to out[q][p], P of p: 64 columns of a wave at a time.
 template <typename S, typename O>
 __device__ __forceinline__ void put_tile(const f32x16 (&acc)[S::AB][S::BB], char* lds, O* out, int p0, int P, int64_t q0,
@@ -705,6 +760,16 @@ GatedPlan gated_plan(const GatedShape& s, bool backward) {
 
 hipError_t launch_gated(const GatedArgs& a, const GatedShape& s, const GatedPlan& p, hipStream_t st) {
     GatedK g = args_of(a, s);
+    if (s.M <= kFewTokens)
+        return with_io(s.io, [&](auto t) {
+            typedef decltype(t) T;
+            const unsigned blocks = (unsigned)tiles_of(s.K, 4);
+            if (s.M == 1) k_gated_few<T, 1><<<blocks, 256, 0, st>>>(g);
+            else if (s.M == 2) k_gated_few<T, 2><<<blocks, 256, 0, st>>>(g);
+            else if (s.M <= 4) k_gated_few<T, 4><<<blocks, 256, 0, st>>>(g);
+            else k_gated_few<T, 8><<<blocks, 256, 0, st>>>(g);
+            return hipGetLastError();
+        });
     return with_all<true>(g, s.io, p.first, [&](auto t, auto sh, auto direct) {
         typedef decltype(sh) S;
         g.tiles = tiles_of(s.K, S::kA / 2);
