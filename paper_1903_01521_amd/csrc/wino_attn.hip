@@ -6,7 +6,8 @@ namespace wino {
 
 namespace {
 
-constexpr int64_t kMostItems = (int64_t)1 << 30;
+// A launch has fewer than 2^32 threads, 256 a workgroup.
+constexpr int64_t kMostItems = ((int64_t)1 << 24) - 1;
 // Workgroups that fill the card: two on each of 256 CUs.
 constexpr int64_t kFill = 512;
 

@@ -513,8 +513,13 @@ struct KeyTiles<T, D16, KT, NT, true> {      // straight to LDS: 16-bit, 16-byte
 // ---------------------------------------------------------------- forward
 // One pass over the keys with a running maximum and sum.  The maximum moves, and what
 // is summed is scaled, only where it grows by more than 2^8: exponentials stay below
-// 2^8, and most tiles skip the scaling.  kFew: the NW waves share 32 rows and take 32
+// 2^8, and most tiles skip the scaling.  fp16 exponentials are held 2^7 times as large, below
+// 2^15, and lose what is below 2^-32 of a row's largest (2^-25 without; of 65536 keys of 2^-17
+// each, half a row's weight, every one would be off by as much as 2^-8).  kFew: the NW waves share 32 rows and take 32
 // keys of a tile each, and join at the end (single tokens: memory bound).
+
+template <typename T>
+constexpr float kExpUp = std::is_same_v<T, _Float16> ? 7.0f : 0.0f;
 
 template <typename T, int D16, bool kFew>
 struct FwdCut {
@@ -604,7 +609,7 @@ __global__ __launch_bounds__((FwdCut<T, D16, kFew>::kThreads), (waves_of<T, D16>
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[d][i] *= a;
         }
-        const float off = top == -INFINITY ? 0.0f : -top * c2;
+        const float off = top == -INFINITY ? 0.0f : kExpUp<T> - top * c2;
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -687,7 +692,7 @@ __global__ __launch_bounds__((FwdCut<T, D16, kFew>::kThreads), (waves_of<T, D16>
                    o[d][4 * b + 3] * inv);
     if (g.a.lse && h == 0)
         g.a.lse[((int64_t)n * s.Hq + me.head) * s.Lq + me.t] =
-            sum == 0.0f ? -INFINITY : __builtin_fmaf(top, s.scale, __builtin_amdgcn_logf(sum) * kLn2);
+            sum == 0.0f ? -INFINITY : __builtin_fmaf(top, s.scale, (__builtin_amdgcn_logf(sum) - kExpUp<T>) * kLn2);
 }
 
 // The parts of a row: y = sum w o / sum w l with w = 2^(top - the largest top).  A
@@ -714,7 +719,7 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnK g) {
     ((T*)g.a.y)[(((int64_t)n * s.Lq + t) * s.Hq + head) * s.D + d] = (T)(sum == 0.0f ? 0.0f : o / sum);
     if (g.a.lse && d == 0)
         g.a.lse[((int64_t)n * s.Hq + head) * s.Lq + t] =
-            sum == 0.0f ? -INFINITY : __builtin_fmaf(top, s.scale, __builtin_amdgcn_logf(sum) * kLn2);
+            sum == 0.0f ? -INFINITY : __builtin_fmaf(top, s.scale, (__builtin_amdgcn_logf(sum) - kExpUp<T>) * kLn2);
 }
 
 // ---------------------------------------------------------------- backward

@@ -710,7 +710,7 @@ int parts_of(int64_t tiles, int64_t most) {
     return n < 1 ? 1 : n > 64 ? 64 : (int)n;
 }
 
-// f(type, shape, straight to LDS); kUnits: a unit's gate and value are to be in one wave
+// f(type, shape, straight to LDS); kPairs: a unit's gate and value are to be in one wave
 template <bool kPairs, typename F>
 hipError_t with_all(const GatedK& g, Io io, int shape, F f) {
     // offsets of a tile's rows, and from a unit's gate to its value, below 2^31
@@ -732,15 +732,15 @@ hipError_t with_all(const GatedK& g, Io io, int shape, F f) {
 
 GatedPlan gated_plan(const GatedShape& s, bool backward) {
     GatedPlan p{};
-    const int64_t most = (int64_t)1 << 30, F = 2 * (int64_t)s.K;
-    // counts of the smallest tiles
-    const int64_t mt = tiles_of(s.M, Small::kB), ut = tiles_of(s.K, Narrow::kA / 2), ct = tiles_of(s.C, Small::kA);
-    p.fits = s.M <= INT32_MAX && s.K <= INT32_MAX / 2 && mt * ut <= most && mt * ct <= most &&
-             ct * tiles_of(F, Small::kB) <= most / 64 && (int64_t)s.K * s.C < (int64_t)1 << 37;
+    const int64_t F = 2 * (int64_t)s.K;
+    // a launch has fewer than 2^32 threads, 256 a workgroup; grids are rounded up to eight
+    auto fits = [](int64_t items) { return items <= ((int64_t)1 << 24) - 8; };
+    p.fits = s.M <= INT32_MAX && s.K <= INT32_MAX / 2 && (int64_t)s.K * s.C < (int64_t)1 << 37;
     if (!p.fits) return p;
     p.first = shape_of(F, s.M, 1, s.io);
     if (p.first == kSmall) p.first = kNarrow;
-    if (!backward) return p;
+    p.fits = !backward && s.M <= kFewTokens ? fits(tiles_of(s.K, 4)) : fits(tiles_by(p.first, F, s.M));
+    if (!p.fits || !backward) return p;
     // parts of 256 units or tokens at least
     p.dx = shape_of(s.C, s.M, 1, s.io);
     p.dx_splits = p.dx == kSmall ? parts_of(tiles_by(kSmall, s.C, s.M), F / 256) : 1;
@@ -749,6 +749,9 @@ GatedPlan gated_plan(const GatedShape& s, bool backward) {
     // no wider than the channels are
     if (p.dw < kNarrow && s.C <= Narrow::kA) p.dw = kNarrow;
     p.dw_splits = parts_of(tiles_by(p.dw, s.C, F), parts);
+    p.fits = fits(tiles_by(p.dx, s.C, s.M) * p.dx_splits) && fits(tiles_by(p.dw, s.C, F) * p.dw_splits) &&
+             fits(tiles_of(F, 16));
+    if (!p.fits) return p;
     p.dz = round_up((size_t)s.M * F * io_size(s.io), 16);
     p.dbias = round_up((size_t)tiles_of(s.M, Narrow::kB) * F * 4, 16);
     const size_t x = p.dx_splits > 1 ? (size_t)p.dx_splits * s.M * s.C * 4 : 0;

@@ -326,6 +326,8 @@ QkPlan qk_plan(const QkShape& s, const QkSide (&t)[2], bool backward, bool align
         const int64_t blocks = (p.items[w] + 256 / p.team - 1) / (256 / p.team);
         p.blocks[w] = (int)(backward && blocks > kBackBlocks / 2 ? kBackBlocks / 2 : blocks);
     }
+    // a launch has fewer than 2^32 threads
+    if ((int64_t)p.blocks[0] + p.blocks[1] >= (int64_t)1 << 24) p.fits = false;
     p.need = backward ? round_up((size_t)(p.blocks[0] + p.blocks[1]) * s.D * 4, 16) : 0;
     return p;
 }

@@ -165,6 +165,20 @@ def test_gated_backward_refuses(kw, status):
     assert _gated_back(**kw) == status
 
 
+def test_launches_of_2_to_the_32_threads_are_refused():
+    """256 threads a workgroup: fewer than 2^24 workgroups a launch."""
+    assert _attn(N=2**24, Lq=1, Lk=1, Hq=1, Hk=1, D=1, ldq=1, ldk=1, ldv=1) == UNS               # a token's workgroup each
+    assert B.wino_cross_attention_workspace_bytes(2**24, 1, 1, 1, 1, 1, 0) == MAX
+    assert B.wino_cross_attention_workspace_bytes(2**24 - 8, 1, 1, 1, 1, 1, 0) == 0
+    assert B.wino_cross_attention_backward_workspace_bytes(2**23, 1, 65, 2, 2, 1, 0) == MAX      # two workgroups' keys
+    f, b = B.wino_gated_layer_workspace_bytes, B.wino_gated_layer_backward_workspace_bytes
+    assert f(1, 1, 1, 1, 2**26, 0) == MAX and f(1, 1, 1, 1, 2**26 - 64, 0) == 0                  # a wave for each unit
+    assert f(2**14, 1, 2**8, 2**8, 2**9, 0) == MAX and f(2**12, 1, 2**8, 2**8, 2**8, 0) == 0     # tiles
+    assert b(2**14, 1, 2**8, 2**8, 2**9, 0) == MAX
+    # 4 tokens a workgroup where heads of 128 are not on 16 bytes
+    assert _norm(N=2**26, Lq=1, Lk=1, Hq=1, Hk=1, D=128, R=0, ldq=129, ldk=129) == UNS
+
+
 def test_gated_workspace_bytes():
     f, b = B.wino_gated_layer_workspace_bytes, B.wino_gated_layer_backward_workspace_bytes
     assert f(32, 512, 14, 14, 2048, B.WINO_IO_BF16) == 0

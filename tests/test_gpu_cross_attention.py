@@ -147,6 +147,28 @@ def test_scores_of_hundreds(dtype, rising):
     check(-np.abs(q), k, v, dtype, scale=0.5)
 
 
+@pytest.mark.parametrize("Lq", [1, 40])
+def test_half_precision_keeps_many_small_shares(Lq):
+    """One key of score 0 and 16384 of some -11.8: shares of 2^-17, half of fp16's normal
+    range away from the largest, that sum to an eighth of a row.  Each is off by its own
+    rounding alone, and by 2^-32 of the largest."""
+    Lk, D = 16385, 8
+    q, k, v = np.zeros((1, Lq, 1, D)), np.zeros((1, Lk, 1, D)), np.zeros((1, Lk, 1, D))
+    q[..., 0] = 1.0
+    k[0, :, 0, 0] = -11.78125 - np.arange(Lk) % 7 / 128.0
+    k[0, 77, 0, 0] = 0.0
+    v[0, :, 0, 0], v[0, :, 0, 1] = 1.0, np.arange(Lk) % 5 - 2.0
+    v[0, 77] = 0.0
+    y, lse, p = O.attention(q, k, v, 1.0, np.ones((1, Lk), bool))
+    got, st = attend(q, k, v, 1.0, "f16")
+    # in 32 bits scores are exact here; an exponent of 17 and its sum with the largest, exp2 and
+    # the sums over the keys: (17 * 4 + 8 + Lk) 2^-24; P's rounding, 2^-11; y's, 2^-11
+    rel = (17 * 4 + 8 + Lk) * 2.0 ** -24 + 2.0 ** -11
+    tol = (p @ np.abs(v.transpose(0, 2, 1, 3))).transpose(0, 2, 1, 3) * (2 * rel) + 2.0 ** -32 * np.abs(v).sum(1)[:, None]
+    within(got, y, tol + 2.0 ** -11 * np.abs(y) + 2.0 ** -25, "y")
+    within(st, lse, np.full(lse.shape, 2 * rel), "lse")
+
+
 @pytest.mark.parametrize("scale", [2.0 ** -140, 1e-30, 3.0])
 def test_scales(scale):
     q, k, v, _ = make(1, 9, 70, 2, 1, 16, "f32", 29, sharp=0.5)
