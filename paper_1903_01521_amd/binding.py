@@ -357,15 +357,20 @@ WINO_IO_MASK = 0x0C0
 _io_dtypes = None      # WINO_IO_* -> torch's type, once a tensor was passed
 
 
-def _tptr(t, flags):
-    """A tensor of the element type that WINO_IO_* names."""
+def _type(flags):
+    """torch's type of the tensors that WINO_IO_* names."""
     global _io_dtypes
-    if t is None or isinstance(t, int):
-        return t
     if _io_dtypes is None:
         torch = _import_torch()
         _io_dtypes = {0: torch.float32, WINO_IO_F16: torch.float16, WINO_IO_BF16: torch.bfloat16}
-    if t.dtype is not _io_dtypes.get(flags & WINO_IO_MASK):
+    return _io_dtypes.get(flags & WINO_IO_MASK)
+
+
+def _tptr(t, flags):
+    """A tensor of the element type that WINO_IO_* names."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.dtype is not _type(flags):
         raise ValueError("tensors must have the element type that the flags name")
     return _ptr(t)
 
@@ -441,36 +446,43 @@ def wino_conv2d_wgrad_nhwc(x, dy, dg, stats, gamma, beta, G, N, C, H, W, K, pad,
 WINO_FLAG_PAIRS = 0x008
 
 
-def _rows(t, flags, ld):
-    """[N][L][heads][D] of the element type that WINO_IO_* names, tokens ld elements apart:
-    a dense tensor, or a view of one projection's."""
+def _rows(t, dtype, ld):
+    """[N][L][heads][D] of `dtype`, tokens ld elements apart: a dense tensor, or a view of
+    one projection's."""
     if t is None or isinstance(t, int):
         return t
-    if t.is_contiguous():
-        p = _tptr(t, flags)
-        if t.dim() == 4 and t.shape[0] * t.shape[1] > 1 and t.stride(1) != ld:
-            raise ValueError("a tensor's tokens must be ld elements apart")
-        return p
+    if t.dtype is not dtype:
+        raise ValueError("tensors must have the element type that the flags name")
+    if not t.is_cuda:
+        raise ValueError("device buffers must be CUDA (HIP) tensors")
+    if not (t.is_contiguous() and (t.dim() != 4 or t.stride(1) == ld)):
+        _check_rows(t, ld)
+    return t.data_ptr()
+
+
+def _check_rows(t, ld):
     if t.dim() != 4:
         raise ValueError("device buffers must be contiguous, or views [N][L][heads][D]")
     (N, L, H, D), (sn, sl, sh, sd) = t.shape, t.stride()
     if (D > 1 and sd != 1) or (H > 1 and sh != D) or (L > 1 and sl != ld) or (N > 1 and sn != L * ld):
         raise ValueError("a token's heads must lie together, tokens ld elements apart and images L * ld")
+
+
+def _dense(t, dtype, what="tensors must have the element type that the flags name"):
+    """A dense tensor of `dtype`, or None."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.dtype is not dtype:
+        raise ValueError(what)
     if not t.is_cuda:
         raise ValueError("device buffers must be CUDA (HIP) tensors")
-    if _io_dtypes is None:
-        _tptr(t.new_empty(0), flags)
-    if t.dtype is not _io_dtypes.get(flags & WINO_IO_MASK):
-        raise ValueError("tensors must have the element type that the flags name")
+    if not t.is_contiguous():
+        raise ValueError("device buffers must be contiguous")
     return t.data_ptr()
 
 
 def _iptr(t):
-    if t is None or isinstance(t, int):
-        return t
-    if t.dtype is not (_torch or _import_torch()).int32:
-        raise ValueError("positions and lengths must be int32")
-    return _ptr(t)
+    return _dense(t, (_torch or _import_torch()).int32, "positions and lengths must be int32")
 
 
 def _mptr(t):
@@ -483,8 +495,9 @@ def _mptr(t):
 
 def wino_qk_norm_nhwc(q, k, gq, gk, rot, qpos, kpos, yq, yk, N, Lq, Lk, Hq, Hk, D, R, T, ldq, ldk, eps, flags=0,
                       stream=None) -> int:
-    return lib().wino_qk_norm_nhwc(_rows(q, flags, ldq), _rows(k, flags, ldk), _fptr(gq), _fptr(gk), _fptr(rot),
-                                   _iptr(qpos), _iptr(kpos), _tptr(yq, flags), _tptr(yk, flags), N, Lq, Lk, Hq, Hk, D,
+    t, f32 = _type(flags), _type(0)
+    return lib().wino_qk_norm_nhwc(_rows(q, t, ldq), _rows(k, t, ldk), _dense(gq, f32), _dense(gk, f32), _dense(rot, f32),
+                                   _iptr(qpos), _iptr(kpos), _dense(yq, t), _dense(yk, t), N, Lq, Lk, Hq, Hk, D,
                                    R, T, ldq, ldk, eps, flags, _stream(stream))
 
 
@@ -494,9 +507,10 @@ def wino_qk_norm_backward_workspace_bytes(N, Lq, Lk, Hq, Hk, D, flags=0) -> int:
 
 def wino_qk_norm_backward_nhwc(dyq, dyk, q, k, gq, gk, rot, qpos, kpos, dq, dk, dgq, dgk, N, Lq, Lk, Hq, Hk, D, R, T,
                                ldq, ldk, eps, flags=0, workspace=None, workspace_bytes=0, stream=None) -> int:
+    t, f32 = _type(flags), _type(0)
     return lib().wino_qk_norm_backward_nhwc(
-        _tptr(dyq, flags), _tptr(dyk, flags), _rows(q, flags, ldq), _rows(k, flags, ldk), _fptr(gq), _fptr(gk),
-        _fptr(rot), _iptr(qpos), _iptr(kpos), _rows(dq, flags, ldq), _rows(dk, flags, ldk), _fptr(dgq), _fptr(dgk), N,
+        _dense(dyq, t), _dense(dyk, t), _rows(q, t, ldq), _rows(k, t, ldk), _dense(gq, f32), _dense(gk, f32),
+        _dense(rot, f32), _iptr(qpos), _iptr(kpos), _rows(dq, t, ldq), _rows(dk, t, ldk), _dense(dgq, f32), _dense(dgk, f32), N,
         Lq, Lk, Hq, Hk, D, R, T, ldq, ldk, eps, flags, _ptr(workspace), workspace_bytes, _stream(stream))
 
 
@@ -506,8 +520,9 @@ def wino_cross_attention_workspace_bytes(N, Lq, Lk, Hq, Hk, D, flags=0) -> int:
 
 def wino_cross_attention_nhwc(q, k, v, klen, mask, y, lse, N, Lq, Lk, Hq, Hk, D, ldq, ldk, ldv, scale, flags=0,
                               workspace=None, workspace_bytes=0, stream=None) -> int:
-    return lib().wino_cross_attention_nhwc(_rows(q, flags, ldq), _rows(k, flags, ldk), _rows(v, flags, ldv),
-                                           _iptr(klen), _mptr(mask), _tptr(y, flags), _fptr(lse), N, Lq, Lk, Hq, Hk, D,
+    t, f32 = _type(flags), _type(0)
+    return lib().wino_cross_attention_nhwc(_rows(q, t, ldq), _rows(k, t, ldk), _rows(v, t, ldv),
+                                           _iptr(klen), _mptr(mask), _dense(y, t), _dense(lse, f32), N, Lq, Lk, Hq, Hk, D,
                                            ldq, ldk, ldv, scale, flags, _ptr(workspace), workspace_bytes,
                                            _stream(stream))
 
@@ -518,9 +533,10 @@ def wino_cross_attention_backward_workspace_bytes(N, Lq, Lk, Hq, Hk, D, flags=0)
 
 def wino_cross_attention_backward_nhwc(dy, q, k, v, y, lse, klen, mask, dq, dk, dv, N, Lq, Lk, Hq, Hk, D, ldq, ldk,
                                        ldv, scale, flags=0, workspace=None, workspace_bytes=0, stream=None) -> int:
+    t, f32 = _type(flags), _type(0)
     return lib().wino_cross_attention_backward_nhwc(
-        _tptr(dy, flags), _rows(q, flags, ldq), _rows(k, flags, ldk), _rows(v, flags, ldv), _tptr(y, flags),
-        _fptr(lse), _iptr(klen), _mptr(mask), _rows(dq, flags, ldq), _rows(dk, flags, ldk), _rows(dv, flags, ldv), N,
+        _dense(dy, t), _rows(q, t, ldq), _rows(k, t, ldk), _rows(v, t, ldv), _dense(y, t),
+        _dense(lse, f32), _iptr(klen), _mptr(mask), _rows(dq, t, ldq), _rows(dk, t, ldk), _rows(dv, t, ldv), N,
         Lq, Lk, Hq, Hk, D, ldq, ldk, ldv, scale, flags, _ptr(workspace), workspace_bytes, _stream(stream))
 
 
@@ -529,7 +545,8 @@ def wino_gated_layer_workspace_bytes(N, C, H, W, K, flags=0) -> int:
 
 
 def wino_gated_layer_nhwc(x, w, bias, y, N, C, H, W, K, flags=0, workspace=None, workspace_bytes=0, stream=None) -> int:
-    return lib().wino_gated_layer_nhwc(_tptr(x, flags), _tptr(w, flags), _fptr(bias), _tptr(y, flags), N, C, H, W, K,
+    t, f32 = _type(flags), _type(0)
+    return lib().wino_gated_layer_nhwc(_dense(x, t), _dense(w, t), _dense(bias, f32), _dense(y, t), N, C, H, W, K,
                                        flags, _ptr(workspace), workspace_bytes, _stream(stream))
 
 
@@ -539,8 +556,9 @@ def wino_gated_layer_backward_workspace_bytes(N, C, H, W, K, flags=0) -> int:
 
 def wino_gated_layer_backward_nhwc(dy, x, w, bias, dx, dw, dbias, N, C, H, W, K, flags=0, workspace=None,
                                    workspace_bytes=0, stream=None) -> int:
-    return lib().wino_gated_layer_backward_nhwc(_tptr(dy, flags), _tptr(x, flags), _tptr(w, flags), _fptr(bias),
-                                                _tptr(dx, flags), _tptr(dw, flags), _fptr(dbias), N, C, H, W, K, flags,
+    t, f32 = _type(flags), _type(0)
+    return lib().wino_gated_layer_backward_nhwc(_dense(dy, t), _dense(x, t), _dense(w, t), _dense(bias, f32),
+                                                _dense(dx, t), _dense(dw, t), _dense(dbias, f32), N, C, H, W, K, flags,
                                                 _ptr(workspace), workspace_bytes, _stream(stream))
 
 

@@ -45,7 +45,7 @@ struct AttnCut {
 };
 struct AttnPlan {
     bool fits;
-    bool few;                                // forward: a workgroup's waves share 32 rows
+    bool few;                                // forward: a workgroup of one wave, 32 rows
     AttnCut rows, keys;                      // of the launch over rows, and backward over keys
     size_t delta, part, stat, need;          // workspace: bytes of each region (16-byte aligned)
 };

@@ -8,12 +8,12 @@ namespace {
 
 // A launch has fewer than 2^32 threads, 256 a workgroup.
 constexpr int64_t kMostItems = ((int64_t)1 << 24) - 1;
-// Workgroups that fill the card: two on each of 256 CUs.
-constexpr int64_t kFill = 512;
+// Workgroups that fill the card: two on each of 256 CUs, four of those of one wave.
+constexpr int64_t kFill = 512, kFillFew = 1024;
 
 // Parts of `length` (steps of `step`, two at least a part) that fill the card.
-int splits_of(int64_t groups, int64_t length, int step) {
-    const int64_t want = (kFill + groups - 1) / groups, most = length / (2 * (int64_t)step);
+int splits_of(int64_t fill, int64_t groups, int64_t length, int step) {
+    const int64_t want = (fill + groups - 1) / groups, most = length / (2 * (int64_t)step);
     const int64_t s = want < most ? want : most;
     return s < 1 ? 1 : s > 64 ? 64 : (int)s;
 }
@@ -39,10 +39,10 @@ AttnPlan attn_plan(const AttnShape& s, bool backward) {
     p.few = !backward && s.rows <= 32;
     const int per = p.few ? 32 : 128;
     p.rows.tiles = (s.rows + per - 1) / per;
-    p.rows.splits = splits_of(pairs * p.rows.tiles, s.Lk, p.few ? 128 : 64);
+    p.rows.splits = splits_of(p.few ? kFillFew : kFill, pairs * p.rows.tiles, s.Lk, 64);
     const int64_t all = pairs * s.rows;
     p.keys.tiles = (s.Lk + kOwnKeys - 1) / kOwnKeys;
-    p.keys.splits = splits_of(pairs * p.keys.tiles, s.rows, 64);
+    p.keys.splits = splits_of(kFill, pairs * p.keys.tiles, s.rows, 64);
     // pairs are rounded up to eight; a row of a tile past 2^31 would pass 32 bits
     const int64_t eights = (pairs + 7) / 8 * 8;
     p.fits = eights * p.rows.tiles * p.rows.splits <= kMostItems && eights * p.keys.tiles * p.keys.splits <= kMostItems &&
@@ -69,6 +69,7 @@ hipError_t launch_attn(const AttnArgs& a, const AttnShape& s, const AttnPlan& p,
     g.a = a;
     g.vec = all16(s, {a.q, a.k, a.v, a.y});
     g.rep = make_fastdiv((uint32_t)s.rep);
+    g.heads = make_fastdiv((uint32_t)s.Hk);
     g.part = (float*)ws;
     g.stat = (float*)((char*)ws + p.part);
     return run(g, p, false, st);
@@ -80,6 +81,7 @@ hipError_t launch_attn_backward(const AttnBwd& b, const AttnShape& s, const Attn
     g.b = b;
     g.vec = all16(s, {b.dy, b.q, b.k, b.v, b.y, b.dq, b.dk, b.dv});
     g.rep = make_fastdiv((uint32_t)s.rep);
+    g.heads = make_fastdiv((uint32_t)s.Hk);
     g.delta = (float*)ws;
     const size_t each = round_up((size_t)s.N * s.Hk * s.rows * 4, 16);
     g.offset = (float*)((char*)ws + each);

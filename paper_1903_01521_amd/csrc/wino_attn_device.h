@@ -343,20 +343,24 @@ struct Direct {
         d.issue(t, p, bytes);
     }
 };
-// 64 floats at p, `left` of them and zeros behind, to LDS by one wave.
-__device__ __forceinline__ void load_floats(float* t, const float* p, int64_t left) {
+// 64 floats (or bytes, each a word of LDS) at p, `left` of them and zeros behind, to LDS by one wave.
+template <typename V>
+__device__ __forceinline__ void load_words(void* t, const V* p, int64_t left) {
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
     const uint64_t at = (uint64_t)p;
     const u32x4 r = {(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at),
                      (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)) & 0xffffu,
-                     (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(left < 64 ? left : 64) * 4), 0x00020000u};
-    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(char*)t;
+                     (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(left < 64 ? left : 64) * (uint32_t)sizeof(V)), 0x00020000u};
+    const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(char*)t);
+    const uint32_t off = (threadIdx.x & 63) * (uint32_t)sizeof(V);
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(
-                     __builtin_amdgcn_readfirstlane(lds)),
-                 "v"((threadIdx.x & 63) * 4), "s"(r)
-                 : "memory", "m0");
+    if constexpr (sizeof(V) == 4)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(r)
+                     : "memory", "m0");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_ubyte %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(r)
+                     : "memory", "m0");
 #pragma clang diagnostic pop
 }
 // This wave's loads to LDS have arrived, but the last n, and its own LDS accesses are
@@ -386,7 +390,7 @@ struct AttnK {
     float *delta, *offset, *share;
     float *part, *part2, *stat;
     bool vec;
-    FastDiv rep;                             // by s.rep; rows are below 2^31
+    FastDiv rep, heads;                      // by s.rep (rows are below 2^31), by s.Hk
 };
 
 // token and head of row `row` of a pair
@@ -415,8 +419,8 @@ __device__ __forceinline__ Work work_of(const AttnK& g) {
     Work w;
     w.pair = g.by_xcd ? p * 8 + (id & 7) : p;
     w.none = w.pair >= (int64_t)g.s.N * g.s.Hk;
-    w.n = (int)(w.pair / g.s.Hk);
-    w.hk = (int)(w.pair - (int64_t)w.n * g.s.Hk);
+    w.n = (int)fdiv((uint32_t)w.pair, g.heads);
+    w.hk = (int)w.pair - w.n * g.s.Hk;
     w.tile = tile;
     w.split = (int)(at - tile * (uint32_t)g.splits);
     return w;
@@ -427,9 +431,9 @@ __device__ __forceinline__ int keys_of(const int* klen, int n, int Lk) {
     return klen ? min(max(klen[n], 0), Lk) : Lk;
 }
 
-// part `split` of `n` in whole steps of `step`
+// part `split` of n < 2^31 in whole steps of `step`
 __device__ __forceinline__ void part_of(int64_t n, int step, int split, int splits, int64_t& lo, int64_t& hi) {
-    const int64_t each = ((n + step - 1) / step + splits - 1) / splits * step;
+    const int64_t each = (int64_t)(((uint32_t)((n + step - 1) / step) + (uint32_t)splits - 1) / (uint32_t)splits) * step;
     lo = min(each * split, n);
     hi = min(lo + each, n);
 }
@@ -449,7 +453,7 @@ constexpr int kCopies = sizeof(T) == 2 ? 2 : 1;
 
 // The keys' and values' tiles of a walk over keys up to hi.
 template <typename T, int D16, int KT, int NT, bool kDirect>
-struct KeyTiles {                            // by way of registers: any address, type and mask
+struct KeyTiles {                            // by way of registers: any address and type
     Moving<T, D16, KT, NT> mk, mv;
     float mb;
     const AttnShape* s;
@@ -458,7 +462,7 @@ struct KeyTiles {                            // by way of registers: any address
     const uint8_t* mask;
     int64_t hi;
     __device__ __forceinline__ void init(const AttnShape& s_, bool vec_, const T* k, const T* v, const uint8_t* mask_,
-                                         int64_t hi_) {
+                                         int64_t hi_, float*) {
         s = &s_; vec = vec_; kbase = k; vbase = v; mask = mask_; hi = hi_;
         mb = 0.0f;
     }
@@ -478,34 +482,75 @@ struct KeyTiles {                            // by way of registers: any address
         __syncthreads();
         if (k0 + KT < hi) load(k0 + KT);
     }
-    // what is added to the scores of keys at .. at + 3 of the tile at k0
-    __device__ __forceinline__ f32x4v left_out(const float* bias, int at, int64_t) const { return *(const f32x4v*)&bias[at]; }
+    // what is added to the scores of the tile's keys at + 4 h .. + 3
+    __device__ __forceinline__ f32x4v left_out(const float* bias, int at, int h) const {
+        return *(const f32x4v*)&bias[at + 4 * h];
+    }
 };
 template <typename T, int D16, int KT, int NT>
-struct KeyTiles<T, D16, KT, NT, true> {      // straight to LDS: 16-bit, 16-byte words, no mask
+struct KeyTiles<T, D16, KT, NT, true> {      // straight to LDS: 16-bit, 16-byte words
     using Tl = Tile<T, D16, KT>;
     Direct<Tl, KT, NT> dk, dv;
     const T *kbase, *vbase;
+    const uint8_t* mask;
     int64_t hi;
     int ldk, ldv, D;
-    __device__ __forceinline__ void init(const AttnShape& s, bool, const T* k, const T* v, const uint8_t*, int64_t hi_) {
-        kbase = k; vbase = v; hi = hi_; ldk = s.ldk; ldv = s.ldv; D = s.D;
+    uint64_t bits, coming;                   // keys kept of the tile at work and of the one on its way
+    float* marks;                            // a word of LDS for each key's byte, of two tiles in turn
+    __device__ __forceinline__ void init(const AttnShape& s, bool, const T* k, const T* v, const uint8_t* mask_, int64_t hi_,
+                                         float* marks_) {
+        kbase = k; vbase = v; mask = mask_; hi = hi_; ldk = s.ldk; ldv = s.ldv; D = s.D;
+        bits = coming = 0;
+        marks = marks_;
         dk.init(D / 8, [&](int row, int chunk) { return (uint32_t)row * (uint32_t)s.ldk * 2 + chunk * 16; });
         dv.init(D / 8, [&](int row, int chunk) { return (uint32_t)row * (uint32_t)s.ldv * 2 + chunk * 16; });
     }
+    // the mask of the tile at k0 on its way, to LDS too: a wait for a register of the loop's next
+    // step would be one for the tiles
+    __device__ __forceinline__ void look(int64_t k0) const {
+        if (k0 < hi && __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) == 0) load_words(marks + (k0 / KT & 1) * 64, mask + k0, hi - k0);
+    }
+    // keys that are left out are not read: their places get zeros
+    __device__ __forceinline__ void some(const Direct<Tl, KT, NT>& d, char* t, const void* p, uint32_t bytes) const {
+        Direct<Tl, KT, NT> x;
+#pragma unroll
+        for (int i = 0; i < x.kN; ++i)
+            x.off[i] = coming >> ((threadIdx.x + i * NT) / x.kRowChunks) & 1 ? d.off[i] : 0x80000000u;
+        x.issue(t, p, bytes);
+    }
+    __device__ __forceinline__ void issue(char* sk, char* sv, int64_t k0) {
+        const int64_t left = hi - k0;
+        const uint32_t last = (uint32_t)(left < KT ? left : KT) - 1;
+        const uint32_t bk = (last * (uint32_t)ldk + (uint32_t)D) * 2, bv = (last * (uint32_t)ldv + (uint32_t)D) * 2;
+        if (mask) {
+            const uint32_t mark = __float_as_uint(marks[(k0 / KT & 1) * 64 + (threadIdx.x & 63)]);
+            coming = __ballot(mark != 0);
+            some(dk, sk, kbase + k0 * ldk, bk);
+            some(dv, sv, vbase + k0 * ldv, bv);
+            look(k0 + KT);
+        } else {
+            coming = left < 64 ? ((uint64_t)1 << left) - 1 : ~(uint64_t)0;
+            dk.issue(sk, kbase + k0 * ldk, bk);
+            dv.issue(sv, vbase + k0 * ldv, bv);
+        }
+    }
     __device__ __forceinline__ void first(char* sk, char* sv, int64_t k0) {
-        const uint32_t last = (uint32_t)min((int64_t)KT, hi - k0) - 1;
-        dk.issue(sk, kbase + k0 * ldk, (last * (uint32_t)ldk + (uint32_t)D) * 2);
-        dv.issue(sv, vbase + k0 * ldv, (last * (uint32_t)ldv + (uint32_t)D) * 2);
+        if (mask) {
+            look(k0);
+            ready<0>();
+        }
+        issue(sk, sv, k0);
     }
     __device__ __forceinline__ void step(char*, char*, float*, char* nk, char* nv, int64_t k0) {
         ready<0>();
-        if (k0 + KT < hi) first(nk, nv, k0 + KT);
+        bits = coming;
+        if (k0 + KT < hi) issue(nk, nv, k0 + KT);
     }
-    __device__ __forceinline__ f32x4v left_out(const float*, int at, int64_t k0) const {
+    __device__ __forceinline__ f32x4v left_out(const float*, int at, int h) const {
+        const uint32_t b = (uint32_t)((h ? bits >> 4 : bits) >> at);
         f32x4v m;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) m[i] = k0 + at + i < hi ? 0.0f : -INFINITY;
+        for (int i = 0; i < 4; ++i) m[i] = b >> i & 1 ? 0.0f : -INFINITY;
         return m;
     }
 };
@@ -515,17 +560,19 @@ struct KeyTiles<T, D16, KT, NT, true> {      // straight to LDS: 16-bit, 16-byte
 // is summed is scaled, only where it grows by more than 2^8: exponentials stay below
 // 2^8, and most tiles skip the scaling.  fp16 exponentials are held 2^7 times as large, below
 // 2^15, and lose what is below 2^-32 of a row's largest (2^-25 without; of 65536 keys of 2^-17
-// each, half a row's weight, every one would be off by as much as 2^-8).  kFew: the NW waves share 32 rows and take 32
-// keys of a tile each, and join at the end (single tokens: memory bound).
+// each, half a row's weight, every one would be off by as much as 2^-8).  kFew: one wave
+// has 32 rows and takes 32 keys a step (single tokens, memory bound: four such workgroups a
+// CU, each with its own start and end.  One of four waves, 128 keys a step, a CU took 77 us for
+// 32 tokens to 0..4096 keys, 8 heads of 128, bf16, in place of 64).
 
 template <typename T>
 constexpr float kExpUp = std::is_same_v<T, _Float16> ? 7.0f : 0.0f;
 
 template <typename T, int D16, bool kFew>
 struct FwdCut {
-    static constexpr int kWaves = kFew && sizeof(T) == 4 ? 2 : 4;
-    static constexpr int kKeys = kFew ? 32 * kWaves : 64;
-    static constexpr int kRows = kFew ? 32 : 32 * kWaves;
+    static constexpr int kWaves = kFew ? 1 : 4;
+    static constexpr int kKeys = kFew ? 32 : 64;
+    static constexpr int kRows = 32 * kWaves;
     static constexpr int kThreads = 64 * kWaves;
 };
 
@@ -536,20 +583,20 @@ __global__ __launch_bounds__((FwdCut<T, D16, kFew>::kThreads), (waves_of<T, D16>
     using Tl = Tile<T, D16, KT>;
     __shared__ alignas(16) char tk[kCopies<T>][Tl::kBytes];
     __shared__ alignas(16) char tv[kCopies<T>][Tl::kBytes];
-    __shared__ alignas(16) float biases[kCopies<T>][KT];
+    __shared__ alignas(16) float biases[kCopies<T>][kDirect ? 64 : KT];
     const AttnShape& s = g.s;
     const Work wk = work_of(g);
     if (wk.none) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
     const int split = wk.split, n = wk.n, hk = wk.hk;
     const int64_t tile = wk.tile, pair = wk.pair;
-    const int64_t row = tile * Cut::kRows + (kFew ? 0 : wave * 32) + (lane & 31);
+    const int64_t row = tile * Cut::kRows + wave * 32 + (lane & 31);
     const bool live = row < s.rows;
     const RowAt me = row_at(g, n, hk, row);
     const T* q = live ? (const T*)g.a.q + me.tok * s.ldq + (int64_t)me.head * s.D : nullptr;
     Frag<T> fq[D16];
 #pragma unroll
-    for (int c = 0; c < D16; ++c) fq[c] = load_frag(q, c, h, s.D, g.vec);
+    for (int c = 0; c < D16; ++c) fq[c] = load_frag(q, c, h, s.D, kDirect || g.vec);
 
     int64_t lo, hi;
     const int len = keys_of(g.a.klen, n, s.Lk);
@@ -559,7 +606,7 @@ __global__ __launch_bounds__((FwdCut<T, D16, kFew>::kThreads), (waves_of<T, D16>
     const uint8_t* mask = g.a.mask ? g.a.mask + (int64_t)n * s.Lk : nullptr;
 
     KeyTiles<T, D16, KT, NT, kDirect> in;
-    in.init(s, g.vec, kbase, vbase, mask, hi);
+    in.init(s, g.vec, kbase, vbase, mask, hi, biases[0]);
 
     const float c2 = s.scale * kLog2e, slack = fminf(8.0f / c2, 0x1p127f);
     float top = -INFINITY, sum = 0.0f;
@@ -576,20 +623,19 @@ __global__ __launch_bounds__((FwdCut<T, D16, kFew>::kThreads), (waves_of<T, D16>
         in.step(tk[copy], tv[copy], biases[copy], tk[next], tv[next], k0);
         copy = next;
         const bool whole = !mask && k0 + KT <= hi;
-        const int kb0 = kFew ? wave : 0;
         f32x16 p[KB];
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
             p[kb] = f32x16{};
 #pragma unroll
-            for (int c = 0; c < D16; ++c) p[kb] = mma(Tl::read(sk, (kb0 + kb) * 32 + (lane & 31), c, h), fq[c], p[kb]);
+            for (int c = 0; c < D16; ++c) p[kb] = mma(Tl::read(sk, kb * 32 + (lane & 31), c, h), fq[c], p[kb]);
         }
         if (!whole) {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
-                    const f32x4v m = in.left_out(bias, (kb0 + kb) * 32 + 8 * b + 4 * h, k0);
+                    const f32x4v m = in.left_out(bias, kb * 32 + 8 * b, h);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) p[kb][4 * b + i] += m[i];
                 }
@@ -623,49 +669,10 @@ __global__ __launch_bounds__((FwdCut<T, D16, kFew>::kThreads), (waves_of<T, D16>
             for (int e = 0; e < 2; ++e) {
                 const Frag<T> f = pack<T>(p[kb], e);
 #pragma unroll
-                for (int d = 0; d < DB; ++d) o[d] = mma(Tl::turned(sv, (kb0 + kb) * 32 + 16 * e, d, lane), f, o[d]);
+                for (int d = 0; d < DB; ++d) o[d] = mma(Tl::turned(sv, kb * 32 + 16 * e, d, lane), f, o[d]);
             }
     }
     sum = add_halves(sum);
-    if constexpr (kFew) {
-        // the waves' sums over their keys, by way of LDS: a wave's 32 rows at a time
-        __shared__ float st[Cut::kWaves][32][2];
-        static_assert(Tl::kBytes >= 32 * 32 * sizeof(float));
-        if (h == 0) {
-            st[wave][lane][0] = top;
-            st[wave][lane][1] = sum;
-        }
-        __syncthreads();
-        float all = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < Cut::kWaves; ++w) all = fmaxf(all, st[w][lane & 31][0]);
-        sum = 0.0f;
-        const float base = all == -INFINITY ? 0.0f : all;
-#pragma unroll
-        for (int w = 0; w < Cut::kWaves; ++w)
-            sum += st[w][lane & 31][1] * __builtin_amdgcn_exp2f((st[w][lane & 31][0] - base) * c2);
-        const float a = __builtin_amdgcn_exp2f((top - base) * c2);
-        top = all;
-        float* x = (float*)tk[0];
-#pragma unroll
-        for (int d = 0; d < DB; ++d)
-            for (int w = 0; w < Cut::kWaves; ++w) {
-                if (wave == w) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int e = (8 * (i >> 2) + 4 * h + (i & 3)) * 32 + (lane & 31);
-                        x[e] = (w ? x[e] : 0.0f) + o[d][i] * a;
-                    }
-                }
-                __syncthreads();
-                if (w == Cut::kWaves - 1 && wave == 0) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[d][i] = x[(8 * (i >> 2) + 4 * h + (i & 3)) * 32 + (lane & 31)];
-                }
-                __syncthreads();
-            }
-        if (wave) return;
-    }
     if (!live) return;
     if (g.splits > 1) {
         const int64_t id = ((int64_t)split * s.N * s.Hk + pair) * s.rows + row;
@@ -674,7 +681,7 @@ __global__ __launch_bounds__((FwdCut<T, D16, kFew>::kThreads), (waves_of<T, D16>
         for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int b = 0; b < 4; ++b)
-                store4(part, 32 * d + 8 * b + 4 * h, s.D, (s.D & 3) == 0, o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2],
+                store4(part, 32 * d + 8 * b + 4 * h, s.D, kDirect || (s.D & 3) == 0, o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2],
                        o[d][4 * b + 3]);
         if (h == 0) {
             g.stat[id * 2] = top;
@@ -688,36 +695,73 @@ __global__ __launch_bounds__((FwdCut<T, D16, kFew>::kThreads), (waves_of<T, D16>
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int b = 0; b < 4; ++b)
-            store4(y, 32 * d + 8 * b + 4 * h, s.D, g.vec, o[d][4 * b] * inv, o[d][4 * b + 1] * inv, o[d][4 * b + 2] * inv,
+            store4(y, 32 * d + 8 * b + 4 * h, s.D, kDirect || g.vec, o[d][4 * b] * inv, o[d][4 * b + 1] * inv, o[d][4 * b + 2] * inv,
                    o[d][4 * b + 3] * inv);
     if (g.a.lse && h == 0)
         g.a.lse[((int64_t)n * s.Hq + me.head) * s.Lq + me.t] =
             sum == 0.0f ? -INFINITY : __builtin_fmaf(top, s.scale, (__builtin_amdgcn_logf(sum) - kExpUp<T>) * kLn2);
 }
 
-// The parts of a row: y = sum w o / sum w l with w = 2^(top - the largest top).  A
-// workgroup's 256 threads are 256 / D rows; each thread one value of a row.
-template <typename T>
+// The parts of a row: y = sum w o / sum w l with w = 2^(top - the largest top).  A lane has
+// the weight of one part, a wave every kWaves-th part; kWaves 4 for a row of many parts (64 of
+// them one after the other took 40 us).
+template <typename T, int kWaves>
 __global__ __launch_bounds__(256) void k_attn_join(AttnK g) {
     const AttnShape& s = g.s;
-    const int per = 256 / s.D, r = threadIdx.x / s.D, d = threadIdx.x % s.D;
-    const int64_t all = (int64_t)s.N * s.Hk * s.rows, id = (int64_t)blockIdx.x * per + r;
-    if (r >= per || id >= all) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t all = (int64_t)s.N * s.Hk * s.rows, id = (int64_t)blockIdx.x * (4 / kWaves) + wave / kWaves;
+    if (id >= all) return;                   // of all the row's waves
     const float c2 = s.scale * kLog2e;
-    float top = -INFINITY, sum = 0.0f, o = 0.0f;
-    for (int i = 0; i < g.splits; ++i) top = fmaxf(top, g.stat[(i * all + id) * 2]);
-    const float base = top == -INFINITY ? 0.0f : top;
-    for (int i = 0; i < g.splits; ++i) {
-        const int64_t at = i * all + id;
-        const float w = __builtin_amdgcn_exp2f((g.stat[at * 2] - base) * c2);
-        sum = __builtin_fmaf(g.stat[at * 2 + 1], w, sum);
-        o = __builtin_fmaf(g.part[at * s.D + d], w, o);
+    float top = lane < g.splits ? g.stat[(lane * all + id) * 2] : -INFINITY;
+    float sum = lane < g.splits ? g.stat[(lane * all + id) * 2 + 1] : 0.0f;
+    const float mine = top;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+    const float w = __builtin_amdgcn_exp2f((mine - (top == -INFINITY ? 0.0f : top)) * c2);
+    sum *= w;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d, 64);
+    float o[2] = {0.0f, 0.0f};
+    const int last = g.splits - 1;
+    for (int i0 = wave % kWaves; i0 <= last; i0 += 8 * kWaves) {
+        float v[8][2];                       // eight parts' values on their way together
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                v[u][e] = lane + 64 * e < s.D ? g.part[(min(i0 + u * kWaves, last) * all + id) * s.D + lane + 64 * e] : 0.0f;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int i = i0 + u * kWaves;
+            if (i > last) break;
+            const float wi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), i));
+            o[0] = __builtin_fmaf(v[u][0], wi, o[0]);
+            o[1] = __builtin_fmaf(v[u][1], wi, o[1]);
+        }
     }
-    const int64_t pair = id / s.rows, row = id % s.rows;
-    const int n = (int)(pair / s.Hk), head = (int)(pair % s.Hk) * s.rep + (int)(row % s.rep);
-    const int64_t t = row / s.rep;
-    ((T*)g.a.y)[(((int64_t)n * s.Lq + t) * s.Hq + head) * s.D + d] = (T)(sum == 0.0f ? 0.0f : o / sum);
-    if (g.a.lse && d == 0)
+    if constexpr (kWaves == 4) {
+        __shared__ float x[3][2][64];
+        if (wave) {
+            x[wave - 1][0][lane] = o[0];
+            x[wave - 1][1][lane] = o[1];
+        }
+        __syncthreads();
+        if (wave) return;
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            o[0] += x[i][0][lane];
+            o[1] += x[i][1][lane];
+        }
+    }
+    // with parts there are fewer than 2^31 rows
+    const uint32_t pair = (uint32_t)id / (uint32_t)s.rows, n = fdiv(pair, g.heads), row = (uint32_t)id - pair * (uint32_t)s.rows;
+    const int64_t t = fdiv(row, g.rep);
+    const int head = (int)(pair - n * s.Hk) * s.rep + (int)(row - (uint32_t)t * s.rep);
+    T* y = (T*)g.a.y + (((int64_t)n * s.Lq + t) * s.Hq + head) * s.D;
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+        if (lane + 64 * e < s.D) y[lane + 64 * e] = (T)(sum == 0.0f ? 0.0f : o[e] / sum);
+    if (g.a.lse && lane == 0)
         g.a.lse[((int64_t)n * s.Hq + head) * s.Lq + t] =
             sum == 0.0f ? -INFINITY : __builtin_fmaf(top, s.scale, (__builtin_amdgcn_logf(sum) - kExpUp<T>) * kLn2);
 }
@@ -780,7 +824,7 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(4))) void k_attn_dq(AttnK g)
     using Tl = Tile<T, D16, KT>;
     __shared__ alignas(16) char tk[kCopies<T>][Tl::kBytes];
     __shared__ alignas(16) char tv[kCopies<T>][Tl::kBytes];
-    __shared__ alignas(16) float biases[kCopies<T>][KT];
+    __shared__ alignas(16) float biases[kCopies<T>][kDirect ? 64 : KT];
     const AttnShape& s = g.s;
     const Work wk = work_of(g);
     if (wk.none) return;
@@ -798,8 +842,8 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(4))) void k_attn_dq(AttnK g)
     float delta = 0.0f;
 #pragma unroll
     for (int c = 0; c < D16; ++c) {
-        fq[c] = load_frag(q, c, h, s.D, g.vec);
-        const Eight<T> ed(dy, c, h, s.D, g.vec), ey(y, c, h, s.D, g.vec);
+        fq[c] = load_frag(q, c, h, s.D, kDirect || g.vec);
+        const Eight<T> ed(dy, c, h, s.D, kDirect || g.vec), ey(y, c, h, s.D, kDirect || g.vec);
         fo[c] = ed.frag();
 #pragma unroll
         for (int j = 0; j < 8; ++j) delta = __builtin_fmaf((float)ed.v[j], (float)ey.v[j], delta);
@@ -815,7 +859,7 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(4))) void k_attn_dq(AttnK g)
     const T* vbase = (const T*)g.b.v + (int64_t)n * s.Lk * s.ldv + (int64_t)hk * s.D;
     const uint8_t* mask = g.b.mask ? g.b.mask + (int64_t)n * s.Lk : nullptr;
     KeyTiles<T, D16, KT, NT, kDirect> in;
-    in.init(s, g.vec, kbase, vbase, mask, hi);
+    in.init(s, g.vec, kbase, vbase, mask, hi, biases[0]);
 
     const float c2 = s.scale * kLog2e;
     float up = kHalf ? 0x1p100f : 1.0f, lack = 0.0f, round = 0.0f;
@@ -844,7 +888,7 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(4))) void k_attn_dq(AttnK g)
             if (!whole) {
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
-                    const f32x4v m = in.left_out(bias, kb * 32 + 8 * b + 4 * h, k0);
+                    const f32x4v m = in.left_out(bias, kb * 32 + 8 * b, h);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) p[4 * b + i] += m[i];
                 }
@@ -899,10 +943,10 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(4))) void k_attn_dq(AttnK g)
         for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
-                store4(part, 32 * d + 8 * b + 4 * h, s.D, (s.D & 3) == 0, acc[d][4 * b] * f, acc[d][4 * b + 1] * f,
+                store4(part, 32 * d + 8 * b + 4 * h, s.D, kDirect || (s.D & 3) == 0, acc[d][4 * b] * f, acc[d][4 * b + 1] * f,
                        acc[d][4 * b + 2] * f, acc[d][4 * b + 3] * f);
                 if constexpr (kFix)
-                    store4(part2, 32 * d + 8 * b + 4 * h, s.D, (s.D & 3) == 0, mean[d][4 * b] * fm,
+                    store4(part2, 32 * d + 8 * b + 4 * h, s.D, kDirect || (s.D & 3) == 0, mean[d][4 * b] * fm,
                            mean[d][4 * b + 1] * fm, mean[d][4 * b + 2] * fm, mean[d][4 * b + 3] * fm);
             }
         if (h == 0) {
@@ -933,7 +977,7 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(4))) void k_attn_dq(AttnK g)
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int b = 0; b < 4; ++b)
-            store4(dq, 32 * d + 8 * b + 4 * h, s.D, g.vec, acc[d][4 * b], acc[d][4 * b + 1], acc[d][4 * b + 2],
+            store4(dq, 32 * d + 8 * b + 4 * h, s.D, kDirect || g.vec, acc[d][4 * b], acc[d][4 * b + 1], acc[d][4 * b + 2],
                    acc[d][4 * b + 3]);
 }
 
@@ -941,10 +985,13 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(4))) void k_attn_dq(AttnK g)
 template <typename T>
 __global__ __launch_bounds__(256) void k_attn_dq_join(AttnK g) {
     const AttnShape& s = g.s;
-    const int64_t rows = (int64_t)s.N * s.Hk * s.rows, i = (int64_t)blockIdx.x * 256 + threadIdx.x, id = i / s.D;
+    // with parts there are fewer than 2^31 values
+    const int64_t rows = (int64_t)s.N * s.Hk * s.rows, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t id = (uint32_t)i / (uint32_t)s.D;
     if (id >= rows) return;
     const int d = (int)(i - id * s.D);
     float sum = 0.0f, mean = 0.0f, lack = 0.0f, round = 0.0f;
+#pragma unroll 8
     for (int k = 0; k < g.splits; ++k) {
         const int64_t at = k * rows + id;
         sum += g.part[at * s.D + d];
@@ -954,8 +1001,8 @@ __global__ __launch_bounds__(256) void k_attn_dq_join(AttnK g) {
             round += g.stat[at * 2 + 1];
         }
     }
-    const int64_t pair = id / s.rows, row = id - pair * s.rows;
-    const int n = (int)(pair / s.Hk);
+    const int64_t pair = (uint32_t)id / (uint32_t)s.rows, row = id - pair * s.rows;
+    const int n = (int)fdiv((uint32_t)pair, g.heads);
     const RowAt me = row_at(g, n, (int)(pair - (int64_t)n * s.Hk), row);
     T* dq = (T*)g.b.dq + me.tok * s.ldq + (int64_t)me.head * s.D;
     if constexpr (sizeof(T) == 2) {
@@ -1061,8 +1108,8 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(kDirect ? 6 : 4))) void k_at
     Frag<T> fk[D16], fv[D16];
 #pragma unroll
     for (int c = 0; c < D16; ++c) {
-        fk[c] = load_frag(k, c, h, s.D, g.vec);
-        fv[c] = load_frag(v, c, h, s.D, g.vec);
+        fk[c] = load_frag(k, c, h, s.D, kDirect || g.vec);
+        fv[c] = load_frag(v, c, h, s.D, kDirect || g.vec);
     }
     int64_t lo, hi;
     part_of(tile * kOwnKeys < len ? s.rows : 0, RT, split, g.splits, lo, hi);
@@ -1074,8 +1121,8 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(kDirect ? 6 : 4))) void k_at
         in.load(r0, sq, so);
         const int64_t at = pair * s.rows + r0;
         if constexpr (kDirect) {
-            if (wave == 0) load_floats(offs, g.offset + at, hi - r0);
-            if (wave == 1) load_floats(deltas, g.delta + at, hi - r0);
+            if (wave == 0) load_words(offs, g.offset + at, hi - r0);
+            if (wave == 1) load_words(deltas, g.delta + at, hi - r0);
         } else if (threadIdx.x < RT) {
             const bool inside = r0 + threadIdx.x < hi;
             moff = inside ? g.offset[at + threadIdx.x] : 0.0f;
@@ -1189,9 +1236,9 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(kDirect ? 6 : 4))) void k_at
     };
     if (g.splits > 1) {
         const int64_t id = (((int64_t)split * s.N * s.Hk + pair) * s.Lk + key) * s.D;
-        put(g.part + id, g.part2 + id, (s.D & 3) == 0);
+        put(g.part + id, g.part2 + id, kDirect || (s.D & 3) == 0);
     } else {
-        put((T*)g.b.dk + tok * s.ldk + (int64_t)hk * s.D, (T*)g.b.dv + tok * s.ldv + (int64_t)hk * s.D, g.vec);
+        put((T*)g.b.dk + tok * s.ldk + (int64_t)hk * s.D, (T*)g.b.dv + tok * s.ldv + (int64_t)hk * s.D, kDirect || g.vec);
     }
 }
 
@@ -1203,8 +1250,10 @@ __global__ __launch_bounds__(256) void k_attn_sum(AttnK g) {
     if (i >= all) return;
     const float* p = blockIdx.y ? g.part2 : g.part;
     float sum = 0.0f;
+#pragma unroll 8
     for (int k = 0; k < g.splits; ++k) sum += p[k * all + i];
-    const int64_t id = i / s.D, pair = id / s.Lk, n = pair / s.Hk;
+    // with parts there are fewer than 2^31 values
+    const int64_t id = (uint32_t)i / (uint32_t)s.D, pair = (uint32_t)id / (uint32_t)s.Lk, n = fdiv((uint32_t)pair, g.heads);
     const int64_t tok = n * s.Lk + (id - pair * s.Lk);
     T* x = (T*)(blockIdx.y ? g.b.dv : g.b.dk) + tok * (blockIdx.y ? s.ldv : s.ldk);
     x[(pair - n * s.Hk) * s.D + (i - id * s.D)] = (T)sum;
@@ -1237,8 +1286,9 @@ hipError_t attn_run_by(const AttnK& g, const AttnPlan& p, bool backward, hipStre
         if (a.splits > 1) {
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
-            const int per = 256 / s.D;
-            k_attn_join<T><<<(unsigned)((pairs * s.rows + per - 1) / per), 256, 0, st>>>(a);
+            // one part a wave at a time
+            if (a.splits > 8) k_attn_join<T, 4><<<(unsigned)(pairs * s.rows), 256, 0, st>>>(a);
+            else k_attn_join<T, 1><<<(unsigned)((pairs * s.rows + 3) / 4), 256, 0, st>>>(a);
         }
         return hipGetLastError();
     }
@@ -1271,7 +1321,7 @@ hipError_t attn_run(const AttnK& g, const AttnPlan& p, bool backward, hipStream_
     constexpr int kMost = 1 << 22;
     if constexpr (sizeof(T) == 2) {
         const AttnShape& s = g.s;
-        if (g.vec && !g.a.mask && !g.b.mask && s.ldq <= kMost && s.ldk <= kMost && s.ldv <= kMost && s.Hq * s.D <= kMost)
+        if (g.vec && s.ldq <= kMost && s.ldk <= kMost && s.ldv <= kMost && s.Hq * s.D <= kMost)
             return attn_run_by<T, D16, true>(g, p, backward, st);
     }
     return attn_run_by<T, D16, false>(g, p, backward, st);

@@ -28,7 +28,7 @@ struct GatedK {
     bool vec;
     void* dz;                                // [M][2 K]
     float *dbias, *part;                     // [token tiles][2 K]; [splits][2 K][C]
-    int64_t items, tiles;                    // tiles: of the faster axis
+    int items, tiles;                        // below 2^24; tiles: of the faster axis
     int splits;
 };
 
@@ -310,9 +310,9 @@ __device__ __forceinline__ float sum16(float (&v)[16]) {
 
 // Workgroups that share a tile's tokens follow each other on one XCD, whose L2 then holds
 // them: workgroup ids go round the eight XCDs.  Item of `all`, or -1.
-__device__ __forceinline__ int64_t item_of(int64_t all) {
-    const int64_t each = (all + 7) / 8, i = (int64_t)(blockIdx.x & 7) * each + (blockIdx.x >> 3);
-    return (blockIdx.x >> 3) < each && i < all ? i : -1;
+__device__ __forceinline__ int item_of(int all) {
+    const int each = (all + 7) / 8, i = (int)(blockIdx.x & 7) * each + (int)(blockIdx.x >> 3);
+    return (int)(blockIdx.x >> 3) < each && i < all ? i : -1;
 }
 inline unsigned grid_of(int64_t items) { return (unsigned)((items + 7) / 8 * 8); }
 
@@ -376,11 +376,11 @@ __global__ __launch_bounds__(256, 2) void k_gated(GatedK g) {
     using B = Side<T, S::kB, false, kDirect>;
     using Rows = Rows64<T>;
     __shared__ alignas(16) char lds[lds_of<S, A, B>(kDirect, Rows::kBytes)];
-    const int64_t item = item_of(g.items);
+    const int item = item_of(g.items);
     if (item < 0) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-    const int64_t mt = item / g.tiles, m0 = mt * S::kB;
-    const int u0 = (int)(item - mt * g.tiles) * kUnits, K = g.K;
+    const int mt = (uint32_t)item / (uint32_t)g.tiles, u0 = (item - mt * g.tiles) * kUnits, K = g.K;
+    const int64_t m0 = (int64_t)mt * S::kB;
     constexpr bool kAhead = BACK && kDirect && S::AB == 4 && sizeof(T) == 2;
     // loaded once: a load between stores would wait for them
     __shared__ alignas(16) float bias[2 * kUnits];
@@ -508,7 +508,7 @@ __global__ __launch_bounds__(256, 2) void k_gated(GatedK g) {
             float v = 0.0f;
 #pragma unroll
             for (int i = 0; i < S::WB; ++i) v += sums[i][w][u];
-            if (u0 + u < K) g.dbias[mt * 2 * K + (int64_t)w * K + u0 + u] = v;
+            if (u0 + u < K) g.dbias[(int64_t)mt * 2 * K + (int64_t)w * K + u0 + u] = v;
         }
     }
 }
@@ -604,10 +604,11 @@ __global__ __launch_bounds__(256, 2) void k_gated_dx(GatedK g) {
     using A = Side<T, S::kA, true, kDirect>;
     using B = Side<T, S::kB, false, kDirect>;
     __shared__ alignas(16) char lds[lds_of<S, A, B>(kDirect, Rows64<float>::kBytes)];
-    const int64_t item = item_of(g.items);
+    const int item = item_of(g.items);
     if (item < 0) return;
-    const int64_t at = item / g.tiles, mt = at / g.splits, m0 = mt * S::kB;
-    const int c0 = (int)(item - at * g.tiles) * S::kA, F = 2 * g.K, split = (int)(at - mt * g.splits);
+    const int at = (uint32_t)item / (uint32_t)g.tiles, mt = (uint32_t)at / (uint32_t)g.splits;
+    const int c0 = (item - at * g.tiles) * S::kA, F = 2 * g.K, split = at - mt * g.splits;
+    const int64_t m0 = (int64_t)mt * S::kB;
     int64_t lo, hi;
     part_of(F, kBk, split, g.splits, lo, hi);
     f32x16 acc[S::AB][S::BB];
@@ -616,7 +617,7 @@ __global__ __launch_bounds__(256, 2) void k_gated_dx(GatedK g) {
     a.init({(const T*)g.a.w + c0, F, g.C - c0, g.C, kBk, 0}, g.vec);
     b.init({(const T*)g.dz + m0 * F, g.M - m0 < S::kB ? g.M - m0 : S::kB, F, F, S::kB, 0}, g.vec);
     product<S>(acc, a, b, lds, lo, hi, kDirect);
-    if (g.splits > 1) put_tile<S>(acc, lds, g.part + split * g.M * g.C, c0, g.C, m0, g.M, (g.C & 3) == 0);
+    if (g.splits > 1) put_tile<S>(acc, lds, g.part + (int64_t)split * g.M * g.C, c0, g.C, m0, g.M, (g.C & 3) == 0);
     else put_tile<S>(acc, lds, (T*)g.a.dx, c0, g.C, m0, g.M, g.vec);
 }
 
@@ -626,11 +627,11 @@ __global__ __launch_bounds__(256, 2) void k_gated_dw(GatedK g) {
     using A = Side<T, S::kA, true, kDirect>;
     using B = Side<T, S::kB, true, kDirect>;
     __shared__ alignas(16) char lds[lds_of<S, A, B>(kDirect, Rows64<float>::kBytes)];
-    const int64_t item = item_of(g.items);
+    const int item = item_of(g.items);
     if (item < 0) return;
     const int F = 2 * g.K;
-    const int64_t ft = (F + S::kB - 1) / S::kB, at = item / g.tiles;
-    const int c0 = (int)(item - at * g.tiles) * S::kA, split = (int)(at / ft), f0 = (int)(at - split * ft) * S::kB;
+    const int ft = (F + S::kB - 1) / S::kB, at = (uint32_t)item / (uint32_t)g.tiles, split = (uint32_t)at / (uint32_t)ft;
+    const int c0 = (item - at * g.tiles) * S::kA, f0 = (at - split * ft) * S::kB;
     int64_t lo, hi;
     part_of(g.M, kBk, split, g.splits, lo, hi);
     f32x16 acc[S::AB][S::BB];
@@ -649,6 +650,7 @@ __global__ __launch_bounds__(256) void k_gated_sum(const float* part, T* out, in
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= n) return;
     float sum = 0.0f;
+#pragma unroll 8
     for (int k = 0; k < splits; ++k) sum += part[k * n + i];
     out[i] = (T)sum;
 }
@@ -658,6 +660,7 @@ __global__ __launch_bounds__(256) void k_gated_db(GatedK g, int64_t rows) {
     const int F = 2 * g.K, f = blockIdx.x * 16 + (threadIdx.x & 15), i0 = threadIdx.x >> 4;
     float sum = 0.0f;
     if (f < F)
+#pragma unroll 8
         for (int64_t i = i0; i < rows; i += 16) sum += g.dbias[i * F + f];
     __shared__ float s[16][17];
     s[i0][threadIdx.x & 15] = sum;
@@ -775,8 +778,8 @@ hipError_t launch_gated(const GatedArgs& a, const GatedShape& s, const GatedPlan
         });
     return with_all<true>(g, s.io, p.first, [&](auto t, auto sh, auto direct) {
         typedef decltype(sh) S;
-        g.tiles = tiles_of(s.K, S::kA / 2);
-        g.items = tiles_of(s.M, S::kB) * g.tiles;
+        g.tiles = (int)tiles_of(s.K, S::kA / 2);
+        g.items = (int)(tiles_of(s.M, S::kB) * g.tiles);
         k_gated<decltype(t), S, false, direct.value><<<grid_of(g.items), 256, 0, st>>>(g);
         return hipGetLastError();
     });
@@ -791,9 +794,9 @@ hipError_t launch_gated_backward(const GatedArgs& a, const GatedShape& s, const 
     int64_t rows = 0;
     hipError_t e = with_all<true>(g, s.io, p.first, [&](auto t, auto sh, auto direct) {
         typedef decltype(sh) S;
-        g.tiles = tiles_of(s.K, S::kA / 2);
+        g.tiles = (int)tiles_of(s.K, S::kA / 2);
         rows = tiles_of(s.M, S::kB);
-        g.items = rows * g.tiles;
+        g.items = (int)(rows * g.tiles);
         k_gated<decltype(t), S, true, direct.value><<<grid_of(g.items), 256, 0, st>>>(g);
         return hipGetLastError();
     });
@@ -811,8 +814,8 @@ hipError_t launch_gated_backward(const GatedArgs& a, const GatedShape& s, const 
         e = with_all<false>(g, s.io, p.dx, [&](auto t, auto sh, auto direct) {
             typedef decltype(sh) S;
             g.splits = p.dx_splits;
-            g.tiles = tiles_of(s.C, S::kA);
-            g.items = tiles_of(s.M, S::kB) * g.tiles * g.splits;
+            g.tiles = (int)tiles_of(s.C, S::kA);
+            g.items = (int)(tiles_of(s.M, S::kB) * g.tiles * g.splits);
             k_gated_dx<decltype(t), S, direct.value><<<grid_of(g.items), 256, 0, st>>>(g);
             const hipError_t e = hipGetLastError();
             return e != hipSuccess ? e : sum(t, a.dx, s.M * s.C);
@@ -823,8 +826,8 @@ hipError_t launch_gated_backward(const GatedArgs& a, const GatedShape& s, const 
     return with_all<false>(g, s.io, p.dw, [&](auto t, auto sh, auto direct) {
         typedef decltype(sh) S;
         g.splits = p.dw_splits;
-        g.tiles = tiles_of(s.C, S::kA);
-        g.items = g.tiles * tiles_of(F, S::kB) * g.splits;
+        g.tiles = (int)tiles_of(s.C, S::kA);
+        g.items = (int)(g.tiles * tiles_of(F, S::kB) * g.splits);
         k_gated_dw<decltype(t), S, direct.value><<<grid_of(g.items), 256, 0, st>>>(g);
         const hipError_t e = hipGetLastError();
         return e != hipSuccess ? e : sum(t, a.dw, F * s.C);

@@ -237,12 +237,14 @@ __global__ __launch_bounds__(256) void k_qk_norm_gamma(QkK g, int blocks1) {
     const float* p = g.part + (int64_t)(w ? g.blocks0 : 0) * g.s.D;
     float sum = 0.0f;
     if (d < g.s.D)
+#pragma unroll 8
         for (int i = i0; i < count; i += 64) sum += p[(int64_t)i * g.s.D + d];
     __shared__ float s[64][4];
     s[i0][threadIdx.x & 3] = sum;
     __syncthreads();
     if (threadIdx.x < 4 && d < g.s.D) {
         float all = 0.0f;
+#pragma unroll 16
         for (int i = 0; i < 64; ++i) all += s[i][threadIdx.x];
         g.t[w].dgamma[d] = all;
     }

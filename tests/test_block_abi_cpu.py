@@ -191,11 +191,11 @@ def test_gated_workspace_bytes():
 def test_binding_checks_tensors():
     t = torch.empty(2, 3, 4, 5)
     with pytest.raises(ValueError):
-        B._rows(t, 0, 20)                                            # not on a GPU
+        B._rows(t, torch.float32, 20)                                            # not on a GPU
     with pytest.raises(ValueError):
-        B._rows(t.transpose(1, 2), 0, 20)                            # heads are not together
+        B._rows(t.transpose(1, 2), torch.float32, 20)                            # heads are not together
     with pytest.raises(ValueError):
-        B._rows(t[:, :, :2], 0, 10)                                  # tokens are 20 apart
+        B._rows(t[:, :, :2], torch.float32, 10)                                  # tokens are 20 apart
     with pytest.raises(ValueError):
         B._iptr(torch.empty(3, dtype=torch.int64))
     with pytest.raises(ValueError):
