@@ -451,25 +451,28 @@ constexpr int waves_of(int most) {
 template <typename T>
 constexpr int kCopies = sizeof(T) == 2 ? 2 : 1;
 
+// How vectors lie in memory: anywhere; in whole 16-byte words; so, and rows of a tile within
+// 2^31 bytes, in 16 bits, straight to LDS.
+enum { kAnywhere, kWords, kStraight };
+
 // The keys' and values' tiles of a walk over keys up to hi.
-template <typename T, int D16, int KT, int NT, bool kDirect>
+template <typename T, int D16, int KT, int NT, int kHow>
 struct KeyTiles {                            // by way of registers: any address and type
     Moving<T, D16, KT, NT> mk, mv;
     float mb;
     const AttnShape* s;
-    bool vec;
     const T *kbase, *vbase;
     const uint8_t* mask;
     int64_t hi;
-    __device__ __forceinline__ void init(const AttnShape& s_, bool vec_, const T* k, const T* v, const uint8_t* mask_,
+    __device__ __forceinline__ void init(const AttnShape& s_, const T* k, const T* v, const uint8_t* mask_,
                                          int64_t hi_, float*) {
-        s = &s_; vec = vec_; kbase = k; vbase = v; mask = mask_; hi = hi_;
+        s = &s_; kbase = k; vbase = v; mask = mask_; hi = hi_;
         mb = 0.0f;
     }
     __device__ __forceinline__ void load(int64_t k0) {
         auto kept = [&](int r) { return k0 + r < hi && (!mask || mask[k0 + r]); };
-        mk.load([&](int r) { return kept(r) ? kbase + (k0 + r) * s->ldk : nullptr; }, s->D, vec);
-        mv.load([&](int r) { return kept(r) ? vbase + (k0 + r) * s->ldv : nullptr; }, s->D, vec);
+        mk.load([&](int r) { return kept(r) ? kbase + (k0 + r) * s->ldk : nullptr; }, s->D, kHow == kWords);
+        mv.load([&](int r) { return kept(r) ? vbase + (k0 + r) * s->ldv : nullptr; }, s->D, kHow == kWords);
         if (threadIdx.x < KT) mb = kept(threadIdx.x) ? 0.0f : -INFINITY;
     }
     __device__ __forceinline__ void first(char*, char*, int64_t k0) { load(k0); }
@@ -488,7 +491,7 @@ struct KeyTiles {                            // by way of registers: any address
     }
 };
 template <typename T, int D16, int KT, int NT>
-struct KeyTiles<T, D16, KT, NT, true> {      // straight to LDS: 16-bit, 16-byte words
+struct KeyTiles<T, D16, KT, NT, kStraight> {      // straight to LDS: 16-bit, 16-byte words
     using Tl = Tile<T, D16, KT>;
     Direct<Tl, KT, NT> dk, dv;
     const T *kbase, *vbase;
@@ -497,7 +500,7 @@ struct KeyTiles<T, D16, KT, NT, true> {      // straight to LDS: 16-bit, 16-byte
     int ldk, ldv, D;
     uint64_t bits, coming;                   // keys kept of the tile at work and of the one on its way
     float* marks;                            // a word of LDS for each key's byte, of two tiles in turn
-    __device__ __forceinline__ void init(const AttnShape& s, bool, const T* k, const T* v, const uint8_t* mask_, int64_t hi_,
+    __device__ __forceinline__ void init(const AttnShape& s, const T* k, const T* v, const uint8_t* mask_, int64_t hi_,
                                          float* marks_) {
         kbase = k; vbase = v; mask = mask_; hi = hi_; ldk = s.ldk; ldv = s.ldv; D = s.D;
         bits = coming = 0;
@@ -576,9 +579,10 @@ struct FwdCut {
     static constexpr int kThreads = 64 * kWaves;
 };
 
-template <typename T, int D16, bool kFew, bool kDirect>
-__global__ __launch_bounds__((FwdCut<T, D16, kFew>::kThreads), (waves_of<T, D16>(kFew && !kDirect ? 6 : 8))) void k_attn(AttnK g) {
+template <typename T, int D16, bool kFew, int kHow>
+__global__ __launch_bounds__((FwdCut<T, D16, kFew>::kThreads), (waves_of<T, D16>(kFew && kHow != kStraight ? 6 : 8))) void k_attn(AttnK g) {
     using Cut = FwdCut<T, D16, kFew>;
+    constexpr bool kDirect = kHow == kStraight, kVec = kHow != kAnywhere;
     constexpr int NT = Cut::kThreads, KT = Cut::kKeys, KB = kFew ? 1 : KT / 32, DB = (D16 + 1) / 2;
     using Tl = Tile<T, D16, KT>;
     __shared__ alignas(16) char tk[kCopies<T>][Tl::kBytes];
@@ -596,7 +600,7 @@ __global__ __launch_bounds__((FwdCut<T, D16, kFew>::kThreads), (waves_of<T, D16>
     const T* q = live ? (const T*)g.a.q + me.tok * s.ldq + (int64_t)me.head * s.D : nullptr;
     Frag<T> fq[D16];
 #pragma unroll
-    for (int c = 0; c < D16; ++c) fq[c] = load_frag(q, c, h, s.D, kDirect || g.vec);
+    for (int c = 0; c < D16; ++c) fq[c] = load_frag(q, c, h, s.D, kVec);
 
     int64_t lo, hi;
     const int len = keys_of(g.a.klen, n, s.Lk);
@@ -605,8 +609,8 @@ __global__ __launch_bounds__((FwdCut<T, D16, kFew>::kThreads), (waves_of<T, D16>
     const T* vbase = (const T*)g.a.v + (int64_t)n * s.Lk * s.ldv + (int64_t)hk * s.D;
     const uint8_t* mask = g.a.mask ? g.a.mask + (int64_t)n * s.Lk : nullptr;
 
-    KeyTiles<T, D16, KT, NT, kDirect> in;
-    in.init(s, g.vec, kbase, vbase, mask, hi, biases[0]);
+    KeyTiles<T, D16, KT, NT, kHow> in;
+    in.init(s, kbase, vbase, mask, hi, biases[0]);
 
     const float c2 = s.scale * kLog2e, slack = fminf(8.0f / c2, 0x1p127f);
     float top = -INFINITY, sum = 0.0f;
@@ -681,7 +685,7 @@ __global__ __launch_bounds__((FwdCut<T, D16, kFew>::kThreads), (waves_of<T, D16>
         for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int b = 0; b < 4; ++b)
-                store4(part, 32 * d + 8 * b + 4 * h, s.D, kDirect || (s.D & 3) == 0, o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2],
+                store4(part, 32 * d + 8 * b + 4 * h, s.D, kVec || (s.D & 3) == 0, o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2],
                        o[d][4 * b + 3]);
         if (h == 0) {
             g.stat[id * 2] = top;
@@ -695,7 +699,7 @@ __global__ __launch_bounds__((FwdCut<T, D16, kFew>::kThreads), (waves_of<T, D16>
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int b = 0; b < 4; ++b)
-            store4(y, 32 * d + 8 * b + 4 * h, s.D, kDirect || g.vec, o[d][4 * b] * inv, o[d][4 * b + 1] * inv, o[d][4 * b + 2] * inv,
+            store4(y, 32 * d + 8 * b + 4 * h, s.D, kVec, o[d][4 * b] * inv, o[d][4 * b + 1] * inv, o[d][4 * b + 2] * inv,
                    o[d][4 * b + 3] * inv);
     if (g.a.lse && h == 0)
         g.a.lse[((int64_t)n * s.Hq + me.head) * s.Lq + me.t] =
@@ -817,8 +821,9 @@ __device__ __forceinline__ void keep_range(const f32x16 (&ds)[NB], float& up, f3
 __device__ __forceinline__ float share_of(float sum) { return sum == 0.0f ? 0.0f : 1.0f / sum; }
 
 // dq of 128 rows, and delta.
-template <typename T, int D16, bool kDirect>
+template <typename T, int D16, int kHow>
 __global__ __launch_bounds__(256, (waves_of<T, D16>(4))) void k_attn_dq(AttnK g) {
+    constexpr bool kDirect = kHow == kStraight, kVec = kHow != kAnywhere;
     constexpr int NT = 256, KT = 64, KB = 2, DB = (D16 + 1) / 2;
     constexpr bool kHalf = std::is_same_v<T, _Float16>, kFix = sizeof(T) == 2;
     using Tl = Tile<T, D16, KT>;
@@ -842,8 +847,8 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(4))) void k_attn_dq(AttnK g)
     float delta = 0.0f;
 #pragma unroll
     for (int c = 0; c < D16; ++c) {
-        fq[c] = load_frag(q, c, h, s.D, kDirect || g.vec);
-        const Eight<T> ed(dy, c, h, s.D, kDirect || g.vec), ey(y, c, h, s.D, kDirect || g.vec);
+        fq[c] = load_frag(q, c, h, s.D, kVec);
+        const Eight<T> ed(dy, c, h, s.D, kVec), ey(y, c, h, s.D, kVec);
         fo[c] = ed.frag();
 #pragma unroll
         for (int j = 0; j < 8; ++j) delta = __builtin_fmaf((float)ed.v[j], (float)ey.v[j], delta);
@@ -858,8 +863,8 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(4))) void k_attn_dq(AttnK g)
     const T* kbase = (const T*)g.b.k + (int64_t)n * s.Lk * s.ldk + (int64_t)hk * s.D;
     const T* vbase = (const T*)g.b.v + (int64_t)n * s.Lk * s.ldv + (int64_t)hk * s.D;
     const uint8_t* mask = g.b.mask ? g.b.mask + (int64_t)n * s.Lk : nullptr;
-    KeyTiles<T, D16, KT, NT, kDirect> in;
-    in.init(s, g.vec, kbase, vbase, mask, hi, biases[0]);
+    KeyTiles<T, D16, KT, NT, kHow> in;
+    in.init(s, kbase, vbase, mask, hi, biases[0]);
 
     const float c2 = s.scale * kLog2e;
     float up = kHalf ? 0x1p100f : 1.0f, lack = 0.0f, round = 0.0f;
@@ -943,10 +948,10 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(4))) void k_attn_dq(AttnK g)
         for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
-                store4(part, 32 * d + 8 * b + 4 * h, s.D, kDirect || (s.D & 3) == 0, acc[d][4 * b] * f, acc[d][4 * b + 1] * f,
+                store4(part, 32 * d + 8 * b + 4 * h, s.D, kVec || (s.D & 3) == 0, acc[d][4 * b] * f, acc[d][4 * b + 1] * f,
                        acc[d][4 * b + 2] * f, acc[d][4 * b + 3] * f);
                 if constexpr (kFix)
-                    store4(part2, 32 * d + 8 * b + 4 * h, s.D, kDirect || (s.D & 3) == 0, mean[d][4 * b] * fm,
+                    store4(part2, 32 * d + 8 * b + 4 * h, s.D, kVec || (s.D & 3) == 0, mean[d][4 * b] * fm,
                            mean[d][4 * b + 1] * fm, mean[d][4 * b + 2] * fm, mean[d][4 * b + 3] * fm);
             }
         if (h == 0) {
@@ -977,7 +982,7 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(4))) void k_attn_dq(AttnK g)
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int b = 0; b < 4; ++b)
-            store4(dq, 32 * d + 8 * b + 4 * h, s.D, kDirect || g.vec, acc[d][4 * b], acc[d][4 * b + 1], acc[d][4 * b + 2],
+            store4(dq, 32 * d + 8 * b + 4 * h, s.D, kVec, acc[d][4 * b], acc[d][4 * b + 1], acc[d][4 * b + 2],
                    acc[d][4 * b + 3]);
 }
 
@@ -1015,7 +1020,7 @@ __global__ __launch_bounds__(256) void k_attn_dq_join(AttnK g) {
 }
 
 // The rows' tiles, of q and dy, of a walk over a pair's rows up to hi.
-template <typename T, int D16, int RT, int NT, bool kDirect>
+template <typename T, int D16, int RT, int NT, int kHow>
 struct RowTiles {
     Moving<T, D16, RT, NT> mq, mo;
     const AttnK* g;
@@ -1029,11 +1034,11 @@ struct RowTiles {
         mq.load([&](int r) {
             const RowAt x = row_at(*g, n, hk, r0 + r);
             return r0 + r < hi ? (const T*)g->b.q + x.tok * s.ldq + (int64_t)x.head * s.D : nullptr;
-        }, s.D, g->vec);
+        }, s.D, kHow == kWords);
         mo.load([&](int r) {
             const RowAt x = row_at(*g, n, hk, r0 + r);
             return r0 + r < hi ? (const T*)g->b.dy + (x.tok * s.Hq + x.head) * s.D : nullptr;
-        }, s.D, g->vec);
+        }, s.D, kHow == kWords);
     }
     __device__ __forceinline__ void store(char* sq, char* so) const {
         mq.store(sq);
@@ -1043,7 +1048,7 @@ struct RowTiles {
 // Straight to LDS.  rep divides a tile's rows: its tokens are whole, and offsets the same in
 // every tile.
 template <typename T, int D16, int RT, int NT>
-struct RowTiles<T, D16, RT, NT, true> {
+struct RowTiles<T, D16, RT, NT, kStraight> {
     using Tl = Tile<T, D16, RT>;
     Direct<Tl, RT, NT> mq, mo;
     const T *q, *dy;
@@ -1084,8 +1089,9 @@ struct RowTiles<T, D16, RT, NT, true> {
 // of 225 for 16 images of 3136 by 0 to 1024 tokens, 8 and 4 heads of 64, bf16).  Keys that are
 // left out are columns of their own, so what they hold goes nowhere.
 constexpr int kOwnKeys = 64;
-template <typename T, int D16, bool kDirect>
-__global__ __launch_bounds__(256, (waves_of<T, D16>(kDirect ? 6 : 4))) void k_attn_dkv(AttnK g) {
+template <typename T, int D16, int kHow>
+__global__ __launch_bounds__(256, (kHow == kStraight && D16 == 4 ? 3 : waves_of<T, D16>(kHow == kStraight ? 6 : 4))) void k_attn_dkv(AttnK g) {
+    constexpr bool kDirect = kHow == kStraight, kVec = kHow != kAnywhere;
     constexpr int NT = 256, RT = 64, DB = (D16 + 1) / 2, CP = kCopies<T>;
     constexpr bool kHalf = std::is_same_v<T, _Float16>, kShare = sizeof(T) == 4;
     using Tl = Tile<T, D16, RT>;
@@ -1108,12 +1114,12 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(kDirect ? 6 : 4))) void k_at
     Frag<T> fk[D16], fv[D16];
 #pragma unroll
     for (int c = 0; c < D16; ++c) {
-        fk[c] = load_frag(k, c, h, s.D, kDirect || g.vec);
-        fv[c] = load_frag(v, c, h, s.D, kDirect || g.vec);
+        fk[c] = load_frag(k, c, h, s.D, kVec);
+        fv[c] = load_frag(v, c, h, s.D, kVec);
     }
     int64_t lo, hi;
     part_of(tile * kOwnKeys < len ? s.rows : 0, RT, split, g.splits, lo, hi);
-    RowTiles<T, D16, RT, NT, kDirect> in;
+    RowTiles<T, D16, RT, NT, kHow> in;
     in.init(g, n, hk, hi);
     float moff = 0.0f, mdel = 0.0f, mshare = 0.0f;
     // rows past hi: P = 1, but their q and dy are zeros
@@ -1236,9 +1242,9 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(kDirect ? 6 : 4))) void k_at
     };
     if (g.splits > 1) {
         const int64_t id = (((int64_t)split * s.N * s.Hk + pair) * s.Lk + key) * s.D;
-        put(g.part + id, g.part2 + id, kDirect || (s.D & 3) == 0);
+        put(g.part + id, g.part2 + id, kVec || (s.D & 3) == 0);
     } else {
-        put((T*)g.b.dk + tok * s.ldk + (int64_t)hk * s.D, (T*)g.b.dv + tok * s.ldv + (int64_t)hk * s.D, kDirect || g.vec);
+        put((T*)g.b.dk + tok * s.ldk + (int64_t)hk * s.D, (T*)g.b.dv + tok * s.ldv + (int64_t)hk * s.D, kVec);
     }
 }
 
@@ -1272,7 +1278,7 @@ inline unsigned cut(AttnK& a, const AttnCut& c) {
     return (unsigned)((a.by_xcd ? (pairs + 7) / 8 * 8 : pairs) * c.tiles * c.splits);
 }
 
-template <typename T, int D16, bool kDirect>
+template <typename T, int D16, int kHow>
 hipError_t attn_run_by(const AttnK& g, const AttnPlan& p, bool backward, hipStream_t st) {
     AttnK a = g;
     const AttnShape& s = g.s;
@@ -1280,9 +1286,9 @@ hipError_t attn_run_by(const AttnK& g, const AttnPlan& p, bool backward, hipStre
     unsigned blocks = cut(a, p.rows);
     if (!backward) {
         if (p.few)
-            k_attn<T, D16, true, kDirect><<<blocks, FwdCut<T, D16, true>::kThreads, 0, st>>>(a);
+            k_attn<T, D16, true, kHow><<<blocks, FwdCut<T, D16, true>::kThreads, 0, st>>>(a);
         else
-            k_attn<T, D16, false, kDirect><<<blocks, FwdCut<T, D16, false>::kThreads, 0, st>>>(a);
+            k_attn<T, D16, false, kHow><<<blocks, FwdCut<T, D16, false>::kThreads, 0, st>>>(a);
         if (a.splits > 1) {
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
@@ -1293,7 +1299,7 @@ hipError_t attn_run_by(const AttnK& g, const AttnPlan& p, bool backward, hipStre
         return hipGetLastError();
     }
     a.part2 = a.part + (size_t)a.splits * pairs * s.rows * s.D;
-    k_attn_dq<T, D16, kDirect><<<blocks, 256, 0, st>>>(a);
+    k_attn_dq<T, D16, kHow><<<blocks, 256, 0, st>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (a.splits > 1) {
@@ -1302,29 +1308,27 @@ hipError_t attn_run_by(const AttnK& g, const AttnPlan& p, bool backward, hipStre
     }
     blocks = cut(a, p.keys);
     a.part2 = a.part + (size_t)a.splits * pairs * s.Lk * s.D;
-    bool direct = false;
-    if constexpr (kDirect) {
-        direct = 64 % s.rep == 0;
-        if (direct) k_attn_dkv<T, D16, true><<<blocks, 256, 0, st>>>(a);
-    }
-    if (!direct) k_attn_dkv<T, D16, false><<<blocks, 256, 0, st>>>(a);
+    // straight to LDS tokens are whole in a tile of 64 rows
+    if (kHow == kStraight && 64 % s.rep) k_attn_dkv<T, D16, kWords><<<blocks, 256, 0, st>>>(a);
+    else k_attn_dkv<T, D16, kHow><<<blocks, 256, 0, st>>>(a);
     e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
     k_attn_sum<T><<<dim3((unsigned)((pairs * s.Lk * s.D + 255) / 256), 2), 256, 0, st>>>(a);
     return hipGetLastError();
 }
 
-// Tiles go straight to LDS where words and offsets allow: 16-byte words, and the rows of a
-// tile, 128 of them at most, within 2^31 bytes.
+// vec: vectors of whole 16-byte words.  16-bit tiles of them go straight to LDS where the rows
+// of a tile, 64 of them, are within 2^31 bytes.
 template <typename T, int D16>
 hipError_t attn_run(const AttnK& g, const AttnPlan& p, bool backward, hipStream_t st) {
     constexpr int kMost = 1 << 22;
-    if constexpr (sizeof(T) == 2) {
-        const AttnShape& s = g.s;
-        if (g.vec && s.ldq <= kMost && s.ldk <= kMost && s.ldv <= kMost && s.Hq * s.D <= kMost)
-            return attn_run_by<T, D16, true>(g, p, backward, st);
+    const AttnShape& s = g.s;
+    if constexpr (sizeof(T) == 4) {
+        if (g.vec) return attn_run_by<T, D16, kWords>(g, p, backward, st);
+    } else if (g.vec && s.ldq <= kMost && s.ldk <= kMost && s.ldv <= kMost && s.Hq * s.D <= kMost) {
+        return attn_run_by<T, D16, kStraight>(g, p, backward, st);
     }
-    return attn_run_by<T, D16, false>(g, p, backward, st);
+    return attn_run_by<T, D16, kAnywhere>(g, p, backward, st);
 }
 
 template <typename T>

@@ -196,26 +196,71 @@ __device__ __forceinline__ void product(f32x16 (&acc)[S::AB][S::BB], A& a, B& b,
         a.load(lds + copy * kBoth, k, hi);
         b.load(lds + copy * kBoth + A::kBytes, k, hi);
     };
+    decltype(A::read(lds, 0, 0, 0)) fa[2][S::AB];
+    decltype(B::read(lds, 0, 0, 0)) fb[2][S::BB];
+    auto read = [&](const char* t, int c) {
+#pragma unroll
+        for (int i = 0; i < S::AB; ++i) fa[c][i] = A::read(t, i * S::WA + wa, c, lane);
+#pragma unroll
+        for (int j = 0; j < S::BB; ++j) fb[c][j] = B::read(t + A::kBytes, wb * S::BB + j, c, lane);
+    };
+    auto multiply = [&](int c) {
+#pragma unroll
+        for (int i = 0; i < S::AB; ++i)
+#pragma unroll
+            for (int j = 0; j < S::BB; ++j) acc[i][j] = mma(fa[c][i], fb[c][j], acc[i][j]);
+    };
+    static_assert(kBk == 32);
     // straight to LDS: one step ahead in two copies, two steps in three
     constexpr int N = copies_of<typename A::Value, S>();
     int copy = 0;
     if (lo < hi) load(0, lo);
-    if (direct && N == 3 && lo + kBk < hi) load(1, lo + kBk);
-    for (int64_t k = lo; k < hi; k += kBk) {
-        char* t = lds + copy * kBoth;
-        if (direct) {
-            if (N == 3 && k + kBk < hi) ready<A::kLoads + B::kLoads>();
-            else if (N == 3 && k > lo) ready<F::kAfter>();
-            else ready<0>();
-            const int before = copy == 0 ? N - 1 : copy - 1;
-            copy = copy == N - 1 ? 0 : copy + 1;
-            if (k + (N - 1) * kBk < hi) {
-                load(before, k + (N - 1) * kBk);
+    if (direct && N == 3) {
+        // Half a step's products run while the other half's operands are on their way, and the
+        // wait for the next tile is between the halves: its first operands, read right after,
+        // have the second half's products to arrive in.  A tile is done with once its step's wait
+        // is passed.
+        constexpr int kLoads = A::kLoads + B::kLoads;
+        if (lo + kBk < hi) {
+            load(1, lo + kBk);
+            ready<kLoads>();
+        } else {
+            ready<0>();
+        }
+        read(lds, 0);
+        for (int64_t k = lo; k < hi; k += kBk) {
+            const char* t = lds + copy * kBoth;
+            const int before = copy == 0 ? 2 : copy - 1;
+            copy = copy == 2 ? 0 : copy + 1;
+            read(t, 1);
+            if (k + 2 * kBk < hi) {
+                load(before, k + 2 * kBk);
             } else if (F::kAfter > 0) {
                 const bool last = k + kBk >= hi;
                 if (!last || k == lo) after(0, lds + before * kBoth);
                 if (last) after(1, lds + (k == lo ? copy : before) * kBoth);
             }
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (k + kBk < hi) {
+                if (k + 2 * kBk < hi) ready<kLoads>();
+                else ready<F::kAfter>();
+                read(lds + copy * kBoth, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(1);
+        }
+        if (F::kAfter > 0) ready<0>();
+        else __syncthreads();                // the tiles' LDS is free
+        return;
+    }
+    for (int64_t k = lo; k < hi; k += kBk) {
+        char* t = lds + copy * kBoth;
+        if (direct) {
+            ready<0>();
+            copy ^= 1;
+            if (k + kBk < hi) load(copy, k + kBk);
         } else {
             __syncthreads();
             a.store(t);
@@ -225,19 +270,11 @@ __device__ __forceinline__ void product(f32x16 (&acc)[S::AB][S::BB], A& a, B& b,
         }
 #pragma unroll
         for (int c = 0; c < kBk / 16; ++c) {
-            decltype(A::read(t, 0, 0, 0)) fa[S::AB], fb[S::BB];
-#pragma unroll
-            for (int i = 0; i < S::AB; ++i) fa[i] = A::read(t, i * S::WA + wa, c, lane);
-#pragma unroll
-            for (int j = 0; j < S::BB; ++j) fb[j] = B::read(t + A::kBytes, wb * S::BB + j, c, lane);
-#pragma unroll
-            for (int i = 0; i < S::AB; ++i)
-#pragma unroll
-                for (int j = 0; j < S::BB; ++j) acc[i][j] = mma(fa[i], fb[j], acc[i][j]);
+            read(t, c);
+            multiply(c);
         }
     }
-    if (F::kAfter > 0) ready<0>();
-    else __syncthreads();                    // the tiles' LDS is free
+    __syncthreads();                         // the tiles' LDS is free
 }
 
 // A wave's 32 rows by 64 columns on their way between a lane's order (a row; columns 32 w
