@@ -293,6 +293,15 @@ struct Moving {
     }
 };
 
+// `bytes` at p, zeros behind them, as loads take it
+typedef uint32_t Buffer __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ Buffer buffer_of(const void* p, uint32_t bytes) {
+    const uint64_t at = (uint64_t)p;
+    return Buffer{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at),
+                  (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)) & 0xffffu,
+                  (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u};
+}
+
 // A tile of R rows from memory straight to LDS, 16 bytes a lane, whose place is fixed there:
 // a lane takes the chunk that belongs to it.  Offsets past 2^31 read zeros, as do rows past
 // the buffer's end; they are the same for every tile.  (In place of Moving: 64 keys of 64
@@ -311,46 +320,42 @@ struct Direct {
             off[i] = chunk < used ? offset(row, chunk) : 0x80000000u;
         }
     }
-    // to the tile at t; bytes: of the buffer at p.  In assembly: the compiler would wait for
-    // every load to LDS before it reads any of LDS, the other copies' tiles too.  What waits for
-    // them is ready().
+    // to the tile at t; bytes: of the buffer at p
     __device__ __forceinline__ void issue(char* t, const void* p, uint32_t bytes) const {
-        typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-        const uint64_t at = (uint64_t)p;
-        const u32x4 r = {(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at),
-                         (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)) & 0xffffu,
-                         (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u};
+        issue_at(place(t), buffer_of(p, bytes), 0);
+    }
+    // this wave's part of the tile at t
+    __device__ static __forceinline__ uint32_t place(char* t) {
         const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)t;
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        return __builtin_amdgcn_readfirstlane(lds + (threadIdx.x >> 6) * 1024);
+    }
+    // at: bytes from the buffer's start.  In assembly: the compiler would wait for every load to
+    // LDS before it reads any of LDS, the other copies' tiles too.  What waits for them is ready().
+    __device__ __forceinline__ void issue_at(uint32_t lds, const Buffer& r, uint32_t at) const {
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"          // m0 on the clobber list
 #pragma unroll
         for (int i = 0; i < kN; ++i)
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(
-                             __builtin_amdgcn_readfirstlane(lds + (i * NT + wave * 64) * 16)),
-                         "v"(off[i]), "s"(r)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds + i * NT * 16),
+                         "v"(off[i]), "s"(r), "s"(at)
                          : "memory", "m0");
 #pragma clang diagnostic pop
     }
     // the same, of each row `used` chunks
-    __device__ __forceinline__ void issue_part(char* t, const void* p, uint32_t bytes, int used) const {
+    __device__ __forceinline__ Direct part(int used) const {
         Direct d;
 #pragma unroll
         for (int i = 0; i < kN; ++i) {
             const int at = threadIdx.x + i * NT, row = at / kRowChunks;
             d.off[i] = ((at % kRowChunks) ^ Tl::twist(row)) < used ? off[i] : 0x80000000u;
         }
-        d.issue(t, p, bytes);
+        return d;
     }
 };
 // 64 floats (or bytes, each a word of LDS) at p, `left` of them and zeros behind, to LDS by one wave.
 template <typename V>
 __device__ __forceinline__ void load_words(void* t, const V* p, int64_t left) {
-    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-    const uint64_t at = (uint64_t)p;
-    const u32x4 r = {(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at),
-                     (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)) & 0xffffu,
-                     (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(left < 64 ? left : 64) * (uint32_t)sizeof(V)), 0x00020000u};
+    const Buffer r = buffer_of(p, (uint32_t)(left < 64 ? left : 64) * (uint32_t)sizeof(V));
     const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(char*)t);
     const uint32_t off = (threadIdx.x & 63) * (uint32_t)sizeof(V);
 #pragma clang diagnostic push
