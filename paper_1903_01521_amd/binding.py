@@ -446,7 +446,7 @@ def wino_conv2d_wgrad_nhwc(x, dy, dg, stats, gamma, beta, G, N, C, H, W, K, pad,
 WINO_FLAG_PAIRS = 0x008
 
 
-def _rows(t, dtype, ld):
+def _rows(t, dtype, L, D, ld):
     """[N][L][heads][D] of `dtype`, tokens ld elements apart: a dense tensor, or a view of
     one projection's."""
     if t is None or isinstance(t, int):
@@ -455,14 +455,17 @@ def _rows(t, dtype, ld):
         raise ValueError("tensors must have the element type that the flags name")
     if not t.is_cuda:
         raise ValueError("device buffers must be CUDA (HIP) tensors")
-    if not (t.is_contiguous() and (t.dim() != 4 or t.stride(1) == ld)):
+    # a small call's host time is that of such checks: first the one that mostly decides
+    if t.stride() != (L * ld, ld, D, 1):
         _check_rows(t, ld)
     return t.data_ptr()
 
 
 def _check_rows(t, ld):
     if t.dim() != 4:
-        raise ValueError("device buffers must be contiguous, or views [N][L][heads][D]")
+        if not t.is_contiguous():
+            raise ValueError("device buffers must be contiguous, or views [N][L][heads][D]")
+        return
     (N, L, H, D), (sn, sl, sh, sd) = t.shape, t.stride()
     if (D > 1 and sd != 1) or (H > 1 and sh != D) or (L > 1 and sl != ld) or (N > 1 and sn != L * ld):
         raise ValueError("a token's heads must lie together, tokens ld elements apart and images L * ld")
@@ -482,7 +485,7 @@ def _dense(t, dtype, what="tensors must have the element type that the flags nam
 
 
 def _iptr(t):
-    return _dense(t, (_torch or _import_torch()).int32, "positions and lengths must be int32")
+    return None if t is None else _dense(t, (_torch or _import_torch()).int32, "positions and lengths must be int32")
 
 
 def _mptr(t):
@@ -496,7 +499,7 @@ def _mptr(t):
 def wino_qk_norm_nhwc(q, k, gq, gk, rot, qpos, kpos, yq, yk, N, Lq, Lk, Hq, Hk, D, R, T, ldq, ldk, eps, flags=0,
                       stream=None) -> int:
     t, f32 = _type(flags), _type(0)
-    return lib().wino_qk_norm_nhwc(_rows(q, t, ldq), _rows(k, t, ldk), _dense(gq, f32), _dense(gk, f32), _dense(rot, f32),
+    return lib().wino_qk_norm_nhwc(_rows(q, t, Lq, D, ldq), _rows(k, t, Lk, D, ldk), _dense(gq, f32), _dense(gk, f32), _dense(rot, f32),
                                    _iptr(qpos), _iptr(kpos), _dense(yq, t), _dense(yk, t), N, Lq, Lk, Hq, Hk, D,
                                    R, T, ldq, ldk, eps, flags, _stream(stream))
 
@@ -509,8 +512,8 @@ def wino_qk_norm_backward_nhwc(dyq, dyk, q, k, gq, gk, rot, qpos, kpos, dq, dk, 
                                ldq, ldk, eps, flags=0, workspace=None, workspace_bytes=0, stream=None) -> int:
     t, f32 = _type(flags), _type(0)
     return lib().wino_qk_norm_backward_nhwc(
-        _dense(dyq, t), _dense(dyk, t), _rows(q, t, ldq), _rows(k, t, ldk), _dense(gq, f32), _dense(gk, f32),
-        _dense(rot, f32), _iptr(qpos), _iptr(kpos), _rows(dq, t, ldq), _rows(dk, t, ldk), _dense(dgq, f32), _dense(dgk, f32), N,
+        _dense(dyq, t), _dense(dyk, t), _rows(q, t, Lq, D, ldq), _rows(k, t, Lk, D, ldk), _dense(gq, f32), _dense(gk, f32),
+        _dense(rot, f32), _iptr(qpos), _iptr(kpos), _rows(dq, t, Lq, D, ldq), _rows(dk, t, Lk, D, ldk), _dense(dgq, f32), _dense(dgk, f32), N,
         Lq, Lk, Hq, Hk, D, R, T, ldq, ldk, eps, flags, _ptr(workspace), workspace_bytes, _stream(stream))
 
 
@@ -521,7 +524,7 @@ def wino_cross_attention_workspace_bytes(N, Lq, Lk, Hq, Hk, D, flags=0) -> int:
 def wino_cross_attention_nhwc(q, k, v, klen, mask, y, lse, N, Lq, Lk, Hq, Hk, D, ldq, ldk, ldv, scale, flags=0,
                               workspace=None, workspace_bytes=0, stream=None) -> int:
     t, f32 = _type(flags), _type(0)
-    return lib().wino_cross_attention_nhwc(_rows(q, t, ldq), _rows(k, t, ldk), _rows(v, t, ldv),
+    return lib().wino_cross_attention_nhwc(_rows(q, t, Lq, D, ldq), _rows(k, t, Lk, D, ldk), _rows(v, t, Lk, D, ldv),
                                            _iptr(klen), _mptr(mask), _dense(y, t), _dense(lse, f32), N, Lq, Lk, Hq, Hk, D,
                                            ldq, ldk, ldv, scale, flags, _ptr(workspace), workspace_bytes,
                                            _stream(stream))
@@ -535,8 +538,8 @@ def wino_cross_attention_backward_nhwc(dy, q, k, v, y, lse, klen, mask, dq, dk, 
                                        ldv, scale, flags=0, workspace=None, workspace_bytes=0, stream=None) -> int:
     t, f32 = _type(flags), _type(0)
     return lib().wino_cross_attention_backward_nhwc(
-        _dense(dy, t), _rows(q, t, ldq), _rows(k, t, ldk), _rows(v, t, ldv), _dense(y, t),
-        _dense(lse, f32), _iptr(klen), _mptr(mask), _rows(dq, t, ldq), _rows(dk, t, ldk), _rows(dv, t, ldv), N,
+        _dense(dy, t), _rows(q, t, Lq, D, ldq), _rows(k, t, Lk, D, ldk), _rows(v, t, Lk, D, ldv), _dense(y, t),
+        _dense(lse, f32), _iptr(klen), _mptr(mask), _rows(dq, t, Lq, D, ldq), _rows(dk, t, Lk, D, ldk), _rows(dv, t, Lk, D, ldv), N,
         Lq, Lk, Hq, Hk, D, ldq, ldk, ldv, scale, flags, _ptr(workspace), workspace_bytes, _stream(stream))
 
 

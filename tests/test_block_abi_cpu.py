@@ -191,11 +191,18 @@ def test_gated_workspace_bytes():
 def test_binding_checks_tensors():
     t = torch.empty(2, 3, 4, 5)
     with pytest.raises(ValueError):
-        B._rows(t, torch.float32, 20)                                            # not on a GPU
+        B._rows(t, torch.float32, 3, 5, 20)                                            # not on a GPU
     with pytest.raises(ValueError):
-        B._rows(t.transpose(1, 2), torch.float32, 20)                            # heads are not together
+        B._rows(t.transpose(1, 2), torch.float32, 4, 5, 20)                            # heads are not together
     with pytest.raises(ValueError):
-        B._rows(t[:, :, :2], torch.float32, 10)                                  # tokens are 20 apart
+        B._rows(t[:, :, :2], torch.float32, 3, 5, 10)                                  # tokens are 20 apart
+    B._check_rows(t, 20)
+    B._check_rows(t[:, :, :2], 20)
+    B._check_rows(t[:1, :1], 999)                                    # one token: any distance
+    B._check_rows(t.view(-1), 999)                                   # sizes are the call's
+    for bad, ld in ((t.transpose(1, 2), 20), (t[:, :, :2], 10), (t, 21), (t[:, ::2], 20), (t.view(-1)[::2], 20)):
+        with pytest.raises(ValueError):
+            B._check_rows(bad, ld)
     with pytest.raises(ValueError):
         B._iptr(torch.empty(3, dtype=torch.int64))
     with pytest.raises(ValueError):
