@@ -704,33 +704,45 @@ __global__ __launch_bounds__(256, 2) void k_gated_dw(GatedK g) {
     else put_tile<S>(acc, lds, (T*)g.a.dw, c0, g.C, f0, F, g.vec);
 }
 
-// n sums of `splits` parts.
+// What a backward call's products left in parts, in one launch (three took 5 us each): dbias, a
+// column's rows by 16 threads, then dx, then dw.
+struct GatedEnd {
+    const float *rows, *px, *pw;             // [tiles][F]; [x_splits][nx]; [w_splits][nw]
+    float* dbias;
+    void *dx, *dw;
+    int64_t tiles, nx, nw;
+    int F, x_splits, w_splits;
+    unsigned db_blocks, dx_blocks;           // workgroups of the first two; 0: none to do
+};
 template <typename T>
-__global__ __launch_bounds__(256) void k_gated_sum(const float* part, T* out, int64_t n, int splits) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+__global__ __launch_bounds__(256) void k_gated_end(GatedEnd g) {
+    __shared__ float s[16][17];
+    if (blockIdx.x < g.db_blocks) {
+        const int f = blockIdx.x * 16 + (threadIdx.x & 15), i0 = threadIdx.x >> 4;
+        float sum = 0.0f;
+        if (f < g.F)
+#pragma unroll 8
+            for (int64_t i = i0; i < g.tiles; i += 16) sum += g.rows[i * g.F + f];
+        s[i0][threadIdx.x & 15] = sum;
+        __syncthreads();
+        if (threadIdx.x < 16 && f < g.F) {
+            float all = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) all += s[i][threadIdx.x];
+            g.dbias[f] = all;
+        }
+        return;
+    }
+    const unsigned at = blockIdx.x - g.db_blocks;
+    const bool x = at < g.dx_blocks;
+    const int64_t i = (int64_t)(x ? at : at - g.dx_blocks) * 256 + threadIdx.x, n = x ? g.nx : g.nw;
     if (i >= n) return;
+    const float* part = x ? g.px : g.pw;
+    const int splits = x ? g.x_splits : g.w_splits;
     float sum = 0.0f;
 #pragma unroll 8
     for (int k = 0; k < splits; ++k) sum += part[k * n + i];
-    out[i] = (T)sum;
-}
-
-// dbias: 16 columns a workgroup, 16 threads a column.
-__global__ __launch_bounds__(256) void k_gated_db(GatedK g, int64_t rows) {
-    const int F = 2 * g.K, f = blockIdx.x * 16 + (threadIdx.x & 15), i0 = threadIdx.x >> 4;
-    float sum = 0.0f;
-    if (f < F)
-#pragma unroll 8
-        for (int64_t i = i0; i < rows; i += 16) sum += g.dbias[i * F + f];
-    __shared__ float s[16][17];
-    s[i0][threadIdx.x & 15] = sum;
-    __syncthreads();
-    if (threadIdx.x < 16 && f < F) {
-        float all = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) all += s[i][threadIdx.x];
-        g.a.dbias[f] = all;
-    }
+    ((T*)(x ? g.dx : g.dw))[i] = (T)sum;
 }
 
 template <typename F>
@@ -813,15 +825,15 @@ GatedPlan gated_plan(const GatedShape& s, bool backward) {
     // no wider than the channels are
     if (p.dw < kNarrow && s.C <= Narrow::kA) p.dw = kNarrow;
     p.dw_splits = parts_of(tiles_by(p.dw, s.C, F), parts);
+    // the last launch: dbias's columns, and sums of at most 256 tiles of 128 by 256 for each product
     p.fits = fits(tiles_by(p.dx, s.C, s.M) * p.dx_splits) && fits(tiles_by(p.dw, s.C, F) * p.dw_splits) &&
-             fits(tiles_of(F, 16));
+             fits(tiles_of(F, 16) + 2 * 256 * (128 * 256 / 256));
     if (!p.fits) return p;
     p.dz = round_up((size_t)s.M * F * io_size(s.io), 16);
     p.dbias = round_up((size_t)tiles_of(s.M, Narrow::kB) * F * 4, 16);
-    const size_t x = p.dx_splits > 1 ? (size_t)p.dx_splits * s.M * s.C * 4 : 0;
-    const size_t w = p.dw_splits > 1 ? (size_t)p.dw_splits * F * s.C * 4 : 0;
-    p.part = round_up(x > w ? x : w, 16);
-    p.need = p.dz + p.dbias + p.part;
+    p.px = p.dx_splits > 1 ? round_up((size_t)p.dx_splits * s.M * s.C * 4, 16) : 0;
+    p.pw = p.dw_splits > 1 ? round_up((size_t)p.dw_splits * F * s.C * 4, 16) : 0;
+    p.need = p.dz + p.dbias + p.px + p.pw;
     return p;
 }
 
@@ -851,47 +863,67 @@ hipError_t launch_gated_backward(const GatedArgs& a, const GatedShape& s, const 
     const int64_t F = 2 * (int64_t)s.K;
     g.dz = ws;
     g.dbias = (float*)((char*)ws + p.dz);
-    g.part = (float*)((char*)ws + p.dz + p.dbias);
-    int64_t rows = 0;
+    char* parts = (char*)ws + p.dz + p.dbias;
+    GatedEnd end{};
+    end.F = (int)F;
     hipError_t e = with_all<true>(g, s.io, p.first, [&](auto t, auto sh, auto direct) {
         typedef decltype(sh) S;
         g.tiles = (int)tiles_of(s.K, S::kA / 2);
-        rows = tiles_of(s.M, S::kB);
-        g.items = (int)(rows * g.tiles);
+        end.tiles = tiles_of(s.M, S::kB);
+        g.items = (int)(end.tiles * g.tiles);
         k_gated<decltype(t), S, true, direct.value><<<grid_of(g.items), 256, 0, st>>>(g);
         return hipGetLastError();
     });
     if (e != hipSuccess) return e;
     if (a.dbias) {
-        k_gated_db<<<(unsigned)tiles_of(F, 16), 256, 0, st>>>(g, rows);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
+        end.rows = g.dbias;
+        end.dbias = a.dbias;
+        end.db_blocks = (unsigned)tiles_of(F, 16);
     }
-    auto sum = [&](auto t, void* out, int64_t n) {
-        if (g.splits == 1) return hipSuccess;
-        k_gated_sum<<<(unsigned)tiles_of(n, 256), 256, 0, st>>>(g.part, (decltype(t)*)out, n, g.splits);
-        return hipGetLastError();
-    };
     if (a.dx) {
+        g.part = (float*)parts;
+        g.splits = p.dx_splits;
+        if (g.splits > 1) {
+            end.px = g.part;
+            end.dx = a.dx;
+            end.nx = s.M * s.C;
+            end.x_splits = g.splits;
+            end.dx_blocks = (unsigned)tiles_of(end.nx, 256);
+        }
         e = with_all<false>(g, s.io, p.dx, [&](auto t, auto sh, auto direct) {
             typedef decltype(sh) S;
-            g.splits = p.dx_splits;
             g.tiles = (int)tiles_of(s.C, S::kA);
             g.items = (int)(tiles_of(s.M, S::kB) * g.tiles * g.splits);
             k_gated_dx<decltype(t), S, direct.value><<<grid_of(g.items), 256, 0, st>>>(g);
-            const hipError_t e = hipGetLastError();
-            return e != hipSuccess ? e : sum(t, a.dx, s.M * s.C);
+            return hipGetLastError();
         });
         if (e != hipSuccess) return e;
     }
-    if (!a.dw) return hipSuccess;
-    return with_all<false>(g, s.io, p.dw, [&](auto t, auto sh, auto direct) {
-        typedef decltype(sh) S;
+    unsigned dw_blocks = 0;
+    if (a.dw) {
+        g.part = (float*)(parts + p.px);
         g.splits = p.dw_splits;
-        g.tiles = (int)tiles_of(s.C, S::kA);
-        g.items = (int)(g.tiles * tiles_of(F, S::kB) * g.splits);
-        k_gated_dw<decltype(t), S, direct.value><<<grid_of(g.items), 256, 0, st>>>(g);
-        const hipError_t e = hipGetLastError();
-        return e != hipSuccess ? e : sum(t, a.dw, F * s.C);
+        if (g.splits > 1) {
+            end.pw = g.part;
+            end.dw = a.dw;
+            end.nw = F * s.C;
+            end.w_splits = g.splits;
+            dw_blocks = (unsigned)tiles_of(end.nw, 256);
+        }
+        e = with_all<false>(g, s.io, p.dw, [&](auto t, auto sh, auto direct) {
+            typedef decltype(sh) S;
+            g.tiles = (int)tiles_of(s.C, S::kA);
+            g.items = (int)(g.tiles * tiles_of(F, S::kB) * g.splits);
+            k_gated_dw<decltype(t), S, direct.value><<<grid_of(g.items), 256, 0, st>>>(g);
+            return hipGetLastError();
+        });
+        if (e != hipSuccess) return e;
+    }
+    const unsigned blocks = end.db_blocks + end.dx_blocks + dw_blocks;
+    if (!blocks) return hipSuccess;
+    return with_io(s.io, [&](auto t) {
+        k_gated_end<decltype(t)><<<blocks, 256, 0, st>>>(end);
+        return hipGetLastError();
     });
 }
 
