@@ -765,25 +765,47 @@ GatedK args_of(const GatedArgs& a, const GatedShape& s) {
 }
 
 
-// Shapes for a product of p by q results whose sum may go in `parts` parts: the widest whose
-// tiles fill the card twice over (fp32: operands of the wide one pass a wave's registers).
+// A product's tile shape and the parts of its sum.
 enum { kWide, kSquare, kNarrow, kSmall };
-int shape_of(int64_t p, int64_t q, int64_t parts, Io io) {
-    if (io != Io::F32 && tiles_of(p, Wide::kA) * tiles_of(q, Wide::kB) * parts >= 512) return kWide;
-    if (tiles_of(p, Square::kA) * tiles_of(q, Square::kB) * parts >= 512) return kSquare;
-    return tiles_of(p, Narrow::kA) * tiles_of(q, Narrow::kB) * parts >= 512 ? kNarrow : kSmall;
-}
+struct Cut {
+    int shape, splits;
+};
 int64_t tiles_by(int shape, int64_t p, int64_t q) {
     return shape == kWide     ? tiles_of(p, Wide::kA) * tiles_of(q, Wide::kB)
            : shape == kSquare ? tiles_of(p, Square::kA) * tiles_of(q, Square::kB)
            : shape == kNarrow ? tiles_of(p, Narrow::kA) * tiles_of(q, Narrow::kB)
                               : tiles_of(p, Small::kA) * tiles_of(q, Small::kB);
 }
-// Parts that fill the card once with 512 workgroups, `most` at most (640 in place of 480 of them,
-// 6272 tokens of 256 channels by 640 units, bf16, backward: 55.8 us and 48.0).
-int parts_of(int64_t tiles, int64_t most) {
-    const int64_t want = 512 / tiles, n = want < most ? want : most;
-    return n < 1 ? 1 : n > 64 ? 64 : (int)n;
+// The cut of a product of p by q results of n terms, in `most` parts at most, that takes the
+// least time by an estimate: the fullest CU's tiles at the rate that the shape reaches (of 16
+// bits some 3.6 GFLOP a ms and CU with the wide one; 0.6 of a shape's where a CU has one
+// workgroup), and the parts, 4 bytes a result, written and read again.  Measured against it, bf16:
+// 6272 tokens of 512 channels by 2048 units, forward, wide 43.6 us, square 39.4, narrow 48.0 (four
+// tiles a CU of 32768 results, seven of 16384); by 1024 units, backward, the last product wide in
+// 16 parts 106 us, square in 8 98.6, narrow in 4 91.4.  fp32 operands of the wide shape pass a
+// wave's registers.
+Cut cut_of(int64_t p, int64_t q, int64_t n, int64_t most, Io io, bool pairs) {
+    constexpr double kResults[] = {128 * 256, 128 * 128, 64 * 128, 64 * 64};
+    constexpr double kRate16[] = {1.0, 0.9, 0.75, 0.5}, kRate32[] = {0.0, 0.2, 0.17, 0.12};
+    const int64_t steps = tiles_of(n, kBk);
+    most = most < 1 ? 1 : most > 64 ? 64 : most;
+    Cut best{io == Io::F32 ? kSquare : kWide, 1};
+    double least = 1e300;
+    for (int shape = best.shape; shape <= (pairs ? kNarrow : kSmall); ++shape) {
+        const int64_t tiles = tiles_by(shape, p, q);
+        for (int k = 0; k <= 4; ++k) {                   // so many a CU
+            const int64_t want = k * 256 / tiles, s = want < 1 ? 1 : want > most ? most : want;
+            const int64_t full = tiles_of(tiles * s, 256);
+            const double rate = 3.6e6 * (io == Io::F32 ? kRate32 : kRate16)[shape] * (full == 1 ? 0.6 : 1.0);
+            const double us = full * kResults[shape] * tiles_of(steps, (int)s) * (2 * kBk) / rate +
+                              (s > 1 ? 3.0 + s * (double)p * q * 8 / 5e6 : 0.0);
+            if (us < least) {
+                least = us;
+                best = {shape, (int)s};
+            }
+        }
+    }
+    return best;
 }
 
 // f(type, shape, straight to LDS); kPairs: a unit's gate and value are to be in one wave
@@ -813,21 +835,16 @@ GatedPlan gated_plan(const GatedShape& s, bool backward) {
     auto fits = [](int64_t items) { return items <= ((int64_t)1 << 24) - 8; };
     p.fits = s.M <= INT32_MAX && s.K <= INT32_MAX / 2 && (int64_t)s.K * s.C < (int64_t)1 << 37;
     if (!p.fits) return p;
-    p.first = shape_of(F, s.M, 1, s.io);
-    if (p.first == kSmall) p.first = kNarrow;
+    p.first = cut_of(F, s.M, s.C, 1, s.io, true).shape;
     p.fits = !backward && s.M <= kFewTokens ? fits(tiles_of(s.K, 4)) : fits(tiles_by(p.first, F, s.M));
     if (!p.fits || !backward) return p;
     // parts of 256 units or tokens at least
-    p.dx = shape_of(s.C, s.M, 1, s.io);
-    p.dx_splits = p.dx == kSmall ? parts_of(tiles_by(kSmall, s.C, s.M), F / 256) : 1;
-    const int64_t parts = s.M / 256 < 1 ? 1 : s.M / 256 < 64 ? s.M / 256 : 64;
-    p.dw = shape_of(s.C, F, parts, s.io);
-    // no wider than the channels are
-    if (p.dw < kNarrow && s.C <= Narrow::kA) p.dw = kNarrow;
-    p.dw_splits = parts_of(tiles_by(p.dw, s.C, F), parts);
-    // the last launch: dbias's columns, and sums of at most 256 tiles of 128 by 256 for each product
+    const Cut x = cut_of(s.C, s.M, F, F / 256, s.io, false), w = cut_of(s.C, F, s.M, s.M / 256, s.io, false);
+    p.dx = x.shape; p.dx_splits = x.splits;
+    p.dw = w.shape; p.dw_splits = w.splits;
+    // the last launch: dbias's columns, and sums of at most 512 tiles of 128 by 256 for each product
     p.fits = fits(tiles_by(p.dx, s.C, s.M) * p.dx_splits) && fits(tiles_by(p.dw, s.C, F) * p.dw_splits) &&
-             fits(tiles_of(F, 16) + 2 * 256 * (128 * 256 / 256));
+             fits(tiles_of(F, 16) + 2 * 512 * (128 * 256 / 256));
     if (!p.fits) return p;
     p.dz = round_up((size_t)s.M * F * io_size(s.io), 16);
     p.dbias = round_up((size_t)tiles_of(s.M, Narrow::kB) * F * 4, 16);
