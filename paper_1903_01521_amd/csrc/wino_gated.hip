@@ -328,10 +328,11 @@ struct Rows64 {
             const int r = r0 + lane / kLanes;
             char* q = t + r * kRow + c * (int)sizeof(O);
             if (r >= rows) continue;
-            if (vec) {
+            if (vec || c + kEach <= cols) {
                 if (c >= cols) continue;
-                if constexpr (kStore) *(uint4*)(p + r * ld + c) = *(const uint4*)q;
-                else *(uint4*)q = *(const uint4*)(p + r * ld + c);
+                // 16 bytes on any address
+                if constexpr (kStore) __builtin_memcpy(p + r * ld + c, __builtin_assume_aligned(q, 16), 16);
+                else __builtin_memcpy(__builtin_assume_aligned(q, 16), p + r * ld + c, 16);
             } else {
                 for (int i = 0; i < kEach; ++i) {
                     if (c + i >= cols) break;
