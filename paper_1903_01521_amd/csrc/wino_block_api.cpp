@@ -152,7 +152,7 @@ int wino_qk_norm_nhwc(const void* q, const void* k, const float* gq, const float
     if (st != WINO_OK) return st;
     c.t[0].y = yq;
     if (k) c.t[1].y = yk;
-    const QkPlan p = qk_plan(c.s, c.t, false, qk_aligned(c.s, c.t));
+    const QkPlan p = qk_plan(c.s, c.t, false);
     if (!p.fits) return WINO_ERR_UNSUPPORTED;
     const Io io = c.s.io;
     const size_t g = (size_t)D * sizeof(float);
@@ -174,8 +174,7 @@ size_t wino_qk_norm_backward_workspace_bytes(int N, int Lq, int Lk, int Hq, int 
     if (make_qk(&c, &x, both ? &x : nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, N, Lq, Lk, Hq, Hk, D, 0, 0,
                 (int)wq, both ? (int)wk : 0, 0.0f, flags) != WINO_OK)
         return (size_t)-1;
-    // what unaligned tensors need, which is the most: a team of more lanes, more workgroups
-    const QkPlan p = qk_plan(c.s, c.t, true, false);
+    const QkPlan p = qk_plan(c.s, c.t, true);
     return p.fits ? p.need : (size_t)-1;
 }
 
@@ -190,7 +189,7 @@ int wino_qk_norm_backward_nhwc(const void* dyq, const void* dyk, const void* q, 
     if (st != WINO_OK) return st;
     c.t[0].dy = dyq; c.t[0].dx = dq; c.t[0].dgamma = dgq;
     if (k) { c.t[1].dy = dyk; c.t[1].dx = dk; c.t[1].dgamma = dgk; }
-    const QkPlan p = qk_plan(c.s, c.t, true, qk_aligned(c.s, c.t));
+    const QkPlan p = qk_plan(c.s, c.t, true);
     if (!p.fits) return WINO_ERR_UNSUPPORTED;
     const size_t need = dgq || c.t[1].dgamma ? p.need : 0;
     const int sp = space(workspace, workspace_bytes, need);

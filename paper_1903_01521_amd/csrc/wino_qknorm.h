@@ -36,8 +36,7 @@ struct QkPlan {
     int64_t items[2];
     size_t need;
 };
-QkPlan qk_plan(const QkShape& s, const QkSide (&t)[2], bool backward, bool aligned);
-bool qk_aligned(const QkShape& s, const QkSide (&t)[2]);
+QkPlan qk_plan(const QkShape& s, const QkSide (&t)[2], bool backward);
 hipError_t launch_qk_norm(const QkShape& s, const QkSide (&t)[2], const QkPlan& p, hipStream_t st);
 hipError_t launch_qk_norm_backward(const QkShape& s, const QkSide (&t)[2], const QkPlan& p, void* ws, hipStream_t st);
 

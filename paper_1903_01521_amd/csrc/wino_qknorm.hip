@@ -46,9 +46,10 @@ __device__ __forceinline__ void get(const T* p, int d, int D, float* v) {
     if constexpr (VP == 1) {
         v[0] = d < D ? (float)p[d] : 0.0f;
     } else {
-        const Raw<T, VP> r = *(const Raw<T, VP>*)(p + d);
+        T r[VP];
+        __builtin_memcpy(r, p + d, sizeof(r));           // one load, on any address
 #pragma unroll
-        for (int i = 0; i < VP; ++i) v[i] = (float)r.v[i];
+        for (int i = 0; i < VP; ++i) v[i] = (float)r[i];
     }
 }
 template <typename T, int VP>
@@ -56,10 +57,10 @@ __device__ __forceinline__ void set(T* p, int d, int D, const float* v) {
     if constexpr (VP == 1) {
         if (d < D) p[d] = (T)v[0];
     } else {
-        Raw<T, VP> r;
+        T r[VP];
 #pragma unroll
-        for (int i = 0; i < VP; ++i) r.v[i] = (T)v[i];
-        *(Raw<T, VP>*)(p + d) = r;
+        for (int i = 0; i < VP; ++i) r[i] = (T)v[i];
+        __builtin_memcpy(p + d, r, sizeof(r));
     }
 }
 
@@ -294,6 +295,7 @@ void with_plan(const QkShape& s, const QkPlan& p, F f) {
         if constexpr (sizeof(T) == 2)
             if (p.vp == 8) return with_team<T, 8>(p.team, s.pairs, f);
         if (p.vp == 4) return with_team<T, 4>(p.team, s.pairs, f);
+        if (p.vp == 2) return with_team<T, 2>(p.team, s.pairs, f);
         with_team<T, 1>(p.team, s.pairs, f);
     };
     if (s.io == Io::F32) type(float());
@@ -303,23 +305,12 @@ void with_plan(const QkShape& s, const QkPlan& p, F f) {
 
 }  // namespace
 
-bool qk_aligned(const QkShape& s, const QkSide (&t)[2]) {
-    for (const QkSide& w : t)
-        if (!aligned16(w.x) || !aligned16(w.dy) || !aligned16(w.y) || !aligned16(w.dx) ||
-            (int64_t)w.ld * io_size(s.io) % 16)
-            return false;
-    return true;
-}
-
-// aligned: 16-byte addresses and token strides.  Loads of VP values then lie on their own
-// size where D, R and R/2 are multiples of VP, and pairs that do not turn together
-// (channels from R on) come in whole lanes.
-QkPlan qk_plan(const QkShape& s, const QkSide (&t)[2], bool backward, bool aligned) {
+// Loads of VP values where D, R and R/2 are multiples of VP, so that pairs that do not turn
+// together (channels from R on) come in whole lanes.
+QkPlan qk_plan(const QkShape& s, const QkSide (&t)[2], bool backward) {
     QkPlan p{};
-    auto whole = [&](int vp) {
-        return aligned && s.D % (2 * vp) == 0 && (s.pairs ? s.R % (2 * vp) == 0 : s.R / 2 % vp == 0);
-    };
-    p.vp = s.io != Io::F32 && whole(8) ? 8 : whole(4) ? 4 : 1;
+    auto whole = [&](int vp) { return s.D % (2 * vp) == 0 && (s.pairs ? s.R % (2 * vp) == 0 : s.R / 2 % vp == 0); };
+    p.vp = s.io != Io::F32 && whole(8) ? 8 : whole(4) ? 4 : whole(2) ? 2 : 1;
     p.team = team_of(((s.D + 1) / 2 + p.vp - 1) / p.vp);
     p.fits = true;
     for (int w = 0; w < 2; ++w) {
@@ -330,7 +321,12 @@ QkPlan qk_plan(const QkShape& s, const QkSide (&t)[2], bool backward, bool align
     }
     // a launch has fewer than 2^32 threads
     if ((int64_t)p.blocks[0] + p.blocks[1] >= (int64_t)1 << 24) p.fits = false;
-    p.need = backward ? round_up((size_t)(p.blocks[0] + p.blocks[1]) * s.D * 4, 16) : 0;
+    if (!backward) return p;
+    // whatever R is: teams of the most lanes have the most workgroups
+    const int per = 256 / team_of((s.D + 1) / 2);
+    size_t rows = 0;
+    for (int w = 0; w < 2; ++w) rows += (size_t)(p.items[w] / per + 1 < kBackBlocks / 2 ? p.items[w] / per + 1 : kBackBlocks / 2);
+    p.need = round_up(rows * s.D * 4, 16);
     return p;
 }
 

@@ -175,8 +175,8 @@ def test_launches_of_2_to_the_32_threads_are_refused():
     assert f(1, 1, 1, 1, 2**26, 0) == MAX and f(1, 1, 1, 1, 2**26 - 64, 0) == 0                  # a wave for each unit
     assert f(2**14, 1, 2**8, 2**8, 2**9, 0) == MAX and f(2**12, 1, 2**8, 2**8, 2**8, 0) == 0     # tiles
     assert b(2**14, 1, 2**8, 2**8, 2**9, 0) == MAX
-    # 4 tokens a workgroup where heads of 128 are not on 16 bytes
-    assert _norm(N=2**26, Lq=1, Lk=1, Hq=1, Hk=1, D=128, R=0, ldq=129, ldk=129) == UNS
+    # 4 tokens a workgroup where heads are of 127
+    assert _norm(N=2**26, Lq=1, Lk=1, Hq=1, Hk=1, D=127, R=0, ldq=127, ldk=127) == UNS
 
 
 def test_gated_workspace_bytes():
