@@ -445,7 +445,10 @@ int wino_conv2d_wgrad_nhwc(const void* x, const void* dy, float* dg, const float
  *   All others are dense.  Outputs must not overlap each other or any input (rows
  *   of equal ld that lie between each other do not overlap).  D <= 128 (UNSUPPORTED
  *   past it).  Tensors may have any address that suits their element type; 16-byte
- *   addresses, and D and ld of whole 16-byte words, run faster.  Workspaces on
+ *   addresses, and widths and ld of whole 16-byte words, run faster.  A call whose largest
+ *   launch would need 2^24 workgroups or more is UNSUPPORTED (one for each 32 to 128 rows
+ *   and for each 64 keys of an image's key head; 4 to 128 tokens' heads of the norm; tiles of
+ *   64 x 64 and more of the gated layer).  Workspaces on
  *   16-byte addresses, else WINO_ERR_INVALID_ARG; they may be NULL where their size is
  *   0; (size_t)-1 on invalid arguments. */
 
@@ -488,7 +491,8 @@ int wino_qk_norm_backward_nhwc(const void* dyq, const void* dyk, const void* q, 
  *   y    : [N][Lq][Hq][D], dense.
  *   lse  : [N][Hq][Lq], log of the sum of exp(S), for the backward pass, or NULL.
  * What a key that is left out holds is not read.  An image without keys gives y = 0,
- * lse = -infinity.  exp(S - a running maximum) is rounded to 16-bit tensors' type once. */
+ * lse = -infinity.  exp(S - a running maximum) is rounded to 16-bit tensors' type once (fp16:
+ * 2^7 times as large; what is below 2^-32 of a row's largest is lost). */
 size_t wino_cross_attention_workspace_bytes(int N, int Lq, int Lk, int Hq, int Hk, int D, unsigned flags);
 int wino_cross_attention_nhwc(const void* q, const void* k, const void* v, const int* klen, const unsigned char* mask,
                               void* y, float* lse, int N, int Lq, int Lk, int Hq, int Hk, int D, int ldq, int ldk,

@@ -499,9 +499,9 @@ def _mptr(t):
 def wino_qk_norm_nhwc(q, k, gq, gk, rot, qpos, kpos, yq, yk, N, Lq, Lk, Hq, Hk, D, R, T, ldq, ldk, eps, flags=0,
                       stream=None) -> int:
     t, f32 = _type(flags), _type(0)
-    return lib().wino_qk_norm_nhwc(_rows(q, t, Lq, D, ldq), _rows(k, t, Lk, D, ldk), _dense(gq, f32), _dense(gk, f32), _dense(rot, f32),
-                                   _iptr(qpos), _iptr(kpos), _dense(yq, t), _dense(yk, t), N, Lq, Lk, Hq, Hk, D,
-                                   R, T, ldq, ldk, eps, flags, _stream(stream))
+    return lib().wino_qk_norm_nhwc(_rows(q, t, Lq, D, ldq), _rows(k, t, Lk, D, ldk), _dense(gq, f32),
+                                   _dense(gk, f32), _dense(rot, f32), _iptr(qpos), _iptr(kpos), _dense(yq, t),
+                                   _dense(yk, t), N, Lq, Lk, Hq, Hk, D, R, T, ldq, ldk, eps, flags, _stream(stream))
 
 
 def wino_qk_norm_backward_workspace_bytes(N, Lq, Lk, Hq, Hk, D, flags=0) -> int:
@@ -513,8 +513,9 @@ def wino_qk_norm_backward_nhwc(dyq, dyk, q, k, gq, gk, rot, qpos, kpos, dq, dk, 
     t, f32 = _type(flags), _type(0)
     return lib().wino_qk_norm_backward_nhwc(
         _dense(dyq, t), _dense(dyk, t), _rows(q, t, Lq, D, ldq), _rows(k, t, Lk, D, ldk), _dense(gq, f32), _dense(gk, f32),
-        _dense(rot, f32), _iptr(qpos), _iptr(kpos), _rows(dq, t, Lq, D, ldq), _rows(dk, t, Lk, D, ldk), _dense(dgq, f32), _dense(dgk, f32), N,
-        Lq, Lk, Hq, Hk, D, R, T, ldq, ldk, eps, flags, _ptr(workspace), workspace_bytes, _stream(stream))
+        _dense(rot, f32), _iptr(qpos), _iptr(kpos), _rows(dq, t, Lq, D, ldq), _rows(dk, t, Lk, D, ldk),
+        _dense(dgq, f32), _dense(dgk, f32), N, Lq, Lk, Hq, Hk, D, R, T, ldq, ldk, eps, flags, _ptr(workspace),
+        workspace_bytes, _stream(stream))
 
 
 def wino_cross_attention_workspace_bytes(N, Lq, Lk, Hq, Hk, D, flags=0) -> int:
@@ -539,8 +540,9 @@ def wino_cross_attention_backward_nhwc(dy, q, k, v, y, lse, klen, mask, dq, dk, 
     t, f32 = _type(flags), _type(0)
     return lib().wino_cross_attention_backward_nhwc(
         _dense(dy, t), _rows(q, t, Lq, D, ldq), _rows(k, t, Lk, D, ldk), _rows(v, t, Lk, D, ldv), _dense(y, t),
-        _dense(lse, f32), _iptr(klen), _mptr(mask), _rows(dq, t, Lq, D, ldq), _rows(dk, t, Lk, D, ldk), _rows(dv, t, Lk, D, ldv), N,
-        Lq, Lk, Hq, Hk, D, ldq, ldk, ldv, scale, flags, _ptr(workspace), workspace_bytes, _stream(stream))
+        _dense(lse, f32), _iptr(klen), _mptr(mask), _rows(dq, t, Lq, D, ldq), _rows(dk, t, Lk, D, ldk),
+        _rows(dv, t, Lk, D, ldv), N, Lq, Lk, Hq, Hk, D, ldq, ldk, ldv, scale, flags, _ptr(workspace), workspace_bytes,
+        _stream(stream))
 
 
 def wino_gated_layer_workspace_bytes(N, C, H, W, K, flags=0) -> int:

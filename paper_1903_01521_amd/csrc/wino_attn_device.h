@@ -594,7 +594,8 @@ struct FwdCut {
 };
 
 template <typename T, int D16, bool kFew, int kHow>
-__global__ __launch_bounds__((FwdCut<T, D16, kFew>::kThreads), (waves_of<T, D16>(kFew && kHow != kStraight ? 6 : 8))) void k_attn(AttnK g) {
+__global__ __launch_bounds__((FwdCut<T, D16, kFew>::kThreads), (waves_of<T, D16>(kFew && kHow != kStraight ? 6 : 8)))
+void k_attn(AttnK g) {
     using Cut = FwdCut<T, D16, kFew>;
     constexpr bool kDirect = kHow == kStraight, kVec = kHow != kAnywhere;
     constexpr int NT = Cut::kThreads, KT = Cut::kKeys, KB = kFew ? 1 : KT / 32, DB = (D16 + 1) / 2;
@@ -1101,10 +1102,13 @@ struct RowTiles<T, D16, RT, NT, kStraight> {
 // the two waves of 32 keys join at the end (128 keys a workgroup, a wave to 32: half as many
 // workgroups, each twice as long, one wave a SIMD where lengths are ragged, 288 us in place
 // of 225 for 16 images of 3136 by 0 to 1024 tokens, 8 and 4 heads of 64, bf16).  Keys that are
-// left out are columns of their own, so what they hold goes nowhere.
+// left out are columns of their own, so what they hold goes nowhere.  Heads of 64 are held to the
+// registers of three workgroups a CU: of ragged images no more than 544 of 1024 have keys, and
+// with two a CU the last 32 ran alone (217 us and 190; 512 that all have keys 2% slower).
 constexpr int kOwnKeys = 64;
 template <typename T, int D16, int kHow>
-__global__ __launch_bounds__(256, (kHow == kStraight && D16 == 4 ? 3 : waves_of<T, D16>(kHow == kStraight ? 6 : 4))) void k_attn_dkv(AttnK g) {
+__global__ __launch_bounds__(256, (kHow == kStraight && D16 == 4 ? 3 : waves_of<T, D16>(kHow == kStraight ? 6 : 4)))
+void k_attn_dkv(AttnK g) {
     constexpr bool kDirect = kHow == kStraight, kVec = kHow != kAnywhere;
     constexpr int NT = 256, RT = 64, DB = (D16 + 1) / 2, CP = kCopies<T>;
     constexpr bool kHalf = std::is_same_v<T, _Float16>, kShare = sizeof(T) == 4;
