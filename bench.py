@@ -92,8 +92,8 @@ def log(*a):
     print(*a, file=sys.stderr, flush=True)
 
 
-# Sources of the training calls, which no workload here runs.
-TRAINING_SOURCES = ("wino_norm", "wino_wgrad", "wino_train")
+# Sources of the training calls, attention and the gated layer, which no workload here runs.
+TRAINING_SOURCES = ("wino_norm", "wino_wgrad", "wino_train", "wino_qknorm", "wino_attn", "wino_gated", "wino_block")
 
 
 def layer_sources() -> list[str]:
