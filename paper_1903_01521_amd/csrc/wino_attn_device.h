@@ -573,7 +573,10 @@ struct KeyTiles<T, D16, KT, NT, kStraight> {      // straight to LDS: 16-bit, 16
 };
 
 // ---------------------------------------------------------------- forward
-// One pass over the keys with a running maximum and sum.  The maximum moves, and what
+// One pass over the keys with a running maximum and sum, bound by vector instructions: of a
+// score register's 33 cycles the exponential takes 16, its argument, the sum, the maximum
+// and the rounding 13 (16 images of 3136 tokens to 0..2048 keys, 8 heads of 64, bf16: 146 us,
+// 0.72 PFLOP/s).  The maximum moves, and what
 // is summed is scaled, only where it grows by more than 2^8: exponentials stay below
 // 2^8, and most tiles skip the scaling.  fp16 exponentials are held 2^7 times as large, below
 // 2^15, and lose what is below 2^-32 of a row's largest (2^-25 without; of 65536 keys of 2^-17
@@ -1104,10 +1107,12 @@ struct RowTiles<T, D16, RT, NT, kStraight> {
 // of 225 for 16 images of 3136 by 0 to 1024 tokens, 8 and 4 heads of 64, bf16).  Keys that are
 // left out are columns of their own, so what they hold goes nowhere.  Heads of 64 are held to the
 // registers of three workgroups a CU: of ragged images no more than 544 of 1024 have keys, and
-// with two a CU the last 32 ran alone (217 us and 190; 512 that all have keys 2% slower).
+// with two a CU the last 32 ran alone (217 us and 190; 512 that all have keys 2% slower; fp16, whose
+// powers of two would spill, 18%: two).
 constexpr int kOwnKeys = 64;
 template <typename T, int D16, int kHow>
-__global__ __launch_bounds__(256, (kHow == kStraight && D16 == 4 ? 3 : waves_of<T, D16>(kHow == kStraight ? 6 : 4)))
+__global__ __launch_bounds__(256, (kHow == kStraight && D16 == 4 && !std::is_same_v<T, _Float16>
+                                       ? 3 : waves_of<T, D16>(kHow == kStraight ? 6 : 4)))
 void k_attn_dkv(AttnK g) {
     constexpr bool kDirect = kHow == kStraight, kVec = kHow != kAnywhere;
     constexpr int NT = 256, RT = 64, DB = (D16 + 1) / 2, CP = kCopies<T>;

@@ -2,13 +2,15 @@
 // zu = x w1^T + b1, and its backward pass
 //   dzg = dy zu act'(zg), dzu = dy act(zg), dx = dzg w0 + dzu w1, dw = dz^T x, db = sum dz.
 //
-// Matrix products on 32x32 matrix-core tiles, their operands staged through LDS.  A
-// workgroup of four waves has 128 x 128 results: the left operand's index runs down a
-// lane's registers and is the output's contiguous one, the right operand's runs over the
-// lanes.  Forward, a workgroup's 128 left rows are 64 units' gates and their values, so
+// Matrix products on 32x32 matrix-core tiles, their operands staged through LDS: the left
+// operand's index runs down a lane's registers and is the output's contiguous one, the right
+// operand's runs over the lanes.  Forward, half a workgroup's left rows are units' gates, half their values, so
 // that both of a unit meet in one lane and neither leaves it.  Backward is three products:
 // zg and zu once more, ending in dz (kept in the tensors' type, as any gradient between two
 // layers), then dx from dz and w, and dw from dz and x, the sum over tokens in parts.
+//
+// 6272 tokens of 512 channels by 2048 units, bf16, forward: 40 us, 0.65 PFLOP/s; 200704 of 256
+// by 1024, backward: 960 us, of which dz's way through memory, 2.4 GB, is 470 at a copy's rate.
 #include "wino_attn_device.h"
 #include "wino_checks.h"
 #include "wino_gated.h"
@@ -33,9 +35,9 @@ struct GatedK {
 };
 
 // How a workgroup's four waves share a tile: WA by WB of them, each AB by BB blocks of 32
-// by 32 results.  A block's step reads AB + BB operands from LDS for AB * BB products, so
-// wide tiles need the least of LDS, whose 128 bytes a cycle the 64x64 ones of a wave just
-// fill; narrow ones fill the card where results are few.
+// by 32 results.  A block's step reads AB + BB operands from LDS for AB * BB products, and a
+// tile's step kA + kB rows of 64 bytes from L2, so wide tiles need the least of both; narrow ones
+// fill the card where results are few (figures at cut_of).
 template <int AB_, int BB_, int WA_, int WB_>
 struct Shape {
     static constexpr int AB = AB_, BB = BB_, WA = WA_, WB = WB_;

@@ -5,7 +5,8 @@
 // of the table at the token's position.  Backward: dz = dy turned back, dgamma = sum dz n,
 // and with dn = dz gamma, dx = r (dn - n mean(dn n)).
 //
-// Both are bound by memory: each value is read once and written once.  A lane has `VP`
+// Both are bound by memory: each value is read once and written once (64 images of 3136 tokens,
+// 8 heads of 64, bf16: 96 us, 4.3 TB/s; backward, fp32, 382 MB: 77 us, 5.0).  A lane has `VP`
 // whole pairs of a vector, two loads of VP values (its parts of the two halves, or
 // neighbours), so that a rotation stays inside it, and keeps the cosines, sines and
 // gammas of its pairs for the heads of a token that it does in turn.  A vector's sum of
