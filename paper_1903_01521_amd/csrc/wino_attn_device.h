@@ -399,7 +399,7 @@ struct AttnK {
     int splits;
     bool by_xcd;
     FastDiv per_pair, per_tile;              // by tiles * splits, by splits
-    // backward, of each pair's rows in turn: delta, the exponent's offset -lse log2 e, and (fp32)
+    // backward, of each pair's rows in turn: delta, the exponent's offset -lse log2 e (fp16: + 12), and (fp32)
     // 1 over the sum of P
     float *delta, *offset, *share;
     float *part, *part2, *stat;
@@ -805,11 +805,12 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnK g) {
 // fp32: lse's own rounding, and that of its product with log2 e, move all of a row's P by some
 // 2^-21; the first launch sums P and both divide by it.
 //
-// fp16 operands: P is held 2^12 times as large (a row's share of 2^-24 keeps its bits),
-// dS times a power of two for each column of the result, which falls, with what is
-// summed, where a larger dS than fp16 holds comes by.
+// fp16 operands: P is held 2^12 times as large (a row's share of 2^-24 keeps its bits; so is
+// dS, and the offset that the first launch leaves says it), and dS times a power of two for
+// each column of the result, which falls, with what is summed, where a larger dS than fp16
+// holds comes by.
 
-constexpr float kPUp = 4096.0f;
+constexpr float kPUp = 4096.0f, kPUpLog = 12.0f;
 
 // Lets up fall where a lane's column of dS times up would pass fp16's range, and what is
 // summed with it.
@@ -873,7 +874,8 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(4))) void k_attn_dq(AttnK g)
     }
     delta = add_halves(delta);
     const float lse = live ? g.b.lse[stat] : -INFINITY;
-    const float off = lse == -INFINITY ? -INFINITY : -lse * kLog2e;
+    // of fp16's P, 2^12 times as large
+    const float off = lse == -INFINITY ? -INFINITY : (kHalf ? kPUpLog : 0.0f) - lse * kLog2e;
 
     int64_t lo, hi;
     const int len = keys_of(g.b.klen, n, s.Lk);
@@ -922,7 +924,7 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(4))) void k_attn_dq(AttnK g)
                 ds[kb][i] = x * (dp[i] - delta);
                 if constexpr (kFix) {
                     lack += ds[kb][i];
-                    ps[kb][i] = kHalf ? x * kPUp : x;
+                    ps[kb][i] = x;
                 } else {
                     lack += x;
                 }
@@ -953,11 +955,12 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(4))) void k_attn_dq(AttnK g)
                 }
             }
     }
-    lack = add_halves(lack);
-    round = add_halves(round) / up;
+    constexpr float kDown = kHalf ? 1.0f / kPUp : 1.0f;
+    lack = add_halves(lack) * kDown;
+    round = add_halves(round) * kDown / up;
     if (!live) return;
     const float share = kFix || g.splits > 1 ? 1.0f : share_of(lack);
-    const float f = s.scale * share / up, fm = s.scale * (kHalf ? 1.0f / kPUp : 1.0f);
+    const float f = s.scale * share * kDown / up, fm = s.scale * kDown;
     if (g.splits > 1) {
         // parts: what dq and the sums P k are so far, and what delta lacks
         const int64_t id = ((int64_t)split * s.N * s.Hk + pair) * s.rows + row;
@@ -1199,7 +1202,7 @@ void k_attn_dkv(AttnK g) {
                 float x = __builtin_amdgcn_exp2f(__builtin_fmaf(p[4 * b + i], c2, o4[i]));
                 if constexpr (kShare) x *= s4[i];
                 ds[0][4 * b + i] = x * (ds[0][4 * b + i] - d4[i]);
-                p[4 * b + i] = kHalf ? x * kPUp : x;
+                p[4 * b + i] = x;
             }
         }
         if constexpr (kHalf) {
@@ -1217,7 +1220,7 @@ void k_attn_dkv(AttnK g) {
             }
         }
     }
-    const float f = s.scale / up, fvv = kHalf ? 1.0f / kPUp : 1.0f;
+    const float fvv = kHalf ? 1.0f / kPUp : 1.0f, f = s.scale * fvv / up;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
