@@ -499,9 +499,12 @@ struct KeyTiles {                            // by way of registers: any address
         __syncthreads();
         if (k0 + KT < hi) load(k0 + KT);
     }
-    // what is added to the scores of the tile's keys at + 4 h .. + 3
-    __device__ __forceinline__ f32x4v left_out(const float* bias, int at, int h) const {
-        return *(const f32x4v*)&bias[at + 4 * h];
+    // x[e] .. x[e + 3] belong to the tile's keys at + 4 h .. + 3: `to` for those that are left out (a
+    // sum with -infinity would leave NaN where the row holds what is not finite)
+    __device__ __forceinline__ void leave_out(const float* bias, int at, int h, f32x16& x, int e, float to) const {
+        const f32x4v m = *(const f32x4v*)&bias[at + 4 * h];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[e + i] = m[i] == 0.0f ? x[e + i] : to;
     }
 };
 template <typename T, int D16, int KT, int NT>
@@ -563,12 +566,10 @@ struct KeyTiles<T, D16, KT, NT, kStraight> {      // straight to LDS: 16-bit, 16
         bits = coming;
         if (k0 + KT < hi) issue(nk, nv, k0 + KT);
     }
-    __device__ __forceinline__ f32x4v left_out(const float*, int at, int h) const {
+    __device__ __forceinline__ void leave_out(const float*, int at, int h, f32x16& x, int e, float to) const {
         const uint32_t b = (uint32_t)((h ? bits >> 4 : bits) >> at);
-        f32x4v m;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) m[i] = b >> i & 1 ? 0.0f : -INFINITY;
-        return m;
+        for (int i = 0; i < 4; ++i) x[e + i] = b >> i & 1 ? x[e + i] : to;
     }
 };
 
@@ -656,11 +657,7 @@ void k_attn(AttnK g) {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    const f32x4v m = in.left_out(bias, kb * 32 + 8 * b, h);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) p[kb][4 * b + i] += m[i];
-                }
+                for (int b = 0; b < 4; ++b) in.leave_out(bias, kb * 32 + 8 * b, h, p[kb], 4 * b, -INFINITY);
         }
         float mx = p[0][0];
 #pragma unroll
@@ -912,22 +909,23 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(4))) void k_attn_dq(AttnK g)
             }
             if (!whole) {
 #pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    const f32x4v m = in.left_out(bias, kb * 32 + 8 * b, h);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) p[4 * b + i] += m[i];
-                }
+                for (int b = 0; b < 4; ++b) in.leave_out(bias, kb * 32 + 8 * b, h, p, 4 * b, -INFINITY);
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c2, off));
                 ds[kb][i] = x * (dp[i] - delta);
-                if constexpr (kFix) {
-                    lack += ds[kb][i];
-                    ps[kb][i] = x;
-                } else {
-                    lack += x;
-                }
+                if constexpr (kFix) ps[kb][i] = x;
+                else lack += x;
+            }
+            if (!whole) {
+                // dy that is not finite by a key's zeros
+#pragma unroll
+                for (int b = 0; b < 4; ++b) in.leave_out(bias, kb * 32 + 8 * b, h, ds[kb], 4 * b, 0.0f);
+            }
+            if constexpr (kFix) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) lack += ds[kb][i];
             }
         }
         if constexpr (kHalf) {
