@@ -70,12 +70,13 @@ __device__ __forceinline__ void set(T* p, int d, int D, const float* v) {
 template <int VP, bool PAIRS>
 struct Mine {
     int d0, d1;
-    bool on;
+    bool on, turned;                         // its pairs turn: all of them, or none
     float g[2 * VP], c[VP], s[VP];
     __device__ __forceinline__ void place(const QkShape& k, int lane, int lanes, const float* gamma) {
         on = lane < lanes;
         const int p = lane * VP;
-        if (!PAIRS && p < k.R / 2) {
+        turned = p < k.R / 2;
+        if (!PAIRS && turned) {
             d0 = p;
             d1 = k.R / 2 + p;
         } else {
@@ -93,7 +94,7 @@ struct Mine {
     // Cosines and sines at position `at`; a position outside the table turns to NaN.
     __device__ __forceinline__ void turn(const QkShape& k, int lane, int64_t at) {
         const int p = lane * VP;
-        if (!on || p >= k.R / 2) return;
+        if (!on || !turned) return;
         const bool in = at >= 0 && at < k.T;
         const float* row = k.rot + (in ? at : 0) * k.R + 2 * p;
 #pragma unroll
@@ -101,6 +102,12 @@ struct Mine {
             c[i] = in ? row[2 * i] : NAN;
             s[i] = in ? row[2 * i + 1] : NAN;
         }
+    }
+    // (za, zb) turned by pair i's angle, or back (s negative); channels from R on stay apart, as 0 times
+    // what is not finite is NaN
+    __device__ __forceinline__ void turn_pair(float za, float zb, float c, float s, float& a, float& b) const {
+        a = turned ? za * c - zb * s : za;
+        b = turned ? zb * c + za * s : zb;
     }
     __device__ __forceinline__ static int first(int i) { return PAIRS ? 2 * i : i; }
     __device__ __forceinline__ static int second(int i) { return PAIRS ? 2 * i + 1 : VP + i; }
@@ -160,8 +167,7 @@ __global__ __launch_bounds__(256) void k_qk_norm(QkK g) {
         for (int j = 0; j < VP; ++j) {
             const int a = m.first(j), b = m.second(j);
             const float za = v[i][a] * r * m.g[a], zb = v[i][b] * r * m.g[b];
-            v[i][a] = za * m.c[j] - zb * m.s[j];
-            v[i][b] = zb * m.c[j] + za * m.s[j];
+            m.turn_pair(za, zb, m.c[j], m.s[j], v[i][a], v[i][b]);
         }
         m.store((T*)t.y + (me.tok * t.heads + me.h0 + i) * D, D, v[i]);
     }
@@ -192,9 +198,7 @@ __global__ __launch_bounds__(256) void k_qk_norm_back(QkK g) {
 #pragma unroll
             for (int j = 0; j < VP; ++j) {
                 const int a = m.first(j), b = m.second(j);
-                const float da = dz[a], db = dz[b];
-                dz[a] = da * m.c[j] + db * m.s[j];
-                dz[b] = db * m.c[j] - da * m.s[j];
+                m.turn_pair(dz[a], dz[b], m.c[j], -m.s[j], dz[a], dz[b]);
             }
 #pragma unroll
             for (int j = 0; j < 2 * VP; ++j) {
