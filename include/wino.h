@@ -533,6 +533,13 @@ int wino_gated_layer_backward_nhwc(const void* dy, const void* x, const void* w,
                                    float* dbias, int N, int C, int H, int W, int K, unsigned flags, void* workspace,
                                    size_t workspace_bytes, void* stream);
 
+/* The planner's choice for a gated layer, or its backward pass, for callers that report
+ * it: results[i] = the results of a workgroup's tile (128 x 256, 128 x 128, 64 x 128 or
+ * 64 x 64; 0: a wave for each unit), parts[i] = the parts of its sum, of the products
+ * i = 0: zg and zu, and backward 1: dx, 2: dw (forward both 0).  Errors as for the
+ * call's sizes and flags; null outputs are INVALID_ARG. */
+int wino_gated_layer_plan(int N, int C, int H, int W, int K, unsigned flags, int backward, int results[3], int parts[3]);
+
 /* ---- allocation-free variant ------------------------------------------------
  * For callers that cannot allocate device memory (code under HIP graph
  * capture, tight serving loops, harnesses that forbid hipMalloc): the layer of

@@ -106,6 +106,7 @@ _SIGS = {
     "wino_cross_attention_backward_workspace_bytes": ([_c_int] * 6 + [_c_uint], _c_size),
     "wino_cross_attention_backward_nhwc": ([_vp] * 11 + [_c_int] * 9 + [ctypes.c_float, _c_uint, _vp, _c_size, _vp],
                                            _c_int),
+    "wino_gated_layer_plan": ([_c_int] * 5 + [_c_uint, _c_int, _vp, _vp], _c_int),
     "wino_gated_layer_workspace_bytes": ([_c_int] * 5 + [_c_uint], _c_size),
     "wino_gated_layer_nhwc": ([_vp] * 4 + [_c_int] * 5 + [_c_uint, _vp, _c_size, _vp], _c_int),
     "wino_gated_layer_backward_workspace_bytes": ([_c_int] * 5 + [_c_uint], _c_size),
@@ -543,6 +544,14 @@ def wino_cross_attention_backward_nhwc(dy, q, k, v, y, lse, klen, mask, dq, dk, 
         _dense(lse, f32), _iptr(klen), _mptr(mask), _rows(dq, t, Lq, D, ldq), _rows(dk, t, Lk, D, ldk),
         _rows(dv, t, Lk, D, ldv), N, Lq, Lk, Hq, Hk, D, ldq, ldk, ldv, scale, flags, _ptr(workspace), workspace_bytes,
         _stream(stream))
+
+
+def wino_gated_layer_plan(N, C, H, W, K, flags=0, backward=False):
+    """(status, results, parts): the results of a workgroup's tile and the parts of its sum, of each
+    product."""
+    results, parts = (ctypes.c_int * 3)(), (ctypes.c_int * 3)()
+    st = lib().wino_gated_layer_plan(N, C, H, W, K, flags, int(backward), results, parts)
+    return st, tuple(results), tuple(parts)
 
 
 def wino_gated_layer_workspace_bytes(N, C, H, W, K, flags=0) -> int:

@@ -259,6 +259,22 @@ int wino_cross_attention_backward_nhwc(const void* dy, const void* q, const void
     return hip_status(launch_attn_backward(b, s, p, workspace, (hipStream_t)stream));
 }
 
+int wino_gated_layer_plan(int N, int C, int H, int W, int K, unsigned flags, int backward, int results[3], int parts[3]) {
+    if (!results || !parts) return WINO_ERR_INVALID_ARG;
+    GatedShape s;
+    const int st = make_gated(&s, N, C, H, W, K, flags);
+    if (st != WINO_OK) return st;
+    const GatedPlan p = gated_plan(s, backward != 0);
+    if (!p.fits) return WINO_ERR_UNSUPPORTED;
+    results[0] = !backward && gated_few(s) ? 0 : gated_results(p.first);
+    results[1] = backward ? gated_results(p.dx) : 0;
+    results[2] = backward ? gated_results(p.dw) : 0;
+    parts[0] = 1;
+    parts[1] = backward ? p.dx_splits : 0;
+    parts[2] = backward ? p.dw_splits : 0;
+    return WINO_OK;
+}
+
 size_t wino_gated_layer_workspace_bytes(int N, int C, int H, int W, int K, unsigned flags) {
     return gated_need(N, C, H, W, K, flags, false);
 }

@@ -29,6 +29,8 @@ struct GatedPlan {
     size_t dz, dbias, px, pw, need;          // workspace: bytes of each region
 };
 GatedPlan gated_plan(const GatedShape& s, bool backward);
+int gated_results(int shape);                // of a workgroup's tile
+bool gated_few(const GatedShape& s);         // forward: a wave for each unit
 hipError_t launch_gated(const GatedArgs& a, const GatedShape& s, const GatedPlan& p, hipStream_t st);
 hipError_t launch_gated_backward(const GatedArgs& a, const GatedShape& s, const GatedPlan& p, void* ws, hipStream_t st);
 

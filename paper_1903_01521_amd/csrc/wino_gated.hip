@@ -831,6 +831,14 @@ hipError_t with_all(const GatedK& g, Io io, int shape, F f) {
 
 }  // namespace
 
+int gated_results(int shape) {
+    return shape == kWide     ? Wide::kA * Wide::kB
+           : shape == kSquare ? Square::kA * Square::kB
+           : shape == kNarrow ? Narrow::kA * Narrow::kB
+                              : Small::kA * Small::kB;
+}
+bool gated_few(const GatedShape& s) { return s.M <= kFewTokens; }
+
 GatedPlan gated_plan(const GatedShape& s, bool backward) {
     GatedPlan p{};
     const int64_t F = 2 * (int64_t)s.K;
@@ -839,7 +847,7 @@ GatedPlan gated_plan(const GatedShape& s, bool backward) {
     p.fits = s.M <= INT32_MAX && s.K <= INT32_MAX / 2 && (int64_t)s.K * s.C < (int64_t)1 << 37;
     if (!p.fits) return p;
     p.first = cut_of(F, s.M, s.C, 1, s.io, true).shape;
-    p.fits = !backward && s.M <= kFewTokens ? fits(tiles_of(s.K, 4)) : fits(tiles_by(p.first, F, s.M));
+    p.fits = !backward && gated_few(s) ? fits(tiles_of(s.K, 4)) : fits(tiles_by(p.first, F, s.M));
     if (!p.fits || !backward) return p;
     // parts of 256 units or tokens at least
     const Cut x = cut_of(s.C, s.M, F, F / 256, s.io, false), w = cut_of(s.C, F, s.M, s.M / 256, s.io, false);
@@ -859,7 +867,7 @@ GatedPlan gated_plan(const GatedShape& s, bool backward) {
 
 hipError_t launch_gated(const GatedArgs& a, const GatedShape& s, const GatedPlan& p, hipStream_t st) {
     GatedK g = args_of(a, s);
-    if (s.M <= kFewTokens)
+    if (gated_few(s))
         return with_io(s.io, [&](auto t) {
             typedef decltype(t) T;
             const unsigned blocks = (unsigned)tiles_of(s.K, 4);
