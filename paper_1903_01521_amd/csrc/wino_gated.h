@@ -26,7 +26,7 @@ struct GatedPlan {
     bool fits;
     int first, dx, dw;                       // tile shapes of the products
     int dx_splits, dw_splits;                // parts of the sums over units and over tokens
-    size_t dz, dbias, px, pw, need;          // workspace: bytes of each region
+    size_t dz, dbias, px, pw, tops, need;    // workspace: bytes of each region
 };
 GatedPlan gated_plan(const GatedShape& s, bool backward);
 int gated_results(int shape);                // of a workgroup's tile

@@ -30,6 +30,7 @@ struct GatedK {
     bool vec;
     void* dz;                                // [M][2 K]
     float *dbias, *part;                     // [token tiles][2 K]; [splits][2 K][C]
+    float *tops, *ups;                       // fp16: each tile's largest |dz|; dz's power of two, and 1 over it
     int items, tiles;                        // below 2^24; tiles: of the faster axis
     int splits;
 };
@@ -430,17 +431,46 @@ struct DyTiles {
     }
 };
 
+// fp16's dz is held times a power of two: of 2^6, and where the call's largest would then be past
+// fp16's range, or below 2^-2 (from where 2^-12 of it has all its bits), formed again times one that
+// brings the largest to 2^13 or more.  Infinities and NaN are no part of it.
+constexpr float kFirstUp = 64.0f;
+constexpr int kFirstUpLog = 6;
+// top: the largest times the first power of two
+__device__ __forceinline__ float up_of(float top) {
+    if (top == 0.0f || (top >= 0.25f && top <= 65504.0f)) return kFirstUp;
+    const int e = (int)(__float_as_uint(top) >> 23) - 127;          // of a subnormal -127
+    return __uint_as_float((uint32_t)(min(kFirstUpLog + 13 - e, 126) + 127) << 23);
+}
+
+// The sum, or the largest, of a wave's 64 values (the largest: of numbers from 0 on).
+template <bool kMax = false>
+__device__ __forceinline__ float join64(float x) {
+    auto two = [](float a, float b) { return kMax ? fmaxf(a, b) : a + b; };
+#define WINO_ROTATED(ctrl) __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), ctrl, 15, 15, true))
+    x = two(x, WINO_ROTATED(0x128));         // row_ror:8, 4, 2, 1
+    x = two(x, WINO_ROTATED(0x124));
+    x = two(x, WINO_ROTATED(0x122));
+    x = two(x, WINO_ROTATED(0x121));
+#undef WINO_ROTATED
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = two(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    float a, b;
+    halves(x, a, b);
+    return two(a, b);
+}
+
 // y of a tile's tokens and units (its left rows are their gates, then their values, so that
-// both of a unit meet in one lane), or dz of them and the tile's sums of it.
-template <typename T, typename S, bool BACK, bool kDirect>
-__global__ __launch_bounds__(256, 2) void k_gated(GatedK g) {
+// both of a unit meet in one lane), or dz of them, the tile's sums of it and (fp16) its largest;
+// kAgain: dz alone, times `up`.
+template <typename T, typename S, bool BACK, bool kDirect, bool kAgain>
+__device__ __forceinline__ void gated_tile(const GatedK& g, int item, float up) {
+    constexpr bool kHalf = BACK && std::is_same_v<T, _Float16>;
     constexpr int kUnits = S::kA / 2, UB = S::AB / 2;
     using A = Side<T, S::kA, false, kDirect>;
     using B = Side<T, S::kB, false, kDirect>;
     using Rows = Rows64<T>;
     __shared__ alignas(16) char lds[lds_of<S, A, B>(kDirect, Rows::kBytes)];
-    const int item = item_of(g.items);
-    if (item < 0) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     const int mt = (uint32_t)item / (uint32_t)g.tiles, u0 = (item - mt * g.tiles) * kUnits, K = g.K;
     const int64_t m0 = (int64_t)mt * S::kB;
@@ -480,7 +510,7 @@ __global__ __launch_bounds__(256, 2) void k_gated(GatedK g) {
     // unit of (block i, b, i): blocks of a wave's units are 32 (i WA + wa)
     const int cols = 32 * UB, ub = u0 + 32 * wa;
     const int have = K - ub < cols ? K - ub : cols;     // may be negative
-    float db[2][UB][16];
+    float db[2][UB][16], top = 0.0f;
     if constexpr (BACK) {
 #pragma unroll
         for (int w = 0; w < 2; ++w)
@@ -517,6 +547,10 @@ __global__ __launch_bounds__(256, 2) void k_gated(GatedK g) {
                     // past the tokens LDS holds what was there
                     if (left < 32 && (lane & 31) >= left) dy[0] = dy[1] = dy[2] = dy[3] = 0.0f;
                 }
+                if constexpr (kHalf && !kAgain) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) dy[e] *= kFirstUp;
+                }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float zg = acc[i][j][4 * b + e] + bg[e], zu = acc[UB + i][j][4 * b + e] + bu[e];
@@ -532,13 +566,36 @@ __global__ __launch_bounds__(256, 2) void k_gated(GatedK g) {
                     }
                 }
             }
+        if constexpr (kHalf && !kAgain) {
+            float mx = 0.0f;
+#pragma unroll
+            for (int i = 0; i < UB; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) mx = fmaxf(mx, fmaxf(fabsf(og[i][e]), fabsf(ou[i][e])));
+            // what is past the units is any value
+            if (have < cols || __any(!(mx < INFINITY))) {
+                mx = 0.0f;
+#pragma unroll
+                for (int i = 0; i < UB; ++i)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float a = fabsf(og[i][e]), b = fabsf(ou[i][e]);
+                        const bool in = 32 * i + 8 * (e >> 2) + 4 * h + (e & 3) < have;
+                        if (in && a < INFINITY) mx = fmaxf(mx, a);
+                        if (in && b < INFINITY) mx = fmaxf(mx, b);
+                    }
+            }
+            top = fmaxf(top, mx);
+        }
         auto out = [&](const float (&o)[UB][16], T* p, int64_t ld) {
             wave_sync();
+            const float f = kAgain ? up : 1.0f;
 #pragma unroll
             for (int i = 0; i < UB; ++i)
 #pragma unroll
                 for (int b = 0; b < 4; ++b)
-                    rows.put4(32 * i + 8 * b + 4 * h, o[i][4 * b], o[i][4 * b + 1], o[i][4 * b + 2], o[i][4 * b + 3]);
+                    rows.put4(32 * i + 8 * b + 4 * h, o[i][4 * b] * f, o[i][4 * b + 1] * f, o[i][4 * b + 2] * f,
+                              o[i][4 * b + 3] * f);
             wave_sync();
             rows.template move<true>(p, ld, left, have, g.vec);
         };
@@ -552,10 +609,10 @@ __global__ __launch_bounds__(256, 2) void k_gated(GatedK g) {
             wave_sync();
         }
     }
-    if constexpr (BACK) {
-        if (!g.a.dbias) return;
+    if constexpr (BACK && !kAgain) {
+        if (!kHalf && !g.a.dbias) return;
         // over the lanes, then over the waves that have these units
-        __shared__ float sums[S::WB][2][kUnits];
+        __shared__ float sums[S::WB][2][kUnits], largest[4];
 #pragma unroll
         for (int w = 0; w < 2; ++w)
 #pragma unroll
@@ -565,14 +622,46 @@ __global__ __launch_bounds__(256, 2) void k_gated(GatedK g) {
                 const int val = (lane >> 4 & 1) * 8 + (lane >> 3 & 1) * 4 + (lane >> 2 & 1) * 2 + (lane >> 1 & 1);
                 if (!(lane & 1)) sums[wb][w][32 * (i * S::WA + wa) + 8 * (val >> 2) + 4 * h + (val & 3)] = v;
             }
+        if constexpr (kHalf) {
+            top = join64<true>(top);
+            if (lane == 0) largest[wave] = top;
+        }
         __syncthreads();
-        if (threadIdx.x < 2 * kUnits) {
+        if (kHalf && threadIdx.x == 0) g.tops[item] = fmaxf(fmaxf(largest[0], largest[1]), fmaxf(largest[2], largest[3]));
+        if (g.a.dbias && threadIdx.x < 2 * kUnits) {
             const int w = threadIdx.x / kUnits, u = threadIdx.x % kUnits;
             float v = 0.0f;
 #pragma unroll
             for (int i = 0; i < S::WB; ++i) v += sums[i][w][u];
-            if (u0 + u < K) g.dbias[(int64_t)mt * 2 * K + (int64_t)w * K + u0 + u] = v;
+            if (u0 + u < K) g.dbias[(int64_t)mt * 2 * K + (int64_t)w * K + u0 + u] = kHalf ? v * (1.0f / kFirstUp) : v;
         }
+    }
+}
+
+template <typename T, typename S, bool BACK, bool kDirect>
+__global__ __launch_bounds__(256, 2) void k_gated(GatedK g) {
+    const int item = item_of(g.items);
+    if (item >= 0) gated_tile<T, S, BACK, kDirect, false>(g, item, kFirstUp);
+}
+
+// dz's power of two from its tiles' largest; dz again where it is not the first one.
+template <typename S, bool kDirect>
+__global__ __launch_bounds__(256, 2) void k_gated_again(GatedK g) {
+    __shared__ float largest[4];
+    float top = 0.0f;
+    for (int i = threadIdx.x; i < g.items; i += 256) top = fmaxf(top, g.tops[i]);
+    top = join64<true>(top);
+    if ((threadIdx.x & 63) == 0) largest[threadIdx.x >> 6] = top;
+    __syncthreads();
+    const float up = up_of(fmaxf(fmaxf(largest[0], largest[1]), fmaxf(largest[2], largest[3])));
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        g.ups[0] = up;
+        g.ups[1] = 1.0f / up;
+    }
+    if (up == kFirstUp) return;                          // of every workgroup
+    for (int item = blockIdx.x; item < g.items; item += gridDim.x) {
+        gated_tile<_Float16, S, true, kDirect, true>(g, item, up);
+        __syncthreads();                                 // the tile's LDS is free
     }
 }
 
@@ -580,17 +669,6 @@ __global__ __launch_bounds__(256, 2) void k_gated(GatedK g) {
 // there is to do is to read the weights once (in tiles of 32 units 2048 of them are 64
 // workgroups: one token of 512 channels 9.1 us).
 constexpr int kFewTokens = 8;
-
-__device__ __forceinline__ float sum64(float x) {
-#define WINO_ROTATED(ctrl) __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), ctrl, 15, 15, true))
-    x += WINO_ROTATED(0x128);                // row_ror:8, 4, 2, 1
-    x += WINO_ROTATED(0x124);
-    x += WINO_ROTATED(0x122);
-    x += WINO_ROTATED(0x121);
-#undef WINO_ROTATED
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return add_halves(__uint_as_float(r[0]) + __uint_as_float(r[1]));
-}
 
 template <typename T, int MT>
 __global__ __launch_bounds__(256) void k_gated_few(GatedK g) {
@@ -617,7 +695,7 @@ __global__ __launch_bounds__(256) void k_gated_few(GatedK g) {
     float zg = 0.0f, zu = 0.0f;              // of token `lane`
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-        const float a = sum64(z[0][m]), b = sum64(z[1][m]);
+        const float a = join64(z[0][m]), b = join64(z[1][m]);
         if (lane == m) {
             zg = a;
             zu = b;
@@ -629,6 +707,20 @@ __global__ __launch_bounds__(256) void k_gated_few(GatedK g) {
         zu += g.a.bias[g.K + u];
     }
     ((T*)g.a.y)[(int64_t)lane * g.K + u] = (T)(gate(zg, g.act) * zu);
+}
+
+// dz's power of two taken out of a product.
+template <typename T, typename S>
+__device__ __forceinline__ void take_down(f32x16 (&acc)[S::AB][S::BB], const float* ups) {
+    if constexpr (std::is_same_v<T, _Float16>) {
+        const float down = ups[1];
+#pragma unroll
+        for (int i = 0; i < S::AB; ++i)
+#pragma unroll
+            for (int j = 0; j < S::BB; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[i][j][e] *= down;
+    }
 }
 
 // A tile's results to out[q][p], P of p: 64 columns of a wave at a time.
@@ -680,6 +772,7 @@ __global__ __launch_bounds__(256, 2) void k_gated_dx(GatedK g) {
     a.init({(const T*)g.a.w + c0, F, g.C - c0, g.C, kBk, 0}, g.vec);
     b.init({(const T*)g.dz + m0 * F, g.M - m0 < S::kB ? g.M - m0 : S::kB, F, F, S::kB, 0}, g.vec);
     product<S>(acc, a, b, lds, lo, hi, kDirect);
+    take_down<T, S>(acc, g.ups);
     if (g.splits > 1) put_tile<S>(acc, lds, g.part + (int64_t)split * g.M * g.C, c0, g.C, m0, g.M, (g.C & 3) == 0);
     else put_tile<S>(acc, lds, (T*)g.a.dx, c0, g.C, m0, g.M, g.vec);
 }
@@ -703,6 +796,7 @@ __global__ __launch_bounds__(256, 2) void k_gated_dw(GatedK g) {
     a.init({(const T*)g.a.x + c0, g.M, g.C - c0, g.C, kBk, 0}, g.vec);
     b.init({(const T*)g.dz + f0, g.M, F - f0, F, kBk, 0}, g.vec);
     product<S>(acc, a, b, lds, lo, hi, kDirect);
+    take_down<T, S>(acc, g.ups);
     if (g.splits > 1) put_tile<S>(acc, lds, g.part + (int64_t)split * F * g.C, c0, g.C, f0, F, (g.C & 3) == 0);
     else put_tile<S>(acc, lds, (T*)g.a.dw, c0, g.C, f0, F, g.vec);
 }
@@ -861,7 +955,8 @@ GatedPlan gated_plan(const GatedShape& s, bool backward) {
     p.dbias = round_up((size_t)tiles_of(s.M, Narrow::kB) * F * 4, 16);
     p.px = p.dx_splits > 1 ? round_up((size_t)p.dx_splits * s.M * s.C * 4, 16) : 0;
     p.pw = p.dw_splits > 1 ? round_up((size_t)p.dw_splits * F * s.C * 4, 16) : 0;
-    p.need = p.dz + p.dbias + p.px + p.pw;
+    p.tops = s.io == Io::F16 ? round_up((size_t)tiles_by(p.first, F, s.M) * 4, 16) + 16 : 0;
+    p.need = p.dz + p.dbias + p.px + p.pw + p.tops;
     return p;
 }
 
@@ -892,6 +987,8 @@ hipError_t launch_gated_backward(const GatedArgs& a, const GatedShape& s, const 
     g.dz = ws;
     g.dbias = (float*)((char*)ws + p.dz);
     char* parts = (char*)ws + p.dz + p.dbias;
+    g.ups = (float*)(parts + p.px + p.pw);
+    g.tops = g.ups + 4;
     GatedEnd end{};
     end.F = (int)F;
     hipError_t e = with_all<true>(g, s.io, p.first, [&](auto t, auto sh, auto direct) {
@@ -900,6 +997,11 @@ hipError_t launch_gated_backward(const GatedArgs& a, const GatedShape& s, const 
         end.tiles = tiles_of(s.M, S::kB);
         g.items = (int)(end.tiles * g.tiles);
         k_gated<decltype(t), S, true, direct.value><<<grid_of(g.items), 256, 0, st>>>(g);
+        if constexpr (std::is_same_v<decltype(t), _Float16>) {
+            const hipError_t first = hipGetLastError();
+            if (first != hipSuccess) return first;
+            k_gated_again<S, direct.value><<<g.items < 512 ? g.items : 512, 256, 0, st>>>(g);
+        }
         return hipGetLastError();
     });
     if (e != hipSuccess) return e;
