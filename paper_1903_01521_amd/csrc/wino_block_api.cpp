@@ -70,13 +70,11 @@ Buf dense(const void* p, int N, int L, int heads, int D, Io io, bool out) {
 struct QkCall {
     QkShape s;
     QkSide t[2];
-    bool both;
 };
 
 int make_qk(QkCall* c, const void* q, const void* k, const float* gq, const float* gk, const float* rot, const int* qpos,
             const int* kpos, int N, int Lq, int Lk, int Hq, int Hk, int D, int R, int T, int ldq, int ldk, float eps,
             unsigned flags) {
-    c->both = k != nullptr;
     if (!q || !(eps >= 0.0f) || !tokens_ok(N, Lq, Hq, D, ldq) || (k && !tokens_ok(N, Lk, Hk, D, ldk)))
         return WINO_ERR_INVALID_ARG;
     int64_t e;
