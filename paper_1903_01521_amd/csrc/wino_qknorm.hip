@@ -41,6 +41,40 @@ __device__ __forceinline__ float team_sum(float x) {
     return x;
 }
 
+template <int TEAM>
+__device__ __forceinline__ float team_max(float x) {
+#pragma unroll
+    for (int d = 1; d < TEAM; d <<= 1) x = fmaxf(x, __shfl_xor(x, d, 64));
+    return x;
+}
+
+// 1 / sqrt(mean x^2 + eps) from the sum of squares.  Where that is out of range (past 2^100, or so small
+// that squares may have lost bits; fp16's are in it), of a vector of the wave, x is taken times a power
+// of two, `up`, which the result belongs to, and `again` sums anew: n = x r is as before, and r of the
+// vector as it was is r up.
+template <typename T, int TEAM, int N, typename F>
+__device__ __forceinline__ float unit(float (&x)[N], float sq, int D, float eps, float& up, const F& again) {
+    up = 1.0f;
+    float mean = sq / (float)D + eps;
+    if constexpr (sizeof(T) == 4 || std::is_same_v<T, __bf16>) {
+        const bool out = !(mean >= 0x1p-80f && mean <= 0x1p100f);
+        if (__any(out)) {
+            float top = 0.0f;
+#pragma unroll
+            for (int j = 0; j < N; ++j) top = fmaxf(top, fabsf(x[j]));
+            top = fmaxf(team_max<TEAM>(top), sqrtf(eps));
+            if (out && top > 0.0f && top < INFINITY) {
+                const int e = (int)(__float_as_uint(top) >> 23) - 127;
+                up = __uint_as_float((uint32_t)(min(max(-e, -126), 126) + 127) << 23);
+            }
+#pragma unroll
+            for (int j = 0; j < N; ++j) x[j] *= up;
+            mean = again() / (float)D + eps * up * up;
+        }
+    }
+    return 1.0f / sqrtf(mean);
+}
+
 // VP values at p + d as floats; those from D on are zero.
 template <typename T, int VP>
 __device__ __forceinline__ void get(const T* p, int d, int D, float* v) {
@@ -159,10 +193,14 @@ __global__ __launch_bounds__(256) void k_qk_norm(QkK g) {
 #pragma unroll
     for (int i = 0; i < kHeads; ++i) {
         if (me.h0 + i >= me.h1) break;
-        float sq = 0.0f;
+        auto squares = [&] {
+            float sq = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 2 * VP; ++j) sq = __builtin_fmaf(v[i][j], v[i][j], sq);
-        const float r = 1.0f / sqrtf(team_sum<TEAM>(sq) / (float)D + g.s.eps);
+            for (int j = 0; j < 2 * VP; ++j) sq = __builtin_fmaf(v[i][j], v[i][j], sq);
+            return team_sum<TEAM>(sq);
+        };
+        float up;
+        const float r = unit<T, TEAM>(v[i], squares(), D, g.s.eps, up, squares);
 #pragma unroll
         for (int j = 0; j < VP; ++j) {
             const int a = m.first(j), b = m.second(j);
@@ -194,24 +232,29 @@ __global__ __launch_bounds__(256) void k_qk_norm_back(QkK g) {
             float x[2 * VP], dz[2 * VP];
             m.load((const T*)t.x + me.tok * t.ld + (int64_t)head * D, D, x);
             m.load((const T*)t.dy + (me.tok * t.heads + head) * D, D, dz);
-            float sq = 0.0f, dot = 0.0f;
 #pragma unroll
             for (int j = 0; j < VP; ++j) {
                 const int a = m.first(j), b = m.second(j);
                 m.turn_pair(dz[a], dz[b], m.c[j], -m.s[j], dz[a], dz[b]);
             }
+            float dot, up;
+            auto sums = [&] {
+                float sq = 0.0f;
+                dot = 0.0f;
 #pragma unroll
-            for (int j = 0; j < 2 * VP; ++j) {
-                sq = __builtin_fmaf(x[j], x[j], sq);
-                dot = __builtin_fmaf(dz[j] * m.g[j], x[j], dot);
-            }
-            const float r = 1.0f / sqrtf(team_sum<TEAM>(sq) / (float)D + g.s.eps);
-            const float mean = team_sum<TEAM>(dot) * r / (float)D;
+                for (int j = 0; j < 2 * VP; ++j) {
+                    sq = __builtin_fmaf(x[j], x[j], sq);
+                    dot = __builtin_fmaf(dz[j] * m.g[j], x[j], dot);
+                }
+                return team_sum<TEAM>(sq);
+            };
+            const float r = unit<T, TEAM>(x, sums(), D, g.s.eps, up, sums);
+            const float mean = team_sum<TEAM>(dot) * r / (float)D, rx = r * up;
 #pragma unroll
             for (int j = 0; j < 2 * VP; ++j) {
                 const float n = x[j] * r;
                 sum[j] = __builtin_fmaf(dz[j], n, sum[j]);
-                x[j] = r * (dz[j] * m.g[j] - n * mean);
+                x[j] = rx * (dz[j] * m.g[j] - n * mean);
             }
             m.store((T*)t.dx + me.tok * t.ld + (int64_t)head * D, D, x);
         }
