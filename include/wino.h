@@ -484,7 +484,7 @@ int wino_qk_norm_backward_nhwc(const void* dyq, const void* dyk, const void* q, 
 /* Attention of Lq tokens to Lk keys of the same image, for query head h over key head
  * h / (Hq / Hk) (Hq % Hk == 0):
  *   S = scale * q k^T, y = softmax(S) v over the keys that klen and mask leave.
- *   k, v : [N][Lk][Hk][D], ldk, ldv.   scale > 0 and finite.
+ *   k, v : [N][Lk][Hk][D], ldk, ldv.   scale > 0, scale * log2(e) finite.
  *   klen : [N] lengths, keys from klen[n] on are left out (values outside 0..Lk are taken
  *          as 0 or Lk), or NULL.
  *   mask : [N][Lk] bytes, keys of zero bytes are left out, or NULL.

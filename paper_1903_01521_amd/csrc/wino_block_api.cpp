@@ -13,6 +13,7 @@ using namespace wino;
 namespace {
 
 constexpr int kMostD = 128;
+constexpr float kLog2e = 1.44269504088896340736f;
 
 int io_of(unsigned flags, unsigned more, Io* io) {
     const unsigned t = flags & WINO_IO_MASK;
@@ -95,7 +96,7 @@ size_t table_bytes(const QkShape& s) { return (size_t)s.T * s.R * sizeof(float);
 int make_attn(AttnShape* s, int N, int Lq, int Lk, int Hq, int Hk, int D, int ldq, int ldk, int ldv, float scale,
               unsigned flags) {
     if (!tokens_ok(N, Lq, Hq, D, ldq) || !tokens_ok(N, Lk, Hk, D, ldk) || !tokens_ok(N, Lk, Hk, D, ldv) || Hq % Hk ||
-        !(scale > 0.0f) || isinf(scale))
+        !(scale > 0.0f) || isinf(scale * kLog2e))           // exponents of two take the product
         return WINO_ERR_INVALID_ARG;
     if (D > kMostD) return WINO_ERR_UNSUPPORTED;
     s->N = N; s->Lq = Lq; s->Lk = Lk; s->Hq = Hq; s->Hk = Hk; s->D = D;
