@@ -2,8 +2,9 @@
 pass fp16's range: both ends, one token that is not finite, and tokens of both ends."""
 import numpy as np
 import pytest
+import torch
 
-from block_helpers import O, gated_back, gated_back_tol, host, within
+from block_helpers import B, DEV, O, dev, gated_back, gated_back_tol, host, space, within
 from train_helpers import rounded
 
 pytestmark = pytest.mark.gpu
@@ -82,3 +83,37 @@ def test_zero_gradients():
     (dy, x, w, b), _ = make(SIZES[0], 1.0, 1.0, 1.0, 1.0)
     for g in gated_back(0 * dy, x, w, b, "f16", "silu"):
         assert (host(g) == 0).all()
+
+
+def test_a_captured_call_finds_its_power_at_every_replay():
+    """Gradients within the range, below it and above it, by one graph and one workspace."""
+    N, H, W, C, K, _ = SIZES[3]
+    rng = np.random.default_rng(94)
+    x, w, dy = (dev(rng.standard_normal(s) * f, "f16") for s, f in (((N, H, W, C), 1.0), ((2, K, C), 0.01), ((N, H, W, K), 1.0)))
+    dx, dw, db = torch.zeros_like(x), torch.zeros_like(w), torch.zeros((2, K), device=DEV)
+    size = (N, C, H, W, K, B.WINO_IO_F16 | B.WINO_FLAG_SILU)
+    need = B.wino_gated_layer_backward_workspace_bytes(*size)
+    ws = space(need)
+
+    def step():
+        B.check(B.wino_gated_layer_backward_nhwc(dy, x, w, None, dx, dw, db, *size, ws, need))
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    first = dy.clone()
+    for f in (1.0, 2.0 ** -14, 2.0 ** 12, 2.0 ** -10, 1.0):
+        dy.copy_(first * f)
+        for t in (ws, dx, dw, db):
+            t.fill_(float("nan"))
+        graph.replay()
+        got = [t.clone() for t in (dx, dw, db)]
+        for t in (ws, dx, dw, db):
+            t.fill_(float("nan"))
+        step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, (dx, dw, db)))
+        # of 2^12, dzu is some 2^12 * 0.04 and dw, over 12544 tokens, 2^12 * 0.04 * 112 = 18000 in the mean
+        # square: four times as much, which some of its 16384 values reach, is past fp16 itself
+        assert all(bool(torch.isfinite(t).all()) for t in ((dx, db) if f > 1 else (dx, dw, db)))
