@@ -649,7 +649,13 @@ template <typename S, bool kDirect>
 __global__ __launch_bounds__(256, 2) void k_gated_again(GatedK g) {
     __shared__ float largest[4];
     float top = 0.0f;
-    for (int i = threadIdx.x; i < g.items; i += 256) top = fmaxf(top, g.tops[i]);
+    for (int i0 = threadIdx.x; i0 < g.items; i0 += 16 * 256) {
+        float v[16];                                     // on their way together (12544 one by one took 20 us)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j] = i0 + 256 * j < g.items ? g.tops[i0 + 256 * j] : 0.0f;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) top = fmaxf(top, v[j]);
+    }
     top = join64<true>(top);
     if ((threadIdx.x & 63) == 0) largest[threadIdx.x >> 6] = top;
     __syncthreads();
