@@ -96,3 +96,16 @@ def test_queries_keys_and_values_of_one_tensor(N, L, Hq, Hk, D, dtype):
                                attend_back_tol(more, scale, kept, D, dtype, *want, host(lse))):
         within(x, w, tol, name)
     assert bool((g[:, :, H:] == 7).all())
+
+
+@pytest.mark.parametrize("which", ["q", "kv"])
+@pytest.mark.parametrize("ld", [1 << 22, (1 << 22) + 8])
+def test_the_limit_of_tiles_straight_to_lds(ld, which):
+    """Tokens 2^22 elements apart, and past it: rows of a tile reach over 2^29 bytes."""
+    N, Lq, Lk, Hq, Hk, D = size = 1, 67, 70, 2, 1, 64
+    q, k, v, rng = make(*size, "bf16", 105)
+    dy = rounded(rng.standard_normal(q.shape), "bf16").astype(np.float64)
+    lds = (ld if which == "q" else None, *(2 * (ld if which == "kv" else None,)))
+    check(q, k, v, "bf16", mask=rng.integers(0, 2, (N, Lk)), ld=lds)
+    check(q[:, :3], k, v, "bf16", ld=lds)
+    check_back(dy, q, k, v, "bf16", klen=[66], ld=lds)
