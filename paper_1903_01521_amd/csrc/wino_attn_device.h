@@ -674,13 +674,17 @@ void k_attn(AttnK g) {
                 for (int i = 0; i < 16; ++i) o[d][i] *= a;
         }
         const float off = top == -INFINITY ? 0.0f : kExpUp<T> - top * c2;
+        // a step's sum of its own: one addition to the running one, whose roundings all go one way where
+        // keys weigh alike (65536 of them, one by one: off by 3e-4)
+        float part = 0.0f;
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 p[kb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[kb][i], c2, off));
-                sum += p[kb][i];
+                part += p[kb][i];
             }
+        sum += part;
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -901,6 +905,7 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(4))) void k_attn_dq(AttnK g)
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
             f32x16 p{}, dp{};
+            float part = 0.0f;
 #pragma unroll
             for (int c = 0; c < D16; ++c) {
                 p = mma(Tl::read(sk, kb * 32 + (lane & 31), c, h), fq[c], p);
@@ -915,7 +920,7 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(4))) void k_attn_dq(AttnK g)
                 const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c2, off));
                 ds[kb][i] = x * (dp[i] - delta);
                 if constexpr (kFix) ps[kb][i] = x;
-                else lack += x;
+                else part += x;
             }
             if (!whole) {
                 // dy that is not finite by a key's zeros
@@ -924,8 +929,9 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(4))) void k_attn_dq(AttnK g)
             }
             if constexpr (kFix) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) lack += ds[kb][i];
+                for (int i = 0; i < 16; ++i) part += ds[kb][i];
             }
+            lack += part;
         }
         if constexpr (kHalf) {
             keep_range(ds, up, acc, round);
