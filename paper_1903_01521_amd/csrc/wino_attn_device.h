@@ -499,12 +499,12 @@ struct KeyTiles {                            // by way of registers: any address
         __syncthreads();
         if (k0 + KT < hi) load(k0 + KT);
     }
-    // x[e] .. x[e + 3] belong to the tile's keys at + 4 h .. + 3: `to` for those that are left out (a
-    // sum with -infinity would leave NaN where the row holds what is not finite)
-    __device__ __forceinline__ void leave_out(const float* bias, int at, int h, f32x16& x, int e, float to) const {
+    // x[e] .. x[e + 3] are the scores of the tile's keys at + 4 h .. + 3: -infinity for those that are left
+    // out (a sum with -infinity would leave NaN where the row holds what is not finite)
+    __device__ __forceinline__ void leave_out(const float* bias, int at, int h, f32x16& x, int e) const {
         const f32x4v m = *(const f32x4v*)&bias[at + 4 * h];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[e + i] = m[i] == 0.0f ? x[e + i] : to;
+        for (int i = 0; i < 4; ++i) x[e + i] = m[i] == 0.0f ? x[e + i] : -INFINITY;
     }
 };
 template <typename T, int D16, int KT, int NT>
@@ -566,10 +566,10 @@ struct KeyTiles<T, D16, KT, NT, kStraight> {      // straight to LDS: 16-bit, 16
         bits = coming;
         if (k0 + KT < hi) issue(nk, nv, k0 + KT);
     }
-    __device__ __forceinline__ void leave_out(const float*, int at, int h, f32x16& x, int e, float to) const {
+    __device__ __forceinline__ void leave_out(const float*, int at, int h, f32x16& x, int e) const {
         const uint32_t b = (uint32_t)((h ? bits >> 4 : bits) >> at);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[e + i] = b >> i & 1 ? x[e + i] : to;
+        for (int i = 0; i < 4; ++i) x[e + i] = b >> i & 1 ? x[e + i] : -INFINITY;
     }
 };
 
@@ -656,7 +656,7 @@ void k_attn(AttnK g) {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-                for (int b = 0; b < 4; ++b) in.leave_out(bias, kb * 32 + 8 * b, h, p[kb], 4 * b, -INFINITY);
+                for (int b = 0; b < 4; ++b) in.leave_out(bias, kb * 32 + 8 * b, h, p[kb], 4 * b);
         }
         float mx = p[0][0];
 #pragma unroll
@@ -913,23 +913,18 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(4))) void k_attn_dq(AttnK g)
             }
             if (!whole) {
 #pragma unroll
-                for (int b = 0; b < 4; ++b) in.leave_out(bias, kb * 32 + 8 * b, h, p, 4 * b, -INFINITY);
+                for (int b = 0; b < 4; ++b) in.leave_out(bias, kb * 32 + 8 * b, h, p, 4 * b);
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c2, off));
                 ds[kb][i] = x * (dp[i] - delta);
-                if constexpr (kFix) ps[kb][i] = x;
-                else part += x;
-            }
-            if (!whole) {
-                // dy that is not finite by a key's zeros
-#pragma unroll
-                for (int b = 0; b < 4; ++b) in.leave_out(bias, kb * 32 + 8 * b, h, ds[kb], 4 * b, 0.0f);
-            }
-            if constexpr (kFix) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) part += ds[kb][i];
+                if constexpr (kFix) {
+                    part += ds[kb][i];
+                    ps[kb][i] = x;
+                } else {
+                    part += x;
+                }
             }
             lack += part;
         }
@@ -962,6 +957,12 @@ __global__ __launch_bounds__(256, (waves_of<T, D16>(4))) void k_attn_dq(AttnK g)
     lack = add_halves(lack) * kDown;
     round = add_halves(round) * kDown / up;
     if (!live) return;
+    if (lse == -INFINITY) {
+        // a row without keys: dy that is not finite by their zeros
+        delta = lack = round = 0.0f;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) acc[d] = mean[d] = f32x16{};
+    }
     const float share = kFix || g.splits > 1 ? 1.0f : share_of(lack);
     const float f = s.scale * share * kDown / up, fm = s.scale * kDown;
     if (g.splits > 1) {
