@@ -528,7 +528,8 @@ int wino_gated_layer_nhwc(const void* x, const void* w, const float* bias, void*
  *   dx : as x; dw : as w; dbias : [2][K] fp32.  Each may be NULL, not all (INVALID_ARG).
  * dzg and dzu go through the workspace in the tensors' type, one rounding (fp16: times a power
  * of two that brings the call's largest finite one to 2^-2 at least and into range; what is
- * below 2^-23 of it is lost); dbias is summed before it.  N*H*W and 2*K must be below 2^31, K*C below 2^37 (UNSUPPORTED). */
+ * below 2^-23 of it is lost); dbias is summed before it.  N*H*W and 2*K must be below 2^31,
+ * K*C below 2^37 (UNSUPPORTED). */
 size_t wino_gated_layer_backward_workspace_bytes(int N, int C, int H, int W, int K, unsigned flags);
 int wino_gated_layer_backward_nhwc(const void* dy, const void* x, const void* w, const float* bias, void* dx, void* dw,
                                    float* dbias, int N, int C, int H, int W, int K, unsigned flags, void* workspace,

@@ -577,13 +577,13 @@ struct KeyTiles<T, D16, KT, NT, kStraight> {      // straight to LDS: 16-bit, 16
 // One pass over the keys with a running maximum and sum, bound by vector instructions: of a
 // score register's 33 cycles the exponential takes 16, its argument, the sum, the maximum
 // and the rounding 13 (16 images of 3136 tokens to 0..2048 keys, 8 heads of 64, bf16: 142 to 152 us,
-// 0.69 to 0.74 PFLOP/s).  The maximum moves, and what is summed is scaled, only where it grows by more
-// than 2^8: exponentials stay below 2^8, and most tiles skip the scaling.  fp16 exponentials are held 2^7 times as large, below
-// 2^15, and lose what is below 2^-32 of a row's largest (2^-25 without; of 65536 keys of 2^-17
-// each, half a row's weight, every one would be off by as much as 2^-8).  kFew: one wave
-// has 32 rows and takes 32 keys a step (single tokens, memory bound: four such workgroups a
-// CU, each with its own start and end.  One of four waves, 128 keys a step, a CU took 77 us for
-// 32 tokens to 0..4096 keys, 8 heads of 128, bf16, in place of 64).
+// 0.69 to 0.74 PFLOP/s).  The maximum moves, and what is summed is scaled, only where it grows by
+// more than 2^8: exponentials stay below 2^8, and most tiles skip the scaling.  fp16 exponentials are
+// held 2^7 times as large, below 2^15, and lose what is below 2^-32 of a row's largest (2^-25 without; of
+// 65536 keys of 2^-17 each, half a row's weight, every one would be off by as much as 2^-8).  kFew: one
+// wave has 32 rows and takes 32 keys a step (single tokens, memory bound: four such workgroups a CU, each
+// with its own start and end.  One of four waves, 128 keys a step, a CU took 77 us for 32 tokens to
+// 0..4096 keys, 8 heads of 128, bf16, in place of 64).
 
 template <typename T>
 constexpr float kExpUp = std::is_same_v<T, _Float16> ? 7.0f : 0.0f;
